@@ -529,6 +529,110 @@ int kvc_gate_weights(const double *dist_sq, int32_t n_anchors, double temperatur
                      double *entropy, void *stream);
 
 /*
+ * Requests over a cache: what a serving step does with a (corrected) cache next.  kvc_append writes the new tokens' keys
+ * and values of one layer, kvc_attend computes the attention of the new tokens over the cache.  Both take the same
+ * description of the step, whose lists are DEVICE arrays, so that a captured graph can be replayed with other lengths:
+ *   n            requests
+ *   max_q        HOST bound on the new tokens of any request, max_kv HOST bound on kv_len of any request
+ *                (they size the launch; a graph captured with them serves every step that stays within them)
+ *   q_begin      DEVICE int32 [n + 1], ascending: request i owns the packed rows q_begin[i] .. q_begin[i+1]-1 of the new
+ *                tokens; a request may have none.  Rows outside every request (padding) are neither read nor written.
+ *   kv_len       DEVICE int32 [n]: tokens of request i in the cache, its new ones included: new token j of n_q sits at
+ *                position kv_len - n_q + j
+ *   page_table   DEVICE int32 [n, table_stride]: pages of request i (KVC_PAGED pools; the pool's own T and page_table
+ *                are not used).  NULL: every request reads the cache as described by the kvc_cache itself (its page
+ *                table, or its contiguous rows): several requests then share one context.
+ * A request whose numbers break these rules (a length above its bound, rows outside n_rows, a negative length) is
+ * skipped, and KVC_FLAG_BAD_LENGTH is raised in the status word.  A page id outside the pool raises KVC_FLAG_BAD_PAGE;
+ * kvc_append skips the row, kvc_attend takes the page's keys and values as zeros.  max_kv beyond what the table (or the
+ * cache) holds: KVC_E_SHAPE.
+ */
+typedef struct kvc_requests {
+  int32_t n, max_q, max_kv, table_stride;
+  const int32_t *q_begin;
+  const int32_t *kv_len;
+  const int32_t *page_table;
+} kvc_requests;
+
+/*
+ * Packed rows of new tokens: bf16 [n_rows, n_heads, d], channels contiguous, strides in elements (0: dense), rows
+ * 16-byte aligned.  A slice of a fused projection's output needs no copy.
+ */
+typedef struct kvc_heads {
+  void *data;                 /* DEVICE bf16                                       */
+  int32_t n_rows, n_heads;
+  int64_t s_row, s_head;
+} kvc_heads;
+
+/*
+ * A cache held in 8 bits: e4m3 codes laid out like a kvc_cache (k, v one BYTE per element; strides in elements, multiples
+ * of 16) and one exponent byte per row (token, layer, head), keys and values separately:
+ *     value = code * 2^(exponent - 127)      (exponent 255: the row reads as NaN)
+ * Element (l, h, t) of the exponents is at l*e_layer + h*e_head + t*e_tok (KVC_CONTIG) or
+ * l*e_layer + p*e_page + h*e_head + (t % page_size)*e_tok (KVC_PAGED); strides 0 select the dense default [L, H, T] or
+ * [L, n_phys_pages, H, page_size].
+ * The scale is a power of two, the smallest that brings the row's largest magnitude to at most 448 (e4m3's largest
+ * number; never below 2^-127): e4m3 carries its own exponent, so a finer scale would buy no precision, and every value
+ * of the cache is a bf16 number (magnitudes stop at 240 * 2^120, the largest such one): reading it back adds no rounding.  A row's error is that of e4m3: half a step, 2^-4 of
+ * the value, or 2^-10 of the scale for values below 2^-6 of it.
+ */
+typedef struct kvc_qcache {
+  kvc_cache codes;
+  uint8_t *scale_k;           /* DEVICE exponents                                  */
+  uint8_t *scale_v;
+  int64_t e_layer, e_page, e_head, e_tok;
+} kvc_qcache;
+
+/*
+ * kvc_quantize   -- dst = e4m3(src) for rows t < T of every layer and head (a finished agent's cache put away in half the
+ *                   bytes).  Codes are rounded to nearest even.  An infinity or NaN in src becomes the code NaN and does
+ *                   not count towards its row's scale.
+ * kvc_dequantize -- dst = bf16(value) (exact but for numbers below bf16's subnormal step).
+ * src and dst agree in L, H, T, d; layouts, strides and page tables may differ.  Pages that the tables do not name and
+ * rows >= T are left as they were.  Errors as kvc_apply (KVC_E_ALIAS: the buffers overlap).
+ */
+int kvc_quantize(const kvc_cache *src, kvc_qcache *dst, void *stream);
+int kvc_dequantize(const kvc_qcache *src, kvc_cache *dst, void *stream);
+
+/*
+ * kvc_append -- write new tokens into a cache: row q_begin[i] + j of k_new, v_new ([n_rows, H, d]) goes to position
+ * kv_len[i] - n_q + j of request i in `layer` of dst.  kvc_append_q8: the same with rows quantised as they are written,
+ * exactly as kvc_quantize would.  Rows whose position is negative are skipped (KVC_FLAG_BAD_LENGTH).  Requests must
+ * not write one and the same place (shared pages hold finished tokens); a request list without a page table therefore
+ * needs n == 1 (KVC_E_INVALID_ARG otherwise).
+ */
+int kvc_append(const kvc_requests *req, const kvc_heads *k_new, const kvc_heads *v_new, int32_t layer, kvc_cache *dst,
+               void *stream);
+int kvc_append_q8(const kvc_requests *req, const kvc_heads *k_new, const kvc_heads *v_new, int32_t layer, kvc_qcache *dst,
+                  void *stream);
+
+/*
+ * kvc_attend -- attention of the requests' new tokens over one layer of a cache: for row r (token j of request i) and
+ * query head a, with g = n_heads / H query heads per KV head,
+ *     out[r, a, :] = sum_t p_t V[a / g, t, :] ,  p = softmax_t( scale * q[r, a, :] . K[a / g, t, :] )
+ * over the keys t < kv_len[i], with causal != 0 only t <= kv_len[i] - n_q + j (the new tokens are the last ones of the
+ * cache).  A row that sees no key gets zeros and a log-sum-exp of minus infinity.
+ *   q, out   [n_rows, n_heads, d], n_heads a multiple of the cache's H, up to 64 query heads per KV head (KVC_E_UNSUPPORTED
+ *            beyond); out must not overlap q (KVC_E_ALIAS)
+ *   scale    finite and positive, usually 1 / sqrt(d)
+ *   lse      DEVICE float32 [n_rows, n_heads] or NULL: log sum_t exp(scale * q . K), natural logarithm, with which the
+ *            results over two parts of a context can be joined
+ *   workspace DEVICE, kvc_attend_workspace_bytes(...) bytes, 256-byte aligned, written before it is read; calls that may
+ *            overlap on the GPU need one each
+ * Keys past kv_len are never used, whatever they hold (NaN included).  A NaN or infinity in a VALUE row below kv_len may
+ * reach every row of its request, also those that the causal mask keeps from seeing that token.
+ * Logits, maxima, sums and outputs are held in float32.  Over a bf16 cache the probabilities are rounded to bf16 before
+ * they meet the values.  Results do not depend on the order in which blocks run.
+ */
+int kvc_attend(const kvc_requests *req, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale, int32_t causal,
+               kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int kvc_attend_q8(const kvc_requests *req, const kvc_heads *q, const kvc_qcache *cache, int32_t layer, double scale,
+                  int32_t causal, kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+/* Scratch of either call for requests within max_q, max_kv (0 on bad arguments); a function of n, max_q, max_kv, the head
+ * counts, d and the current device's SM count alone. */
+size_t kvc_attend_workspace_bytes(const kvc_requests *req, int32_t n_heads, int32_t H, int32_t d);
+
+/*
  * Device-side anomalies never trap or hang: a kernel that meets a page id outside
  * [0, n_phys_pages) or whose bounded wait on an asynchronous copy runs out skips
  * that tile and ORs a bit into a per-device status word.
@@ -540,6 +644,7 @@ int kvc_gate_weights(const double *dist_sq, int32_t n_anchors, double temperatur
 #define KVC_FLAG_BAD_PAGE     1u
 #define KVC_FLAG_WAIT_EXPIRED 2u
 #define KVC_FLAG_NOT_CONVERGED 4u   /* eigensolver hit its sweep limit             */
+#define KVC_FLAG_BAD_LENGTH   8u    /* a request's rows or length outside its bounds */
 int kvc_status_poll(uint32_t *flags);
 int kvc_status_reset(void);
 

@@ -26,7 +26,7 @@ KVC_PROJECT, KVC_FIT, KVC_FIT_FAST = 0, 1, 2
 KVC_PATH_AUTO, KVC_PATH_GENERIC, KVC_PATH_TC, KVC_PATH_MIXED = 0, 1, 2, 3
 KVC_MAX_SEGMENTS, KVC_COORDS_TARGET, KVC_COORDS_SOURCE = 16, 0, 1
 KVC_GROUP_HEAD, KVC_GROUP_LAYER = 0, 1
-KVC_FLAG_BAD_PAGE, KVC_FLAG_WAIT_EXPIRED, KVC_FLAG_NOT_CONVERGED = 1, 2, 4
+KVC_FLAG_BAD_PAGE, KVC_FLAG_WAIT_EXPIRED, KVC_FLAG_NOT_CONVERGED, KVC_FLAG_BAD_LENGTH = 1, 2, 4, 8
 KVC_OK = 0
 (KVC_E_INVALID_ARG, KVC_E_SHAPE, KVC_E_UNSUPPORTED, KVC_E_ALIAS, KVC_E_CUDA, KVC_E_WORKSPACE, KVC_E_DEVICE_FLAG,
  KVC_E_TOO_LARGE) = (-1, -2, -3, -4, -5, -6, -7, -8)
@@ -38,6 +38,7 @@ EXPORTS = (
     "kvc_apply_multi", "kvc_multi_workspace_bytes", "kvc_token_weights", "kvc_token_weights_workspace_bytes",
     "kvc_state_realign", "kvc_effective_rank", "kvc_fit_eigenvalues", "kvc_fit_solver", "kvc_group_fit_eigenvalues", "kvc_group_fit_solver", "kvc_selftest_wait_expiry", "kvc_apply_segmented", "kvc_state_update_segmented", "kvc_state_update_check", "kvc_state_update_chain",
     "kvc_chain_update_workspace_bytes", "kvc_chain_update_edge_stride", "kvc_chain_fused", "kvc_chain_workspace_bytes",
+    "kvc_quantize", "kvc_dequantize", "kvc_append", "kvc_append_q8", "kvc_attend", "kvc_attend_q8", "kvc_attend_workspace_bytes",
 )
 
 
@@ -70,6 +71,20 @@ class kvc_segments(C.Structure):
 class kvc_item(C.Structure):
     _fields_ = [("src", kvc_cache), ("dst", kvc_cache), ("st", kvc_state), ("shift", C.c_int32),
                 ("t_begin", C.c_int32), ("t_end", C.c_int32), ("reserved", C.c_int32)]
+
+
+class kvc_qcache(C.Structure):
+    _fields_ = [("codes", kvc_cache), ("scale_k", C.c_void_p), ("scale_v", C.c_void_p), ("e_layer", C.c_int64),
+                ("e_page", C.c_int64), ("e_head", C.c_int64), ("e_tok", C.c_int64)]
+
+
+class kvc_requests(C.Structure):
+    _fields_ = [("n", C.c_int32), ("max_q", C.c_int32), ("max_kv", C.c_int32), ("table_stride", C.c_int32),
+                ("q_begin", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p)]
+
+
+class kvc_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n_rows", C.c_int32), ("n_heads", C.c_int32), ("s_row", C.c_int64), ("s_head", C.c_int64)]
 
 
 _lib = None
@@ -127,6 +142,15 @@ def load(path: Optional[str] = None):
     lib.kvc_token_weights_workspace_bytes.restype = sz
     lib.kvc_gate_distance.argtypes = [PC, PS, i32, i32, vp, vp]
     lib.kvc_gate_weights.argtypes = [vp, i32, C.c_double, vp, vp, vp]
+    PQ, PRq, PH = C.POINTER(kvc_qcache), C.POINTER(kvc_requests), C.POINTER(kvc_heads)
+    lib.kvc_quantize.argtypes = [PC, PQ, vp]
+    lib.kvc_dequantize.argtypes = [PQ, PC, vp]
+    lib.kvc_append.argtypes = [PRq, PH, PH, i32, PC, vp]
+    lib.kvc_append_q8.argtypes = [PRq, PH, PH, i32, PQ, vp]
+    lib.kvc_attend.argtypes = [PRq, PH, PC, i32, C.c_double, i32, PH, vp, vp, sz, vp]
+    lib.kvc_attend_q8.argtypes = [PRq, PH, PQ, i32, C.c_double, i32, PH, vp, vp, sz, vp]
+    lib.kvc_attend_workspace_bytes.argtypes = [PRq, i32, i32, i32]
+    lib.kvc_attend_workspace_bytes.restype = sz
     lib.kvc_status_poll.argtypes = [C.POINTER(C.c_uint32)]
     lib.kvc_status_reset.argtypes = []
     lib.kvc_set_path.argtypes = [i32]
@@ -217,6 +241,91 @@ class Cache:
 
     def nbytes(self) -> int:
         return self.k.numel() * 2 + self.v.numel() * 2
+
+    @staticmethod
+    def pool(k: torch.Tensor, v: torch.Tensor, token_major: bool = False) -> "Cache":
+        """A paged pool without a table of its own: its pages belong to requests (:class:`Requests`)."""
+        return Cache(k, v, T=0, page_table=torch.empty(0, dtype=torch.int32, device=k.device), token_major=token_major)
+
+
+class QCache:
+    """A cache held in 8 bits: ``k``, ``v`` float8_e4m3fn codes in the shapes of :class:`Cache`, ``scale_k``, ``scale_v``
+    uint8 exponents of the same shapes without the channel axis (value = code * 2^(exponent - 127))."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, scale_k: torch.Tensor, scale_v: torch.Tensor, T: Optional[int] = None,
+                 page_table: Optional[torch.Tensor] = None, token_major: bool = False):
+        assert k.dtype == torch.float8_e4m3fn and v.dtype == torch.float8_e4m3fn
+        assert k.is_contiguous() and v.is_contiguous() and k.shape == v.shape
+        for e in (scale_k, scale_v):
+            assert e.dtype == torch.uint8 and e.is_contiguous() and e.shape == k.shape[:-1]
+        self.k, self.v, self.scale_k, self.scale_v = k, v, scale_k, scale_v
+        self.page_table, self.token_major = page_table, bool(token_major)
+        if page_table is None:
+            self.L, self.T, self.H, self.d = (int(x) for x in (k.shape if token_major else k.transpose(1, 2).shape))
+            self.page, self.P = 0, 0
+        else:
+            assert page_table.dtype == torch.int32 and page_table.is_contiguous() and T is not None
+            self.L, self.P, self.page, self.H, self.d = (int(x) for x in (k.shape if token_major else k.transpose(2, 3).shape))
+            self.T = int(T)
+
+    @staticmethod
+    def pool(k, v, scale_k, scale_v, token_major: bool = False) -> "QCache":
+        """A paged pool without a table of its own: its pages belong to requests (:class:`Requests`)."""
+        return QCache(k, v, scale_k, scale_v, T=0, page_table=torch.empty(0, dtype=torch.int32, device=k.device),
+                      token_major=token_major)
+
+    @staticmethod
+    def like(c: Cache) -> "QCache":
+        """An empty 8-bit cache of ``c``'s geometry (and page table)."""
+        code = lambda t: torch.zeros(t.shape, dtype=torch.float8_e4m3fn, device=t.device)
+        exp = lambda t: torch.zeros(t.shape[:-1], dtype=torch.uint8, device=t.device)
+        return QCache(code(c.k), code(c.v), exp(c.k), exp(c.v), T=None if c.page_table is None else c.T,
+                      page_table=c.page_table, token_major=c.token_major)
+
+    def struct(self) -> kvc_qcache:
+        q = kvc_qcache()
+        s = q.codes
+        s.k, s.v = self.k.data_ptr(), self.v.data_ptr()
+        s.L, s.H, s.T, s.d = self.L, self.H, self.T, self.d
+        q.scale_k, q.scale_v = self.scale_k.data_ptr(), self.scale_v.data_ptr()
+        if self.page_table is not None:
+            s.layout, s.page_size, s.n_phys_pages, s.page_table = KVC_PAGED, self.page, self.P, self.page_table.data_ptr()
+        if self.token_major:
+            rows = self.T if self.page_table is None else self.page
+            s.s_tok, s.s_head, q.e_tok, q.e_head = self.H * self.d, self.d, self.H, 1
+            if self.page_table is None:
+                s.s_layer, q.e_layer = rows * s.s_tok, rows * self.H
+            else:
+                s.s_page, q.e_page = rows * s.s_tok, rows * self.H
+                s.s_layer, q.e_layer = self.P * s.s_page, self.P * q.e_page
+        return q
+
+    def nbytes(self) -> int:
+        return 2 * (self.k.numel() + self.scale_k.numel())
+
+
+class Requests:
+    """A serving step's requests: ``q_begin`` int32 [n+1], ``kv_len`` int32 [n] and ``page_table`` int32 [n, pages] on the
+    GPU (None: every request reads the cache's own table or rows), and host bounds on their values."""
+
+    def __init__(self, q_begin: torch.Tensor, kv_len: torch.Tensor, max_q: int, max_kv: int, page_table: Optional[torch.Tensor] = None):
+        assert q_begin.dtype == kv_len.dtype == torch.int32 and q_begin.is_contiguous() and kv_len.is_contiguous()
+        assert q_begin.numel() == kv_len.numel() + 1
+        self.q_begin, self.kv_len, self.page_table = q_begin, kv_len, page_table
+        self.n, self.max_q, self.max_kv = int(kv_len.numel()), int(max_q), int(max_kv)
+        stride = 0
+        if page_table is not None:
+            assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == self.n
+            assert page_table.shape[1] <= 1 or page_table.stride(1) == 1
+            stride = int(page_table.stride(0)) if self.n > 1 else int(page_table.shape[1])
+            assert stride >= int(page_table.shape[1])
+            assert self.max_kv >= 0
+        self._pages = 0 if page_table is None else int(page_table.shape[1])
+        self._struct = kvc_requests(self.n, self.max_q, self.max_kv, stride, q_begin.data_ptr(), kv_len.data_ptr(),
+                                    0 if page_table is None else page_table.data_ptr())
+
+    def struct(self) -> kvc_requests:
+        return self._struct
 
 
 class State:
@@ -639,6 +748,77 @@ def kvc_gate_weights(dist_sq: torch.Tensor, g: torch.Tensor, entropy: torch.Tens
     assert dist_sq.dtype == g.dtype == entropy.dtype == torch.float64 and g.numel() >= n and entropy.numel() >= 1
     _check(load().kvc_gate_weights(dist_sq.data_ptr(), n, float(temperature), g.data_ptr(), entropy.data_ptr(),
                                    _stream(stream)), "kvc_gate_weights")
+
+
+def _heads(t: torch.Tensor, what: str) -> kvc_heads:
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1:
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: bf16 [rows, heads, d] with contiguous channels expected")
+    rows, heads, _ = t.shape
+    if (rows > 1 and t.stride(0) == 0) or (heads > 1 and t.stride(1) == 0):
+        raise KvcError(KVC_E_UNSUPPORTED, f"{what}: broadcast rows")
+    return kvc_heads(t.data_ptr(), rows, heads, t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 else 0)
+
+
+def _one_device(what: str, *tensors) -> None:
+    """All on the current CUDA device (the one the library launches on)."""
+    cur = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != cur):
+            raise KvcError(KVC_E_INVALID_ARG, f"{what}: tensors on cuda:{cur}, the current device, expected")
+
+
+def _cache_tensors(c):
+    return (c.k, c.v, c.page_table) + ((c.scale_k, c.scale_v) if isinstance(c, QCache) else ())
+
+
+def _step_check(req: Requests, c, d: int, what: str) -> None:
+    if d != c.d:
+        raise KvcError(KVC_E_SHAPE, what)
+    if req.page_table is not None and c.page_table is not None and req.max_kv > req._pages * c.page:
+        raise KvcError(KVC_E_SHAPE, what)
+
+
+def kvc_quantize(src: Cache, dst: QCache, stream=None) -> None:
+    """dst = e4m3(src), one power-of-two scale per (layer, head, token)."""
+    _one_device("kvc_quantize", *_cache_tensors(src), *_cache_tensors(dst))
+    s, d = src.struct(), dst.struct()
+    _check(load().kvc_quantize(C.byref(s), C.byref(d), _stream(stream)), "kvc_quantize")
+
+
+def kvc_dequantize(src: QCache, dst: Cache, stream=None) -> None:
+    """dst = bf16(code * 2^(exponent - 127))."""
+    _one_device("kvc_dequantize", *_cache_tensors(src), *_cache_tensors(dst))
+    s, d = src.struct(), dst.struct()
+    _check(load().kvc_dequantize(C.byref(s), C.byref(d), _stream(stream)), "kvc_dequantize")
+
+
+def kvc_append(req: Requests, k_new: torch.Tensor, v_new: torch.Tensor, cache, layer: int, stream=None) -> None:
+    """Write the new tokens' rows [rows, H, d] into `layer` of a Cache, or quantised into a QCache."""
+    _one_device("kvc_append", k_new, v_new, req.q_begin, req.kv_len, req.page_table, *_cache_tensors(cache))
+    _step_check(req, cache, k_new.shape[-1], "kvc_append")
+    _step_check(req, cache, v_new.shape[-1], "kvc_append")
+    c, k, v = cache.struct(), _heads(k_new, "k_new"), _heads(v_new, "v_new")
+    fn = load().kvc_append_q8 if isinstance(cache, QCache) else load().kvc_append
+    _check(fn(C.byref(req._struct), C.byref(k), C.byref(v), int(layer), C.byref(c), _stream(stream)), "kvc_append")
+
+
+def kvc_attend_workspace_bytes(req: Requests, cache, n_heads: int) -> int:
+    return int(load().kvc_attend_workspace_bytes(C.byref(req._struct), int(n_heads), cache.H, cache.d))
+
+
+def kvc_attend(req: Requests, q: torch.Tensor, cache, layer: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+               scale: Optional[float] = None, causal: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of the new tokens' queries [rows, heads, d] over `layer` of a Cache or QCache (scale: 1 / sqrt(d))."""
+    _one_device("kvc_attend", q, out, workspace, lse, req.q_begin, req.kv_len, req.page_table, *_cache_tensors(cache))
+    _step_check(req, cache, q.shape[-1], "kvc_attend")
+    _step_check(req, cache, out.shape[-1], "kvc_attend")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != tuple(q.shape[:2])):
+        raise KvcError(KVC_E_INVALID_ARG, "kvc_attend: lse must be float32 [rows, heads]")
+    c, hq, ho = cache.struct(), _heads(q, "q"), _heads(out, "out")
+    fn = load().kvc_attend_q8 if isinstance(cache, QCache) else load().kvc_attend
+    _check(fn(C.byref(req._struct), C.byref(hq), C.byref(c), int(layer), cache.d ** -0.5 if scale is None else float(scale),
+              int(bool(causal)), C.byref(ho), 0 if lse is None else lse.data_ptr(), 0 if workspace is None else workspace.data_ptr(),
+              0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "kvc_attend")
 
 
 def kvc_status_poll() -> int:

@@ -7,6 +7,7 @@
 #include <new>
 
 #include "../../include/kvc.h"
+#include "kvc_attend.h"
 #include "kvc_dev.cuh"
 #include "kvc_launch.h"
 #include "kvc_tc.h"
@@ -26,6 +27,9 @@ uint32_t* status_word_ptr() {
 
 static uint32_t* status_ptr() { return status_word_ptr(); }
 
+int path_force() { return tl_path_force; }
+void set_last_path(int path) { tl_last_path = path; }
+
 static int ilog2_exact(int x) {
   if (x <= 0 || (x & (x - 1))) return -1;
   int s = 0;
@@ -34,7 +38,7 @@ static int ilog2_exact(int x) {
 }
 
 // Validate one cache descriptor and resolve it for the kernels.
-static int resolve_cache(const kvc_cache* c, DevCache* out) {
+int resolve_cache(const kvc_cache* c, DevCache* out) {
   if (!c || !c->k || !c->v) return KVC_E_INVALID_ARG;
   if (c->L <= 0 || c->H <= 0 || c->T < 0 || c->d <= 0) return KVC_E_INVALID_ARG;
   if (c->d != 64 && c->d != 128) return KVC_E_UNSUPPORTED;
