@@ -66,7 +66,7 @@ int resolve_requests(const kvc_requests* r, const kvc_cache* c, int n_rows, DevR
   out->table = r->page_table;
   out->table_stride = r->table_stride;
   out->n = r->n;
-  out->max_q = r->max_q < n_rows ? r->max_q : n_rows;
+  out->max_q = r->max_q;
   out->max_kv = r->max_kv;
   out->n_rows = n_rows;
   return KVC_OK;
@@ -98,7 +98,7 @@ int append_common(const kvc_requests* req, const kvc_heads* kn, const kvc_heads*
   if (overlap(ck, cv) || overlap(ck, ek) || overlap(ck, ev) || overlap(cv, ek) || overlap(cv, ev)) return KVC_E_ALIAS;
   a.H = geo->H;
   a.layer = layer;
-  if (req->n == 0 || a.req.max_q == 0) return KVC_OK;
+  if (req->n == 0 || a.req.max_q == 0 || a.req.n_rows == 0) return KVC_OK;
   if (!(a.status = status_word_ptr())) return KVC_E_CUDA;
   if (launch_append(a, geo->d, reinterpret_cast<cudaStream_t>(stream)) != cudaSuccess) return KVC_E_CUDA;
   set_last_path(KVC_PATH_GENERIC);
@@ -138,12 +138,13 @@ int attend_common(const kvc_requests* req, const kvc_heads* q, const kvc_cache* 
   if (q->n_heads / geo->H > 64 || geo->H > 65535) return KVC_E_UNSUPPORTED;
   if ((rc = resolve_requests(req, geo, q->n_rows, &a.req)) != KVC_OK) return rc;
   if (reinterpret_cast<uintptr_t>(lse) & 3) return KVC_E_UNSUPPORTED;
+  if ((int64_t)req->max_q * (q->n_heads / geo->H) >= (int64_t)1 << 30) return KVC_E_UNSUPPORTED;
   const int64_t reach = cache_reach(geo, a.c);
   const Extent ck = extent_of(geo->k, reach, elem), cv = extent_of(geo->v, reach, elem);
   const Extent el = extent_of(lse, lse ? (int64_t)q->n_rows * q->n_heads : 0, 4);
   if (overlap(eo, eq) || overlap(eo, ck) || overlap(eo, cv) || overlap(el, eo) || overlap(el, eq) || overlap(el, ck) || overlap(el, cv))
     return KVC_E_ALIAS;
-  if (req->n == 0 || a.req.max_q == 0) return KVC_OK;
+  if (req->n == 0 || a.req.max_q == 0 || a.req.n_rows == 0) return KVC_OK;
   const size_t need = kvc_attend_workspace_bytes(req, q->n_heads, geo->H, geo->d);
   if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return KVC_E_WORKSPACE;
   a.H = geo->H;

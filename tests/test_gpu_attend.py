@@ -53,10 +53,13 @@ def test_attend_matches_the_oracle(name, q8, path):
     kvc.kvc_set_path(kvc.KVC_PATH_GENERIC if path == "generic" else kvc.KVC_PATH_AUTO)
     try:
         out, lse = b.run()
+        used = kvc.kvc_last_path()
     finally:
         kvc.kvc_set_path(kvc.KVC_PATH_AUTO)
     b.check(out, lse)
     assert kvc.kvc_status_poll() == 0
+    if path == "auto" and b.req.max_q > 0:
+        assert used == kvc.KVC_PATH_TC, "these shapes belong to the tensor-core kernels"
 
 
 @pytest.mark.parametrize("seed", range(24))
