@@ -26,6 +26,7 @@
 #include "kvc_launch.h"
 #include "kvc_tc.h"
 #include "kvc_tc_attend.cuh"
+#include "kvc_tc_attend_few.h"
 
 namespace kvc {
 namespace {
@@ -552,19 +553,40 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
 
 }  // namespace
 
+// Which kernels a call launches: requests of up to `rc` rows a KV head go to the few-rows kernel (rc = 0: none), the
+// others to this one (chunk = false: there are none).  Decided from the bounds alone: all requests within the few-rows
+// kernel's 32 rows take it; a batch of several requests with longer ones among them is served by both, single tokens by
+// the few-rows kernel; one long request by this kernel.
+struct Plan {
+  int rc;
+  bool chunk;
+};
+static Plan attend_plan(int n, int max_q, int G, bool q8) {
+  const int64_t rows = (int64_t)max_q * G;
+  if (const int rc = few_capacity(rows, q8)) return {rc, false};
+  return {n > 1 ? few_capacity(G, q8) : 0, true};
+}
+
+// 8-bit and bf16 caches need the same: the larger of the two plans
 size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d) {
-  const int64_t units = (int64_t)n * H * chunk_units(max_q, G);
-  const int ns = chunk_splits(units, max_kv);
-  return ns == 1 ? 0 : (size_t)(units * ns * kUnitRows * (d + 2) * 4);
+  const Plan p = attend_plan(n, max_q, G, false);
+  size_t bytes = p.rc ? (few_workspace_bytes(n, max_kv, H, d, p.rc) + 255) / 256 * 256 : 0;
+  if (p.chunk) {
+    const int64_t units = (int64_t)n * H * chunk_units(max_q, G);
+    const int ns = chunk_splits(units, max_kv);
+    if (ns > 1) bytes += (size_t)(units * ns * kUnitRows * (d + 2) * 4);
+  }
+  return bytes;
 }
 
 int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   (void)L;
   const bool q8 = a.e.k != nullptr;
+  const Plan plan = attend_plan(a.req.n, a.req.max_q, a.G, q8);
   ChunkLaunch p;
   p.a = a;
   p.units_u = chunk_units(a.req.max_q, a.G);
-  p.min_rows = 1;
+  p.min_rows = plan.rc + 1;
   const int64_t units = (int64_t)a.req.n * a.H * p.units_u;
   p.nsplit = chunk_splits(units, a.req.max_kv);
   if (units * p.nsplit >= (int64_t)1 << 31 || a.req.n > 65535) return KVC_E_UNSUPPORTED;
@@ -576,6 +598,12 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   else
     ok = encode_attend_tile(&mk, &p.g, a.c, a.c.k, a.layer, a.H, d) && encode_attend_tile(&mv, &p.g, a.c, a.c.v, a.layer, a.H, d);
   if (!ok) return KVC_E_UNSUPPORTED;
+  if (plan.rc) {
+    if (launch_attend_few(a, p.g, mk, mv, plan.rc, d, a.part, s) != cudaSuccess) return KVC_E_CUDA;
+    const Plan bf = attend_plan(a.req.n, a.req.max_q, a.G, false);   // as the workspace was sized
+    p.a.part = a.part + (few_workspace_bytes(a.req.n, a.req.max_kv, a.H, d, bf.rc) + 255) / 256 * 64;
+  }
+  if (!plan.chunk) return KVC_OK;
   cudaError_t e;
   if (d == 128)
     e = q8 ? launch_chunk<128, true>(p, mk, mv, units * p.nsplit, s) : launch_chunk<128, false>(p, mk, mv, units * p.nsplit, s);

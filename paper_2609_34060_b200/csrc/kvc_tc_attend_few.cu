@@ -1,0 +1,749 @@
+// kvc_attend for few rows a request and KV head (single tokens, short drafts): the keys are the long side, so they take
+// the long side of the products.
+//
+//     S^T = K Q^T   (128 tokens x rows) ,   O^T += V^T P^T   (d x rows) ,
+// a tile of 128 tokens lies in the 128 lanes of tensor memory, a softmax thread owns one token and holds its logits of
+// all rows.  Bound: the bytes of K and V.  The tiles go from HBM to shared memory by TMA and straight into the tensor
+// cores; registers only see rows x 128 logits a tile.
+//
+// Work: all (request, KV head) pairs one after the other form one line of key tiles, of which every SM's block takes an
+// equal part (ragged batches balance to a tile, whatever their lengths).  A block finishes the pairs that lie inside its
+// part; of a pair cut by its borders it leaves a float32 partial result (at most two a block), and a second kernel joins
+// those in a fixed order.
+//
+// Softmax: the running maximum of a row moves only when a logit exceeds it by 2^kLazy (one vote a tile, no reduction
+// otherwise); the sum is kept per thread and added up at the end.
+//
+// 8-bit caches are not converted: the tensor cores take the codes.  A query row is split into two e4m3 parts,
+//     q 2^-b = t1 + t2 / 16   (b the row's exponent; bf16 has 8 significant bits, each part 4: exact but for channels
+//                              below 2^-15 of the row's largest, which are off by at most 2^-22 of it) ,
+// as separate columns of one product, K's scale multiplies the finished logit (a token's scale is its thread's), and
+// V's scale goes into the probability, split into three parts 16 apart (12 bits and a step of 2^-24 of the largest):
+//     p 2^(e_v - E) 64 = t1 + t2 / 16 + t3 / 256 ,   E the largest exponent of a value row so far .
+// Sums and joins are float32.  Over bf16 caches P is rounded to bf16 as in the chunk kernel.
+//
+// Warps: 0-3 softmax and epilogue, 4 TMA producer, 5 MMA issue (one thread), 6 queries of the next pair, 8-11 exponents
+// of the next tiles (8-bit caches).  Every wait is bounded.
+#include <cuda_runtime.h>
+
+#include "kvc_launch.h"
+#include "kvc_tc.h"
+#include "kvc_tc_attend.cuh"
+#include "kvc_tc_attend_few.h"
+
+namespace kvc {
+namespace {
+
+using namespace tc;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct FewLaunch {
+  AttendLaunch a;
+  TileGeo g;
+  int32_t blocks;              // of the main kernel
+  float* part;                 // [blocks][2][RC][D], then [blocks][2][RC][2]
+};
+
+// tiles of a (request, head) pair; 0: the request is not this kernel's
+__device__ __forceinline__ int few_tiles(const AttendLaunch& a, int rc, int nq, int kv) {
+  const int64_t rows = (int64_t)nq * a.G;
+  return rows == 0 || rows > rc ? 0 : kv <= 0 ? 1 : (kv + 127) >> 7;
+}
+
+struct Piece {
+  int b, h, q0, nq, kv, nt, t0, t1;
+};
+
+// A position on the line of tiles: request, head, tile, and how many tiles the walk still takes.
+struct Walk {
+  int64_t left;
+  int b, h, t;
+  __device__ __forceinline__ bool next(const AttendLaunch& a, int rc, Piece& x) {
+    if (left <= 0) return false;
+    for (;; ++b) {
+      if (b >= a.req.n) return false;
+      request_span(a.req, b, nullptr, x.q0, x.nq, x.kv);
+      x.nt = few_tiles(a, rc, x.nq, x.kv);
+      if (x.nt > 0) break;
+    }
+    x.b = b;
+    x.h = h;
+    x.t0 = t;
+    x.t1 = (int64_t)(x.nt - t) < left ? x.nt : t + (int)left;
+    left -= x.t1 - x.t0;
+    t = 0;
+    if (++h == a.H) {
+      h = 0;
+      ++b;
+    }
+    return true;
+  }
+};
+
+__device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {   // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+// tiles of requests [0, n), and with find >= 0 the request in which tile `find` lies (whole warp)
+__device__ __forceinline__ int64_t line_scan(const AttendLaunch& a, int rc, int lane, int n, int64_t find, uint32_t* status, int* fb, int64_t* before) {
+  int64_t total = 0;
+  for (int b0 = 0; b0 < n; b0 += 32) {
+    int64_t mine = 0;
+    if (b0 + lane < n) {
+      int q0, nq, kv;
+      request_span(a.req, b0 + lane, status, q0, nq, kv);
+      mine = (int64_t)few_tiles(a, rc, nq, kv) * a.H;
+    }
+    const int64_t incl = warp_scan(mine, lane);
+    if (find >= 0) {
+      const unsigned hit = __ballot_sync(0xffffffffu, total + incl > find);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        *fb = b0 + l;
+        *before = total + __shfl_sync(0xffffffffu, incl - mine, l);
+        return total;
+      }
+    }
+    total += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return total;
+}
+
+template <int D, bool Q8, int RC>
+struct Few {
+  static constexpr int E = Q8 ? 1 : 2;
+  static constexpr int kTile = 128 * D * E;
+  static constexpr int kSlots = kTile == 32768 ? 6 : Q8 && D == 128 && RC == 32 ? 10 : 12;
+  static constexpr int kQRows = Q8 ? 2 * RC : RC;              // rows of the query operand: N of the first product
+  static constexpr int kQ = kQRows * D * E;
+  static constexpr int kPCols = Q8 ? (RC == 8 ? 32 : 3 * RC) : RC;   // N of the second product
+  static constexpr int kPRow = Q8 ? (RC == 8 ? 32 : RC == 16 ? 64 : 128) : 2 * RC;   // bytes of a token's probabilities
+  static constexpr uint32_t kPSwizzle = kPRow == 32 ? 6 : kPRow == 64 ? 4 : 2;
+  static constexpr uint32_t kRowSwizzle = Q8 && D == 64 ? 4 : 2;
+  static constexpr int kP = 128 * kPRow;
+  static constexpr int kThreads = Q8 ? 384 : 256;
+  static constexpr int kExpRing = 8;
+  static constexpr int kQAlign = (kQ + 1023) / 1024 * 1024;
+  static constexpr int kSmem = 1024 + kSlots * kTile + 2 * kQAlign + 2 * kP + (Q8 ? kExpRing * 1024 : 0);
+  static constexpr uint32_t kTmem = 256;
+  static constexpr uint32_t kOCol = 2 * kQRows;
+  static_assert(kOCol + kPCols <= kTmem, "tensor memory");
+  static_assert(kSmem <= 231000, "shared memory");
+  // p <= 2^kLazy; with 8-bit values 64 p has to stay below 448
+  static constexpr float kLazy = Q8 ? 2.f : 8.f;
+};
+
+struct FewBars {
+  uint64_t full[12], empty[12], s_full[2], p_ready[2], pv_done[2], q_full[2], q_empty[2], e_full[8], e_empty[8];
+  int64_t left;
+  int b, h, t;
+  uint32_t tmem;
+  int abort_flag;
+  float red[4][32];
+  float qs[2][32];
+  int red_e[4], fail[4];
+};
+
+__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// kind::f8f6f4, A = B = e4m3, D = f32
+constexpr uint32_t idesc_e4m3(int M, int N, int a_mn, int b_mn) {
+  return (1u << 4) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* v) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, float* v) {
+  static_assert(N % 8 == 0, "columns");
+#pragma unroll
+  for (int k = 0; k < N; k += 8) tmem_ld8(taddr + k, v + k);
+}
+// 16-byte chunk of a token's row of probabilities under the row's swizzle
+template <int ROW>
+__device__ __forceinline__ int p_chunk(int chunk, int tok) {
+  return ROW == 32 ? chunk ^ ((tok >> 2) & 1) : ROW == 64 ? chunk ^ ((tok >> 1) & 3) : chunk ^ (tok & 7);
+}
+
+template <int D, bool Q8, int RC>
+__global__ void __launch_bounds__(Few<D, Q8, RC>::kThreads, 1)
+attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using F = Few<D, Q8, RC>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ FewBars bars;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* skv = smem;
+  uint8_t* sq = skv + F::kSlots * F::kTile;
+  uint8_t* sp = sq + 2 * F::kQAlign;
+  float* sexp = reinterpret_cast<float*>(sp + 2 * F::kP);          // [kExpRing][2][128]
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  volatile int* abort_flag = &bars.abort_flag;
+  const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), s_full = smem_u32(bars.s_full), p_ready = smem_u32(bars.p_ready);
+  const uint32_t pv_done = smem_u32(bars.pv_done), q_full = smem_u32(bars.q_full), q_empty = smem_u32(bars.q_empty);
+  const uint32_t e_full = smem_u32(bars.e_full), e_empty = smem_u32(bars.e_empty);
+  if (tid == 0) {
+    for (int s = 0; s < F::kSlots; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(s_full + 8 * s, 1);
+      mbar_init(p_ready + 8 * s, 128);
+      mbar_init(pv_done + 8 * s, 1);
+      mbar_init(q_full + 8 * s, 32);
+      mbar_init(q_empty + 8 * s, 1 + 4);                             // the products and the four softmax warps
+    }
+    for (int s = 0; s < F::kExpRing; ++s) {
+      mbar_init(e_full + 8 * s, 32);
+      mbar_init(e_empty + 8 * s, 128);
+    }
+    bars.abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == 5) {
+    tmem_alloc(smem_u32(&bars.tmem), F::kTmem);
+    tmem_relinquish();
+  }
+  if (warp == 4) {
+    // this block's part of the line
+    const int64_t total = line_scan(p.a, RC, lane, p.a.req.n, -1, blockIdx.x == 0 ? p.a.status : nullptr, nullptr, nullptr);
+    const int64_t lo = total * blockIdx.x / p.blocks, hi = total * (blockIdx.x + 1) / p.blocks;
+    int fb = 0;
+    int64_t before = 0;
+    if (hi > lo) line_scan(p.a, RC, lane, p.a.req.n, lo, nullptr, &fb, &before);
+    if (lane == 0) {
+      bars.left = hi - lo;
+      bars.b = fb;
+      bars.h = bars.t = 0;
+      if (hi > lo) {
+        int q0, nq, kv;
+        request_span(p.a.req, fb, nullptr, q0, nq, kv);
+        const int nt = few_tiles(p.a, RC, nq, kv);
+        bars.h = (int)((lo - before) / nt);
+        bars.t = (int)((lo - before) % nt);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars.tmem;
+  Walk walk{bars.left, bars.b, bars.h, bars.t};
+  Piece x;
+  const uint32_t gs = (uint32_t)p.g.gs, ps = (uint32_t)p.g.ps;
+
+  if (warp < 4) {
+    const uint32_t lane_at = tmem + ((uint32_t)(warp * 32) << 16);
+    const uint32_t o_at = lane_at + F::kOCol;
+    const float minus_inf = __uint_as_float(0xff800000u);
+    const float c = p.a.scale * kLog2e;
+    int g = 0, piece = 0;
+    // a failed wait (ok) becomes a decision of all four warps (stop) at the vote of the next tile: a warp that left alone
+    // would leave the others at a barrier
+    bool ok = true, stop = false;
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && wait_all(bar, parity, abort_flag); };
+    while (!stop && walk.next(p.a, RC, x)) {
+      const int R = x.nq * p.a.G;
+      float m[RC], l[RC];
+      int eref = -1000;                                             // 8-bit values: exponent their sums are held under
+#pragma unroll
+      for (int r = 0; r < RC; ++r) {
+        m[r] = minus_inf;
+        l[r] = 0.f;
+      }
+      wait(q_full + 8 * (piece & 1), (piece >> 1) & 1);
+      for (int i = x.t0; i < x.t1; ++i, ++g) {
+        const int buf = g & 1;
+        const int tok = i * 128 + tid;
+        float ek = 1.f;
+        int ev = 0;
+        if (Q8) {
+          const int es = g % F::kExpRing;
+          wait(e_full + 8 * es, (g / F::kExpRing) & 1);
+          ek = sexp[es * 256 + tid];
+          ev = __float_as_int(sexp[es * 256 + 128 + tid]);
+          mbar_arrive(e_empty + 8 * es);
+        }
+        wait(s_full + 8 * buf, (g >> 1) & 1);
+        tc_fence_after();
+        float s[F::kQRows];
+        tmem_ld<F::kQRows>(lane_at + buf * F::kQRows, s);
+        tmem_ld_wait();
+#pragma unroll
+        for (int r = 0; r < RC; ++r) s[r] = Q8 ? fmaf(s[(Q8 ? RC : 0) + r], 0.0625f, s[r]) * (bars.qs[piece & 1][r] * ek) : s[r] * c;
+        if (x.kv - x.nq < i * 128 + 128) {                          // the last keys, or some that early rows do not see
+          const int first = p.a.causal ? x.kv - x.nq : x.kv - 1;
+#pragma unroll
+          for (int r = 0; r < RC; ++r)
+            if (tok > first + (p.a.causal ? r / p.a.G : 0) || r >= R) s[r] = minus_inf;
+        }
+        const bool mine = tok < x.kv;                               // rows behind the last key hold anything
+        bool grow = Q8 && mine && ev > eref;
+#pragma unroll
+        for (int r = 0; r < RC; ++r) grow |= s[r] - m[r] > F::kLazy;
+        if (named_bar_or(1, 128, grow || !ok)) {
+          float keep[RC];
+#pragma unroll
+          for (int r = 0; r < RC; ++r) {
+            float v = s[r];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+            if (lane == 0) bars.red[warp][r] = v;
+          }
+          if (Q8) {
+            const int top = __reduce_max_sync(0xffffffffu, mine ? ev : -1000);
+            if (lane == 0) bars.red_e[warp] = top;
+          }
+          if (lane == 0) bars.fail[warp] = !ok;
+          named_bar_sync(1, 128);
+          if (bars.fail[0] | bars.fail[1] | bars.fail[2] | bars.fail[3]) {
+            stop = true;
+            break;
+          }
+          float oscale = 1.f;
+          if (Q8) {
+            const int top = max(eref, max(max(bars.red_e[0], bars.red_e[1]), max(bars.red_e[2], bars.red_e[3])));
+            oscale = eref == top ? 1.f : top - eref > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (top - eref)) << 23);
+            eref = top;
+          }
+#pragma unroll
+          for (int r = 0; r < RC; ++r) {
+            const float top = fmaxf(m[r], fmaxf(fmaxf(bars.red[0][r], bars.red[1][r]), fmaxf(bars.red[2][r], bars.red[3][r])));
+            keep[r] = top == m[r] ? 1.f : exp2_fast(m[r] - top);
+            m[r] = top;
+            l[r] *= keep[r];
+          }
+          if (i > x.t0) {
+            // the sums so far, once the product that wrote them last is done
+            wait(pv_done + 8 * (buf ^ 1), ((g - 1) >> 1) & 1);
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < (Q8 ? 3 * RC : RC); k += 8) {
+              float o[8];
+              tmem_ld8(o_at + k, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 8; ++j) o[j] *= keep[(k + j) % RC] * oscale;
+              tmem_st8(o_at + k, o);
+            }
+            tmem_st_wait();
+          }
+        }
+        // probabilities; the buffer is free once the product before the last one is done
+        wait(pv_done + 8 * buf, ((g >> 1) & 1) ^ 1);
+        uint8_t* row = sp + buf * F::kP + tid * F::kPRow;
+        float scale_v = 64.f;
+        if (Q8) scale_v = !mine || eref - ev > 120 ? 0.f : 64.f * __uint_as_float((uint32_t)(127 - (eref - ev)) << 23);
+        uint32_t w[F::kPRow / 4];
+#pragma unroll
+        for (int r = 0; r < RC; r += Q8 ? 4 : 2) {
+          float e[4];
+#pragma unroll
+          for (int j = 0; j < (Q8 ? 4 : 2); ++j) {
+            e[j] = exp2_fast(s[r + j] - (m[r + j] == minus_inf ? 0.f : m[r + j]));
+            l[r + j] += e[j];
+          }
+          if (Q8) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] *= scale_v;
+#pragma unroll
+            for (int term = 0; term < 3; ++term) {
+              const uint32_t lo = e4m3x2(e[0], e[1]), hi = e4m3x2(e[2], e[3]);
+              w[(term * RC + r) / 4] = lo | (hi << 16);
+              const float2 a = e4m3x2_to_float2(lo), b = e4m3x2_to_float2(hi);
+              e[0] = (e[0] - a.x) * 16.f;
+              e[1] = (e[1] - a.y) * 16.f;
+              e[2] = (e[2] - b.x) * 16.f;
+              e[3] = (e[3] - b.y) * 16.f;
+            }
+          } else {
+            w[r / 2] = pack2(e[0], e[1]);
+          }
+        }
+#pragma unroll
+        for (int k = (Q8 ? 3 * RC : 2 * RC) / 4; k < F::kPRow / 4; ++k) w[k] = 0;
+#pragma unroll
+        for (int k = 0; k < F::kPRow / 16; ++k)
+          *reinterpret_cast<uint4*>(row + (p_chunk<F::kPRow>(k, tid) << 4)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        if (x.kv < i * 128 + 128) {
+          // stale rows behind the last key: P is zero there, but zero times a stale NaN would not be
+          const int vs = (2 * g + 1) % F::kSlots;
+          wait(full + 8 * vs, ((2 * g + 1) / F::kSlots) & 1);
+          if (tok >= x.kv) {
+            uint8_t* v = skv + vs * F::kTile + (tid >> 3) * gs + (tid & 7) * (Q8 ? D : 128);
+#pragma unroll
+            for (int k = 0; k < D * F::E / 16; ++k) *reinterpret_cast<uint4*>(v + (Q8 ? k << 4 : (k >> 3) * ps + ((k & 7) << 4))) = make_uint4(0, 0, 0, 0);
+          }
+        }
+        fence_proxy_async();
+        tc_fence_before();
+        mbar_arrive(p_ready + 8 * buf);
+      }
+      if (stop) break;
+      // ---- the pair's (or piece's) result
+      wait(pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1);
+      tc_fence_after();
+      float o[F::kPCols];
+      tmem_ld<F::kPCols>(o_at, o);
+      tmem_ld_wait();
+      tc_fence_before();
+      named_bar_sync(1, 128);                                       // everyone is done with red
+#pragma unroll
+      for (int r = 0; r < RC; ++r) {
+        float v = l[r];
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
+        if (lane == 0) bars.red[warp][r] = v;
+      }
+      named_bar_sync(1, 128);
+      const bool whole = x.t0 == 0 && x.t1 == x.nt;
+      const int64_t slot = ((int64_t)blockIdx.x * 2 + (x.t0 > 0 ? 0 : 1)) * RC;
+      float* ml = p.part + (int64_t)p.blocks * 2 * RC * D;
+      const float back = Q8 ? (eref < -900 ? 0.f : exponent_up((uint32_t)eref) * 0.015625f) : 1.f;
+#pragma unroll
+      for (int r = 0; r < RC; ++r) {
+        if (r >= R || !ok) continue;
+        const float sum = (bars.red[0][r] + bars.red[1][r]) + (bars.red[2][r] + bars.red[3][r]);
+        float v = o[r];
+        if (Q8) v = fmaf(fmaf(o[(Q8 ? 2 * RC : 0) + r], 0.0625f, o[(Q8 ? RC : 0) + r]), 0.0625f, v) * back;
+        const bool dead = sum == 0.f;
+        if (dead) v = 0.f;
+        if (whole) {
+          const int64_t at = x.q0 + r / p.a.G;
+          const int head = x.h * p.a.G + r % p.a.G;
+          if (tid < D) p.a.out.p[at * p.a.out.s_row + (int64_t)head * p.a.out.s_head + tid] = __float2bfloat16(dead ? 0.f : v / sum);
+          if (p.a.lse && tid == 0) p.a.lse[at * (p.a.H * p.a.G) + head] = dead ? minus_inf : (m[r] + log2f(sum)) * kLn2;
+        } else {
+          if (tid < D) p.part[(slot + r) * D + tid] = v;
+          if (tid == 0) {
+            ml[(slot + r) * 2] = m[r];
+            ml[(slot + r) * 2 + 1] = sum;
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty + 8 * (piece & 1));
+      ++piece;
+    }
+  } else if (warp == 4) {
+    // ---- producer
+    const uint32_t ring = smem_u32(skv);
+    int slot = 0, phase = 0;
+    bool ok = true;
+    while (ok && walk.next(p.a, RC, x)) {
+      for (int i = x.t0; i < x.t1 && ok; ++i) {
+        const int rows = max(0, min(128, x.kv - i * 128));
+        const int page = tile_page(p.a, p.g, x.b, i * 128, rows, lane);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          if (!wait_all(empty + 8 * slot, phase ^ 1, abort_flag)) {
+            ok = false;
+            break;
+          }
+          tile_load(kv ? &map_v : &map_k, p.a, p.g, ring + slot * F::kTile, full + 8 * slot, i * 128, rows, x.h, page, lane);
+          if (++slot == F::kSlots) {
+            slot = 0;
+            phase ^= 1;
+          }
+        }
+      }
+    }
+  } else if (warp == 5) {
+    // ---- products: the next tile's logits are issued before this tile's values
+    if (lane == 0) {
+      constexpr uint32_t idesc_s = Q8 ? idesc_e4m3(128, F::kQRows, 0, 0) : idesc_bf16(128, F::kQRows, 0, 0);
+      constexpr uint32_t idesc_o = Q8 ? idesc_e4m3(128, F::kPCols, 1, 1) : idesc_bf16(128, F::kPCols, 1, 1);
+      constexpr int kStepsS = Q8 ? D / 32 : D / 16, kStepsO = Q8 ? 4 : 8;
+      constexpr uint32_t kQGroup = Q8 ? 8 * D : 1024;
+      const uint32_t kv0 = smem_u32(skv), q0 = smem_u32(sq), p0 = smem_u32(sp);
+      const uint32_t v_lbo = D == 128 && !Q8 ? ps : 0u;             // d = 64: the upper 64 rows of the product repeat the lower
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (ok) ok = mbar_wait(bar, parity, abort_flag);
+        return ok;
+      };
+      // two walks: one for the logits, which run a tile ahead, one for the values
+      int gk = 0, pk = 0, ik = 0;
+      Piece xk;
+      bool more = walk.next(p.a, RC, xk);
+      if (more) ik = xk.t0;
+      auto score = [&]() {
+        const int ks = (2 * gk) % F::kSlots;
+        if (ik == xk.t0 && !wait(q_full + 8 * (pk & 1), (pk >> 1) & 1)) return;
+        if (!wait(full + 8 * ks, ((2 * gk) / F::kSlots) & 1)) return;
+        tc_fence_after();
+        const uint32_t ka = kv0 + ks * F::kTile, qa = q0 + (pk & 1) * F::kQAlign;
+#pragma unroll
+        for (int k = 0; k < kStepsS; ++k) {
+          if (Q8)
+            umma_f8(tmem + (gk & 1) * F::kQRows, operand_desc(ka + k * 32, 16, gs, F::kRowSwizzle), operand_desc(qa + k * 32, 16, kQGroup, F::kRowSwizzle),
+                    idesc_s, k > 0);
+          else
+            umma_bf16(tmem + (gk & 1) * F::kQRows, operand_desc(ka + (k >> 2) * ps + (k & 3) * 32, 16, gs, 2),
+                      operand_desc(qa + (k >> 2) * (RC * 128) + (k & 3) * 32, 16, kQGroup, 2), idesc_s, k > 0);
+        }
+        umma_commit(s_full + 8 * (gk & 1));
+        umma_commit(empty + 8 * ks);
+        ++gk;
+        if (++ik == xk.t1) {
+          umma_commit(q_empty + 8 * (pk & 1));
+          ++pk;
+          more = walk.next(p.a, RC, xk);
+          if (more) ik = xk.t0;
+        }
+      };
+      int gv = 0;
+      Walk wv{bars.left, bars.b, bars.h, bars.t};
+      if (more) score();
+      while (ok && wv.next(p.a, RC, x)) {
+        for (int i = x.t0; i < x.t1 && ok; ++i, ++gv) {
+          if (more) score();
+          const int vs = (2 * gv + 1) % F::kSlots;
+          if (!wait(p_ready + 8 * (gv & 1), (gv >> 1) & 1) || !wait(full + 8 * vs, ((2 * gv + 1) / F::kSlots) & 1)) break;
+          tc_fence_after();
+          const uint32_t va = kv0 + vs * F::kTile, pa = p0 + (gv & 1) * F::kP;
+#pragma unroll
+          for (int k = 0; k < kStepsO; ++k) {
+            const uint64_t bd = operand_desc(pa + k * (Q8 ? 32 : 16) * F::kPRow, 0, 8 * F::kPRow, F::kPSwizzle);
+            if (Q8)
+              umma_f8(tmem + F::kOCol, operand_desc(va + k * 4 * gs, v_lbo, gs, F::kRowSwizzle), bd, idesc_o, i > x.t0 || k > 0);
+            else
+              umma_bf16(tmem + F::kOCol, operand_desc(va + k * 2 * gs, v_lbo, gs, 2), bd, idesc_o, i > x.t0 || k > 0);
+          }
+          umma_commit(empty + 8 * vs);
+          umma_commit(pv_done + 8 * (gv & 1));
+        }
+      }
+    }
+  } else if (warp == 6) {
+    // ---- queries of the pairs, one pair ahead
+    constexpr int LPR = D / 8, RPP = 32 / LPR;
+    const int ch = lane % LPR;
+    const float c = p.a.scale * kLog2e;
+    int piece = 0;
+    while (walk.next(p.a, RC, x)) {
+      if (!wait_all(q_empty + 8 * (piece & 1), ((piece >> 1) & 1) ^ 1, abort_flag)) break;
+      uint8_t* dst = sq + (piece & 1) * F::kQAlign;
+      const int R = x.nq * p.a.G;
+#pragma unroll 4
+      for (int r0 = 0; r0 < RC; r0 += RPP) {
+        const int r = r0 + lane / LPR;
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (r < R)
+          raw = *reinterpret_cast<const uint4*>(p.a.q.p + (int64_t)(x.q0 + r / p.a.G) * p.a.q.s_row + (int64_t)(x.h * p.a.G + r % p.a.G) * p.a.q.s_head + ch * 8);
+        if (!Q8) {
+          *reinterpret_cast<uint4*>(dst + (ch >> 3) * (RC * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = raw;
+        } else {
+          float v[8];
+          unpack8(raw, v);
+          float top = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
+#pragma unroll
+          for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const bool finite = top < __uint_as_float(0x7f800000u);
+          const uint32_t b = finite ? row_exponent(top) : 127u;
+          const float down = exponent_down(b);
+#pragma unroll
+          for (int term = 0; term < 2; ++term) {
+            uint2 code;
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float lo = v[2 * j], hi = v[2 * j + 1];
+              if (term == 0) {
+                lo *= down;
+                hi *= down;
+                if (!(fabsf(lo) < __uint_as_float(0x7f800000u))) lo = __uint_as_float(0x7fc00000u);   // infinities give NaN logits
+                if (!(fabsf(hi) < __uint_as_float(0x7f800000u))) hi = __uint_as_float(0x7fc00000u);
+              }
+              w[j] = e4m3x2(lo, hi);
+              const float2 f = e4m3x2_to_float2(w[j]);
+              v[2 * j] = (lo - f.x) * 16.f;
+              v[2 * j + 1] = (hi - f.y) * 16.f;
+            }
+            code.x = w[0] | (w[1] << 16);
+            code.y = w[2] | (w[3] << 16);
+            const int rr = term * RC + r;
+            const int chunk = D == 128 ? (ch >> 1) ^ (rr & 7) : (ch >> 1) ^ ((rr >> 1) & 3);
+            *reinterpret_cast<uint2*>(dst + rr * D + (chunk << 4) + (ch & 1) * 8) = code;
+          }
+          if (ch == 0) bars.qs[piece & 1][r] = exponent_up(b) * c;
+        }
+      }
+      fence_proxy_async();
+      mbar_arrive(q_full + 8 * (piece & 1));
+      ++piece;
+    }
+  } else if (Q8 && warp >= 8) {
+    // ---- exponents of the tiles, four tokens a lane, every fourth tile a warp
+    int g = 0;
+    bool ok = true;
+    while (ok && walk.next(p.a, RC, x)) {
+      for (int i = x.t0; i < x.t1 && ok; ++i, ++g) {
+        if ((g & 3) != warp - 8) continue;
+        const int es = g % F::kExpRing, tok = i * 128 + lane * 4;
+        float k4[4];
+        int v4[4];
+        int page = 0;
+        if (tok < x.kv && p.g.paged) page = request_page(p.a.req, p.a.c, x.b, tok, nullptr);
+        const int64_t base = (int64_t)p.a.layer * p.a.e.s_layer + (int64_t)x.h * p.a.e.s_head +
+                             (p.g.paged ? (int64_t)page * p.a.e.s_page + (int64_t)(tok & p.a.c.page_mask) * p.a.e.s_tok : (int64_t)tok * p.a.e.s_tok);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          k4[j] = 1.f;
+          v4[j] = 0;
+          if (tok + j < x.kv && page >= 0) {
+            k4[j] = exponent_up(p.a.e.k[base + j * p.a.e.s_tok]);
+            v4[j] = p.a.e.v[base + j * p.a.e.s_tok];
+          }
+        }
+        if (!wait_all(e_empty + 8 * es, ((g / F::kExpRing) & 1) ^ 1, abort_flag)) {
+          ok = false;
+          break;
+        }
+        *reinterpret_cast<float4*>(sexp + es * 256 + lane * 4) = make_float4(k4[0], k4[1], k4[2], k4[3]);
+        *reinterpret_cast<int4*>(sexp + es * 256 + 128 + lane * 4) = make_int4(v4[0], v4[1], v4[2], v4[3]);
+        mbar_arrive(e_full + 8 * es);
+      }
+    }
+  }
+  __syncthreads();
+  if (*abort_flag) {
+    // copies may still be in flight: give them time to land before the block's memory is handed on
+    const long long t0 = clock64();
+    while (clock64() - t0 < kWaitLimitCycles / 8) {
+    }
+    if (tid == 0) atomicOr(p.a.status, KVC_FLAG_WAIT_EXPIRED);
+    __syncthreads();
+  }
+  if (warp == 5) {
+    tc_fence_after();
+    tmem_dealloc(tmem, F::kTmem);
+  }
+}
+
+// ---- join of the pieces of a pair that block borders cut; grid: x = (request, head) pairs, y = groups of 4 rows
+template <int D, int RC>
+__global__ void __launch_bounds__(4 * D) attend_few_join_kernel(const __grid_constant__ FewLaunch p) {
+  __shared__ int64_t s_total, s_before;
+  __shared__ int s_nt;
+  const int b = (int)(blockIdx.x / p.a.H), h = (int)(blockIdx.x % p.a.H);
+  const int r = (int)blockIdx.y * 4 + threadIdx.x / D, ch = threadIdx.x % D;
+  int q0, nq, kv;
+  request_span(p.a.req, b, nullptr, q0, nq, kv);
+  const int nt = few_tiles(p.a, RC, nq, kv), R = nq * p.a.G;
+  if (nt == 0 || (int)blockIdx.y * 4 >= R) return;
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    const int64_t before = line_scan(p.a, RC, lane, b, -1, nullptr, nullptr, nullptr);
+    const int64_t total = line_scan(p.a, RC, lane, p.a.req.n, -1, nullptr, nullptr, nullptr);
+    if (lane == 0) {
+      s_before = before;
+      s_total = total;
+      s_nt = nt;
+    }
+  }
+  __syncthreads();
+  const int64_t w0 = s_before + (int64_t)h * nt, w1 = w0 + nt, total = s_total, C = p.blocks;
+  const int64_t c0 = ((w0 + 1) * C + total - 1) / total - 1, c1 = (w1 * C + total - 1) / total - 1;   // blocks of the first and last tile
+  if (c0 == c1 || r >= R) return;
+  const float minus_inf = __uint_as_float(0xff800000u);
+  const float* ml = p.part + C * 2 * RC * D;
+  float m = minus_inf;
+  for (int64_t cc = c0; cc <= c1; ++cc) {
+    const int64_t lo = total * cc / C, hi = total * (cc + 1) / C;
+    if (hi <= lo) continue;
+    const int64_t at = (cc * 2 + (lo > w0 ? 0 : 1)) * RC + r;
+    if (ml[2 * at + 1] != 0.f) m = fmaxf(m, ml[2 * at]);
+  }
+  float l = 0.f, acc = 0.f;
+#pragma unroll 4
+  for (int64_t cc = c0; cc <= c1; ++cc) {
+    const int64_t lo = total * cc / C, hi = total * (cc + 1) / C;
+    if (hi <= lo) continue;
+    const int64_t at = (cc * 2 + (lo > w0 ? 0 : 1)) * RC + r;
+    const float ls = ml[2 * at + 1], w = ls == 0.f ? 0.f : exp2f(ml[2 * at] - m);
+    l += w * ls;
+    acc += w * p.part[at * D + ch];
+  }
+  const bool dead = l == 0.f;
+  const int64_t row = q0 + r / p.a.G;
+  const int head = h * p.a.G + r % p.a.G;
+  p.a.out.p[row * p.a.out.s_row + (int64_t)head * p.a.out.s_head + ch] = __float2bfloat16(dead ? 0.f : acc / l);
+  if (p.a.lse && ch == 0) p.a.lse[row * (p.a.H * p.a.G) + head] = dead ? minus_inf : (m + log2f(l)) * kLn2;
+}
+
+template <int D, bool Q8, int RC>
+cudaError_t launch(const FewLaunch& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
+  using F = Few<D, Q8, RC>;
+  static DeviceOnce once;
+  int dev;
+  if (once.pending(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(attend_few_kernel<D, Q8, RC>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem);
+    if (e != cudaSuccess) return e;
+    once.mark(dev);
+  }
+  attend_few_kernel<D, Q8, RC><<<(unsigned)p.blocks, F::kThreads, F::kSmem, s>>>(p, mk, mv);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const dim3 g((unsigned)((int64_t)p.a.req.n * p.a.H), (unsigned)((RC + 3) / 4));
+  attend_few_join_kernel<D, RC><<<g, 4 * D, 0, s>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+// rows the kernel is built for, from the rows a request may have (0: more than it takes)
+int few_capacity(int64_t rows, bool q8) { return rows <= 8 && q8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 0; }
+
+int few_blocks(int n, int max_kv, int H) {
+  const int64_t tiles = (int64_t)n * H * (max_kv <= 0 ? 1 : (max_kv + 127) / 128);
+  const int sms = device_sm_count();
+  return (int)(tiles < sms ? tiles : sms);
+}
+
+size_t few_workspace_bytes(int n, int max_kv, int H, int d, int rc) { return (size_t)few_blocks(n, max_kv, H) * 2 * rc * (d + 2) * 4; }
+
+cudaError_t launch_attend_few(const AttendLaunch& a, const tc::TileGeo& g, const CUtensorMap& mk, const CUtensorMap& mv, int rc, int d, float* part,
+                              cudaStream_t s) {
+  FewLaunch p;
+  p.a = a;
+  p.g = g;
+  p.blocks = few_blocks(a.req.n, a.req.max_kv, a.H);
+  p.part = part;
+  const bool q8 = a.e.k != nullptr;
+  if (p.blocks <= 0) return cudaErrorInvalidConfiguration;
+#define KVC_FEW(D, Q, R) \
+  if (d == D && q8 == Q && rc == R) return launch<D, Q, R>(p, mk, mv, s);
+  KVC_FEW(128, false, 16) KVC_FEW(128, false, 32) KVC_FEW(64, false, 16) KVC_FEW(64, false, 32)
+  KVC_FEW(128, true, 8) KVC_FEW(128, true, 16) KVC_FEW(128, true, 32) KVC_FEW(64, true, 8) KVC_FEW(64, true, 16) KVC_FEW(64, true, 32)
+#undef KVC_FEW
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace kvc
