@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import torch
@@ -142,14 +143,11 @@ def load(path: Optional[str] = None):
     lib.kvc_token_weights_workspace_bytes.restype = sz
     lib.kvc_gate_distance.argtypes = [PC, PS, i32, i32, vp, vp]
     lib.kvc_gate_weights.argtypes = [vp, i32, C.c_double, vp, vp, vp]
-    PQ, PRq, PH = C.POINTER(kvc_qcache), C.POINTER(kvc_requests), C.POINTER(kvc_heads)
-    lib.kvc_quantize.argtypes = [PC, PQ, vp]
-    lib.kvc_dequantize.argtypes = [PQ, PC, vp]
-    lib.kvc_append.argtypes = [PRq, PH, PH, i32, PC, vp]
-    lib.kvc_append_q8.argtypes = [PRq, PH, PH, i32, PQ, vp]
-    lib.kvc_attend.argtypes = [PRq, PH, PC, i32, C.c_double, i32, PH, vp, vp, sz, vp]
-    lib.kvc_attend_q8.argtypes = [PRq, PH, PQ, i32, C.c_double, i32, PH, vp, vp, sz, vp]
-    lib.kvc_attend_workspace_bytes.argtypes = [PRq, i32, i32, i32]
+    # the calls of a serving step: descriptors go in as addresses (no pointer objects are made per call)
+    lib.kvc_quantize.argtypes = lib.kvc_dequantize.argtypes = [vp, vp, vp]
+    lib.kvc_append.argtypes = lib.kvc_append_q8.argtypes = [vp, vp, vp, i32, vp, vp]
+    lib.kvc_attend.argtypes = lib.kvc_attend_q8.argtypes = [vp, vp, vp, i32, C.c_double, i32, vp, vp, vp, sz, vp]
+    lib.kvc_attend_workspace_bytes.argtypes = [vp, i32, i32, i32]
     lib.kvc_attend_workspace_bytes.restype = sz
     lib.kvc_status_poll.argtypes = [C.POINTER(C.c_uint32)]
     lib.kvc_status_reset.argtypes = []
@@ -323,6 +321,9 @@ class Requests:
         self._pages = 0 if page_table is None else int(page_table.shape[1])
         self._struct = kvc_requests(self.n, self.max_q, self.max_kv, stride, q_begin.data_ptr(), kv_len.data_ptr(),
                                     0 if page_table is None else page_table.data_ptr())
+        self._at = C.addressof(self._struct)
+        devs = {t.get_device() for t in (q_begin, kv_len, page_table) if t is not None}
+        self._dev = devs.pop() if len(devs) == 1 else -1
 
     def struct(self) -> kvc_requests:
         return self._struct
@@ -750,75 +751,90 @@ def kvc_gate_weights(dist_sq: torch.Tensor, g: torch.Tensor, entropy: torch.Tens
                                    _stream(stream)), "kvc_gate_weights")
 
 
-def _heads(t: torch.Tensor, what: str) -> kvc_heads:
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.stride(2) != 1:
-        raise KvcError(KVC_E_INVALID_ARG, f"{what}: bf16 [rows, heads, d] with contiguous channels expected")
-    rows, heads, _ = t.shape
-    if (rows > 1 and t.stride(0) == 0) or (heads > 1 and t.stride(1) == 0):
-        raise KvcError(KVC_E_UNSUPPORTED, f"{what}: broadcast rows")
-    return kvc_heads(t.data_ptr(), rows, heads, t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 else 0)
+_HEADS = struct.Struct("@QiiQQ")      # kvc_heads
 
 
-def _one_device(what: str, *tensors) -> None:
-    """All on the current CUDA device (the one the library launches on)."""
-    cur = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != cur):
-            raise KvcError(KVC_E_INVALID_ARG, f"{what}: tensors on cuda:{cur}, the current device, expected")
-
-
-def _cache_tensors(c):
-    return (c.k, c.v, c.page_table) + ((c.scale_k, c.scale_v) if isinstance(c, QCache) else ())
-
-
-def _step_check(req: Requests, c, d: int, what: str) -> None:
-    if d != c.d:
+def _heads(t: torch.Tensor, d: int, what: str) -> bytes:
+    """A kvc_heads over bf16 [rows, heads, d] with contiguous channels."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 3:
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: bf16 [rows, heads, d] expected")
+    (rows, heads, dd), (s_row, s_head, s_ch) = t.shape, t.stride()
+    if dd != d:
         raise KvcError(KVC_E_SHAPE, what)
+    if s_ch != 1 or (rows > 1 and s_row == 0) or (heads > 1 and s_head == 0):
+        raise KvcError(KVC_E_UNSUPPORTED, f"{what}: contiguous channels and no broadcast rows expected")
+    return _HEADS.pack(t.data_ptr(), rows, heads, s_row if rows > 1 else 0, s_head if heads > 1 else 0)
+
+
+def _desc(c):
+    """(address of the descriptor of a Cache or QCache, its device), made again when its tensors or length changed."""
+    q8 = type(c) is QCache
+    key = (c.k.data_ptr(), c.v.data_ptr(), c.T, -1 if c.page_table is None else c.page_table.data_ptr()) + \
+        ((c.scale_k.data_ptr(), c.scale_v.data_ptr()) if q8 else ())
+    got = c.__dict__.get("_made")
+    if got is None or got[0] != key:
+        devs = {t.get_device() for t in (c.k, c.v, c.page_table) + ((c.scale_k, c.scale_v) if q8 else ()) if t is not None}
+        s = c.struct()
+        got = c.__dict__["_made"] = (key, C.addressof(s), devs.pop() if len(devs) == 1 else -1, s)
+    return got
+
+
+def _here(what: str, stream, made, *tensors):
+    """The stream to launch on; everything has to live on the current CUDA device, the one the library launches on."""
+    cur = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+    for dev in made:
+        if dev != cur:
+            raise KvcError(KVC_E_INVALID_ARG, f"{what}: tensors on the current CUDA device expected")
+    for t in tensors:
+        if t is not None and t.get_device() != cur:
+            raise KvcError(KVC_E_INVALID_ARG, f"{what}: tensors on the current CUDA device expected")
+    return torch._C._cuda_getCurrentRawStream(cur) if stream is None else _stream(stream)
+
+
+def _holds(req: Requests, c, what: str) -> None:
     if req.page_table is not None and c.page_table is not None and req.max_kv > req._pages * c.page:
         raise KvcError(KVC_E_SHAPE, what)
 
 
 def kvc_quantize(src: Cache, dst: QCache, stream=None) -> None:
     """dst = e4m3(src), one power-of-two scale per (layer, head, token)."""
-    _one_device("kvc_quantize", *_cache_tensors(src), *_cache_tensors(dst))
-    s, d = src.struct(), dst.struct()
-    _check(load().kvc_quantize(C.byref(s), C.byref(d), _stream(stream)), "kvc_quantize")
+    s, d = _desc(src), _desc(dst)
+    st = _here("kvc_quantize", stream, (s[2], d[2]))
+    _check(load().kvc_quantize(s[1], d[1], st), "kvc_quantize")
 
 
 def kvc_dequantize(src: QCache, dst: Cache, stream=None) -> None:
     """dst = bf16(code * 2^(exponent - 127))."""
-    _one_device("kvc_dequantize", *_cache_tensors(src), *_cache_tensors(dst))
-    s, d = src.struct(), dst.struct()
-    _check(load().kvc_dequantize(C.byref(s), C.byref(d), _stream(stream)), "kvc_dequantize")
+    s, d = _desc(src), _desc(dst)
+    st = _here("kvc_dequantize", stream, (s[2], d[2]))
+    _check(load().kvc_dequantize(s[1], d[1], st), "kvc_dequantize")
 
 
 def kvc_append(req: Requests, k_new: torch.Tensor, v_new: torch.Tensor, cache, layer: int, stream=None) -> None:
     """Write the new tokens' rows [rows, H, d] into `layer` of a Cache, or quantised into a QCache."""
-    _one_device("kvc_append", k_new, v_new, req.q_begin, req.kv_len, req.page_table, *_cache_tensors(cache))
-    _step_check(req, cache, k_new.shape[-1], "kvc_append")
-    _step_check(req, cache, v_new.shape[-1], "kvc_append")
-    c, k, v = cache.struct(), _heads(k_new, "k_new"), _heads(v_new, "v_new")
-    fn = load().kvc_append_q8 if isinstance(cache, QCache) else load().kvc_append
-    _check(fn(C.byref(req._struct), C.byref(k), C.byref(v), int(layer), C.byref(c), _stream(stream)), "kvc_append")
+    c, k, v = _desc(cache), _heads(k_new, cache.d, "k_new"), _heads(v_new, cache.d, "v_new")
+    st = _here("kvc_append", stream, (c[2], req._dev), k_new, v_new)
+    _holds(req, cache, "kvc_append")
+    fn = load().kvc_append_q8 if type(cache) is QCache else load().kvc_append
+    _check(fn(req._at, k, v, int(layer), c[1], st), "kvc_append")
 
 
 def kvc_attend_workspace_bytes(req: Requests, cache, n_heads: int) -> int:
-    return int(load().kvc_attend_workspace_bytes(C.byref(req._struct), int(n_heads), cache.H, cache.d))
+    return int(load().kvc_attend_workspace_bytes(req._at, int(n_heads), cache.H, cache.d))
 
 
 def kvc_attend(req: Requests, q: torch.Tensor, cache, layer: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
                scale: Optional[float] = None, causal: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
     """Attention of the new tokens' queries [rows, heads, d] over `layer` of a Cache or QCache (scale: 1 / sqrt(d))."""
-    _one_device("kvc_attend", q, out, workspace, lse, req.q_begin, req.kv_len, req.page_table, *_cache_tensors(cache))
-    _step_check(req, cache, q.shape[-1], "kvc_attend")
-    _step_check(req, cache, out.shape[-1], "kvc_attend")
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != tuple(q.shape[:2])):
+    c, hq, ho = _desc(cache), _heads(q, cache.d, "q"), _heads(out, cache.d, "out")
+    st = _here("kvc_attend", stream, (c[2], req._dev), q, out, workspace, lse)
+    _holds(req, cache, "kvc_attend")
+    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
         raise KvcError(KVC_E_INVALID_ARG, "kvc_attend: lse must be float32 [rows, heads]")
-    c, hq, ho = cache.struct(), _heads(q, "q"), _heads(out, "out")
-    fn = load().kvc_attend_q8 if isinstance(cache, QCache) else load().kvc_attend
-    _check(fn(C.byref(req._struct), C.byref(hq), C.byref(c), int(layer), cache.d ** -0.5 if scale is None else float(scale),
-              int(bool(causal)), C.byref(ho), 0 if lse is None else lse.data_ptr(), 0 if workspace is None else workspace.data_ptr(),
-              0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "kvc_attend")
+    fn = load().kvc_attend_q8 if type(cache) is QCache else load().kvc_attend
+    _check(fn(req._at, hq, c[1], int(layer), cache.d ** -0.5 if scale is None else float(scale), bool(causal), ho,
+              None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
+              0 if workspace is None else workspace.numel() * workspace.element_size(), st), "kvc_attend")
 
 
 def kvc_status_poll() -> int:

@@ -19,9 +19,16 @@ __device__ uint32_t g_status_word;
 static thread_local int tl_path_force = KVC_PATH_AUTO;
 static thread_local int tl_last_path = KVC_PATH_AUTO;
 
+// The word's address is fixed for as long as the library is loaded on a device: looked up once per device.
 uint32_t* status_word_ptr() {
-  uint32_t* p = nullptr;
+  static std::atomic<uint32_t*> cache[64];
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  const bool cacheable = dev >= 0 && dev < 64;
+  uint32_t* p = cacheable ? cache[dev].load(std::memory_order_acquire) : nullptr;
+  if (p) return p;
   if (cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_status_word) != cudaSuccess) return nullptr;
+  if (cacheable) cache[dev].store(p, std::memory_order_release);
   return p;
 }
 

@@ -90,7 +90,7 @@ int append_common(const kvc_requests* req, const kvc_heads* kn, const kvc_heads*
   if (layer < 0 || layer >= geo->L) return KVC_E_INVALID_ARG;
   if ((rc = resolve_heads(kn, geo->d, &a.kn, &ek)) != KVC_OK || (rc = resolve_heads(vn, geo->d, &a.vn, &ev)) != KVC_OK) return rc;
   if (kn->n_heads != geo->H || vn->n_heads != geo->H || kn->n_rows != vn->n_rows) return KVC_E_SHAPE;
-  if (geo->H > 32767) return KVC_E_UNSUPPORTED;
+  if (geo->H > 32767 || (req && (int64_t)req->max_q * geo->H * 2 >= (int64_t)1 << 31)) return KVC_E_UNSUPPORTED;
   if ((rc = resolve_requests(req, geo, kn->n_rows, &a.req)) != KVC_OK) return rc;
   if (!req->page_table && req->n > 1) return KVC_E_INVALID_ARG;
   const int64_t reach = cache_reach(geo, a.dst);

@@ -6,8 +6,9 @@
 // Multiplying by a power of two is exact, so the only rounding is the one to e4m3 (to nearest even), and decoding is
 // exact in bf16 (at e = 120, where 256 * 2^e would leave its range, magnitudes stop at 240 * 2^e).  All of it is bound by the bytes moved: 3 d + 1 a row to convert, 4 d or 3 d + 1 to append.
 //
-// Layout of the work: d / 8 neighbouring lanes hold one row (a 16-byte load of 8 bf16 values a lane, an 8-byte store of
-// 8 codes), the row's maximum is a butterfly over those lanes.
+// Layout of the work: d / 16 neighbouring lanes hold one row, 16 channels each (two 16-byte loads of bf16, one 16-byte
+// store of codes).  The row's maximum is taken on the bit patterns (magnitudes of bf16 order like integers), two at a
+// time, then a butterfly over the row's lanes.
 #include <cuda_runtime.h>
 
 #include "kvc_attend.h"
@@ -16,47 +17,63 @@
 namespace kvc {
 namespace {
 
-// 8 values of a row -> 8 codes and the row's exponent (the same in all LPR lanes of the row)
+// 16 values of a row -> 16 codes and the row's exponent (the same in all LPR lanes of the row)
 template <int LPR>
-__device__ __forceinline__ uint2 encode8(const uint4& raw, uint32_t& b) {
-  float x[8];
-  unpack8(raw, x);
-  float m = 0.f;
+__device__ __forceinline__ uint4 encode16(const uint4& lo, const uint4& hi, uint32_t& b) {
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  uint32_t m = w[0] & 0x7fff7fffu;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+  uint32_t top = max(m & 0xffffu, m >> 16);
+  const bool odd = top >= 0x7f00u;             // near the end of the range, or an infinity or NaN in the row (the same in all its lanes)
+  if (__any_sync(0xffffffffu, odd)) {
+    // infinities become NaN too (e4m3 has none, and 448 would be a plausible number); neither counts towards the scale
+    uint32_t f = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t a = w[i] & 0x7fffu, c = (w[i] >> 16) & 0x7fffu;
+      if (a < 0x7f80u) f = max(f, a);
+      if (c < 0x7f80u) f = max(f, c);
+      if (a >= 0x7f80u) w[i] |= 0x7fffu;
+      if (c >= 0x7f80u) w[i] |= 0x7fff0000u;
+    }
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) f = max(f, __shfl_xor_sync(0xffffffffu, f, o));
+    top = f;
+  }
+  b = row_exponent(__uint_as_float(top << 16));
+  const float s = exponent_down(b);
+  float x[16];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float a = fabsf(x[i]);
-    if (a < __uint_as_float(0x7f800000u))
-      m = fmaxf(m, a);
-    else
-      x[i] = __uint_as_float(0x7fc00000u);   // infinities too: e4m3 has none, and 448 would be a plausible number
+    x[2 * i] = __uint_as_float(w[i] << 16) * s;
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u) * s;
   }
+  if (b == 247u) {                             // the next code, 256 * 2^120 = 2^128, is no finite bf16
 #pragma unroll
-  for (int o = LPR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  b = row_exponent(m);
-  const float s = exponent_down(b);
-  if (b == 247u) {                           // the next code, 256 * 2^120 = 2^128, is no finite bf16
-    const float top = 240.f * exponent_up(b);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (fabsf(x[i]) > top) x[i] = copysignf(top, x[i]);
+    for (int i = 0; i < 16; ++i)
+      if (fabsf(x[i]) > 240.f) x[i] = copysignf(240.f, x[i]);
   }
-  uint2 c;
-  c.x = e4m3x2(x[0] * s, x[1] * s) | (e4m3x2(x[2] * s, x[3] * s) << 16);
-  c.y = e4m3x2(x[4] * s, x[5] * s) | (e4m3x2(x[6] * s, x[7] * s) << 16);
-  return c;
+  uint32_t c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = e4m3x2(x[4 * i], x[4 * i + 1]) | (e4m3x2(x[4 * i + 2], x[4 * i + 3]) << 16);
+  return make_uint4(c[0], c[1], c[2], c[3]);
 }
 
-__device__ __forceinline__ uint4 decode8(const uint2& c, uint32_t b) {
+__device__ __forceinline__ void decode16(const uint4& c, uint32_t b, uint4& lo, uint4& hi) {
   const float s = exponent_up(b);
-  float x[8];
-  const uint32_t w[4] = {c.x & 0xffffu, c.x >> 16, c.y & 0xffffu, c.y >> 16};
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+  uint32_t o[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 f = e4m3x2_to_float2(w[i]);
-    x[2 * i] = f.x * s;
-    x[2 * i + 1] = f.y * s;
+    const float2 f = e4m3x2_to_float2(w[i] & 0xffffu), g = e4m3x2_to_float2(w[i] >> 16);
+    o[2 * i] = pack2(f.x * s, f.y * s);
+    o[2 * i + 1] = pack2(g.x * s, g.y * s);
   }
-  return pack8(x);
+  lo = make_uint4(o[0], o[1], o[2], o[3]);
+  hi = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
 // element offset of row (l, h, t); -1 when the table names no page
@@ -77,122 +94,153 @@ __device__ __forceinline__ int own_page(const DevCache& c, int t, uint32_t* stat
 }
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
 
-// grid: x = token blocks, y = head x (K|V), z = layers (strided)
-template <int D, bool TO8>
+// grid: x = token blocks, y = head x (K|V), z = layers (strided).  A thread keeps kUnroll rows in flight.
+template <int D, bool TO8, int kUnroll>
 __global__ void __launch_bounds__(kThreads) convert_kernel(const __grid_constant__ ConvertLaunch p) {
-  constexpr int LPR = D / 8, RPP = kThreads / LPR;
+  constexpr int LPR = D / 16, RPP = kThreads / LPR;
   const int lane = threadIdx.x % LPR, row = threadIdx.x / LPR;
   const int h = blockIdx.y >> 1, is_v = blockIdx.y & 1;
   const int t0 = blockIdx.x * (RPP * kUnroll);
-  __nv_bfloat16* bf = is_v ? p.bf.v : p.bf.k;
-  uint8_t* q8 = reinterpret_cast<uint8_t*>(is_v ? p.q8.v : p.q8.k);
+  __nv_bfloat16* bf = (is_v ? p.bf.v : p.bf.k) + lane * 16;
+  uint8_t* q8 = reinterpret_cast<uint8_t*>(is_v ? p.q8.v : p.q8.k) + lane * 16;
   uint8_t* ex = is_v ? p.e.v : p.e.k;
+  int pb[kUnroll], pq[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int t = t0 + u * RPP + row;
+    pb[u] = t < p.T ? own_page(p.bf, t, p.status) : -1;
+    pq[u] = t < p.T ? own_page(p.q8, t, p.status) : -1;
+  }
   for (int l = blockIdx.z; l < p.L; l += gridDim.z) {
-    int64_t ob[kUnroll], oq[kUnroll], oe[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int t = t0 + u * RPP + row;
-      ob[u] = oq[u] = oe[u] = -1;
-      if (t < p.T) {
-        const int pb = own_page(p.bf, t, p.status), pq = own_page(p.q8, t, p.status);
-        if (pb >= 0 && pq >= 0) {
-          ob[u] = row_off(p.bf, l, h, t, pb) + lane * 8;
-          oq[u] = row_off(p.q8, l, h, t, pq) + lane * 8;
-          oe[u] = exp_off(p.e, p.q8, l, h, t, pq);
-        }
-      }
-    }
     if (TO8) {
-      uint4 raw[kUnroll];
+      uint4 lo[kUnroll], hi[kUnroll];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) raw[u] = ob[u] >= 0 ? __ldcs(reinterpret_cast<const uint4*>(bf + ob[u])) : make_uint4(0, 0, 0, 0);
+      for (int u = 0; u < kUnroll; ++u) {
+        lo[u] = hi[u] = make_uint4(0, 0, 0, 0);
+        if (pb[u] < 0 || pq[u] < 0) continue;
+        const uint4* src = reinterpret_cast<const uint4*>(bf + row_off(p.bf, l, h, t0 + u * RPP + row, pb[u]));
+        lo[u] = __ldcs(src);
+        hi[u] = __ldcs(src + 1);
+      }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         uint32_t b;
-        const uint2 c = encode8<LPR>(raw[u], b);   // every lane takes part in the shuffles
-        if (ob[u] >= 0) {
-          *reinterpret_cast<uint2*>(q8 + oq[u]) = c;
-          if (lane == 0) ex[oe[u]] = (uint8_t)b;
-        }
+        const uint4 c = encode16<LPR>(lo[u], hi[u], b);   // every lane takes part in the shuffles
+        if (pb[u] < 0 || pq[u] < 0) continue;
+        const int t = t0 + u * RPP + row;
+        *reinterpret_cast<uint4*>(q8 + row_off(p.q8, l, h, t, pq[u])) = c;
+        if (lane == 0) ex[exp_off(p.e, p.q8, l, h, t, pq[u])] = (uint8_t)b;
       }
     } else {
-      uint2 c[kUnroll];
+      uint4 c[kUnroll];
       uint32_t b[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        c[u] = ob[u] >= 0 ? __ldcs(reinterpret_cast<const uint2*>(q8 + oq[u])) : make_uint2(0, 0);
-        b[u] = ob[u] >= 0 ? ex[oe[u]] : 0;
+        c[u] = make_uint4(0, 0, 0, 0);
+        b[u] = 0;
+        if (pb[u] < 0 || pq[u] < 0) continue;
+        const int t = t0 + u * RPP + row;
+        c[u] = __ldcs(reinterpret_cast<const uint4*>(q8 + row_off(p.q8, l, h, t, pq[u])));
+        b[u] = ex[exp_off(p.e, p.q8, l, h, t, pq[u])];
       }
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (ob[u] >= 0) *reinterpret_cast<uint4*>(bf + ob[u]) = decode8(c[u], b[u]);
+      for (int u = 0; u < kUnroll; ++u) {
+        if (pb[u] < 0 || pq[u] < 0) continue;
+        uint4 lo, hi;
+        decode16(c[u], b[u], lo, hi);
+        uint4* dst = reinterpret_cast<uint4*>(bf + row_off(p.bf, l, h, t0 + u * RPP + row, pb[u]));
+        dst[0] = lo;
+        dst[1] = hi;
+      }
     }
   }
 }
 
 // grid: x = blocks of (token, head, K|V) rows of one request, y = requests (strided)
-template <int D, bool TO8>
+template <int D, bool TO8, int kUnroll>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendLaunch p) {
-  constexpr int LPR = D / 8, RPP = kThreads / LPR;
+  constexpr int LPR = D / 16, RPP = kThreads / LPR;
   const int lane = threadIdx.x % LPR;
-  const int64_t item = (int64_t)blockIdx.x * RPP + threadIdx.x / LPR;
   for (int b = blockIdx.y; b < p.req.n; b += gridDim.y) {
     int q0, nq, kv;
     request_span(p.req, b, threadIdx.x == 0 && blockIdx.x == 0 ? p.status : nullptr, q0, nq, kv);
-    const int j = (int)(item / (2 * p.H)), rest = (int)(item % (2 * p.H));
-    const int is_v = rest & 1, h = rest >> 1;
-    const int pos = kv - nq + j;
-    bool live = j < nq;
-    if (live && pos < 0) {
-      if (lane == 0) atomicOr(p.status, KVC_FLAG_BAD_LENGTH);
-      live = false;
-    }
-    int page = 0;
-    if (live && is_paged(p.dst)) {
-      page = request_page(p.req, p.dst, b, pos, p.status);
-      live = page >= 0;
-    }
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (live) {
-      const DevHeads& src = is_v ? p.vn : p.kn;
-      raw = *reinterpret_cast<const uint4*>(src.p + (int64_t)(q0 + j) * src.s_row + (int64_t)h * src.s_head + lane * 8);
-    }
-    if (TO8) {
-      uint32_t e;
-      const uint2 c = encode8<LPR>(raw, e);
-      if (live) {
-        uint8_t* q8 = reinterpret_cast<uint8_t*>(is_v ? p.dst.v : p.dst.k);
-        *reinterpret_cast<uint2*>(q8 + row_off(p.dst, p.layer, h, pos, page) + lane * 8) = c;
-        if (lane == 0) (is_v ? p.e.v : p.e.k)[exp_off(p.e, p.dst, p.layer, h, pos, page)] = (uint8_t)e;
+    const uint32_t items = (uint32_t)nq * (uint32_t)p.H * 2u;      // the host checked that this fits
+    if (blockIdx.x * (uint32_t)(RPP * kUnroll) >= items) continue;
+    uint4 lo[kUnroll], hi[kUnroll];
+    int64_t at[kUnroll], eat[kUnroll];
+    bool isv[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint32_t item = blockIdx.x * (uint32_t)(RPP * kUnroll) + u * RPP + threadIdx.x / LPR;
+      const int j = (int)(item / (2u * p.H)), rest = (int)(item - (uint32_t)j * (2u * p.H));
+      const int is_v = rest >= p.H, h = is_v ? rest - p.H : rest;
+      const int pos = kv - nq + j;
+      lo[u] = hi[u] = make_uint4(0, 0, 0, 0);
+      at[u] = -1;
+      isv[u] = is_v;
+      if (item >= items) continue;
+      if (pos < 0) {
+        if (lane == 0) atomicOr(p.status, KVC_FLAG_BAD_LENGTH);
+        continue;
       }
-    } else if (live) {
-      *reinterpret_cast<uint4*>((is_v ? p.dst.v : p.dst.k) + row_off(p.dst, p.layer, h, pos, page) + lane * 8) = raw;
+      const int page = is_paged(p.dst) ? request_page(p.req, p.dst, b, pos, p.status) : 0;
+      if (page < 0) continue;
+      at[u] = row_off(p.dst, p.layer, h, pos, page) + lane * 16;
+      if (TO8) eat[u] = exp_off(p.e, p.dst, p.layer, h, pos, page);
+      const DevHeads& src = is_v ? p.vn : p.kn;
+      const uint4* x = reinterpret_cast<const uint4*>(src.p + (int64_t)(q0 + j) * src.s_row + (int64_t)h * src.s_head + lane * 16);
+      lo[u] = x[0];
+      hi[u] = x[1];
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (TO8) {
+        uint32_t e;
+        const uint4 c = encode16<LPR>(lo[u], hi[u], e);
+        if (at[u] < 0) continue;
+        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(isv[u] ? p.dst.v : p.dst.k) + at[u]) = c;
+        if (lane == 0) (isv[u] ? p.e.v : p.e.k)[eat[u]] = (uint8_t)e;
+      } else if (at[u] >= 0) {
+        uint4* dst = reinterpret_cast<uint4*>((isv[u] ? p.dst.v : p.dst.k) + at[u]);
+        dst[0] = lo[u];
+        dst[1] = hi[u];
+      }
     }
   }
+}
+
+template <int D, bool TO8>
+void convert(const ConvertLaunch& c, cudaStream_t s) {
+  constexpr int U = 2, rows = kThreads / (D / 16) * U;
+  const dim3 g((unsigned)((c.T + rows - 1) / rows), (unsigned)(2 * c.H), (unsigned)(c.L < 65535 ? c.L : 65535));
+  convert_kernel<D, TO8, U><<<g, kThreads, 0, s>>>(c);
+}
+
+template <int D, bool TO8>
+void append(const AppendLaunch& a, cudaStream_t s) {
+  constexpr int U = 2, rows = kThreads / (D / 16) * U;
+  const int64_t items = (int64_t)a.req.max_q * a.H * 2;
+  const dim3 g((unsigned)((items + rows - 1) / rows), (unsigned)(a.req.n < 65535 ? a.req.n : 65535));
+  append_kernel<D, TO8, U><<<g, kThreads, 0, s>>>(a);
 }
 
 }  // namespace
 
 cudaError_t launch_convert(const ConvertLaunch& c, int d, cudaStream_t s) {
-  const int rows = kThreads / (d / 8) * kUnroll;
-  const dim3 g((unsigned)((c.T + rows - 1) / rows), (unsigned)(2 * c.H), (unsigned)(c.L < 65535 ? c.L : 65535));
   if (d == 128)
-    c.to8 ? convert_kernel<128, true><<<g, kThreads, 0, s>>>(c) : convert_kernel<128, false><<<g, kThreads, 0, s>>>(c);
+    c.to8 ? convert<128, true>(c, s) : convert<128, false>(c, s);
   else
-    c.to8 ? convert_kernel<64, true><<<g, kThreads, 0, s>>>(c) : convert_kernel<64, false><<<g, kThreads, 0, s>>>(c);
+    c.to8 ? convert<64, true>(c, s) : convert<64, false>(c, s);
   return cudaGetLastError();
 }
 
 cudaError_t launch_append(const AppendLaunch& a, int d, cudaStream_t s) {
-  const int64_t items = (int64_t)a.req.max_q * a.H * 2, rows = kThreads / (d / 8);
-  const dim3 g((unsigned)((items + rows - 1) / rows), (unsigned)(a.req.n < 65535 ? a.req.n : 65535));
   const bool q8 = a.e.k != nullptr;
   if (d == 128)
-    q8 ? append_kernel<128, true><<<g, kThreads, 0, s>>>(a) : append_kernel<128, false><<<g, kThreads, 0, s>>>(a);
+    q8 ? append<128, true>(a, s) : append<128, false>(a, s);
   else
-    q8 ? append_kernel<64, true><<<g, kThreads, 0, s>>>(a) : append_kernel<64, false><<<g, kThreads, 0, s>>>(a);
+    q8 ? append<64, true>(a, s) : append<64, false>(a, s);
   return cudaGetLastError();
 }
 

@@ -462,6 +462,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       }
     }
   }
+  grid_dependents_launch();
   __syncthreads();
   if (*abort_flag) {
     // copies may still be in flight: give them time to land before the block's memory is handed on
@@ -486,6 +487,7 @@ __global__ void __launch_bounds__(256) attend_chunk_join_kernel(const __grid_con
   int q0, nq, kv;
   request_span(p.a.req, b, nullptr, q0, nq, kv);
   const int rows = nq * p.a.G;
+  grid_dependency_wait();                                         // in every block, also those with nothing to join
   if (rows < p.min_rows) return;
   const int64_t slots = (int64_t)p.a.req.n * units * p.nsplit * kUnitRows;
   const int64_t base = (((int64_t)b * p.a.H + h) * p.units_u + u) * p.nsplit;
@@ -547,8 +549,7 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || p.nsplit == 1) return e;
   const dim3 g((unsigned)(p.units_u * p.a.H * (kUnitRows / 32)), (unsigned)p.a.req.n);
-  attend_chunk_join_kernel<D><<<g, 256, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch_after(attend_chunk_join_kernel<D>, g, 256, s, p);
 }
 
 }  // namespace

@@ -114,6 +114,13 @@ __device__ __forceinline__ int64_t line_scan(const AttendLaunch& a, int rc, int 
   return total;
 }
 
+// Where block c's part of a line of `total` tiles begins; with fewer tiles than blocks, the first `total` blocks take one each.
+__device__ __forceinline__ int64_t line_cut(int64_t total, int c, int blocks) {
+  if (total <= blocks) return c < total ? c : total;
+  if (total < ((int64_t)1 << 31) / blocks) return (uint32_t)total * (uint32_t)c / (uint32_t)blocks;
+  return total * c / blocks;
+}
+
 template <int D, bool Q8, int RC>
 struct Few {
   static constexpr int E = Q8 ? 1 : 2;
@@ -231,7 +238,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
   if (warp == 4) {
     // this block's part of the line
     const int64_t total = line_scan(p.a, RC, lane, p.a.req.n, -1, blockIdx.x == 0 ? p.a.status : nullptr, nullptr, nullptr);
-    const int64_t lo = total * blockIdx.x / p.blocks, hi = total * (blockIdx.x + 1) / p.blocks;
+    const int64_t lo = line_cut(total, blockIdx.x, p.blocks), hi = line_cut(total, blockIdx.x + 1, p.blocks);
     int fb = 0;
     int64_t before = 0;
     if (hi > lo) line_scan(p.a, RC, lane, p.a.req.n, lo, nullptr, &fb, &before);
@@ -455,9 +462,12 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     int slot = 0, phase = 0;
     bool ok = true;
     while (ok && walk.next(p.a, RC, x)) {
+      // page ids a tile ahead: the look-up's latency would otherwise be paid once a tile
+      int ahead = tile_page(p.a, p.g, x.b, x.t0 * 128, max(0, min(128, x.kv - x.t0 * 128)), lane);
       for (int i = x.t0; i < x.t1 && ok; ++i) {
         const int rows = max(0, min(128, x.kv - i * 128));
-        const int page = tile_page(p.a, p.g, x.b, i * 128, rows, lane);
+        const int page = ahead;
+        if (i + 1 < x.t1) ahead = tile_page(p.a, p.g, x.b, (i + 1) * 128, min(128, x.kv - (i + 1) * 128), lane);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if (!wait_all(empty + 8 * slot, phase ^ 1, abort_flag)) {
@@ -632,6 +642,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       }
     }
   }
+  grid_dependents_launch();
   __syncthreads();
   if (*abort_flag) {
     // copies may still be in flight: give them time to land before the block's memory is handed on
@@ -648,54 +659,82 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
 }
 
 // ---- join of the pieces of a pair that block borders cut; grid: x = (request, head) pairs, y = groups of 4 rows
+constexpr int kJoinPieces = 160;   // pieces whose weights are kept at a time
 template <int D, int RC>
 __global__ void __launch_bounds__(4 * D) attend_few_join_kernel(const __grid_constant__ FewLaunch p) {
   __shared__ int64_t s_total, s_before;
-  __shared__ int s_nt;
+  __shared__ float s_w[4][kJoinPieces], s_m[4], s_l[4];
   const int b = (int)(blockIdx.x / p.a.H), h = (int)(blockIdx.x % p.a.H);
-  const int r = (int)blockIdx.y * 4 + threadIdx.x / D, ch = threadIdx.x % D;
+  const int rr = threadIdx.x / D, r = (int)blockIdx.y * 4 + rr, ch = threadIdx.x % D;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int q0, nq, kv;
   request_span(p.a.req, b, nullptr, q0, nq, kv);
   const int nt = few_tiles(p.a, RC, nq, kv), R = nq * p.a.G;
-  if (nt == 0 || (int)blockIdx.y * 4 >= R) return;
-  if (threadIdx.x < 32) {
-    const int lane = threadIdx.x;
-    const int64_t before = line_scan(p.a, RC, lane, b, -1, nullptr, nullptr, nullptr);
-    const int64_t total = line_scan(p.a, RC, lane, p.a.req.n, -1, nullptr, nullptr, nullptr);
+  const bool none = nt == 0 || (int)blockIdx.y * 4 >= R;
+  if (!none && warp < 2) {
+    const int64_t sum = line_scan(p.a, RC, lane, warp ? p.a.req.n : b, -1, nullptr, nullptr, nullptr);
+    if (lane == 0) (warp ? s_total : s_before) = sum;
+  }
+  // launched while the main kernel ends: its results are there after this wait.  Every block waits, also those with
+  // nothing to join: this kernel's end must not come before the main kernel's.
+  grid_dependency_wait();
+  if (none) return;
+  __syncthreads();
+  const int64_t total = s_total, w0 = s_before + (int64_t)h * nt, w1 = w0 + nt;
+  const int C = (int)(total < p.blocks ? total : p.blocks);
+  int c0 = (int)(((w0 + 1) * C + total - 1) / total) - 1, c1 = (int)((w1 * C + total - 1) / total) - 1;   // blocks of the first and last tile
+  if (c0 == c1) return;
+  const float minus_inf = __uint_as_float(0xff800000u);
+  const float* ml = p.part + (int64_t)p.blocks * 2 * RC * D;
+  // where block c left its piece: slot 1 holds a piece that begins with the pair, slot 0 one cut in front
+  auto place = [&](int c) { return ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * RC; };
+  // maxima: a warp a row
+  if (warp < 4) {
+    const int row = (int)blockIdx.y * 4 + warp;
+    float m = minus_inf;
+    if (row < R)
+      for (int c = c0 + lane; c <= c1; c += 32) {
+        const float2 v = *reinterpret_cast<const float2*>(ml + 2 * (place(c) + row));
+        if (v.y != 0.f) m = fmaxf(m, v.x);
+      }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if (lane == 0) {
-      s_before = before;
-      s_total = total;
-      s_nt = nt;
+      s_m[warp] = m;
+      s_l[warp] = 0.f;
     }
   }
-  __syncthreads();
-  const int64_t w0 = s_before + (int64_t)h * nt, w1 = w0 + nt, total = s_total, C = p.blocks;
-  const int64_t c0 = ((w0 + 1) * C + total - 1) / total - 1, c1 = (w1 * C + total - 1) / total - 1;   // blocks of the first and last tile
-  if (c0 == c1 || r >= R) return;
-  const float minus_inf = __uint_as_float(0xff800000u);
-  const float* ml = p.part + C * 2 * RC * D;
-  float m = minus_inf;
-  for (int64_t cc = c0; cc <= c1; ++cc) {
-    const int64_t lo = total * cc / C, hi = total * (cc + 1) / C;
-    if (hi <= lo) continue;
-    const int64_t at = (cc * 2 + (lo > w0 ? 0 : 1)) * RC + r;
-    if (ml[2 * at + 1] != 0.f) m = fmaxf(m, ml[2 * at]);
+  float acc = 0.f;
+  for (int cb = c0; cb <= c1; cb += kJoinPieces) {
+    const int n = min(kJoinPieces, c1 + 1 - cb);
+    __syncthreads();
+    if (warp < 4) {
+      const int row = (int)blockIdx.y * 4 + warp;
+      float sum = 0.f;
+      if (row < R)
+        for (int k = lane; k < n; k += 32) {
+          const float2 v = *reinterpret_cast<const float2*>(ml + 2 * (place(cb + k) + row));
+          const float w = v.y == 0.f ? 0.f : exp2f(v.x - s_m[warp]);
+          s_w[warp][k] = w;
+          sum += w * v.y;
+        }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (lane == 0) s_l[warp] += sum;
+    }
+    __syncthreads();
+    if (r < R) {
+#pragma unroll 8
+      for (int k = 0; k < n; ++k) acc += s_w[rr][k] * p.part[(place(cb + k) + r) * D + ch];
+    }
   }
-  float l = 0.f, acc = 0.f;
-#pragma unroll 4
-  for (int64_t cc = c0; cc <= c1; ++cc) {
-    const int64_t lo = total * cc / C, hi = total * (cc + 1) / C;
-    if (hi <= lo) continue;
-    const int64_t at = (cc * 2 + (lo > w0 ? 0 : 1)) * RC + r;
-    const float ls = ml[2 * at + 1], w = ls == 0.f ? 0.f : exp2f(ml[2 * at] - m);
-    l += w * ls;
-    acc += w * p.part[at * D + ch];
-  }
+  if (r >= R) return;
+  const float l = s_l[rr];
   const bool dead = l == 0.f;
   const int64_t row = q0 + r / p.a.G;
   const int head = h * p.a.G + r % p.a.G;
   p.a.out.p[row * p.a.out.s_row + (int64_t)head * p.a.out.s_head + ch] = __float2bfloat16(dead ? 0.f : acc / l);
-  if (p.a.lse && ch == 0) p.a.lse[row * (p.a.H * p.a.G) + head] = dead ? minus_inf : (m + log2f(l)) * kLn2;
+  if (p.a.lse && ch == 0) p.a.lse[row * (p.a.H * p.a.G) + head] = dead ? minus_inf : (s_m[rr] + log2f(l)) * kLn2;
 }
 
 template <int D, bool Q8, int RC>
@@ -711,9 +750,9 @@ cudaError_t launch(const FewLaunch& p, const CUtensorMap& mk, const CUtensorMap&
   attend_few_kernel<D, Q8, RC><<<(unsigned)p.blocks, F::kThreads, F::kSmem, s>>>(p, mk, mv);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const dim3 g((unsigned)((int64_t)p.a.req.n * p.a.H), (unsigned)((RC + 3) / 4));
-  attend_few_join_kernel<D, RC><<<g, 4 * D, 0, s>>>(p);
-  return cudaGetLastError();
+  const int64_t rows = (int64_t)p.a.req.max_q * p.a.G;
+  const dim3 g((unsigned)((int64_t)p.a.req.n * p.a.H), (unsigned)(((rows < RC ? rows : RC) + 3) / 4));
+  return launch_after(attend_few_join_kernel<D, RC>, g, 4 * D, s, p);
 }
 
 }  // namespace

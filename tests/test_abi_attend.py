@@ -121,10 +121,15 @@ def test_binding_refusals():
         kvc.Requests(torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), 1, 1,
                      page_table=torch.zeros(1, 4, dtype=torch.int32).expand(2, 4))
     with pytest.raises(kvc.KvcError):
-        kvc._heads(torch.zeros(2, 2, 64), "q")
+        kvc._heads(torch.zeros(2, 2, 64), 64, "q")
     with pytest.raises(kvc.KvcError):
-        kvc._heads(bf(1, 2, 64).expand(3, 2, 64), "q")      # a broadcast row
+        kvc._heads(bf(2, 2, 64), 128, "q")
     with pytest.raises(kvc.KvcError):
-        kvc._heads(bf(3, 2, 128)[..., ::2], "q")
+        kvc._heads(bf(1, 2, 64).expand(3, 2, 64), 64, "q")      # a broadcast row
+    with pytest.raises(kvc.KvcError):
+        kvc._heads(bf(3, 2, 128)[..., ::2], 64, "q")
+    with pytest.raises(kvc.KvcError):                       # tensors that are not on the current CUDA device
+        kvc.kvc_append(kvc.Requests(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 1, 8), bf(1, 3, 64), bf(1, 3, 64),
+                       kvc.Cache(bf(2, 3, 8, 64), bf(2, 3, 8, 64)), 0)
     q = kvc.QCache.like(kvc.Cache(bf(2, 3, 8, 64), bf(2, 3, 8, 64)))
     assert q.struct().codes.T == 8 and q.nbytes() == 2 * (2 * 3 * 8 * 64 + 2 * 3 * 8)
