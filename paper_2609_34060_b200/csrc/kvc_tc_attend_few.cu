@@ -11,6 +11,10 @@
 // part; of a pair cut by its borders it leaves a float32 partial result (at most two a block), and a second kernel joins
 // those in a fixed order.
 //
+// Two groups of four softmax warps take the tiles in turn, each with running maxima, sums and accumulators of its own (a
+// tile's way from logits to probabilities is a chain of latencies, longer than a tile's bytes take); a pair's two halves
+// are put together like the pieces of a split.
+//
 // Softmax: the running maximum of a row moves only when a logit exceeds it by 2^kLazy (one vote a tile, no reduction
 // otherwise); the sum is kept per thread and added up at the end.
 //
@@ -22,8 +26,9 @@
 //     p 2^(e_v - E) 64 = t1 + t2 / 16 + t3 / 256 ,   E the largest exponent of a value row so far .
 // Sums and joins are float32.  Over bf16 caches P is rounded to bf16 as in the chunk kernel.
 //
-// Warps: 0-3 softmax and epilogue, 4 TMA producer, 5 MMA issue (one thread), 6 queries of the next pair, 8-11 exponents
-// of the next tiles (8-bit caches).  Every wait is bounded.
+// Warps: 0-3 and 4-7 softmax (0-3 epilogue), 8 and 11 TMA producers of keys and values (two: a 16-token page is one small
+// box, and one warp issuing them all was the bound), 9 MMA issue (one thread), 10 queries of the next pair, 12-15
+// exponents of the next tiles (8-bit caches).  Every wait is bounded.
 #include <cuda_runtime.h>
 
 #include "kvc_launch.h"
@@ -133,27 +138,30 @@ struct Few {
   static constexpr uint32_t kPSwizzle = kPRow == 32 ? 6 : kPRow == 64 ? 4 : 2;
   static constexpr uint32_t kRowSwizzle = Q8 && D == 64 ? 4 : 2;
   static constexpr int kP = 128 * kPRow;
-  static constexpr int kThreads = Q8 ? 384 : 256;
+  static constexpr int kThreads = Q8 ? 512 : 384;
   static constexpr int kExpRing = 8;
   static constexpr int kQAlign = (kQ + 1023) / 1024 * 1024;
   static constexpr int kSmem = 1024 + kSlots * kTile + 2 * kQAlign + 2 * kP + (Q8 ? kExpRing * 1024 : 0);
-  static constexpr uint32_t kTmem = 256;
+  // logits of two tiles, then accumulators of (pair parity, group)
   static constexpr uint32_t kOCol = 2 * kQRows;
-  static_assert(kOCol + kPCols <= kTmem, "tensor memory");
+  static constexpr uint32_t kTmem = kOCol + 4 * kPCols <= 128 ? 128 : kOCol + 4 * kPCols <= 256 ? 256 : 512;
+  static_assert(kOCol + 4 * kPCols <= 512, "tensor memory");
   static_assert(kSmem <= 231000, "shared memory");
   // p <= 2^kLazy; with 8-bit values 64 p has to stay below 448
   static constexpr float kLazy = Q8 ? 2.f : 8.f;
 };
 
 struct FewBars {
-  uint64_t full[12], empty[12], s_full[2], p_ready[2], pv_done[2], q_full[2], q_empty[2], e_full[8], e_empty[8];
+  uint64_t full[12], empty[12], s_full[2], p_ready[2], pv_done[2], q_full[2], q_empty[2], o_free[2], e_full[8], e_empty[8];
   int64_t left;
   int b, h, t;
   uint32_t tmem;
   int abort_flag;
-  float red[4][32];
+  float red[2][4][32];
   float qs[2][32];
-  int red_e[4], fail[4];
+  float half_m[32], half_l[32];      // group 1's maxima and sums of a finished piece
+  int half_e;
+  int red_e[2][4], fail[2][4];
 };
 
 __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -211,7 +219,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
   volatile int* abort_flag = &bars.abort_flag;
   const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), s_full = smem_u32(bars.s_full), p_ready = smem_u32(bars.p_ready);
   const uint32_t pv_done = smem_u32(bars.pv_done), q_full = smem_u32(bars.q_full), q_empty = smem_u32(bars.q_empty);
-  const uint32_t e_full = smem_u32(bars.e_full), e_empty = smem_u32(bars.e_empty);
+  const uint32_t o_free = smem_u32(bars.o_free), e_full = smem_u32(bars.e_full), e_empty = smem_u32(bars.e_empty);
   if (tid == 0) {
     for (int s = 0; s < F::kSlots; ++s) {
       mbar_init(full + 8 * s, 1);
@@ -222,7 +230,8 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       mbar_init(p_ready + 8 * s, 128);
       mbar_init(pv_done + 8 * s, 1);
       mbar_init(q_full + 8 * s, 32);
-      mbar_init(q_empty + 8 * s, 1 + 4);                             // the products and the four softmax warps
+      mbar_init(q_empty + 8 * s, 1 + 8);                             // the products and the eight softmax warps
+      mbar_init(o_free + 8 * s, 128);
     }
     for (int s = 0; s < F::kExpRing; ++s) {
       mbar_init(e_full + 8 * s, 32);
@@ -231,11 +240,11 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     bars.abort_flag = 0;
     fence_barrier_init();
   }
-  if (warp == 5) {
+  if (warp == 9) {
     tmem_alloc(smem_u32(&bars.tmem), F::kTmem);
     tmem_relinquish();
   }
-  if (warp == 4) {
+  if (warp == 8) {
     // this block's part of the line
     const int64_t total = line_scan(p.a, RC, lane, p.a.req.n, -1, blockIdx.x == 0 ? p.a.status : nullptr, nullptr, nullptr);
     const int64_t lo = line_cut(total, blockIdx.x, p.blocks), hi = line_cut(total, blockIdx.x + 1, p.blocks);
@@ -263,18 +272,20 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
   Piece x;
   const uint32_t gs = (uint32_t)p.g.gs, ps = (uint32_t)p.g.ps;
 
-  if (warp < 4) {
-    const uint32_t lane_at = tmem + ((uint32_t)(warp * 32) << 16);
-    const uint32_t o_at = lane_at + F::kOCol;
+  if (warp < 8) {
+    regs_inc<Q8 ? 184 : 216>();
+    const int wg = warp >> 2, tid4 = tid & 127, w4 = warp & 3;
+    const uint32_t lane_at = tmem + ((uint32_t)(w4 * 32) << 16);
     const float minus_inf = __uint_as_float(0xff800000u);
     const float c = p.a.scale * kLog2e;
     int g = 0, piece = 0;
-    // a failed wait (ok) becomes a decision of all four warps (stop) at the vote of the next tile: a warp that left alone
-    // would leave the others at a barrier
-    bool ok = true, stop = false;
+    // a failed wait (ok) becomes a decision of the group's four warps (stop) at the vote of its next tile: a warp that
+    // left alone would leave the others at a barrier.  The groups meet at one barrier a piece, which both always reach.
+    bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && wait_all(bar, parity, abort_flag); };
-    while (!stop && walk.next(p.a, RC, x)) {
+    while (walk.next(p.a, RC, x)) {
       const int R = x.nq * p.a.G;
+      const uint32_t o_at = lane_at + F::kOCol + ((piece & 1) * 2 + wg) * F::kPCols;
       float m[RC], l[RC];
       int eref = -1000;                                             // 8-bit values: exponent their sums are held under
 #pragma unroll
@@ -283,70 +294,74 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         l[r] = 0.f;
       }
       wait(q_full + 8 * (piece & 1), (piece >> 1) & 1);
-      for (int i = x.t0; i < x.t1; ++i, ++g) {
-        const int buf = g & 1;
-        const int tok = i * 128 + tid;
+      const int g0 = g, g1 = g + x.t1 - x.t0;                       // the piece's tiles in the block's count
+      const int first = g0 + ((g0 ^ wg) & 1);                       // this group's first
+      bool stop = false;
+      for (g = first; g < g1; g += 2) {
+        const int i = x.t0 + g - g0;
+        const int tok = i * 128 + tid4;
+        const uint32_t use = (uint32_t)(g >> 1) & 1u;               // of buffer wg
         float ek = 1.f;
         int ev = 0;
         if (Q8) {
           const int es = g % F::kExpRing;
           wait(e_full + 8 * es, (g / F::kExpRing) & 1);
-          ek = sexp[es * 256 + tid];
-          ev = __float_as_int(sexp[es * 256 + 128 + tid]);
+          ek = sexp[es * 256 + tid4];
+          ev = __float_as_int(sexp[es * 256 + 128 + tid4]);
           mbar_arrive(e_empty + 8 * es);
         }
-        wait(s_full + 8 * buf, (g >> 1) & 1);
+        wait(s_full + 8 * wg, use);
         tc_fence_after();
         float s[F::kQRows];
-        tmem_ld<F::kQRows>(lane_at + buf * F::kQRows, s);
+        tmem_ld<F::kQRows>(lane_at + wg * F::kQRows, s);
         tmem_ld_wait();
 #pragma unroll
         for (int r = 0; r < RC; ++r) s[r] = Q8 ? fmaf(s[(Q8 ? RC : 0) + r], 0.0625f, s[r]) * (bars.qs[piece & 1][r] * ek) : s[r] * c;
         if (x.kv - x.nq < i * 128 + 128) {                          // the last keys, or some that early rows do not see
-          const int first = p.a.causal ? x.kv - x.nq : x.kv - 1;
+          const int lim = p.a.causal ? x.kv - x.nq : x.kv - 1;
 #pragma unroll
           for (int r = 0; r < RC; ++r)
-            if (tok > first + (p.a.causal ? r / p.a.G : 0) || r >= R) s[r] = minus_inf;
+            if (tok > lim + (p.a.causal ? r / p.a.G : 0) || r >= R) s[r] = minus_inf;
         }
         const bool mine = tok < x.kv;                               // rows behind the last key hold anything
         bool grow = Q8 && mine && ev > eref;
 #pragma unroll
         for (int r = 0; r < RC; ++r) grow |= s[r] - m[r] > F::kLazy;
-        if (named_bar_or(1, 128, grow || !ok)) {
+        if (named_bar_or(1 + wg, 128, grow || !ok)) {
           float keep[RC];
 #pragma unroll
           for (int r = 0; r < RC; ++r) {
             float v = s[r];
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-            if (lane == 0) bars.red[warp][r] = v;
+            if (lane == 0) bars.red[wg][w4][r] = v;
           }
           if (Q8) {
             const int top = __reduce_max_sync(0xffffffffu, mine ? ev : -1000);
-            if (lane == 0) bars.red_e[warp] = top;
+            if (lane == 0) bars.red_e[wg][w4] = top;
           }
-          if (lane == 0) bars.fail[warp] = !ok;
-          named_bar_sync(1, 128);
-          if (bars.fail[0] | bars.fail[1] | bars.fail[2] | bars.fail[3]) {
+          if (lane == 0) bars.fail[wg][w4] = !ok;
+          named_bar_sync(1 + wg, 128);
+          if (bars.fail[wg][0] | bars.fail[wg][1] | bars.fail[wg][2] | bars.fail[wg][3]) {
             stop = true;
             break;
           }
           float oscale = 1.f;
           if (Q8) {
-            const int top = max(eref, max(max(bars.red_e[0], bars.red_e[1]), max(bars.red_e[2], bars.red_e[3])));
+            const int top = max(eref, max(max(bars.red_e[wg][0], bars.red_e[wg][1]), max(bars.red_e[wg][2], bars.red_e[wg][3])));
             oscale = eref == top ? 1.f : top - eref > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (top - eref)) << 23);
             eref = top;
           }
 #pragma unroll
           for (int r = 0; r < RC; ++r) {
-            const float top = fmaxf(m[r], fmaxf(fmaxf(bars.red[0][r], bars.red[1][r]), fmaxf(bars.red[2][r], bars.red[3][r])));
+            const float top = fmaxf(m[r], fmaxf(fmaxf(bars.red[wg][0][r], bars.red[wg][1][r]), fmaxf(bars.red[wg][2][r], bars.red[wg][3][r])));
             keep[r] = top == m[r] ? 1.f : exp2_fast(m[r] - top);
             m[r] = top;
             l[r] *= keep[r];
           }
-          if (i > x.t0) {
+          if (g > first) {
             // the sums so far, once the product that wrote them last is done
-            wait(pv_done + 8 * (buf ^ 1), ((g - 1) >> 1) & 1);
+            wait(pv_done + 8 * wg, use ^ 1);
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < (Q8 ? 3 * RC : RC); k += 8) {
@@ -360,9 +375,9 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
             tmem_st_wait();
           }
         }
-        // probabilities; the buffer is free once the product before the last one is done
-        wait(pv_done + 8 * buf, ((g >> 1) & 1) ^ 1);
-        uint8_t* row = sp + buf * F::kP + tid * F::kPRow;
+        // probabilities; the buffer is free once the product that read it last is done
+        wait(pv_done + 8 * wg, use ^ 1);
+        uint8_t* row = sp + wg * F::kP + tid4 * F::kPRow;
         float scale_v = 64.f;
         if (Q8) scale_v = !mine || eref - ev > 120 ? 0.f : 64.f * __uint_as_float((uint32_t)(127 - (eref - ev)) << 23);
         uint32_t w[F::kPRow / 4];
@@ -395,94 +410,142 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         for (int k = (Q8 ? 3 * RC : 2 * RC) / 4; k < F::kPRow / 4; ++k) w[k] = 0;
 #pragma unroll
         for (int k = 0; k < F::kPRow / 16; ++k)
-          *reinterpret_cast<uint4*>(row + (p_chunk<F::kPRow>(k, tid) << 4)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+          *reinterpret_cast<uint4*>(row + (p_chunk<F::kPRow>(k, tid4) << 4)) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
         if (x.kv < i * 128 + 128) {
           // stale rows behind the last key: P is zero there, but zero times a stale NaN would not be
           const int vs = (2 * g + 1) % F::kSlots;
           wait(full + 8 * vs, ((2 * g + 1) / F::kSlots) & 1);
           if (tok >= x.kv) {
-            uint8_t* v = skv + vs * F::kTile + (tid >> 3) * gs + (tid & 7) * (Q8 ? D : 128);
+            uint8_t* v = skv + vs * F::kTile + (tid4 >> 3) * gs + (tid4 & 7) * (Q8 ? D : 128);
 #pragma unroll
             for (int k = 0; k < D * F::E / 16; ++k) *reinterpret_cast<uint4*>(v + (Q8 ? k << 4 : (k >> 3) * ps + ((k & 7) << 4))) = make_uint4(0, 0, 0, 0);
           }
         }
         fence_proxy_async();
         tc_fence_before();
-        mbar_arrive(p_ready + 8 * buf);
+        mbar_arrive(p_ready + 8 * wg);
       }
-      if (stop) break;
-      // ---- the pair's (or piece's) result
-      wait(pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1);
+      g = g1;
+      const int last = g1 - 1 - (((g1 - 1) ^ wg) & 1);              // this group's last tile; before g0: it had none
+      if (last >= g0 && !stop) wait(pv_done + 8 * wg, (uint32_t)(last >> 1) & 1u);
       tc_fence_after();
-      float o[F::kPCols];
-      tmem_ld<F::kPCols>(o_at, o);
-      tmem_ld_wait();
-      tc_fence_before();
-      named_bar_sync(1, 128);                                       // everyone is done with red
+      // sums of the rows over the group's threads
+      named_bar_sync(1 + wg, 128);                                  // everyone is done with red
 #pragma unroll
       for (int r = 0; r < RC; ++r) {
         float v = l[r];
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
-        if (lane == 0) bars.red[warp][r] = v;
+        if (lane == 0) bars.red[wg][w4][r] = v;
       }
-      named_bar_sync(1, 128);
-      const bool whole = x.t0 == 0 && x.t1 == x.nt;
-      const int64_t slot = ((int64_t)blockIdx.x * 2 + (x.t0 > 0 ? 0 : 1)) * RC;
-      float* ml = p.part + (int64_t)p.blocks * 2 * RC * D;
-      const float back = Q8 ? (eref < -900 ? 0.f : exponent_up((uint32_t)eref) * 0.015625f) : 1.f;
+      named_bar_sync(1 + wg, 128);
+      if (wg == 1) {
+        named_bar_sync(4, 256);                                     // group 0 has read the last piece's half
+        if (tid4 < RC) bars.half_l[tid4] = last >= g0 ? (bars.red[1][0][tid4] + bars.red[1][1][tid4]) + (bars.red[1][2][tid4] + bars.red[1][3][tid4]) : 0.f;
+        if (tid4 == 0) {
 #pragma unroll
-      for (int r = 0; r < RC; ++r) {
-        if (r >= R || !ok) continue;
-        const float sum = (bars.red[0][r] + bars.red[1][r]) + (bars.red[2][r] + bars.red[3][r]);
-        float v = o[r];
-        if (Q8) v = fmaf(fmaf(o[(Q8 ? 2 * RC : 0) + r], 0.0625f, o[(Q8 ? RC : 0) + r]), 0.0625f, v) * back;
-        const bool dead = sum == 0.f;
-        if (dead) v = 0.f;
-        if (whole) {
-          const int64_t at = x.q0 + r / p.a.G;
-          const int head = x.h * p.a.G + r % p.a.G;
-          if (tid < D) p.a.out.p[at * p.a.out.s_row + (int64_t)head * p.a.out.s_head + tid] = __float2bfloat16(dead ? 0.f : v / sum);
-          if (p.a.lse && tid == 0) p.a.lse[at * (p.a.H * p.a.G) + head] = dead ? minus_inf : (m[r] + log2f(sum)) * kLn2;
-        } else {
-          if (tid < D) p.part[(slot + r) * D + tid] = v;
-          if (tid == 0) {
-            ml[(slot + r) * 2] = m[r];
-            ml[(slot + r) * 2 + 1] = sum;
+          for (int r = 0; r < RC; ++r) bars.half_m[r] = m[r];
+          bars.half_e = eref;
+        }
+        named_bar_sync(3, 256);
+      } else {
+        named_bar_sync(4, 256);
+        named_bar_sync(3, 256);
+        const bool had0 = last >= g0, had1 = g1 - g0 > 1 || !had0;  // which groups had tiles
+        const uint32_t o0 = o_at, o1 = o_at + F::kPCols;
+        const bool whole = x.t0 == 0 && x.t1 == x.nt;
+        const int64_t slot = ((int64_t)blockIdx.x * 2 + (x.t0 > 0 ? 0 : 1)) * RC;
+        float* ml = p.part + (int64_t)p.blocks * 2 * RC * D;
+        auto unit = [](int e) { return e < -900 ? 0.f : exponent_up((uint32_t)e) * 0.015625f; };
+        const float back0 = Q8 ? unit(eref) : 1.f, back1 = Q8 ? unit(bars.half_e) : 1.f;
+#pragma unroll
+        for (int rb = 0; rb < RC; rb += 8) {
+          if (rb >= R) continue;
+          float v0[8], v1[8];
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            float* v = half ? v1 : v0;
+            const uint32_t at = half ? o1 : o0;
+            if (!(half ? had1 : had0)) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = 0.f;
+              continue;
+            }
+            tmem_ld8(at + rb, v);
+            if (Q8) {
+              float a[8], b[8];
+              tmem_ld8(at + (Q8 ? RC : 0) + rb, a);
+              tmem_ld8(at + (Q8 ? 2 * RC : 0) + rb, b);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = fmaf(fmaf(b[j], 0.0625f, a[j]), 0.0625f, v[j]) * (half ? back1 : back0);
+            } else {
+              tmem_ld_wait();
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = rb + j;
+            if (r >= R || !ok) continue;
+            const float l0 = (bars.red[0][0][r] + bars.red[0][1][r]) + (bars.red[0][2][r] + bars.red[0][3][r]), l1 = bars.half_l[r];
+            const float m1 = bars.half_m[r];
+            // a half that saw no key of the row (l = 0) has written no sums of it worth a weight
+            const float top = l1 == 0.f ? m[r] : l0 == 0.f ? m1 : fmaxf(m[r], m1);
+            const float w0 = l0 == 0.f ? 0.f : exp2_fast(m[r] - top), w1 = l1 == 0.f ? 0.f : exp2_fast(m1 - top);
+            const float sum = w0 * l0 + w1 * l1;
+            const bool dead = sum == 0.f;
+            const float v = (l0 == 0.f ? 0.f : v0[j] * w0) + (l1 == 0.f ? 0.f : v1[j] * w1);
+            if (whole) {
+              const int64_t at = x.q0 + r / p.a.G;
+              const int head = x.h * p.a.G + r % p.a.G;
+              if (tid4 < D) p.a.out.p[at * p.a.out.s_row + (int64_t)head * p.a.out.s_head + tid4] = __float2bfloat16(dead ? 0.f : v / sum);
+              if (p.a.lse && tid4 == 0) p.a.lse[at * (p.a.H * p.a.G) + head] = dead ? minus_inf : (top + log2f(sum)) * kLn2;
+            } else {
+              if (tid4 < D) p.part[(slot + r) * D + tid4] = v;
+              if (tid4 == 0) {
+                ml[(slot + r) * 2] = top;
+                ml[(slot + r) * 2 + 1] = sum;
+              }
+            }
           }
         }
+        tc_fence_before();
+        mbar_arrive(o_free + 8 * (piece & 1));
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(q_empty + 8 * (piece & 1));
       ++piece;
     }
-  } else if (warp == 4) {
-    // ---- producer
+  } else {
+    regs_dec<72>();
+    if (warp == 8 || warp == 11) {
+    // ---- producers: keys, values
     const uint32_t ring = smem_u32(skv);
-    int slot = 0, phase = 0;
+    const int is_v = warp == 11;
+    const CUtensorMap* map = is_v ? &map_v : &map_k;
+    int slot = is_v;
+    uint32_t phase = 0;
     bool ok = true;
     while (ok && walk.next(p.a, RC, x)) {
       // page ids a tile ahead: the look-up's latency would otherwise be paid once a tile
       int ahead = tile_page(p.a, p.g, x.b, x.t0 * 128, max(0, min(128, x.kv - x.t0 * 128)), lane);
-      for (int i = x.t0; i < x.t1 && ok; ++i) {
+      for (int i = x.t0; i < x.t1; ++i) {
         const int rows = max(0, min(128, x.kv - i * 128));
         const int page = ahead;
         if (i + 1 < x.t1) ahead = tile_page(p.a, p.g, x.b, (i + 1) * 128, min(128, x.kv - (i + 1) * 128), lane);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          if (!wait_all(empty + 8 * slot, phase ^ 1, abort_flag)) {
-            ok = false;
-            break;
-          }
-          tile_load(kv ? &map_v : &map_k, p.a, p.g, ring + slot * F::kTile, full + 8 * slot, i * 128, rows, x.h, page, lane);
-          if (++slot == F::kSlots) {
-            slot = 0;
-            phase ^= 1;
-          }
+        if (!wait_all(empty + 8 * slot, phase ^ 1, abort_flag)) {
+          ok = false;
+          break;
+        }
+        tile_load(map, p.a, p.g, ring + slot * F::kTile, full + 8 * slot, i * 128, rows, x.h, page, lane);
+        slot += 2;                                                  // the number of slots is even
+        if (slot >= F::kSlots) {
+          slot -= F::kSlots;
+          phase ^= 1;
         }
       }
     }
-  } else if (warp == 5) {
+  } else if (warp == 9) {
     // ---- products: the next tile's logits are issued before this tile's values
     if (lane == 0) {
       constexpr uint32_t idesc_s = Q8 ? idesc_e4m3(128, F::kQRows, 0, 0) : idesc_bf16(128, F::kQRows, 0, 0);
@@ -526,30 +589,33 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           if (more) ik = xk.t0;
         }
       };
-      int gv = 0;
+      int gv = 0, pv = 0;
       Walk wv{bars.left, bars.b, bars.h, bars.t};
       if (more) score();
-      while (ok && wv.next(p.a, RC, x)) {
+      for (; ok && wv.next(p.a, RC, x); ++pv) {
         for (int i = x.t0; i < x.t1 && ok; ++i, ++gv) {
           if (more) score();
+          if (i == x.t0 && !wait(o_free + 8 * (pv & 1), ((pv >> 1) & 1) ^ 1)) break;
           const int vs = (2 * gv + 1) % F::kSlots;
           if (!wait(p_ready + 8 * (gv & 1), (gv >> 1) & 1) || !wait(full + 8 * vs, ((2 * gv + 1) / F::kSlots) & 1)) break;
           tc_fence_after();
           const uint32_t va = kv0 + vs * F::kTile, pa = p0 + (gv & 1) * F::kP;
+          const uint32_t oa = tmem + F::kOCol + ((pv & 1) * 2 + (gv & 1)) * F::kPCols;
+          const bool acc = i >= x.t0 + 2;                           // the group's first tile of the piece starts its sums
 #pragma unroll
           for (int k = 0; k < kStepsO; ++k) {
             const uint64_t bd = operand_desc(pa + k * (Q8 ? 32 : 16) * F::kPRow, 0, 8 * F::kPRow, F::kPSwizzle);
             if (Q8)
-              umma_f8(tmem + F::kOCol, operand_desc(va + k * 4 * gs, v_lbo, gs, F::kRowSwizzle), bd, idesc_o, i > x.t0 || k > 0);
+              umma_f8(oa, operand_desc(va + k * 4 * gs, v_lbo, gs, F::kRowSwizzle), bd, idesc_o, acc || k > 0);
             else
-              umma_bf16(tmem + F::kOCol, operand_desc(va + k * 2 * gs, v_lbo, gs, 2), bd, idesc_o, i > x.t0 || k > 0);
+              umma_bf16(oa, operand_desc(va + k * 2 * gs, v_lbo, gs, 2), bd, idesc_o, acc || k > 0);
           }
           umma_commit(empty + 8 * vs);
           umma_commit(pv_done + 8 * (gv & 1));
         }
       }
     }
-  } else if (warp == 6) {
+  } else if (warp == 10) {
     // ---- queries of the pairs, one pair ahead
     constexpr int LPR = D / 8, RPP = 32 / LPR;
     const int ch = lane % LPR;
@@ -609,13 +675,13 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       mbar_arrive(q_full + 8 * (piece & 1));
       ++piece;
     }
-  } else if (Q8 && warp >= 8) {
+  } else if (Q8 && warp >= 12) {
     // ---- exponents of the tiles, four tokens a lane, every fourth tile a warp
     int g = 0;
     bool ok = true;
     while (ok && walk.next(p.a, RC, x)) {
       for (int i = x.t0; i < x.t1 && ok; ++i, ++g) {
-        if ((g & 3) != warp - 8) continue;
+        if ((g & 3) != warp - 12) continue;
         const int es = g % F::kExpRing, tok = i * 128 + lane * 4;
         float k4[4];
         int v4[4];
@@ -642,6 +708,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       }
     }
   }
+  }
   grid_dependents_launch();
   __syncthreads();
   if (*abort_flag) {
@@ -652,7 +719,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     if (tid == 0) atomicOr(p.a.status, KVC_FLAG_WAIT_EXPIRED);
     __syncthreads();
   }
-  if (warp == 5) {
+  if (warp == 9) {
     tc_fence_after();
     tmem_dealloc(tmem, F::kTmem);
   }
