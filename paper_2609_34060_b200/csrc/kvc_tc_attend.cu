@@ -61,11 +61,6 @@ struct Bars {
   int abort_flag;
 };
 
-// a whole warp's wait: one answer for all lanes, so that the warp stays together
-__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
-}
-
 // the row unit of this block
 struct Unit {
   int b, h, u, split, q0, nq, kv, rows, tiles0, tiles[2], n[2];   // first key tile, end tile and count of each row tile
@@ -300,9 +295,11 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       const uint32_t fb = Q8 ? rfull : full, eb = Q8 ? rempty : empty;
       int slot = 0, phase = 0;
       bool ok = true;
+      int ahead = n_all > 0 ? tile_entry(p.a, p.g, un.b, un.tiles0 * 128, min(128, un.kv - un.tiles0 * 128), lane) : 0;
       for (int it = 0; it < n_all && ok; ++it) {
         const int t0 = (un.tiles0 + it) * 128, rows = min(128, un.kv - t0);
-        const int page = tile_page(p.a, p.g, un.b, t0, rows, lane);
+        const int page = ahead;
+        if (it + 1 < n_all) ahead = tile_entry(p.a, p.g, un.b, t0 + 128, min(128, un.kv - t0 - 128), lane);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if (!wait_all(eb + 8 * slot, phase ^ 1, abort_flag)) {
@@ -329,26 +326,37 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         }
       }
     } else if (warp == 9) {
-      if (lane == 0 && n_all > 0) {
+      if (n_all > 0) {
         constexpr uint32_t idesc_s = idesc_bf16(128, 128, 0, 0), idesc_o = idesc_bf16(128, D, 0, 1);
         const uint32_t kv0 = smem_u32(skv);
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) {
-          if (ok) ok = mbar_wait(bar, parity, abort_flag);
+          if (ok) ok = wait_all(bar, parity, abort_flag);
           return ok;
         };
-        auto score = [&](int t, uint32_t kslot) {                 // S_t = Q_t K^T
+        // descriptors differ in their start address alone (its 18 bits / 16 are the low word)
+        const uint64_t q_desc = operand_desc(smem_u32(sq), 16, 1024, 2), k_desc = operand_desc(kv0, 16, gs, 2), v_desc = operand_desc(kv0, ps, gs, 2);
+        const uint32_t k_part = ps >> 4, v_step = (2 * gs) >> 4;
+        auto score = [&](int t, int slot) {                       // S_t = Q_t K^T
+          const uint64_t qd = q_desc + (uint32_t)(t * (SH::kTile >> 4)), kd = k_desc + (uint32_t)(slot * (SH::kTile >> 4));
+          if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-            umma_bf16(tmem + t * 128, operand_desc(smem_u32(sq) + t * SH::kTile + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024, 2),
-                      operand_desc(kslot + (k >> 2) * ps + (k & 3) * 32, 16, gs, 2), idesc_s, k > 0);
-          umma_commit(s_full + 8 * t);
+            for (int k = 0; k < D / 16; ++k)
+              umma_bf16(tmem + t * 128, qd + ((k >> 2) * 1024 + (k & 3) * 2), kd + ((k >> 2) * k_part + (k & 3) * 2), idesc_s, k > 0);
+            umma_commit(s_full + 8 * t);
+          }
         };
-        auto values = [&](int t, uint32_t vslot, bool acc) {      // O_t += P_t V
+        auto values = [&](int t, int slot, bool acc) {            // O_t += P_t V
+          const uint64_t vd = v_desc + (uint32_t)(slot * (SH::kTile >> 4));
+          if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, operand_desc(vslot + 2 * k * gs, ps, gs, 2), idesc_o, acc || k > 0);
-          umma_commit(o_done + 8 * t);
+            for (int k = 0; k < 8; ++k)
+              umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, acc || k > 0);
+            umma_commit(o_done + 8 * t);
+          }
+        };
+        auto release = [&](int slot) {
+          if (elect_one()) umma_commit(empty + 8 * slot);
         };
         int slot = 0, phase = 0;
         auto next = [&]() {
@@ -361,9 +369,9 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           for (int t = 0; t < 2; ++t)
             if (un.n[t] > 0 && wait(q_full + 8 * t, 0)) {
               tc_fence_after();
-              score(t, kv0);
+              score(t, 0);
             }
-          umma_commit(empty);
+          release(0);
           next();
         }
         for (int it = 0; it < n_all && ok; ++it) {
@@ -373,21 +381,22 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           const bool more = it + 1 < n_all;
           if (!wait(full + 8 * vs, vphase)) break;
           if (clean && !more && !wait(v_clean, 0)) break;
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (it >= un.n[t]) continue;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!ok || it >= un.n[t]) continue;
             if (!wait(p_ready + 8 * t, it & 1)) break;
             tc_fence_after();
-            values(t, kv0 + vs * SH::kTile, it > 0);
+            values(t, vs, it > 0);
             if (it + 1 < un.n[t]) {
               if (!wait(full + 8 * ks, kphase)) break;
               tc_fence_after();
-              score(t, kv0 + ks * SH::kTile);
+              score(t, ks);
             }
           }
           if (!ok) break;
-          umma_commit(empty + 8 * vs);
+          release(vs);
           if (more) {
-            umma_commit(empty + 8 * ks);
+            release(ks);
             next();
           }
         }

@@ -67,25 +67,45 @@ inline bool encode_attend_tile(CUtensorMap* m, TileGeo* geo, const DevCache& c, 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Issue the loads of tile i of request b (whole warp): keys to kdst / kbar or values to vdst / vbar.  `rows` are the
-// tile's valid rows; pages behind them are not looked up.  A page the table does not name is read from outside the
-// tensor, where the copy fills in zeros.
+// One lane of the warp, always the same.  The control flow around copies and products stays the whole warp's, with
+// operands that are the same in all lanes, and only the instruction itself is the elected lane's: operands then live in
+// uniform registers.  (Inside a branch taken by one lane they are moved there for every instruction: about 110 cycles a
+// product and 100 a copy, which bounded both kernels.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e != 0;
+}
+// a whole warp's wait: one answer for all lanes, so that the warp stays together
+__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+
+// Loads of a tile (whole warp).  `rows` are the tile's valid rows; pages behind them are not looked up.  tile_entry reads
+// the table (a tile ahead, so that nobody waits for it), tile_load checks the ids and issues the copies; a page the table
+// does not name is read from outside the tensor, where the copy fills in zeros.
 __device__ __forceinline__ int tile_boxes(const TileGeo& g, int rows) { return g.paged ? (rows + g.box_rows - 1) / g.box_rows : 1; }
-__device__ __forceinline__ int tile_page(const AttendLaunch& a, const TileGeo& g, int b, int t0, int rows, int lane) {
+__device__ __forceinline__ int tile_entry(const AttendLaunch& a, const TileGeo& g, int b, int t0, int rows, int lane) {
   if (!g.paged || lane >= tile_boxes(g, rows)) return 0;
-  return request_page(a.req, a.c, b, t0 + lane * g.box_rows, a.status);
+  const int32_t* tab = a.req.table ? a.req.table + (int64_t)b * a.req.table_stride : a.c.page_table;
+  return tab[(t0 + lane * g.box_rows) >> a.c.page_shift];
 }
 __device__ __forceinline__ void tile_load(const CUtensorMap* map, const AttendLaunch& a, const TileGeo& g, uint32_t dst, uint32_t bar,
-                                          int t0, int rows, int h, int page, int lane) {
+                                          int t0, int rows, int h, int entry, int lane) {
   const int nb = tile_boxes(g, rows);
-  if (lane == 0) mbar_expect_tx(bar, (uint32_t)(nb * g.box_bytes));
-  __syncwarp();
-  if (lane < nb) {
-    if (g.paged)
-      tma_load_5d(dst + (uint32_t)(lane * g.box_bytes), map, bar, 0, 0, 0, (t0 & a.c.page_mask & ~(g.box_rows - 1)) >> 3,
-                  page < 0 ? -1 : page * g.ratio + h);
-    else
-      tma_load_5d(dst, map, bar, 0, t0, 0, h, 0);
+  if (g.paged) {
+    const bool bad = lane < nb && (unsigned)entry >= (unsigned)a.c.n_phys;
+    if (bad) atomicOr(a.status, KVC_FLAG_BAD_PAGE);
+    const int x = bad ? -1 : entry * g.ratio + h;
+    const int grp = (t0 & a.c.page_mask & ~(g.box_rows - 1)) >> 3;
+    if (elect_one()) mbar_expect_tx(bar, (uint32_t)(nb * g.box_bytes));
+    for (int j = 0; j < nb; ++j) {
+      const int xj = __shfl_sync(0xffffffffu, x, j);
+      if (elect_one()) tma_load_5d(dst + (uint32_t)(j * g.box_bytes), map, bar, 0, 0, 0, grp, xj);
+    }
+  } else if (elect_one()) {
+    mbar_expect_tx(bar, (uint32_t)g.box_bytes);
+    tma_load_5d(dst, map, bar, 0, t0, 0, h, 0);
   }
 }
 

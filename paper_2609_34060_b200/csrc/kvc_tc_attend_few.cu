@@ -164,9 +164,6 @@ struct FewBars {
   int red_e[2][4], fail[2][4];
 };
 
-__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
-}
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -528,11 +525,11 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     bool ok = true;
     while (ok && walk.next(p.a, RC, x)) {
       // page ids a tile ahead: the look-up's latency would otherwise be paid once a tile
-      int ahead = tile_page(p.a, p.g, x.b, x.t0 * 128, max(0, min(128, x.kv - x.t0 * 128)), lane);
+      int ahead = tile_entry(p.a, p.g, x.b, x.t0 * 128, max(0, min(128, x.kv - x.t0 * 128)), lane);
       for (int i = x.t0; i < x.t1; ++i) {
         const int rows = max(0, min(128, x.kv - i * 128));
         const int page = ahead;
-        if (i + 1 < x.t1) ahead = tile_page(p.a, p.g, x.b, (i + 1) * 128, min(128, x.kv - (i + 1) * 128), lane);
+        if (i + 1 < x.t1) ahead = tile_entry(p.a, p.g, x.b, (i + 1) * 128, min(128, x.kv - (i + 1) * 128), lane);
         if (!wait_all(empty + 8 * slot, phase ^ 1, abort_flag)) {
           ok = false;
           break;
@@ -547,71 +544,86 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     }
   } else if (warp == 9) {
     // ---- products: the next tile's logits are issued before this tile's values
-    if (lane == 0) {
-      constexpr uint32_t idesc_s = Q8 ? idesc_e4m3(128, F::kQRows, 0, 0) : idesc_bf16(128, F::kQRows, 0, 0);
-      constexpr uint32_t idesc_o = Q8 ? idesc_e4m3(128, F::kPCols, 1, 1) : idesc_bf16(128, F::kPCols, 1, 1);
-      constexpr int kStepsS = Q8 ? D / 32 : D / 16, kStepsO = Q8 ? 4 : 8;
-      constexpr uint32_t kQGroup = Q8 ? 8 * D : 1024;
-      const uint32_t kv0 = smem_u32(skv), q0 = smem_u32(sq), p0 = smem_u32(sp);
-      const uint32_t v_lbo = D == 128 && !Q8 ? ps : 0u;             // d = 64: the upper 64 rows of the product repeat the lower
-      bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok) ok = mbar_wait(bar, parity, abort_flag);
-        return ok;
-      };
-      // two walks: one for the logits, which run a tile ahead, one for the values
-      int gk = 0, pk = 0, ik = 0;
-      Piece xk;
-      bool more = walk.next(p.a, RC, xk);
-      if (more) ik = xk.t0;
-      auto score = [&]() {
-        const int ks = (2 * gk) % F::kSlots;
-        if (ik == xk.t0 && !wait(q_full + 8 * (pk & 1), (pk >> 1) & 1)) return;
-        if (!wait(full + 8 * ks, ((2 * gk) / F::kSlots) & 1)) return;
-        tc_fence_after();
-        const uint32_t ka = kv0 + ks * F::kTile, qa = q0 + (pk & 1) * F::kQAlign;
+    constexpr uint32_t idesc_s = Q8 ? idesc_e4m3(128, F::kQRows, 0, 0) : idesc_bf16(128, F::kQRows, 0, 0);
+    constexpr uint32_t idesc_o = Q8 ? idesc_e4m3(128, F::kPCols, 1, 1) : idesc_bf16(128, F::kPCols, 1, 1);
+    constexpr int kStepsS = Q8 ? D / 32 : D / 16, kStepsO = Q8 ? 4 : 8;
+    // descriptors differ in their start address alone (its 18 bits / 16 are the low word); d = 64: the upper 64 rows of
+    // the values' product repeat the lower (no distance between the blocks)
+    const uint64_t k_desc = operand_desc(smem_u32(skv), 16, gs, F::kRowSwizzle);
+    const uint64_t v_desc = operand_desc(smem_u32(skv), D == 128 && !Q8 ? ps : 0u, gs, F::kRowSwizzle);
+    const uint64_t q_desc = operand_desc(smem_u32(sq), 16, Q8 ? 8 * D : 1024, F::kRowSwizzle);
+    const uint64_t p_desc = operand_desc(smem_u32(sp), 0, 8 * F::kPRow, F::kPSwizzle);
+    const uint32_t k_part = ps >> 4, v_step = ((Q8 ? 4 : 2) * gs) >> 4;
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (ok) ok = wait_all(bar, parity, abort_flag);
+      return ok;
+    };
+    // two walks: one for the logits, which run a tile ahead, one for the values
+    int gk = 0, pk = 0, ik = 0, kslot = 0, vslot = 1;
+    uint32_t kphase = 0, vphase = 0;
+    Piece xk;
+    bool more = walk.next(p.a, RC, xk);
+    if (more) ik = xk.t0;
+    auto score = [&]() {
+      if (ik == xk.t0 && !wait(q_full + 8 * (pk & 1), (pk >> 1) & 1)) return;
+      if (!wait(full + 8 * kslot, kphase)) return;
+      tc_fence_after();
+      const uint64_t kd = k_desc + (uint32_t)(kslot * (F::kTile >> 4)), qd = q_desc + (uint32_t)((pk & 1) * (F::kQAlign >> 4));
+      const uint32_t to = tmem + (gk & 1) * F::kQRows;
+      const bool end = ik + 1 == xk.t1;
+      if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < kStepsS; ++k) {
           if (Q8)
-            umma_f8(tmem + (gk & 1) * F::kQRows, operand_desc(ka + k * 32, 16, gs, F::kRowSwizzle), operand_desc(qa + k * 32, 16, kQGroup, F::kRowSwizzle),
-                    idesc_s, k > 0);
+            umma_f8(to, kd + k * 2, qd + k * 2, idesc_s, k > 0);
           else
-            umma_bf16(tmem + (gk & 1) * F::kQRows, operand_desc(ka + (k >> 2) * ps + (k & 3) * 32, 16, gs, 2),
-                      operand_desc(qa + (k >> 2) * (RC * 128) + (k & 3) * 32, 16, kQGroup, 2), idesc_s, k > 0);
+            umma_bf16(to, kd + ((k >> 2) * k_part + (k & 3) * 2), qd + ((k >> 2) * (RC * 8) + (k & 3) * 2), idesc_s, k > 0);
         }
         umma_commit(s_full + 8 * (gk & 1));
-        umma_commit(empty + 8 * ks);
-        ++gk;
-        if (++ik == xk.t1) {
-          umma_commit(q_empty + 8 * (pk & 1));
-          ++pk;
-          more = walk.next(p.a, RC, xk);
-          if (more) ik = xk.t0;
-        }
-      };
-      int gv = 0, pv = 0;
-      Walk wv{bars.left, bars.b, bars.h, bars.t};
-      if (more) score();
-      for (; ok && wv.next(p.a, RC, x); ++pv) {
-        for (int i = x.t0; i < x.t1 && ok; ++i, ++gv) {
-          if (more) score();
-          if (i == x.t0 && !wait(o_free + 8 * (pv & 1), ((pv >> 1) & 1) ^ 1)) break;
-          const int vs = (2 * gv + 1) % F::kSlots;
-          if (!wait(p_ready + 8 * (gv & 1), (gv >> 1) & 1) || !wait(full + 8 * vs, ((2 * gv + 1) / F::kSlots) & 1)) break;
-          tc_fence_after();
-          const uint32_t va = kv0 + vs * F::kTile, pa = p0 + (gv & 1) * F::kP;
-          const uint32_t oa = tmem + F::kOCol + ((pv & 1) * 2 + (gv & 1)) * F::kPCols;
-          const bool acc = i >= x.t0 + 2;                           // the group's first tile of the piece starts its sums
+        umma_commit(empty + 8 * kslot);
+        if (end) umma_commit(q_empty + 8 * (pk & 1));
+      }
+      ++gk;
+      kslot += 2;
+      if (kslot >= F::kSlots) {
+        kslot -= F::kSlots;
+        kphase ^= 1;
+      }
+      ++ik;
+      if (end) {
+        ++pk;
+        more = walk.next(p.a, RC, xk);
+        if (more) ik = xk.t0;
+      }
+    };
+    int gv = 0, pv = 0;
+    Walk wv{bars.left, bars.b, bars.h, bars.t};
+    if (more) score();
+    for (; ok && wv.next(p.a, RC, x); ++pv) {
+      for (int i = x.t0; i < x.t1 && ok; ++i, ++gv) {
+        if (more) score();
+        if (i == x.t0 && !wait(o_free + 8 * (pv & 1), ((pv >> 1) & 1) ^ 1)) break;
+        if (!wait(p_ready + 8 * (gv & 1), (gv >> 1) & 1) || !wait(full + 8 * vslot, vphase)) break;
+        tc_fence_after();
+        const uint64_t vd = v_desc + (uint32_t)(vslot * (F::kTile >> 4)), pd = p_desc + (uint32_t)((gv & 1) * (F::kP >> 4));
+        const uint32_t oa = tmem + F::kOCol + ((pv & 1) * 2 + (gv & 1)) * F::kPCols;
+        const bool acc = i >= x.t0 + 2;                             // the group's first tile of the piece starts its sums
+        if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < kStepsO; ++k) {
-            const uint64_t bd = operand_desc(pa + k * (Q8 ? 32 : 16) * F::kPRow, 0, 8 * F::kPRow, F::kPSwizzle);
             if (Q8)
-              umma_f8(oa, operand_desc(va + k * 4 * gs, v_lbo, gs, F::kRowSwizzle), bd, idesc_o, acc || k > 0);
+              umma_f8(oa, vd + k * v_step, pd + k * (32 * F::kPRow / 16), idesc_o, acc || k > 0);
             else
-              umma_bf16(oa, operand_desc(va + k * 2 * gs, v_lbo, gs, 2), bd, idesc_o, acc || k > 0);
+              umma_bf16(oa, vd + k * v_step, pd + k * (16 * F::kPRow / 16), idesc_o, acc || k > 0);
           }
-          umma_commit(empty + 8 * vs);
           umma_commit(pv_done + 8 * (gv & 1));
+          umma_commit(empty + 8 * vslot);
+        }
+        vslot += 2;
+        if (vslot >= F::kSlots) {
+          vslot -= F::kSlots;
+          vphase ^= 1;
         }
       }
     }
