@@ -3,6 +3,7 @@
 //
 // A tile is 128 token rows of one KV head, each row one part of 64 or 128 bytes (two for bf16 at d = 128), parts swizzled
 // over their own width.  Rows come in groups of 8; a group's parts are `ps` bytes apart, groups `gs` bytes:
+// (rows of one part: the group is only a matter of counting)
 //   contiguous caches  one box of 128 rows: [part][128 rows], gs = 8 rows, ps = 128 rows
 //   paged caches       one box a page: (channel, row in group, part, group, page x head): [group][part][8 rows], so the
 //                      boxes of a tile follow each other and gs is the same inside a page and from page to page
@@ -19,10 +20,12 @@ namespace tc {
 
 struct TileGeo {
   int32_t gs, ps;            // bytes from group to group, from part to part
-  int32_t box_rows;          // token rows a box holds (paged), 128 (contiguous)
+  int32_t box_rows;          // token rows a box holds (paged; a power of two), 128 (contiguous)
+  int32_t box_shift;         // its logarithm
   int32_t box_bytes;
   int32_t ratio;             // X = page * ratio + head
   int32_t paged;
+  int32_t flat;              // rows have one part: tensors and boxes of three dimensions (channel, row, head or X)
 };
 
 template <typename T>
@@ -37,13 +40,23 @@ inline bool encode_attend_tile(CUtensorMap* m, TileGeo* geo, const DevCache& c, 
   const CUtensorMapSwizzle sw = pe * E == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
   const cuuint32_t es[5] = {1, 1, 1, 1, 1};
   geo->paged = is_paged(c);
+  geo->flat = np == 1;
+  auto encode3 = [&](int64_t rows, int64_t units, int64_t unit_stride, int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)pe, (cuuint64_t)rows, (cuuint64_t)units};
+    const cuuint64_t st[2] = {(cuuint64_t)c.s_tok * E, (cuuint64_t)unit_stride * E};
+    const cuuint32_t box[3] = {(cuuint32_t)pe, (cuuint32_t)box_rows, 1};
+    return fn(m, type, 3, at, dims, st, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
   if (!geo->paged) {
     geo->gs = 8 * pe * E;
     geo->ps = 128 * pe * E;
     geo->box_rows = 128;
+    geo->box_shift = 7;
     geo->box_bytes = 128 * d * E;
     geo->ratio = 0;
     if (c.T < 1) return false;
+    if (geo->flat) return encode3(c.T, H, c.s_head, 128);
     const cuuint64_t dims[5] = {(cuuint64_t)pe, (cuuint64_t)c.T, (cuuint64_t)np, (cuuint64_t)H, 1};
     const cuuint64_t st[4] = {(cuuint64_t)c.s_tok * E, (cuuint64_t)pe * E, (cuuint64_t)c.s_head * E, (cuuint64_t)pe * E};
     const cuuint32_t box[5] = {(cuuint32_t)pe, 128, (cuuint32_t)np, 1, 1};
@@ -58,8 +71,11 @@ inline bool encode_attend_tile(CUtensorMap* m, TileGeo* geo, const DevCache& c, 
   geo->gs = np * 8 * pe * E;
   geo->ps = 8 * pe * E;
   geo->box_rows = rows;
+  geo->box_shift = 0;
+  while ((1 << geo->box_shift) < rows) ++geo->box_shift;
   geo->box_bytes = rows * d * E;
   geo->ratio = (int32_t)ratio;
+  if (geo->flat) return encode3(page, x, hs, rows);
   const cuuint64_t dims[5] = {(cuuint64_t)pe, 8, (cuuint64_t)np, (cuuint64_t)(page / 8), (cuuint64_t)x};
   const cuuint64_t st[4] = {(cuuint64_t)c.s_tok * E, (cuuint64_t)pe * E, (cuuint64_t)c.s_tok * 8 * E, (cuuint64_t)hs * E};
   const cuuint32_t box[5] = {(cuuint32_t)pe, 8, (cuuint32_t)np, (cuuint32_t)(rows / 8), 1};
@@ -84,7 +100,7 @@ __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile
 // Loads of a tile (whole warp).  `rows` are the tile's valid rows; pages behind them are not looked up.  tile_entry reads
 // the table (a tile ahead, so that nobody waits for it), tile_load checks the ids and issues the copies; a page the table
 // does not name is read from outside the tensor, where the copy fills in zeros.
-__device__ __forceinline__ int tile_boxes(const TileGeo& g, int rows) { return g.paged ? (rows + g.box_rows - 1) / g.box_rows : 1; }
+__device__ __forceinline__ int tile_boxes(const TileGeo& g, int rows) { return g.paged ? (rows + g.box_rows - 1) >> g.box_shift : 1; }
 __device__ __forceinline__ int tile_entry(const AttendLaunch& a, const TileGeo& g, int b, int t0, int rows, int lane) {
   if (!g.paged || lane >= tile_boxes(g, rows)) return 0;
   const int32_t* tab = a.req.table ? a.req.table + (int64_t)b * a.req.table_stride : a.c.page_table;
@@ -97,15 +113,30 @@ __device__ __forceinline__ void tile_load(const CUtensorMap* map, const AttendLa
     const bool bad = lane < nb && (unsigned)entry >= (unsigned)a.c.n_phys;
     if (bad) atomicOr(a.status, KVC_FLAG_BAD_PAGE);
     const int x = bad ? -1 : entry * g.ratio + h;
-    const int grp = (t0 & a.c.page_mask & ~(g.box_rows - 1)) >> 3;
+    const int row = t0 & a.c.page_mask & ~(g.box_rows - 1);         // inside a page longer than a tile
     if (elect_one()) mbar_expect_tx(bar, (uint32_t)(nb * g.box_bytes));
-    for (int j = 0; j < nb; ++j) {
-      const int xj = __shfl_sync(0xffffffffu, x, j);
-      if (elect_one()) tma_load_5d(dst + (uint32_t)(j * g.box_bytes), map, bar, 0, 0, 0, grp, xj);
+    // eight boxes at a time (a tile of 16-token pages), their coordinates fetched first
+    for (int j0 = 0; j0 < nb; j0 += 8) {
+      int xs[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) xs[j] = __shfl_sync(0xffffffffu, x, j0 + j);
+      if (elect_one()) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j0 + j < nb) {
+            if (g.flat)
+              tma_load_3d(dst + (uint32_t)((j0 + j) * g.box_bytes), map, bar, 0, row, xs[j]);
+            else
+              tma_load_5d(dst + (uint32_t)((j0 + j) * g.box_bytes), map, bar, 0, 0, 0, row >> 3, xs[j]);
+          }
+      }
     }
   } else if (elect_one()) {
     mbar_expect_tx(bar, (uint32_t)g.box_bytes);
-    tma_load_5d(dst, map, bar, 0, t0, 0, h, 0);
+    if (g.flat)
+      tma_load_3d(dst, map, bar, 0, t0, h);
+    else
+      tma_load_5d(dst, map, bar, 0, t0, 0, h, 0);
   }
 }
 

@@ -26,9 +26,9 @@
 //     p 2^(e_v - E) 64 = t1 + t2 / 16 + t3 / 256 ,   E the largest exponent of a value row so far .
 // Sums and joins are float32.  Over bf16 caches P is rounded to bf16 as in the chunk kernel.
 //
-// Warps: 0-3 and 4-7 softmax (0-3 epilogue), 8 and 11 TMA producers of keys and values (two: a 16-token page is one small
-// box, and one warp issuing them all was the bound), 9 MMA issue (one thread), 10 queries of the next pair, 12-15
-// exponents of the next tiles (8-bit caches).  Every wait is bounded.
+// Warps: 0-3 and 4-7 softmax (0-3 epilogue), 8 first products, 9 second products, 10 queries of the next pair, 12-15
+// loads: keys and values of even and odd tiles, with the exponents of 8-bit rows (a 16-token page is one small box, and
+// one or two warps issuing them all were the bound: 8-bit batch at 32K 120 us with two).  Every wait is bounded.
 #include <cuda_runtime.h>
 
 #include "kvc_launch.h"
@@ -129,8 +129,9 @@ __device__ __forceinline__ int64_t line_cut(int64_t total, int c, int blocks) {
 template <int D, bool Q8, int RC>
 struct Few {
   static constexpr int E = Q8 ? 1 : 2;
+  static constexpr int kRows = RC;
   static constexpr int kTile = 128 * D * E;
-  static constexpr int kSlots = kTile == 32768 ? 6 : Q8 && D == 128 && RC == 32 ? 10 : 12;
+  static constexpr int kSlots = kTile == 32768 ? 6 : Q8 && D == 128 && RC > 8 ? 10 : 12;
   static constexpr int kQRows = Q8 ? 2 * RC : RC;              // rows of the query operand: N of the first product
   static constexpr int kQ = kQRows * D * E;
   static constexpr int kPCols = Q8 ? (RC == 8 ? 32 : 3 * RC) : RC;   // N of the second product
@@ -138,28 +139,30 @@ struct Few {
   static constexpr uint32_t kPSwizzle = kPRow == 32 ? 6 : kPRow == 64 ? 4 : 2;
   static constexpr uint32_t kRowSwizzle = Q8 && D == 64 ? 4 : 2;
   static constexpr int kP = 128 * kPRow;
-  static constexpr int kThreads = Q8 ? 512 : 384;
-  static constexpr int kExpRing = 8;
+  static constexpr int kThreads = 512;
+  static constexpr int kExpRing = Q8 ? 8 : 2;
   static constexpr int kQAlign = (kQ + 1023) / 1024 * 1024;
   static constexpr int kSmem = 1024 + kSlots * kTile + 2 * kQAlign + 2 * kP + (Q8 ? kExpRing * 1024 : 0);
-  // logits of two tiles, then accumulators of (pair parity, group)
-  static constexpr uint32_t kOCol = 2 * kQRows;
+  // logits of kSBufs tiles (the first products run kSBufs - 1 tiles ahead), then accumulators of (pair parity, group)
+  static constexpr int kSBufs = Q8 && RC == 32 ? 2 : 4;
+  static constexpr uint32_t kOCol = kSBufs * kQRows;
   static constexpr uint32_t kTmem = kOCol + 4 * kPCols <= 128 ? 128 : kOCol + 4 * kPCols <= 256 ? 256 : 512;
   static_assert(kOCol + 4 * kPCols <= 512, "tensor memory");
-  static_assert(kSmem <= 231000, "shared memory");
   // p <= 2^kLazy; with 8-bit values 64 p has to stay below 448
   static constexpr float kLazy = Q8 ? 2.f : 8.f;
 };
 
+template <typename F>
 struct FewBars {
-  uint64_t full[12], empty[12], s_full[2], p_ready[2], pv_done[2], q_full[2], q_empty[2], o_free[2], e_full[8], e_empty[8];
+  uint64_t full[F::kSlots], empty[F::kSlots], s_full[F::kSBufs], s_free[F::kSBufs], p_ready[2], pv_done[2], q_full[2], q_empty[2], o_free[2];
+  uint64_t e_full[F::kExpRing], e_empty[F::kExpRing];
   int64_t left;
   int b, h, t;
   uint32_t tmem;
   int abort_flag;
-  float red[2][4][32];
-  float qs[2][32];
-  float half_m[32], half_l[32];      // group 1's maxima and sums of a finished piece
+  float red[2][4][F::kRows];
+  float qs[2][F::kRows];
+  float half_m[F::kRows], half_l[F::kRows];      // group 1's maxima and sums of a finished piece
   int half_e;
   int red_e[2][4], fail[2][4];
 };
@@ -201,12 +204,18 @@ __device__ __forceinline__ int p_chunk(int chunk, int tok) {
   return ROW == 32 ? chunk ^ ((tok >> 2) & 1) : ROW == 64 ? chunk ^ ((tok >> 1) & 3) : chunk ^ (tok & 7);
 }
 
+static_assert(sizeof(FewBars<Few<128, false, 32>>) + Few<128, false, 32>::kSmem <= 232448, "shared memory");
+static_assert(sizeof(FewBars<Few<128, false, 16>>) + Few<128, false, 16>::kSmem <= 232448, "shared memory");
+static_assert(sizeof(FewBars<Few<128, true, 8>>) + Few<128, true, 8>::kSmem <= 232448, "shared memory");
+static_assert(sizeof(FewBars<Few<128, true, 16>>) + Few<128, true, 16>::kSmem <= 232448, "shared memory");
+static_assert(sizeof(FewBars<Few<128, true, 32>>) + Few<128, true, 32>::kSmem <= 232448, "shared memory");
+
 template <int D, bool Q8, int RC>
 __global__ void __launch_bounds__(Few<D, Q8, RC>::kThreads, 1)
 attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using F = Few<D, Q8, RC>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ FewBars bars;
+  __shared__ FewBars<F> bars;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* skv = smem;
   uint8_t* sq = skv + F::kSlots * F::kTile;
@@ -214,7 +223,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
   float* sexp = reinterpret_cast<float*>(sp + 2 * F::kP);          // [kExpRing][2][128]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort_flag = &bars.abort_flag;
-  const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), s_full = smem_u32(bars.s_full), p_ready = smem_u32(bars.p_ready);
+  const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), s_full = smem_u32(bars.s_full), s_free = smem_u32(bars.s_free), p_ready = smem_u32(bars.p_ready);
   const uint32_t pv_done = smem_u32(bars.pv_done), q_full = smem_u32(bars.q_full), q_empty = smem_u32(bars.q_empty);
   const uint32_t o_free = smem_u32(bars.o_free), e_full = smem_u32(bars.e_full), e_empty = smem_u32(bars.e_empty);
   if (tid == 0) {
@@ -222,8 +231,11 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
     }
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < F::kSBufs; ++s) {
       mbar_init(s_full + 8 * s, 1);
+      mbar_init(s_free + 8 * s, 4);
+    }
+    for (int s = 0; s < 2; ++s) {
       mbar_init(p_ready + 8 * s, 128);
       mbar_init(pv_done + 8 * s, 1);
       mbar_init(q_full + 8 * s, 32);
@@ -231,7 +243,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       mbar_init(o_free + 8 * s, 128);
     }
     for (int s = 0; s < F::kExpRing; ++s) {
-      mbar_init(e_full + 8 * s, 32);
+      mbar_init(e_full + 8 * s, 64);                                 // the tile's two loading warps
       mbar_init(e_empty + 8 * s, 128);
     }
     bars.abort_flag = 0;
@@ -241,7 +253,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     tmem_alloc(smem_u32(&bars.tmem), F::kTmem);
     tmem_relinquish();
   }
-  if (warp == 8) {
+  if (warp == 11) {
     // this block's part of the line
     const int64_t total = line_scan(p.a, RC, lane, p.a.req.n, -1, blockIdx.x == 0 ? p.a.status : nullptr, nullptr, nullptr);
     const int64_t lo = line_cut(total, blockIdx.x, p.blocks), hi = line_cut(total, blockIdx.x + 1, p.blocks);
@@ -270,7 +282,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
   const uint32_t gs = (uint32_t)p.g.gs, ps = (uint32_t)p.g.ps;
 
   if (warp < 8) {
-    regs_inc<Q8 ? 184 : 216>();
+    regs_inc<184>();
     const int wg = warp >> 2, tid4 = tid & 127, w4 = warp & 3;
     const uint32_t lane_at = tmem + ((uint32_t)(w4 * 32) << 16);
     const float minus_inf = __uint_as_float(0xff800000u);
@@ -307,11 +319,15 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           ev = __float_as_int(sexp[es * 256 + 128 + tid4]);
           mbar_arrive(e_empty + 8 * es);
         }
-        wait(s_full + 8 * wg, use);
+        const int sb = g % F::kSBufs;
+        wait(s_full + 8 * sb, (g / F::kSBufs) & 1);
         tc_fence_after();
         float s[F::kQRows];
-        tmem_ld<F::kQRows>(lane_at + wg * F::kQRows, s);
+        tmem_ld<F::kQRows>(lane_at + sb * F::kQRows, s);
         tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_free + 8 * sb);
 #pragma unroll
         for (int r = 0; r < RC; ++r) s[r] = Q8 ? fmaf(s[(Q8 ? RC : 0) + r], 0.0625f, s[r]) * (bars.qs[piece & 1][r] * ek) : s[r] * c;
         if (x.kv - x.nq < i * 128 + 128) {                          // the last keys, or some that early rows do not see
@@ -515,211 +531,216 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     }
   } else {
     regs_dec<72>();
-    if (warp == 8 || warp == 11) {
-    // ---- producers: keys, values
-    const uint32_t ring = smem_u32(skv);
-    const int is_v = warp == 11;
-    const CUtensorMap* map = is_v ? &map_v : &map_k;
-    int slot = is_v;
-    uint32_t phase = 0;
-    bool ok = true;
-    while (ok && walk.next(p.a, RC, x)) {
-      // page ids a tile ahead: the look-up's latency would otherwise be paid once a tile
-      int ahead = tile_entry(p.a, p.g, x.b, x.t0 * 128, max(0, min(128, x.kv - x.t0 * 128)), lane);
-      for (int i = x.t0; i < x.t1; ++i) {
-        const int rows = max(0, min(128, x.kv - i * 128));
-        const int page = ahead;
-        if (i + 1 < x.t1) ahead = tile_entry(p.a, p.g, x.b, (i + 1) * 128, min(128, x.kv - (i + 1) * 128), lane);
-        if (!wait_all(empty + 8 * slot, phase ^ 1, abort_flag)) {
-          ok = false;
-          break;
-        }
-        tile_load(map, p.a, p.g, ring + slot * F::kTile, full + 8 * slot, i * 128, rows, x.h, page, lane);
-        slot += 2;                                                  // the number of slots is even
-        if (slot >= F::kSlots) {
-          slot -= F::kSlots;
-          phase ^= 1;
-        }
-      }
-    }
-  } else if (warp == 9) {
-    // ---- products: the next tile's logits are issued before this tile's values
-    constexpr uint32_t idesc_s = Q8 ? idesc_e4m3(128, F::kQRows, 0, 0) : idesc_bf16(128, F::kQRows, 0, 0);
-    constexpr uint32_t idesc_o = Q8 ? idesc_e4m3(128, F::kPCols, 1, 1) : idesc_bf16(128, F::kPCols, 1, 1);
-    constexpr int kStepsS = Q8 ? D / 32 : D / 16, kStepsO = Q8 ? 4 : 8;
-    // descriptors differ in their start address alone (its 18 bits / 16 are the low word); d = 64: the upper 64 rows of
-    // the values' product repeat the lower (no distance between the blocks)
-    const uint64_t k_desc = operand_desc(smem_u32(skv), 16, gs, F::kRowSwizzle);
-    const uint64_t v_desc = operand_desc(smem_u32(skv), D == 128 && !Q8 ? ps : 0u, gs, F::kRowSwizzle);
-    const uint64_t q_desc = operand_desc(smem_u32(sq), 16, Q8 ? 8 * D : 1024, F::kRowSwizzle);
-    const uint64_t p_desc = operand_desc(smem_u32(sp), 0, 8 * F::kPRow, F::kPSwizzle);
-    const uint32_t k_part = ps >> 4, v_step = ((Q8 ? 4 : 2) * gs) >> 4;
-    bool ok = true;
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-      if (ok) ok = wait_all(bar, parity, abort_flag);
-      return ok;
-    };
-    // two walks: one for the logits, which run a tile ahead, one for the values
-    int gk = 0, pk = 0, ik = 0, kslot = 0, vslot = 1;
-    uint32_t kphase = 0, vphase = 0;
-    Piece xk;
-    bool more = walk.next(p.a, RC, xk);
-    if (more) ik = xk.t0;
-    auto score = [&]() {
-      if (ik == xk.t0 && !wait(q_full + 8 * (pk & 1), (pk >> 1) & 1)) return;
-      if (!wait(full + 8 * kslot, kphase)) return;
-      tc_fence_after();
-      const uint64_t kd = k_desc + (uint32_t)(kslot * (F::kTile >> 4)), qd = q_desc + (uint32_t)((pk & 1) * (F::kQAlign >> 4));
-      const uint32_t to = tmem + (gk & 1) * F::kQRows;
-      const bool end = ik + 1 == xk.t1;
-      if (elect_one()) {
+    if (warp >= 12) {
+      // ---- loads: keys (12, 13) or values (14, 15) of every other tile.  A slot's earlier use was consumed before the
+      // warp's last load but one could be issued, so a slot's phase is never more than one ahead of the wait.
+      const uint32_t ring = smem_u32(skv);
+      const int is_v = warp >= 14, odd = warp & 1;
+      const CUtensorMap* map = is_v ? &map_v : &map_k;
+      const uint8_t* ex = is_v ? p.a.e.v : p.a.e.k;
+      int g = 0;
+      bool ok = true;
+      // exponents, four tokens a lane, handed on one load later than they were asked for
+      int held = -1;
+      uint32_t bytes[4] = {0, 0, 0, 0};
+      bool live[4] = {false, false, false, false};
+      auto hand_on = [&]() {
+        if (held < 0 || !ok) return;
+        const int es = held % F::kExpRing;
+        ok = wait_all(e_empty + 8 * es, ((held / F::kExpRing) & 1) ^ 1, abort_flag);
+        if (!ok) return;
+        float v[4];
 #pragma unroll
-        for (int k = 0; k < kStepsS; ++k) {
-          if (Q8)
-            umma_f8(to, kd + k * 2, qd + k * 2, idesc_s, k > 0);
-          else
-            umma_bf16(to, kd + ((k >> 2) * k_part + (k & 3) * 2), qd + ((k >> 2) * (RC * 8) + (k & 3) * 2), idesc_s, k > 0);
-        }
-        umma_commit(s_full + 8 * (gk & 1));
-        umma_commit(empty + 8 * kslot);
-        if (end) umma_commit(q_empty + 8 * (pk & 1));
-      }
-      ++gk;
-      kslot += 2;
-      if (kslot >= F::kSlots) {
-        kslot -= F::kSlots;
-        kphase ^= 1;
-      }
-      ++ik;
-      if (end) {
-        ++pk;
-        more = walk.next(p.a, RC, xk);
-        if (more) ik = xk.t0;
-      }
-    };
-    int gv = 0, pv = 0;
-    Walk wv{bars.left, bars.b, bars.h, bars.t};
-    if (more) score();
-    for (; ok && wv.next(p.a, RC, x); ++pv) {
-      for (int i = x.t0; i < x.t1 && ok; ++i, ++gv) {
-        if (more) score();
-        if (i == x.t0 && !wait(o_free + 8 * (pv & 1), ((pv >> 1) & 1) ^ 1)) break;
-        if (!wait(p_ready + 8 * (gv & 1), (gv >> 1) & 1) || !wait(full + 8 * vslot, vphase)) break;
-        tc_fence_after();
-        const uint64_t vd = v_desc + (uint32_t)(vslot * (F::kTile >> 4)), pd = p_desc + (uint32_t)((gv & 1) * (F::kP >> 4));
-        const uint32_t oa = tmem + F::kOCol + ((pv & 1) * 2 + (gv & 1)) * F::kPCols;
-        const bool acc = i >= x.t0 + 2;                             // the group's first tile of the piece starts its sums
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < kStepsO; ++k) {
-            if (Q8)
-              umma_f8(oa, vd + k * v_step, pd + k * (32 * F::kPRow / 16), idesc_o, acc || k > 0);
-            else
-              umma_bf16(oa, vd + k * v_step, pd + k * (16 * F::kPRow / 16), idesc_o, acc || k > 0);
-          }
-          umma_commit(pv_done + 8 * (gv & 1));
-          umma_commit(empty + 8 * vslot);
-        }
-        vslot += 2;
-        if (vslot >= F::kSlots) {
-          vslot -= F::kSlots;
-          vphase ^= 1;
-        }
-      }
-    }
-  } else if (warp == 10) {
-    // ---- queries of the pairs, one pair ahead
-    constexpr int LPR = D / 8, RPP = 32 / LPR;
-    const int ch = lane % LPR;
-    const float c = p.a.scale * kLog2e;
-    int piece = 0;
-    while (walk.next(p.a, RC, x)) {
-      if (!wait_all(q_empty + 8 * (piece & 1), ((piece >> 1) & 1) ^ 1, abort_flag)) break;
-      uint8_t* dst = sq + (piece & 1) * F::kQAlign;
-      const int R = x.nq * p.a.G;
-#pragma unroll 4
-      for (int r0 = 0; r0 < RC; r0 += RPP) {
-        const int r = r0 + lane / LPR;
-        uint4 raw = make_uint4(0, 0, 0, 0);
-        if (r < R)
-          raw = *reinterpret_cast<const uint4*>(p.a.q.p + (int64_t)(x.q0 + r / p.a.G) * p.a.q.s_row + (int64_t)(x.h * p.a.G + r % p.a.G) * p.a.q.s_head + ch * 8);
-        if (!Q8) {
-          *reinterpret_cast<uint4*>(dst + (ch >> 3) * (RC * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = raw;
-        } else {
-          float v[8];
-          unpack8(raw, v);
-          float top = 0.f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
-#pragma unroll
-          for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const bool finite = top < __uint_as_float(0x7f800000u);
-          const uint32_t b = finite ? row_exponent(top) : 127u;
-          const float down = exponent_down(b);
-#pragma unroll
-          for (int term = 0; term < 2; ++term) {
-            uint2 code;
-            uint32_t w[4];
+        for (int j = 0; j < 4; ++j) v[j] = is_v ? __int_as_float(live[j] ? (int)bytes[j] : 0) : live[j] ? exponent_up(bytes[j]) : 1.f;
+        *reinterpret_cast<float4*>(sexp + es * 256 + is_v * 128 + lane * 4) = make_float4(v[0], v[1], v[2], v[3]);
+        mbar_arrive(e_full + 8 * es);
+      };
+      while (ok && walk.next(p.a, RC, x)) {
+        const int g0 = g, n = x.t1 - x.t0;
+        g += n;
+        int k = (g0 ^ odd) & 1;                                     // this warp's first tile of the piece
+        auto rows_of = [&](int k) { return max(0, min(128, x.kv - (x.t0 + k) * 128)); };
+        // page ids a load ahead: nobody waits for the look-up
+        int ahead = k < n ? tile_entry(p.a, p.g, x.b, (x.t0 + k) * 128, rows_of(k), lane) : 0;
+        for (; k < n; k += 2) {
+          const int t0 = (x.t0 + k) * 128, rows = rows_of(k), entry = ahead;
+          if (k + 2 < n) ahead = tile_entry(p.a, p.g, x.b, t0 + 256, rows_of(k + 2), lane);
+          uint32_t next[4] = {0, 0, 0, 0};
+          bool nlive[4] = {false, false, false, false};
+          if (Q8) {
+            const int tok = t0 + lane * 4;
+            int64_t at = (int64_t)p.a.layer * p.a.e.s_layer + (int64_t)x.h * p.a.e.s_head;
+            bool good = true;
+            if (p.g.paged) {
+              const int page = __shfl_sync(0xffffffffu, entry, (lane * 4) >> p.g.box_shift);
+              good = (unsigned)page < (unsigned)p.a.c.n_phys;
+              at += (int64_t)page * p.a.e.s_page + (int64_t)(tok & p.a.c.page_mask) * p.a.e.s_tok;
+            } else {
+              at += (int64_t)tok * p.a.e.s_tok;
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              float lo = v[2 * j], hi = v[2 * j + 1];
-              if (term == 0) {
-                lo *= down;
-                hi *= down;
-                if (!(fabsf(lo) < __uint_as_float(0x7f800000u))) lo = __uint_as_float(0x7fc00000u);   // infinities give NaN logits
-                if (!(fabsf(hi) < __uint_as_float(0x7f800000u))) hi = __uint_as_float(0x7fc00000u);
-              }
-              w[j] = e4m3x2(lo, hi);
-              const float2 f = e4m3x2_to_float2(w[j]);
-              v[2 * j] = (lo - f.x) * 16.f;
-              v[2 * j + 1] = (hi - f.y) * 16.f;
+              nlive[j] = good && tok + j < x.kv;
+              if (nlive[j]) next[j] = ex[at + j * p.a.e.s_tok];
             }
-            code.x = w[0] | (w[1] << 16);
-            code.y = w[2] | (w[3] << 16);
-            const int rr = term * RC + r;
-            const int chunk = D == 128 ? (ch >> 1) ^ (rr & 7) : (ch >> 1) ^ ((rr >> 1) & 3);
-            *reinterpret_cast<uint2*>(dst + rr * D + (chunk << 4) + (ch & 1) * 8) = code;
           }
-          if (ch == 0) bars.qs[piece & 1][r] = exponent_up(b) * c;
-        }
-      }
-      fence_proxy_async();
-      mbar_arrive(q_full + 8 * (piece & 1));
-      ++piece;
-    }
-  } else if (Q8 && warp >= 12) {
-    // ---- exponents of the tiles, four tokens a lane, every fourth tile a warp
-    int g = 0;
-    bool ok = true;
-    while (ok && walk.next(p.a, RC, x)) {
-      for (int i = x.t0; i < x.t1 && ok; ++i, ++g) {
-        if ((g & 3) != warp - 12) continue;
-        const int es = g % F::kExpRing, tok = i * 128 + lane * 4;
-        float k4[4];
-        int v4[4];
-        int page = 0;
-        if (tok < x.kv && p.g.paged) page = request_page(p.a.req, p.a.c, x.b, tok, nullptr);
-        const int64_t base = (int64_t)p.a.layer * p.a.e.s_layer + (int64_t)x.h * p.a.e.s_head +
-                             (p.g.paged ? (int64_t)page * p.a.e.s_page + (int64_t)(tok & p.a.c.page_mask) * p.a.e.s_tok : (int64_t)tok * p.a.e.s_tok);
+          const int use = 2 * (g0 + k) + is_v, slot = use % F::kSlots;
+          if (!wait_all(empty + 8 * slot, ((use / F::kSlots) & 1) ^ 1, abort_flag)) {
+            ok = false;
+            break;
+          }
+          tile_load(map, p.a, p.g, ring + slot * F::kTile, full + 8 * slot, t0, rows, x.h, entry, lane);
+          if (Q8) {
+            hand_on();
+            held = g0 + k;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          k4[j] = 1.f;
-          v4[j] = 0;
-          if (tok + j < x.kv && page >= 0) {
-            k4[j] = exponent_up(p.a.e.k[base + j * p.a.e.s_tok]);
-            v4[j] = p.a.e.v[base + j * p.a.e.s_tok];
+            for (int j = 0; j < 4; ++j) {
+              bytes[j] = next[j];
+              live[j] = nlive[j];
+            }
           }
         }
-        if (!wait_all(e_empty + 8 * es, ((g / F::kExpRing) & 1) ^ 1, abort_flag)) {
-          ok = false;
-          break;
+      }
+      if (Q8) hand_on();
+    } else if (warp == 8 || warp == 9) {
+      // ---- products: warp 8 the logits, warp 9 the values
+      // descriptors differ in their start address alone (its 18 bits / 16 are the low word); d = 64: the upper 64 rows of
+      // the values' product repeat the lower (no distance between the blocks)
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (ok) ok = wait_all(bar, parity, abort_flag);
+        return ok;
+      };
+      int g = 0, piece = 0, slot = warp == 8 ? 0 : 1;
+      uint32_t phase = 0;
+      if (warp == 8) {
+        constexpr uint32_t idesc = Q8 ? idesc_e4m3(128, F::kQRows, 0, 0) : idesc_bf16(128, F::kQRows, 0, 0);
+        constexpr int kSteps = Q8 ? D / 32 : D / 16;
+        const uint64_t k_desc = operand_desc(smem_u32(skv), 16, gs, F::kRowSwizzle);
+        const uint64_t q_desc = operand_desc(smem_u32(sq), 16, Q8 ? 8 * D : 1024, F::kRowSwizzle);
+        const uint32_t k_part = ps >> 4;
+        for (; ok && walk.next(p.a, RC, x); ++piece) {
+          if (!wait(q_full + 8 * (piece & 1), (piece >> 1) & 1)) break;
+          for (int i = x.t0; i < x.t1; ++i, ++g) {
+            const int sb = g % F::kSBufs;
+            if (!wait(s_free + 8 * sb, ((g / F::kSBufs) & 1) ^ 1) || !wait(full + 8 * slot, phase)) break;
+            tc_fence_after();
+            const uint64_t kd = k_desc + (uint32_t)(slot * (F::kTile >> 4)), qd = q_desc + (uint32_t)((piece & 1) * (F::kQAlign >> 4));
+            const uint32_t to = tmem + sb * F::kQRows;
+            const bool end = i + 1 == x.t1;
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < kSteps; ++k) {
+                if (Q8)
+                  umma_f8(to, kd + k * 2, qd + k * 2, idesc, k > 0);
+                else
+                  umma_bf16(to, kd + ((k >> 2) * k_part + (k & 3) * 2), qd + ((k >> 2) * (RC * 8) + (k & 3) * 2), idesc, k > 0);
+              }
+              umma_commit(s_full + 8 * sb);
+              umma_commit(empty + 8 * slot);
+              if (end) umma_commit(q_empty + 8 * (piece & 1));
+            }
+            slot += 2;
+            if (slot >= F::kSlots) {
+              slot -= F::kSlots;
+              phase ^= 1;
+            }
+          }
         }
-        *reinterpret_cast<float4*>(sexp + es * 256 + lane * 4) = make_float4(k4[0], k4[1], k4[2], k4[3]);
-        *reinterpret_cast<int4*>(sexp + es * 256 + 128 + lane * 4) = make_int4(v4[0], v4[1], v4[2], v4[3]);
-        mbar_arrive(e_full + 8 * es);
+      } else {
+        constexpr uint32_t idesc = Q8 ? idesc_e4m3(128, F::kPCols, 1, 1) : idesc_bf16(128, F::kPCols, 1, 1);
+        constexpr int kSteps = Q8 ? 4 : 8;
+        const uint64_t v_desc = operand_desc(smem_u32(skv), D == 128 && !Q8 ? ps : 0u, gs, F::kRowSwizzle);
+        const uint64_t p_desc = operand_desc(smem_u32(sp), 0, 8 * F::kPRow, F::kPSwizzle);
+        const uint32_t v_step = ((Q8 ? 4 : 2) * gs) >> 4;
+        for (; ok && walk.next(p.a, RC, x); ++piece) {
+          if (!wait(o_free + 8 * (piece & 1), ((piece >> 1) & 1) ^ 1)) break;
+          for (int i = x.t0; i < x.t1; ++i, ++g) {
+            if (!wait(full + 8 * slot, phase) || !wait(p_ready + 8 * (g & 1), (g >> 1) & 1)) break;
+            tc_fence_after();
+            const uint64_t vd = v_desc + (uint32_t)(slot * (F::kTile >> 4)), pd = p_desc + (uint32_t)((g & 1) * (F::kP >> 4));
+            const uint32_t oa = tmem + F::kOCol + ((piece & 1) * 2 + (g & 1)) * F::kPCols;
+            const bool acc = i >= x.t0 + 2;                         // the group's first tile of the piece starts its sums
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < kSteps; ++k) {
+                if (Q8)
+                  umma_f8(oa, vd + k * v_step, pd + k * (32 * F::kPRow / 16), idesc, acc || k > 0);
+                else
+                  umma_bf16(oa, vd + k * v_step, pd + k * (16 * F::kPRow / 16), idesc, acc || k > 0);
+              }
+              umma_commit(pv_done + 8 * (g & 1));
+              umma_commit(empty + 8 * slot);
+            }
+            slot += 2;
+            if (slot >= F::kSlots) {
+              slot -= F::kSlots;
+              phase ^= 1;
+            }
+          }
+        }
+      }
+    } else if (warp == 10) {
+      // ---- queries of the pairs, one pair ahead
+      constexpr int LPR = D / 8, RPP = 32 / LPR;
+      const int ch = lane % LPR;
+      const float c = p.a.scale * kLog2e;
+      int piece = 0;
+      while (walk.next(p.a, RC, x)) {
+        if (!wait_all(q_empty + 8 * (piece & 1), ((piece >> 1) & 1) ^ 1, abort_flag)) break;
+        uint8_t* dst = sq + (piece & 1) * F::kQAlign;
+        const int R = x.nq * p.a.G;
+#pragma unroll 4
+        for (int r0 = 0; r0 < RC; r0 += RPP) {
+          const int r = r0 + lane / LPR;
+          uint4 raw = make_uint4(0, 0, 0, 0);
+          if (r < R)
+            raw = *reinterpret_cast<const uint4*>(p.a.q.p + (int64_t)(x.q0 + r / p.a.G) * p.a.q.s_row + (int64_t)(x.h * p.a.G + r % p.a.G) * p.a.q.s_head + ch * 8);
+          if (!Q8) {
+            *reinterpret_cast<uint4*>(dst + (ch >> 3) * (RC * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = raw;
+          } else {
+            float v[8];
+            unpack8(raw, v);
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[j]));
+#pragma unroll
+            for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const bool finite = top < __uint_as_float(0x7f800000u);
+            const uint32_t b = finite ? row_exponent(top) : 127u;
+            const float down = exponent_down(b);
+#pragma unroll
+            for (int term = 0; term < 2; ++term) {
+              uint2 code;
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float lo = v[2 * j], hi = v[2 * j + 1];
+                if (term == 0) {
+                  lo *= down;
+                  hi *= down;
+                  if (!(fabsf(lo) < __uint_as_float(0x7f800000u))) lo = __uint_as_float(0x7fc00000u);   // infinities give NaN logits
+                  if (!(fabsf(hi) < __uint_as_float(0x7f800000u))) hi = __uint_as_float(0x7fc00000u);
+                }
+                w[j] = e4m3x2(lo, hi);
+                const float2 f = e4m3x2_to_float2(w[j]);
+                v[2 * j] = (lo - f.x) * 16.f;
+                v[2 * j + 1] = (hi - f.y) * 16.f;
+              }
+              code.x = w[0] | (w[1] << 16);
+              code.y = w[2] | (w[3] << 16);
+              const int rr = term * RC + r;
+              const int chunk = D == 128 ? (ch >> 1) ^ (rr & 7) : (ch >> 1) ^ ((rr >> 1) & 3);
+              *reinterpret_cast<uint2*>(dst + rr * D + (chunk << 4) + (ch & 1) * 8) = code;
+            }
+            if (ch == 0) bars.qs[piece & 1][r] = exponent_up(b) * c;
+          }
+        }
+        fence_proxy_async();
+        mbar_arrive(q_full + 8 * (piece & 1));
+        ++piece;
       }
     }
-  }
   }
   grid_dependents_launch();
   __syncthreads();
