@@ -571,15 +571,14 @@ struct Plan {
   int rc;
   bool chunk;
 };
-static Plan attend_plan(int n, int max_q, int G, bool q8) {
+static Plan attend_plan(int n, int max_q, int G) {
   const int64_t rows = (int64_t)max_q * G;
-  if (const int rc = few_capacity(rows, q8)) return {rc, false};
-  return {n > 1 ? few_capacity(G, q8) : 0, true};
+  if (const int rc = few_capacity(rows)) return {rc, false};
+  return {n > 1 ? few_capacity(G) : 0, true};
 }
 
-// 8-bit and bf16 caches need the same: the larger of the two plans
 size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d) {
-  const Plan p = attend_plan(n, max_q, G, false);
+  const Plan p = attend_plan(n, max_q, G);
   size_t bytes = p.rc ? (few_workspace_bytes(n, max_kv, H, d, p.rc) + 255) / 256 * 256 : 0;
   if (p.chunk) {
     const int64_t units = (int64_t)n * H * chunk_units(max_q, G);
@@ -592,7 +591,7 @@ size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int
 int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   (void)L;
   const bool q8 = a.e.k != nullptr;
-  const Plan plan = attend_plan(a.req.n, a.req.max_q, a.G, q8);
+  const Plan plan = attend_plan(a.req.n, a.req.max_q, a.G);
   ChunkLaunch p;
   p.a = a;
   p.units_u = chunk_units(a.req.max_q, a.G);
@@ -610,8 +609,7 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   if (!ok) return KVC_E_UNSUPPORTED;
   if (plan.rc) {
     if (launch_attend_few(a, p.g, mk, mv, plan.rc, d, a.part, s) != cudaSuccess) return KVC_E_CUDA;
-    const Plan bf = attend_plan(a.req.n, a.req.max_q, a.G, false);   // as the workspace was sized
-    p.a.part = a.part + (few_workspace_bytes(a.req.n, a.req.max_kv, a.H, d, bf.rc) + 255) / 256 * 64;
+    p.a.part = a.part + (few_workspace_bytes(a.req.n, a.req.max_kv, a.H, d, plan.rc) + 255) / 256 * 64;
   }
   if (!plan.chunk) return KVC_OK;
   cudaError_t e;

@@ -83,6 +83,8 @@ inline bool encode_attend_tile(CUtensorMap* m, TileGeo* geo, const DevCache& c, 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
+
 // One lane of the warp, always the same.  The control flow around copies and products stays the whole warp's, with
 // operands that are the same in all lanes, and only the instruction itself is the elected lane's: operands then live in
 // uniform registers.  (Inside a branch taken by one lane they are moved there for every instruction: about 110 cycles a

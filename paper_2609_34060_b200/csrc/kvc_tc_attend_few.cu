@@ -60,22 +60,31 @@ struct Piece {
   int b, h, q0, nq, kv, nt, t0, t1;
 };
 
-// A position on the line of tiles: request, head, tile, and how many tiles the walk still takes.
+// A position on the line of tiles: request, head, tile, and how many tiles the walk still takes; the numbers of the
+// request looked at last (`known`) stay with it.
 struct Walk {
   int64_t left;
   int b, h, t;
+  int known, q0, nq, kv, nt;
   __device__ __forceinline__ bool next(const AttendLaunch& a, int rc, Piece& x) {
     if (left <= 0) return false;
     for (;; ++b) {
       if (b >= a.req.n) return false;
-      request_span(a.req, b, nullptr, x.q0, x.nq, x.kv);
-      x.nt = few_tiles(a, rc, x.nq, x.kv);
-      if (x.nt > 0) break;
+      if (b != known) {
+        request_span(a.req, b, nullptr, q0, nq, kv);
+        nt = few_tiles(a, rc, nq, kv);
+        known = b;
+      }
+      if (nt > 0) break;
     }
     x.b = b;
     x.h = h;
+    x.q0 = q0;
+    x.nq = nq;
+    x.kv = kv;
+    x.nt = nt;
     x.t0 = t;
-    x.t1 = (int64_t)(x.nt - t) < left ? x.nt : t + (int)left;
+    x.t1 = (int64_t)(nt - t) < left ? nt : t + (int)left;
     left -= x.t1 - x.t0;
     t = 0;
     if (++h == a.H) {
@@ -94,29 +103,17 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {   // inclusi
   }
   return v;
 }
-// tiles of requests [0, n), and with find >= 0 the request in which tile `find` lies (whole warp)
-__device__ __forceinline__ int64_t line_scan(const AttendLaunch& a, int rc, int lane, int n, int64_t find, uint32_t* status, int* fb, int64_t* before) {
-  int64_t total = 0;
-  for (int b0 = 0; b0 < n; b0 += 32) {
-    int64_t mine = 0;
-    if (b0 + lane < n) {
-      int q0, nq, kv;
-      request_span(a.req, b0 + lane, status, q0, nq, kv);
-      mine = (int64_t)few_tiles(a, rc, nq, kv) * a.H;
-    }
-    const int64_t incl = warp_scan(mine, lane);
-    if (find >= 0) {
-      const unsigned hit = __ballot_sync(0xffffffffu, total + incl > find);
-      if (hit) {
-        const int l = __ffs(hit) - 1;
-        *fb = b0 + l;
-        *before = total + __shfl_sync(0xffffffffu, incl - mine, l);
-        return total;
-      }
-    }
-    total += __shfl_sync(0xffffffffu, incl, 31);
+// tiles of requests [0, n) (whole warp)
+__device__ __forceinline__ int64_t line_length(const AttendLaunch& a, int rc, int lane, int n) {
+  int64_t mine = 0;
+  for (int b = lane; b < n; b += 32) {
+    int q0, nq, kv;
+    request_span(a.req, b, nullptr, q0, nq, kv);
+    mine += (int64_t)few_tiles(a, rc, nq, kv) * a.H;
   }
-  return total;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  return mine;
 }
 
 // Where block c's part of a line of `total` tiles begins; with fewer tiles than blocks, the first `total` blocks take one each.
@@ -126,16 +123,68 @@ __device__ __forceinline__ int64_t line_cut(int64_t total, int c, int blocks) {
   return total * c / blocks;
 }
 
+// The start of block c's part (whole warp): up to 32 requests are read once.
+__device__ __forceinline__ Walk line_start(const AttendLaunch& a, int rc, int lane, int c, int blocks) {
+  const int n = a.req.n;
+  int q0 = 0, nq = 0, kv = 0, nt = 0;
+  if (lane < n) {
+    request_span(a.req, lane, c == 0 ? a.status : nullptr, q0, nq, kv);
+    nt = few_tiles(a, rc, nq, kv);
+  }
+  int64_t incl = warp_scan((int64_t)nt * a.H, lane), total = __shfl_sync(0xffffffffu, incl, 31);
+  for (int b0 = 32; b0 < n; b0 += 32) {
+    int64_t mine = 0;
+    if (b0 + lane < n) {
+      int x, y, z;
+      request_span(a.req, b0 + lane, c == 0 ? a.status : nullptr, x, y, z);
+      mine = (int64_t)few_tiles(a, rc, y, z) * a.H;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    total += mine;
+  }
+  const int64_t lo = line_cut(total, c, blocks), hi = line_cut(total, c + 1, blocks);
+  Walk w{hi - lo, 0, 0, 0, -1, 0, 0, 0, 0};
+  if (hi <= lo) return w;
+  int64_t before = 0;
+  for (int b0 = 0; b0 < n; b0 += 32) {
+    if (b0 > 0) {
+      q0 = nq = kv = nt = 0;
+      if (b0 + lane < n) {
+        request_span(a.req, b0 + lane, nullptr, q0, nq, kv);
+        nt = few_tiles(a, rc, nq, kv);
+      }
+      incl = warp_scan((int64_t)nt * a.H, lane);
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + incl > lo);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      w.b = w.known = b0 + l;
+      w.q0 = __shfl_sync(0xffffffffu, q0, l);
+      w.nq = __shfl_sync(0xffffffffu, nq, l);
+      w.kv = __shfl_sync(0xffffffffu, kv, l);
+      w.nt = __shfl_sync(0xffffffffu, nt, l);
+      const int64_t off = lo - before - (__shfl_sync(0xffffffffu, incl, l) - (int64_t)w.nt * a.H);   // below H nt
+      w.h = off < ((int64_t)1 << 31) ? (int)((uint32_t)off / (uint32_t)w.nt) : (int)(off / w.nt);
+      w.t = (int)(off - (int64_t)w.h * w.nt);
+      return w;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return w;
+}
+
 template <int D, bool Q8, int RC>
 struct Few {
   static constexpr int E = Q8 ? 1 : 2;
   static constexpr int kRows = RC;
   static constexpr int kTile = 128 * D * E;
   static constexpr int kSlots = kTile == 32768 ? 6 : Q8 && D == 128 && RC > 8 ? 10 : 12;
-  static constexpr int kQRows = Q8 ? 2 * RC : RC;              // rows of the query operand: N of the first product
+  static constexpr int kQRows = Q8 ? 2 * RC : RC < 16 ? 16 : RC;   // rows of the query operand: N of the first product
   static constexpr int kQ = kQRows * D * E;
-  static constexpr int kPCols = Q8 ? (RC == 8 ? 32 : 3 * RC) : RC;   // N of the second product
-  static constexpr int kPRow = Q8 ? (RC == 8 ? 32 : RC == 16 ? 64 : 128) : 2 * RC;   // bytes of a token's probabilities
+  static constexpr int kPCols = Q8 ? (RC == 8 ? 32 : 3 * RC) : RC < 16 ? 16 : RC;   // N of the second product
+  static constexpr int kLogits = Q8 ? 2 * RC : RC;             // columns of logits that are read
+  static constexpr int kPRow = Q8 ? (RC == 8 ? 32 : RC == 16 ? 64 : 128) : RC < 16 ? 32 : 2 * RC;   // bytes of a token's probabilities
   static constexpr uint32_t kPSwizzle = kPRow == 32 ? 6 : kPRow == 64 ? 4 : 2;
   static constexpr uint32_t kRowSwizzle = Q8 && D == 64 ? 4 : 2;
   static constexpr int kP = 128 * kPRow;
@@ -156,13 +205,13 @@ template <typename F>
 struct FewBars {
   uint64_t full[F::kSlots], empty[F::kSlots], s_full[F::kSBufs], s_free[F::kSBufs], p_ready[2], pv_done[2], q_full[2], q_empty[2], o_free[2];
   uint64_t e_full[F::kExpRing], e_empty[F::kExpRing];
-  int64_t left;
-  int b, h, t;
+  Walk start;
   uint32_t tmem;
   int abort_flag;
+  int64_t row_at[F::kRows];         // where a row of the finished pair goes
   float red[2][4][F::kRows];
-  float qs[2][F::kRows];
-  float half_m[F::kRows], half_l[F::kRows];      // group 1's maxima and sums of a finished piece
+  float qs[2][F::E == 1 ? F::kRows : 1];   // scales of the query rows (8-bit caches)
+  float half[2][F::kRows];          // group 1's sums and maxima of a finished piece; then the weights of the two halves
   int half_e;
   int red_e[2][4], fail[2][4];
 };
@@ -249,35 +298,24 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     bars.abort_flag = 0;
     fence_barrier_init();
   }
+  if (tid == 32) {
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
+  }
   if (warp == 9) {
     tmem_alloc(smem_u32(&bars.tmem), F::kTmem);
     tmem_relinquish();
   }
   if (warp == 11) {
-    // this block's part of the line
-    const int64_t total = line_scan(p.a, RC, lane, p.a.req.n, -1, blockIdx.x == 0 ? p.a.status : nullptr, nullptr, nullptr);
-    const int64_t lo = line_cut(total, blockIdx.x, p.blocks), hi = line_cut(total, blockIdx.x + 1, p.blocks);
-    int fb = 0;
-    int64_t before = 0;
-    if (hi > lo) line_scan(p.a, RC, lane, p.a.req.n, lo, nullptr, &fb, &before);
-    if (lane == 0) {
-      bars.left = hi - lo;
-      bars.b = fb;
-      bars.h = bars.t = 0;
-      if (hi > lo) {
-        int q0, nq, kv;
-        request_span(p.a.req, fb, nullptr, q0, nq, kv);
-        const int nt = few_tiles(p.a, RC, nq, kv);
-        bars.h = (int)((lo - before) / nt);
-        bars.t = (int)((lo - before) % nt);
-      }
-    }
+    const Walk w = line_start(p.a, RC, lane, (int)blockIdx.x, p.blocks);
+    if (lane == 0) bars.start = w;
   }
+  grid_dependents_launch();        // the join's blocks may take the SMs that finish first
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars.tmem;
-  Walk walk{bars.left, bars.b, bars.h, bars.t};
+  Walk walk = bars.start;
   Piece x;
   const uint32_t gs = (uint32_t)p.g.gs, ps = (uint32_t)p.g.ps;
 
@@ -322,14 +360,14 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         const int sb = g % F::kSBufs;
         wait(s_full + 8 * sb, (g / F::kSBufs) & 1);
         tc_fence_after();
-        float s[F::kQRows];
-        tmem_ld<F::kQRows>(lane_at + sb * F::kQRows, s);
+        float s[F::kLogits];
+        tmem_ld<F::kLogits>(lane_at + sb * F::kQRows, s);
         tmem_ld_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(s_free + 8 * sb);
 #pragma unroll
-        for (int r = 0; r < RC; ++r) s[r] = Q8 ? fmaf(s[(Q8 ? RC : 0) + r], 0.0625f, s[r]) * (bars.qs[piece & 1][r] * ek) : s[r] * c;
+        for (int r = 0; r < RC; ++r) s[r] = Q8 ? fmaf(s[(Q8 ? RC : 0) + r], 0.0625f, s[r]) * (bars.qs[piece & 1][Q8 ? r : 0] * ek) : s[r] * c;
         if (x.kv - x.nq < i * 128 + 128) {                          // the last keys, or some that early rows do not see
           const int lim = p.a.causal ? x.kv - x.nq : x.kv - 1;
 #pragma unroll
@@ -454,10 +492,10 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       named_bar_sync(1 + wg, 128);
       if (wg == 1) {
         named_bar_sync(4, 256);                                     // group 0 has read the last piece's half
-        if (tid4 < RC) bars.half_l[tid4] = last >= g0 ? (bars.red[1][0][tid4] + bars.red[1][1][tid4]) + (bars.red[1][2][tid4] + bars.red[1][3][tid4]) : 0.f;
+        if (tid4 < RC) bars.half[0][tid4] = last >= g0 ? (bars.red[1][0][tid4] + bars.red[1][1][tid4]) + (bars.red[1][2][tid4] + bars.red[1][3][tid4]) : 0.f;
         if (tid4 == 0) {
 #pragma unroll
-          for (int r = 0; r < RC; ++r) bars.half_m[r] = m[r];
+          for (int r = 0; r < RC; ++r) bars.half[1][r] = m[r];
           bars.half_e = eref;
         }
         named_bar_sync(3, 256);
@@ -468,9 +506,34 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         const uint32_t o0 = o_at, o1 = o_at + F::kPCols;
         const bool whole = x.t0 == 0 && x.t1 == x.nt;
         const int64_t slot = ((int64_t)blockIdx.x * 2 + (x.t0 > 0 ? 0 : 1)) * RC;
-        float* ml = p.part + (int64_t)p.blocks * 2 * RC * D;
-        auto unit = [](int e) { return e < -900 ? 0.f : exponent_up((uint32_t)e) * 0.015625f; };
-        const float back0 = Q8 ? unit(eref) : 1.f, back1 = Q8 ? unit(bars.half_e) : 1.f;
+        // a thread a row: weights of the halves, place of the result
+        if (tid4 < R) {
+          const int r = tid4;
+          float mr = minus_inf;
+#pragma unroll
+          for (int k = 0; k < RC; ++k) mr = k == r ? m[k] : mr;
+          const float l0 = (bars.red[0][0][r] + bars.red[0][1][r]) + (bars.red[0][2][r] + bars.red[0][3][r]), l1 = bars.half[0][r], m1 = bars.half[1][r];
+          // a half that saw no key of the row (l = 0) gets no weight, whatever its accumulators hold
+          const float top = l1 == 0.f ? mr : l0 == 0.f ? m1 : fmaxf(mr, m1);
+          float w0 = l0 == 0.f ? 0.f : exp2_fast(mr - top), w1 = l1 == 0.f ? 0.f : exp2_fast(m1 - top);
+          const float sum = w0 * l0 + w1 * l1;
+          const bool dead = sum == 0.f;
+          auto unit = [](int e) { return e < -900 ? 0.f : exponent_up((uint32_t)e) * 0.015625f; };
+          float scale = whole ? (dead ? 0.f : 1.f / sum) : 1.f;
+          w0 *= scale * (Q8 ? unit(eref) : 1.f);
+          w1 *= scale * (Q8 ? unit(bars.half_e) : 1.f);
+          bars.half[0][r] = had0 && l0 != 0.f ? w0 : 0.f;
+          bars.half[1][r] = had1 && l1 != 0.f ? w1 : 0.f;
+          if (whole) {
+            const int64_t at = x.q0 + r / p.a.G;
+            const int head = x.h * p.a.G + r % p.a.G;
+            bars.row_at[r] = at * p.a.out.s_row + (int64_t)head * p.a.out.s_head;
+            if (p.a.lse && ok) p.a.lse[at * (p.a.H * p.a.G) + head] = dead ? minus_inf : (top + log2f(sum)) * kLn2;
+          } else if (ok) {
+            *reinterpret_cast<float2*>(p.part + (int64_t)p.blocks * 2 * RC * D + (slot + r) * 2) = make_float2(top, sum);
+          }
+        }
+        named_bar_sync(1, 128);
 #pragma unroll
         for (int rb = 0; rb < RC; rb += 8) {
           if (rb >= R) continue;
@@ -479,19 +542,14 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           for (int half = 0; half < 2; ++half) {
             float* v = half ? v1 : v0;
             const uint32_t at = half ? o1 : o0;
-            if (!(half ? had1 : had0)) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = 0.f;
-              continue;
-            }
-            tmem_ld8(at + rb, v);
+            tmem_ld8(at + rb, v);                                   // of a half without tiles: stale, weight zero
             if (Q8) {
               float a[8], b[8];
               tmem_ld8(at + (Q8 ? RC : 0) + rb, a);
               tmem_ld8(at + (Q8 ? 2 * RC : 0) + rb, b);
               tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = fmaf(fmaf(b[j], 0.0625f, a[j]), 0.0625f, v[j]) * (half ? back1 : back0);
+              for (int j = 0; j < 8; ++j) v[j] = fmaf(fmaf(b[j], 0.0625f, a[j]), 0.0625f, v[j]);
             } else {
               tmem_ld_wait();
             }
@@ -500,25 +558,13 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           for (int j = 0; j < 8; ++j) {
             const int r = rb + j;
             if (r >= R || !ok) continue;
-            const float l0 = (bars.red[0][0][r] + bars.red[0][1][r]) + (bars.red[0][2][r] + bars.red[0][3][r]), l1 = bars.half_l[r];
-            const float m1 = bars.half_m[r];
-            // a half that saw no key of the row (l = 0) has written no sums of it worth a weight
-            const float top = l1 == 0.f ? m[r] : l0 == 0.f ? m1 : fmaxf(m[r], m1);
-            const float w0 = l0 == 0.f ? 0.f : exp2_fast(m[r] - top), w1 = l1 == 0.f ? 0.f : exp2_fast(m1 - top);
-            const float sum = w0 * l0 + w1 * l1;
-            const bool dead = sum == 0.f;
-            const float v = (l0 == 0.f ? 0.f : v0[j] * w0) + (l1 == 0.f ? 0.f : v1[j] * w1);
-            if (whole) {
-              const int64_t at = x.q0 + r / p.a.G;
-              const int head = x.h * p.a.G + r % p.a.G;
-              if (tid4 < D) p.a.out.p[at * p.a.out.s_row + (int64_t)head * p.a.out.s_head + tid4] = __float2bfloat16(dead ? 0.f : v / sum);
-              if (p.a.lse && tid4 == 0) p.a.lse[at * (p.a.H * p.a.G) + head] = dead ? minus_inf : (top + log2f(sum)) * kLn2;
-            } else {
-              if (tid4 < D) p.part[(slot + r) * D + tid4] = v;
-              if (tid4 == 0) {
-                ml[(slot + r) * 2] = top;
-                ml[(slot + r) * 2 + 1] = sum;
-              }
+            const float w0 = bars.half[0][r], w1 = bars.half[1][r];
+            const float v = (w0 == 0.f ? 0.f : v0[j] * w0) + (w1 == 0.f ? 0.f : v1[j] * w1);
+            if (tid4 < D) {
+              if (whole)
+                p.a.out.p[bars.row_at[r] + tid4] = __float2bfloat16(v);
+              else
+                p.part[(slot + r) * D + tid4] = v;
             }
           }
         }
@@ -634,7 +680,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
                 if (Q8)
                   umma_f8(to, kd + k * 2, qd + k * 2, idesc, k > 0);
                 else
-                  umma_bf16(to, kd + ((k >> 2) * k_part + (k & 3) * 2), qd + ((k >> 2) * (RC * 8) + (k & 3) * 2), idesc, k > 0);
+                  umma_bf16(to, kd + ((k >> 2) * k_part + (k & 3) * 2), qd + ((k >> 2) * (F::kQRows * 8) + (k & 3) * 2), idesc, k > 0);
               }
               umma_commit(s_full + 8 * sb);
               umma_commit(empty + 8 * slot);
@@ -691,13 +737,13 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         uint8_t* dst = sq + (piece & 1) * F::kQAlign;
         const int R = x.nq * p.a.G;
 #pragma unroll 4
-        for (int r0 = 0; r0 < RC; r0 += RPP) {
+        for (int r0 = 0; r0 < (Q8 ? RC : F::kQRows); r0 += RPP) {
           const int r = r0 + lane / LPR;
           uint4 raw = make_uint4(0, 0, 0, 0);
           if (r < R)
             raw = *reinterpret_cast<const uint4*>(p.a.q.p + (int64_t)(x.q0 + r / p.a.G) * p.a.q.s_row + (int64_t)(x.h * p.a.G + r % p.a.G) * p.a.q.s_head + ch * 8);
           if (!Q8) {
-            *reinterpret_cast<uint4*>(dst + (ch >> 3) * (RC * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = raw;
+            *reinterpret_cast<uint4*>(dst + (ch >> 3) * (F::kQRows * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = raw;
           } else {
             float v[8];
             unpack8(raw, v);
@@ -733,7 +779,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
               const int chunk = D == 128 ? (ch >> 1) ^ (rr & 7) : (ch >> 1) ^ ((rr >> 1) & 3);
               *reinterpret_cast<uint2*>(dst + rr * D + (chunk << 4) + (ch & 1) * 8) = code;
             }
-            if (ch == 0) bars.qs[piece & 1][r] = exponent_up(b) * c;
+            if (ch == 0) bars.qs[piece & 1][Q8 ? r : 0] = exponent_up(b) * c;
           }
         }
         fence_proxy_async();
@@ -742,7 +788,6 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       }
     }
   }
-  grid_dependents_launch();
   __syncthreads();
   if (*abort_flag) {
     // copies may still be in flight: give them time to land before the block's memory is handed on
@@ -772,7 +817,7 @@ __global__ void __launch_bounds__(4 * D) attend_few_join_kernel(const __grid_con
   const int nt = few_tiles(p.a, RC, nq, kv), R = nq * p.a.G;
   const bool none = nt == 0 || (int)blockIdx.y * 4 >= R;
   if (!none && warp < 2) {
-    const int64_t sum = line_scan(p.a, RC, lane, warp ? p.a.req.n : b, -1, nullptr, nullptr, nullptr);
+    const int64_t sum = line_length(p.a, RC, lane, warp ? p.a.req.n : b);
     if (lane == 0) (warp ? s_total : s_before) = sum;
   }
   // launched while the main kernel ends: its results are there after this wait.  Every block waits, also those with
@@ -858,7 +903,7 @@ cudaError_t launch(const FewLaunch& p, const CUtensorMap& mk, const CUtensorMap&
 }  // namespace
 
 // rows the kernel is built for, from the rows a request may have (0: more than it takes)
-int few_capacity(int64_t rows, bool q8) { return rows <= 8 && q8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 0; }
+int few_capacity(int64_t rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 0; }
 
 int few_blocks(int n, int max_kv, int H) {
   const int64_t tiles = (int64_t)n * H * (max_kv <= 0 ? 1 : (max_kv + 127) / 128);
@@ -879,7 +924,7 @@ cudaError_t launch_attend_few(const AttendLaunch& a, const tc::TileGeo& g, const
   if (p.blocks <= 0) return cudaErrorInvalidConfiguration;
 #define KVC_FEW(D, Q, R) \
   if (d == D && q8 == Q && rc == R) return launch<D, Q, R>(p, mk, mv, s);
-  KVC_FEW(128, false, 16) KVC_FEW(128, false, 32) KVC_FEW(64, false, 16) KVC_FEW(64, false, 32)
+  KVC_FEW(128, false, 8) KVC_FEW(64, false, 8) KVC_FEW(128, false, 16) KVC_FEW(128, false, 32) KVC_FEW(64, false, 16) KVC_FEW(64, false, 32)
   KVC_FEW(128, true, 8) KVC_FEW(128, true, 16) KVC_FEW(128, true, 32) KVC_FEW(64, true, 8) KVC_FEW(64, true, 16) KVC_FEW(64, true, 32)
 #undef KVC_FEW
   return cudaErrorInvalidValue;

@@ -4,7 +4,7 @@
 
 namespace kvc {
 
-int few_capacity(int64_t rows, bool q8);
+int few_capacity(int64_t rows);
 size_t few_workspace_bytes(int n, int max_kv, int H, int d, int rc);
 cudaError_t launch_attend_few(const AttendLaunch& a, const tc::TileGeo& g, const CUtensorMap& mk, const CUtensorMap& mv, int rc, int d, float* part,
                               cudaStream_t s);
