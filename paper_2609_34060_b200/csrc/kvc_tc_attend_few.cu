@@ -741,7 +741,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           const int r = r0 + lane / LPR;
           uint4 raw = make_uint4(0, 0, 0, 0);
           if (r < R)
-            raw = *reinterpret_cast<const uint4*>(p.a.q.p + (int64_t)(x.q0 + r / p.a.G) * p.a.q.s_row + (int64_t)(x.h * p.a.G + r % p.a.G) * p.a.q.s_head + ch * 8);
+            raw = __ldg(reinterpret_cast<const uint4*>(p.a.q.p + (int64_t)(x.q0 + r / p.a.G) * p.a.q.s_row + (int64_t)(x.h * p.a.G + r % p.a.G) * p.a.q.s_head + ch * 8));
           if (!Q8) {
             *reinterpret_cast<uint4*>(dst + (ch >> 3) * (F::kQRows * 128) + (r >> 3) * 1024 + (r & 7) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = raw;
           } else {
