@@ -693,12 +693,22 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             const uint32_t f1 = e == 255u ? 0x7fc0u : e > 134u ? 254u << 7 : (e + 120u) << 7;
             const uint32_t scale = f1 | (f1 << 16);
             uint32_t nan = 0;
-            uint4 raw[CH];
+            // two chunks a round, the next round's on their way: unrolled whole, this code and the softmax's displace each
+            // other in the instruction cache
+            uint4 raw[2];
 #pragma unroll
-            for (int ch = 0; ch < CH; ++ch) raw[ch] = valid ? *reinterpret_cast<const uint4*>(in + ((ch ^ sw) << 4)) : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + ((j ^ sw) << 4));
+#pragma unroll 1
+            for (int c0 = 0; c0 < CH; c0 += 2) {
+             const uint4 now[2] = {raw[0], raw[1]};
+             if (c0 + 2 < CH) {
 #pragma unroll
-            for (int ch = 0; ch < CH; ++ch) {
-              const uint32_t w[4] = {raw[ch].x, raw[ch].y, raw[ch].z, raw[ch].w};
+               for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + (((c0 + 2 + j) ^ sw) << 4));
+             }
+#pragma unroll
+             for (int jj = 0; jj < 2; ++jj) {
+              const int ch = c0 + jj;
+              const uint32_t w[4] = {valid ? now[jj].x : 0u, valid ? now[jj].y : 0u, valid ? now[jj].z : 0u, valid ? now[jj].w : 0u};
               uint32_t o[8];
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
@@ -711,10 +721,12 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
               const int j0 = (2 * ch) & 7;
               *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
               *reinterpret_cast<uint4*>(q + (((j0 + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+             }
             }
             if (((nan & 0x80808080u) != 0 || e > 134u) && valid) {
               // a NaN code in the row, or a scale beyond one factor: the plain way
               const float s = exponent_up(e);
+#pragma unroll 1
               for (int ch = 0; ch < CH; ++ch) {
                 const uint4 v = *reinterpret_cast<const uint4*>(in + ((ch ^ sw) << 4));
                 const uint32_t w[4] = {v.x, v.y, v.z, v.w};
