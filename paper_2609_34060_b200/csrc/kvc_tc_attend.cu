@@ -561,7 +561,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           const int slot = use % NS;
           ok = wait_all(eb + 8 * slot, ((use / NS) & 1) ^ 1, abort_flag);
           if (!ok) break;
-          tile_load(map, p.a, p.g, ring + slot * bytes, fb + 8 * slot, t0, rows, x.h, entry, lane);
+          tile_load<Q8 || D == 64>(map, p.a, p.g, ring + slot * bytes, fb + 8 * slot, t0, rows, x.h, entry, lane);
         }
       }
     } else if (warp == 9) {

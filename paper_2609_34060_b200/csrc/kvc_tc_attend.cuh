@@ -108,6 +108,8 @@ __device__ __forceinline__ int tile_entry(const AttendLaunch& a, const TileGeo& 
   const int32_t* tab = a.req.table ? a.req.table + (int64_t)b * a.req.table_stride : a.c.page_table;
   return tab[(t0 + lane * g.box_rows) >> a.c.page_shift];
 }
+// kFlat: rows of one part, as g.flat says (known where the kernel is compiled: half the code)
+template <bool kFlat>
 __device__ __forceinline__ void tile_load(const CUtensorMap* map, const AttendLaunch& a, const TileGeo& g, uint32_t dst, uint32_t bar,
                                           int t0, int rows, int h, int entry, int lane) {
   const int nb = tile_boxes(g, rows);
@@ -126,7 +128,7 @@ __device__ __forceinline__ void tile_load(const CUtensorMap* map, const AttendLa
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if (j0 + j < nb) {
-            if (g.flat)
+            if (kFlat)
               tma_load_3d(dst + (uint32_t)((j0 + j) * g.box_bytes), map, bar, 0, row, xs[j]);
             else
               tma_load_5d(dst + (uint32_t)((j0 + j) * g.box_bytes), map, bar, 0, 0, 0, row >> 3, xs[j]);
@@ -135,7 +137,7 @@ __device__ __forceinline__ void tile_load(const CUtensorMap* map, const AttendLa
     }
   } else if (elect_one()) {
     mbar_expect_tx(bar, (uint32_t)g.box_bytes);
-    if (g.flat)
+    if (kFlat)
       tma_load_3d(dst, map, bar, 0, t0, h);
     else
       tma_load_5d(dst, map, bar, 0, t0, 0, h, 0);

@@ -635,7 +635,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
             ok = false;
             break;
           }
-          tile_load(map, p.a, p.g, ring + slot * F::kTile, full + 8 * slot, t0, rows, x.h, entry, lane);
+          tile_load<Q8 || D == 64>(map, p.a, p.g, ring + slot * F::kTile, full + 8 * slot, t0, rows, x.h, entry, lane);
           if (Q8) {
             hand_on();
             held = g0 + k;
