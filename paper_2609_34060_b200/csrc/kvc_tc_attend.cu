@@ -295,6 +295,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
     tmem_alloc(smem_u32(&bars.tmem), 512);
     tmem_relinquish();
   }
+  grid_dependency_wait();                                         // what follows reads what earlier kernels wrote
   grid_dependents_launch();                                       // the join's blocks may take the SMs that finish first
   tc_fence_before();
   __syncthreads();
@@ -776,6 +777,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
 // whose parts begin inside the unit.
 template <int D>
 __global__ void __launch_bounds__(kUnitRows) attend_chunk_join_kernel(const __grid_constant__ ChunkLaunch p) {
+  grid_dependents_launch();
   grid_dependency_wait();                                         // in every block, also those with nothing to join
   const int lane = threadIdx.x & 31, row = threadIdx.x, ch = (int)blockIdx.y * 16;
   const int j = (int)blockIdx.x + 1;
@@ -847,10 +849,9 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
     if (e != cudaSuccess) return e;
     once.mark(dev);
   }
-  attend_chunk_kernel<D, Q8><<<(unsigned)p.blocks, SH::kThreads, SH::kSmem, s>>>(p, mk, mv);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
   if (e != cudaSuccess || p.blocks < 2) return e;
-  return launch_after(attend_chunk_join_kernel<D>, dim3((unsigned)p.blocks - 1, D / 16), kUnitRows, s, p);
+  return launch_after(attend_chunk_join_kernel<D>, dim3((unsigned)p.blocks - 1, D / 16), kUnitRows, 0, s, p);
 }
 
 }  // namespace

@@ -189,22 +189,24 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// A kernel launched with launch_after() may start while the one before it ends; it reads that one's results after
-// grid_dependency_wait(), in every block.
+// A kernel launched with launch_after() may start while the one before it in the stream ends (once all of that one's
+// blocks have called grid_dependents_launch, or have ended); every block of it calls grid_dependency_wait(), which lasts
+// until the one before is done and its memory is visible, before it touches global memory or ends.
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_dependents_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-template <typename P>
-inline cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, cudaStream_t s, const P& p) {
+template <typename... P>
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, const P&... p) {
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p);
+  return cudaLaunchKernelEx(&cfg, kernel, p...);
 }
 
 template <int R>

@@ -306,6 +306,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
     tmem_alloc(smem_u32(&bars.tmem), F::kTmem);
     tmem_relinquish();
   }
+  grid_dependency_wait();          // what follows reads what earlier kernels wrote
   if (warp == 11) {
     const Walk w = line_start(p.a, RC, lane, (int)blockIdx.x, p.blocks);
     if (lane == 0) bars.start = w;
@@ -812,6 +813,7 @@ __global__ void __launch_bounds__(4 * D) attend_few_join_kernel(const __grid_con
   const int b = (int)(blockIdx.x / p.a.H), h = (int)(blockIdx.x % p.a.H);
   const int rr = threadIdx.x / D, r = (int)blockIdx.y * 4 + rr, ch = threadIdx.x % D;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  grid_dependents_launch();
   int q0, nq, kv;
   request_span(p.a.req, b, nullptr, q0, nq, kv);
   const int nt = few_tiles(p.a, RC, nq, kv), R = nq * p.a.G;
@@ -892,12 +894,11 @@ cudaError_t launch(const FewLaunch& p, const CUtensorMap& mk, const CUtensorMap&
     if (e != cudaSuccess) return e;
     once.mark(dev);
   }
-  attend_few_kernel<D, Q8, RC><<<(unsigned)p.blocks, F::kThreads, F::kSmem, s>>>(p, mk, mv);
-  cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_after(attend_few_kernel<D, Q8, RC>, dim3((unsigned)p.blocks), F::kThreads, F::kSmem, s, p, mk, mv);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)p.a.req.max_q * p.a.G;
   const dim3 g((unsigned)((int64_t)p.a.req.n * p.a.H), (unsigned)(((rows < RC ? rows : RC) + 3) / 4));
-  return launch_after(attend_few_join_kernel<D, RC>, g, 4 * D, s, p);
+  return launch_after(attend_few_join_kernel<D, RC>, g, 4 * D, 0, s, p);
 }
 
 }  // namespace
