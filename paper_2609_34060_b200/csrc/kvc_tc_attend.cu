@@ -141,73 +141,91 @@ struct Walk {
   }
 };
 
-__device__ __forceinline__ int64_t warp_total(int64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-// tiles of one head of request b (whole warp, a lane a unit)
-__device__ __forceinline__ int64_t head_tiles(const ChunkLaunch& p, int nq, int kv, int lane) {
-  const int units = units_of(p, nq);
-  int64_t sum = 0;
-  for (int u = lane; u < units; u += 32) sum += unit_tiles(p.a, nq, kv, nq * p.a.G, u).all;
-  return warp_total(sum);
-}
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
   return (a | b) < ((int64_t)1 << 31) ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// The start of block c's part of the line (whole warp).
+__device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {   // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+// Key tiles of one head of 32 requests, each lane with a request of its own (whole warp): a lane adds up its request's
+// units, or, where one has many, the warp does, a lane a unit.
+__device__ __forceinline__ int64_t head_tiles(const ChunkLaunch& p, int nq, int kv, int lane) {
+  const int units = units_of(p, nq);
+  int64_t sum = 0;
+  if (__reduce_max_sync(0xffffffffu, units) <= 8) {
+    for (int u = 0; u < units; ++u) sum += unit_tiles(p.a, nq, kv, nq * p.a.G, u).all;
+    return sum;
+  }
+  unsigned left = __ballot_sync(0xffffffffu, units > 0);
+  while (left) {
+    const int o = __ffs(left) - 1;
+    left &= left - 1;
+    const int nq_o = __shfl_sync(0xffffffffu, nq, o), kv_o = __shfl_sync(0xffffffffu, kv, o), units_o = __shfl_sync(0xffffffffu, units, o);
+    int64_t mine = 0;
+    for (int u = lane; u < units_o; u += 32) mine += unit_tiles(p.a, nq_o, kv_o, nq_o * p.a.G, u).all;
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, k);
+    if (lane == o) sum = mine;
+  }
+  return sum;
+}
+// The start of block c's part of the line (whole warp); up to 32 requests are looked at once.
 __device__ __forceinline__ Walk line_start(const ChunkLaunch& p, int lane, int c) {
   const int n = p.a.req.n;
-  int64_t total = 0, each = 0;
   int q0 = 0, nq = 0, kv = 0;
-  for (int b = 0; b < n; ++b) {
-    request_span(p.a.req, b, c == 0 && lane == 0 ? p.a.status : nullptr, q0, nq, kv);
+  int64_t each = 0, incl = 0, total = 0;
+  auto look = [&](int b0, uint32_t* status) {                     // requests b0 .. b0 + 31
+    q0 = nq = kv = 0;
+    if (b0 + lane < n) request_span(p.a.req, b0 + lane, status, q0, nq, kv);
     each = head_tiles(p, nq, kv, lane);
-    total += each * p.a.H;
+    incl = warp_scan(each * p.a.H, lane);
+  };
+  for (int b0 = 0; b0 < n; b0 += 32) {
+    look(b0, c == 0 ? p.a.status : nullptr);
+    total += __shfl_sync(0xffffffffu, incl, 31);
   }
   const int64_t blocks = total < p.blocks ? total : p.blocks;
   Walk w{0, 0, 0, 0, 0, -1, 0, 0, 0, 0};
   if (c >= blocks) return w;
   const int64_t lo = divide(total * c, blocks);
-  w.left = divide(total * (c + 1), blocks) - lo;
   int64_t before = 0;
-  for (int b = 0; b < n; ++b) {
-    if (n > 1) {
-      request_span(p.a.req, b, nullptr, q0, nq, kv);
-      each = head_tiles(p, nq, kv, lane);
-    }
-    if (before + each * p.a.H <= lo) {
-      before += each * p.a.H;
+  for (int b0 = 0; b0 < n; b0 += 32) {
+    if (n > 32) look(b0, nullptr);
+    const unsigned hit = __ballot_sync(0xffffffffu, before + incl > lo);
+    if (!hit) {
+      before += __shfl_sync(0xffffffffu, incl, 31);
       continue;
     }
-    w.b = w.known = b;
-    w.q0 = q0;
-    w.nq = nq;
-    w.kv = kv;
-    w.units = units_of(p, nq);
-    w.h = (int)divide(lo - before, each);
-    int64_t off = lo - before - w.h * each;
+    const int l = __ffs(hit) - 1;
+    w.b = w.known = b0 + l;
+    w.q0 = __shfl_sync(0xffffffffu, q0, l);
+    w.nq = __shfl_sync(0xffffffffu, nq, l);
+    w.kv = __shfl_sync(0xffffffffu, kv, l);
+    w.units = units_of(p, w.nq);
+    const int64_t head = __shfl_sync(0xffffffffu, each, l);
+    int64_t off = lo - before - (__shfl_sync(0xffffffffu, incl, l) - head * p.a.H);
+    w.h = (int)divide(off, head);
+    off -= w.h * head;
     for (int u0 = 0; u0 < w.units; u0 += 32) {
-      const int mine = u0 + lane < w.units ? unit_tiles(p.a, nq, kv, nq * p.a.G, u0 + lane).all : 0;
-      int incl = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
-      }
-      const unsigned hit = __ballot_sync(0xffffffffu, (int64_t)incl > off);
-      if (hit) {
-        const int l = __ffs(hit) - 1;
-        w.u = u0 + l;
-        w.t = (int)(off - __shfl_sync(0xffffffffu, incl - mine, l));
+      const int mine = u0 + lane < w.units ? unit_tiles(p.a, w.nq, w.kv, w.nq * p.a.G, u0 + lane).all : 0;
+      const int sum = (int)warp_scan(mine, lane);
+      const unsigned in = __ballot_sync(0xffffffffu, (int64_t)sum > off);
+      if (in) {
+        const int k = __ffs(in) - 1;
+        w.u = u0 + k;
+        w.t = (int)(off - __shfl_sync(0xffffffffu, sum - mine, k));
+        w.left = divide(total * (c + 1), blocks) - lo;
         return w;
       }
-      off -= __shfl_sync(0xffffffffu, incl, 31);
+      off -= __shfl_sync(0xffffffffu, sum, 31);
     }
-    break;
+    return w;                                                     // not reached: the tile lies in one of the units
   }
-  w.left = 0;                                                     // not reached: the tile lies in one of the units
   return w;
 }
 
