@@ -66,7 +66,7 @@ struct Shape {
   static constexpr int kSlots = Q8 ? 4 : (D == 128 ? 5 : 8);
   static constexpr int kRawSlots = Q8 ? 2 : 1;
   static constexpr int kThreads = Q8 ? 512 : 384;
-  static constexpr int kRegs = Q8 ? 176 : 208;                    // of the softmax warps; the others keep 72
+  static constexpr int kRegs = Q8 ? 184 : 208;                    // of the softmax warps; the others keep 72 or 88
   static constexpr int kSmem = 1024 + 2 * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0);
 };
 
@@ -542,7 +542,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       piece_done(piece);
     }
   } else {
-    regs_dec<Q8 ? 80 : 88>();
+    regs_dec<Q8 ? 72 : 88>();
     bool ok = true;
     if (warp == 11) {
       // ---- the block's part of the line
