@@ -26,6 +26,7 @@ class Step:
     causal: bool = True
     spare: int = 0                 # padding rows behind the last request
     key_scale: float = 1.0
+    ramp: float = 0.0              # keys grow (or, negative, shrink) linearly with their position, by up to this factor
     seed: int = 0
 
 
@@ -60,6 +61,9 @@ class Built:
             shared = rnd(T, st.H, st.d) * (1.0 if is_v else st.key_scale)
             for b in range(n):
                 x = (shared[: st.kv[b]] if not st.page else rnd(st.kv[b], st.H, st.d) * (1.0 if is_v else st.key_scale))
+                if st.ramp and not is_v and st.kv[b]:
+                    at = torch.arange(st.kv[b]) / st.kv[b]
+                    x = x * (abs(st.ramp) * (at if st.ramp > 0 else 1 - at))[:, None, None]
                 x = x.to(torch.bfloat16)
                 (self.rows_v if is_v else self.rows_k).append(x)
                 if st.page:

@@ -40,6 +40,14 @@ CASES = {
     "d64_token_major": Step([1, 20], [301, 200], d=64, page=32, token_major=True),
     "peaked": Step([40, 1], [400, 300], key_scale=12.0),
     "flat": Step([40, 1], [400, 300], key_scale=0.0),
+    "rising": Step([40, 1, 90], [900, 1000, 700], ramp=60.0),
+    "rising_steeply": Step([1, 70], [700, 800], ramp=900.0, G=2),
+    "falling": Step([40, 1, 90], [900, 1000, 700], ramp=-60.0),
+    "few12": Step([3, 2], [300, 65]),
+    "few24": Step([3, 1], [300, 131], G=8),
+    "few32_d64": Step([4, 2, 1], [300, 131, 128], G=8, d=64),
+    "few16_d64": Step([4, 2, 1], [300, 131, 128], G=4, d=64),
+    "many_short": Step([1] * 70, [1 + 13 * (i % 17) for i in range(70)], H=3, G=2),
 }
 
 
@@ -124,6 +132,75 @@ def test_replayed_graph_takes_new_lengths(nq):
         got = out.clone(), lse.clone()
         want = b.run()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
+@pytest.mark.parametrize("nq", [[1, 1, 1], [60, 1, 17]])
+def test_requests_share_the_caches_own_table(nq, q8):
+    """Several requests without a table of their own read one paged context, each as much of it as its length says."""
+    lens = [200, 130, 64]
+    big = Built(Step([0], [200], q8=q8))
+    c, tab = big.cache, big.req.page_table[0].contiguous()
+    own = (kvc.QCache(c.k, c.v, c.scale_k, c.scale_v, T=200, page_table=tab) if q8 else kvc.Cache(c.k, c.v, T=200, page_table=tab))
+    b = Built(Step(nq, lens, q8=False, seed=5))
+    b.cache = own
+    b.req = kvc.Requests(b.req.q_begin, b.req.kv_len, max(nq), 200)
+    b.st.q8 = q8
+    b.val_k, b.val_v = [big.val_k[0][:n] for n in lens], [big.val_v[0][:n] for n in lens]
+    out, lse = b.run()
+    b.check(out, lse)
+    with pytest.raises(kvc.KvcError):                       # more than the cache holds
+        kvc.kvc_attend(kvc.Requests(b.req.q_begin, b.req.kv_len, max(nq), 201), b.q, own, 0, out, b.workspace())
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with its own scratch, interleaved many times: the results of calls made alone."""
+    bs = [Built(Step([1, 60, 1], [900, 400, 33], G=8)), Built(Step([1] * 20, [500 + i for i in range(20)], q8=True, seed=3))]
+    want = [b.run() for b in bs]
+    streams = [torch.cuda.Stream() for _ in bs]
+    outs = [(torch.zeros_like(b.q), torch.zeros(b.q.shape[:2], device="cuda"), b.workspace()) for b in bs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, s, (out, lse, ws) in zip(bs, streams, outs):
+            with torch.cuda.stream(s):
+                kvc.kvc_attend(b.req, b.q, b.cache, 0, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    for (out, lse, _), (o, l) in zip(outs, want):
+        assert torch.equal(out, o) and torch.equal(lse, l)
+    assert kvc.kvc_status_poll() == 0
+
+
+def test_calls_in_a_row_share_one_scratch():
+    """One stream, one workspace, calls of both kernels one behind the other: each result that of the call alone."""
+    bs = [Built(Step([1] * 5, [700, 300, 9, 128, 513], seed=1)), Built(Step([200], [700], G=2, seed=2)), Built(Step([1, 80], [640, 300], seed=3))]
+    want = [b.run()[0] for b in bs]
+    n = max(b.workspace().numel() for b in bs)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    outs = [[torch.zeros_like(b.q) for b in bs] for _ in range(10)]
+    for row in outs:
+        for b, out in zip(bs, row):
+            kvc.kvc_attend(b.req, b.q, b.cache, 0, out, ws)
+    torch.cuda.synchronize()
+    for row in outs:
+        for out, w in zip(row, want):
+            assert torch.equal(out, w)
+
+
+def test_nan_in_a_seen_key_or_value_shows():
+    """A NaN that a row does see is not swallowed: the row's output is not finite (bf16 and 8-bit, both kernels)."""
+    for q8 in (False, True):
+        for nq in (1, 70):
+            b = Built(Step([nq], [300], q8=q8))
+            code = b.cache.k.view(torch.uint8) if q8 else b.cache.k
+            page = int(b.req.page_table[0, 3])
+            code[0, page, 0, 5, 7] = 0x7F if q8 else float("nan")
+            out, lse = b.run()
+            assert not torch.isfinite(out[:, : b.st.G]).any() and torch.isfinite(out[:, b.st.G:]).all()
+            b = Built(Step([nq], [300], q8=q8))
+            code = b.cache.v.view(torch.uint8) if q8 else b.cache.v
+            code[0, page, 0, 5, 7] = 0x7F if q8 else float("nan")
+            out, lse = b.run()
+            assert not torch.isfinite(out[:, : b.st.G, 7]).any() and torch.isfinite(out[:, b.st.G:]).all() and torch.isfinite(lse).all()
 
 
 def test_same_call_twice_is_bit_identical():
