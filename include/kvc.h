@@ -621,8 +621,11 @@ int kvc_append_q8(const kvc_requests *req, const kvc_heads *k_new, const kvc_hea
  *            overlap on the GPU need one each
  * Keys past kv_len are never used, whatever they hold (NaN included).  A NaN or infinity in a VALUE row below kv_len may
  * reach every row of its request, also those that the causal mask keeps from seeing that token.
- * Logits, maxima, sums and outputs are held in float32.  Over a bf16 cache the probabilities are rounded to bf16 before
- * they meet the values.  Results do not depend on the order in which blocks run.
+ * Logits, maxima, sums and outputs are held in float32 until the output's rounding to bf16.  Probabilities meet the values
+ * rounded to bf16 (2^-8 of themselves); for up to 32 rows (new tokens x query heads per KV head) over an 8-bit cache they
+ * meet the codes as three e4m3 parts: 2^-12 of themselves, or 2^-24 of the row's largest where the value row's scale is
+ * the largest of the request (a step in the output of that scale: value rows 2^12 and more below the largest lose bits).
+ * Results do not depend on the order in which blocks run, and equal calls give equal bits.
  */
 int kvc_attend(const kvc_requests *req, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale, int32_t causal,
                kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);

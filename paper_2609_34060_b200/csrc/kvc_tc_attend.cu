@@ -7,9 +7,17 @@
 // Bound: 4 d flops a (row, key) pair on the tensor cores and one exponential; at d = 128 a 128 x 128 tile costs 1024
 // cycles of either.  So one block keeps two row tiles going: while the softmax warps of one work, the tensor cores run
 // the other's products.  One warp issues both tiles' in turn (two warps let the tiles fall into step, and then either the
-// softmax warps or the tensor cores wait: 314 us against 256 on 2K tokens behind 8K).  P lies over S in tensor memory (2 x 128 columns of S,
-// 2 x d of O: all 512), and A operands come from there: P never passes through shared memory.  It is handed over in two
-// parts (96 and 32 keys), so that most of the second product runs while the rest is still being computed.
+// softmax warps or the tensor cores wait: 314 us against 256 on 2K tokens behind 8K at that time).  P lies over S in
+// tensor memory (2 x 128 columns of S, 2 x d of O: all 512), and A operands come from there: P never passes through
+// shared memory.  It is handed over in two parts (96 and 32 keys), so that most of the second product runs while the rest
+// is still being computed.
+//
+// Measured, 2048 tokens behind 8K, 32 / 8 heads of 128 (240 GFLOP): 220 us (1.09 PFLOP/s) in a short run, 238-250 us
+// once the power cap has set the clock.  What bounds it: a row tile's own chain, softmax (about 1750 cycles), the second
+// product's tail, the next first product, and the hand-overs between them (about 3200 a tile of keys; tensor cores busy
+// 63 % of it).  There is no tensor memory left for a second S.  Local memory would cost more than anything else (shared
+// memory takes all of L1: with 100 bytes of spills in the loop the kernel ran 310 us), and so does code that the
+// instruction cache does not hold (8-bit conversion unrolled whole: 277 us on the image context, in rounds 233).
 //
 // Exponentials stay on the special-function units (16 a cycle and SM, a tile's time of the tensor cores).  Moving a
 // quarter or half of them to the FMA pipe (rounding to a whole exponent and a degree-5 polynomial) made the kernel
@@ -26,9 +34,11 @@
 // part; ragged and causal batches balance to a tile.  Of a unit cut by its borders a block leaves a float32 partial
 // result (at most two a block); a second kernel joins those in a fixed order.
 //
-// Warps: 0-3 and 4-7 softmax and epilogue of the row tiles (a thread a row), 8 and 10 loads, 9 products, 11 walks the block's part of the line and hands its pieces to the others through shared memory (their registers are
-// for the work itself); 8-bit caches: 12-15 turn raw tiles into bf16 ones (code * 2^e, exact).  Every wait is bounded; on
-// expiry the CTA records KVC_FLAG_WAIT_EXPIRED and returns.
+// Warps: 0-3 and 4-7 softmax and epilogue of the row tiles (a thread a row; two threads a row with sixteen warps were no
+// faster, 235 us), 8 and 10 loads of keys and values, 9 products, 11 walks the block's part of the line and hands its
+// pieces to the others through shared memory (their registers are for the work itself); 8-bit caches: 12-15 turn raw
+// tiles into bf16 ones (code * 2^e, exact).  Every wait is bounded; on expiry the CTA records KVC_FLAG_WAIT_EXPIRED and
+// returns.
 #include <cuda_runtime.h>
 
 #include "kvc_launch.h"

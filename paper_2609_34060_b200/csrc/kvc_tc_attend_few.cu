@@ -26,6 +26,10 @@
 //     p 2^(e_v - E) 64 = t1 + t2 / 16 + t3 / 256 ,   E the largest exponent of a value row so far .
 // Sums and joins are float32.  Over bf16 caches P is rounded to bf16 as in the chunk kernel.
 //
+// Measured: 64 requests of 4K (lognormal), 32 / 8 heads, bf16 pages of 16: 201 us = 6.4 TB/s of 6.55 copied; eight
+// requests of 32K, 64 / 8 heads, 8-bit pages of 16: 111 us (100 with pages of 128: the copies of 2 KB boxes then bound it,
+// and 12 us are start and join); one request of 777 keys: 12 us, of which 3 are the join's.
+//
 // Warps: 0-3 and 4-7 softmax (0-3 epilogue), 8 first products, 9 second products, 10 queries of the next pair, 12-15
 // loads: keys and values of even and odd tiles, with the exponents of 8-bit rows (a 16-token page is one small box, and
 // one or two warps issuing them all were the bound: 8-bit batch at 32K 120 us with two).  Every wait is bounded.
