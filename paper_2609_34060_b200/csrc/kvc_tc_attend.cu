@@ -349,30 +349,20 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
     int g = 0;                                                    // key tiles of the block so far
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && wait_all(bar, parity, abort_flag); };
-    // queries of a piece's row tile, D / 8 lanes a row; 8-bit caches: channels 1 and 2 of every four change places, as
-    // their keys do
+    // queries of a piece's row tile, a thread its row, all loads in flight at once; 8-bit caches: channels 1 and 2 of
+    // every four change places, as their keys do
     auto load_q = [&](const Piece& y) {
-      constexpr int LPR = D / 8, RPP = 32 / LPR;
-      const int mine = y.u * kUnitRows + t * 128 + row, tok = mine / p.a.G;
-      const int64_t at = mine < y.rows ? (int64_t)(y.q0 + tok) * p.a.q.s_row + (int64_t)(y.h * p.a.G + mine - tok * p.a.G) * p.a.q.s_head : -1;
-      const int ch = lane % LPR;
-      // four loads at a time in a loop: code that runs once a piece is paid for by the instructions fetched
-#pragma unroll 1
-      for (int i0 = 0; i0 < 32; i0 += 4 * RPP) {
-        uint4 v[4];
+      const int r = y.u * kUnitRows + t * 128 + row, tok = r / p.a.G;
+      const bool live = r < y.rows;
+      const uint4* src = reinterpret_cast<const uint4*>(p.a.q.p + (live ? (int64_t)(y.q0 + tok) * p.a.q.s_row + (int64_t)(y.h * p.a.G + r - tok * p.a.G) * p.a.q.s_head : 0));
+      uint8_t* dst = sq + t * SH::kTile + (row >> 3) * 1024 + (row & 7) * 128;
+      uint4 v[D / 8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t src = __shfl_sync(0xffffffffu, at, i0 + i * RPP + lane / LPR);
-          v[i] = src >= 0 ? __ldg(reinterpret_cast<const uint4*>(p.a.q.p + src + ch * 8)) : make_uint4(0, 0, 0, 0);
-        }
+      for (int j = 0; j < D / 8; ++j) v[j] = live ? __ldg(src + j) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = (warp & 3) * 32 + i0 + i * RPP + lane / LPR;
-          if (Q8)
-            v[i] = make_uint4(__byte_perm(v[i].x, v[i].y, 0x5410), __byte_perm(v[i].x, v[i].y, 0x7632), __byte_perm(v[i].z, v[i].w, 0x5410),
-                              __byte_perm(v[i].z, v[i].w, 0x7632));
-          *reinterpret_cast<uint4*>(sq + t * SH::kTile + (ch >> 3) * 16384 + (r >> 3) * 1024 + (r & 7) * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[i];
-        }
+      for (int j = 0; j < D / 8; ++j) {
+        if (Q8) v[j] = make_uint4(__byte_perm(v[j].x, v[j].y, 0x5410), __byte_perm(v[j].x, v[j].y, 0x7632), __byte_perm(v[j].z, v[j].w, 0x5410), __byte_perm(v[j].z, v[j].w, 0x7632));
+        *reinterpret_cast<uint4*>(dst + (j >> 3) * 16384 + (((j & 7) ^ (row & 7)) << 4)) = v[j];
       }
       fence_proxy_async();
       mbar_arrive(q_full + 8 * t);
@@ -887,19 +877,25 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
 // Which kernels a call launches: requests of up to `rc` rows a KV head go to the few-rows kernel (rc = 0: none), the
 // others to this one (chunk = false: there are none).  Decided from the bounds alone: all requests within the few-rows
 // kernel's 32 rows take it; a batch of several requests with longer ones among them is served by both, single tokens by
-// the few-rows kernel; one long request by this kernel.
+// the few-rows kernel; one long request by this kernel.  Both cost two more launches one behind the other, about 10 us,
+// and a tile of a single token costs this kernel about twice the other's time (0.02 against 0.01 us with all SMs at
+// work): about a thousand tiles pay for them.  The host knows the longest request only, and lengths about half of it on
+// average are the rule, so batches that could hold up to kBothTiles key tiles stay with this kernel alone (10 requests
+// of 8 heads, 1528 keys on average and 3056 at most: 36 us, by both 53; nine of 2 heads, 1500 keys on average: 35 and 50).
+constexpr int64_t kBothTiles = 2048;
 struct Plan {
   int rc;
   bool chunk;
 };
-static Plan attend_plan(int n, int max_q, int G) {
+static Plan attend_plan(int n, int max_q, int max_kv, int G, int H) {
   const int64_t rows = (int64_t)max_q * G;
   if (const int rc = few_capacity(rows)) return {rc, false};
-  return {n > 1 ? few_capacity(G) : 0, true};
+  const bool both = n > 1 && (int64_t)n * H * ((max_kv + 127) / 128) > kBothTiles;
+  return {both ? few_capacity(G) : 0, true};
 }
 
 size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d) {
-  const Plan p = attend_plan(n, max_q, G);
+  const Plan p = attend_plan(n, max_q, max_kv, G, H);
   size_t bytes = p.rc ? (few_workspace_bytes(n, max_kv, H, d, p.rc) + 255) / 256 * 256 : 0;
   if (p.chunk) {
     const int64_t blocks = chunk_blocks(n, max_q, max_kv, G, H);
@@ -911,7 +907,7 @@ size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int
 int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   (void)L;
   const bool q8 = a.e.k != nullptr;
-  const Plan plan = attend_plan(a.req.n, a.req.max_q, a.G);
+  const Plan plan = attend_plan(a.req.n, a.req.max_q, a.req.max_kv, a.G, a.H);
   ChunkLaunch p;
   p.a = a;
   p.min_rows = plan.rc + 1;
