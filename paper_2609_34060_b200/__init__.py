@@ -304,26 +304,28 @@ class QCache:
 
 class Requests:
     """A serving step's requests: ``q_begin`` int32 [n+1], ``kv_len`` int32 [n] and ``page_table`` int32 [n, pages] on the
-    GPU (None: every request reads the cache's own table or rows), and host bounds on their values."""
+    GPU (None: every request reads the cache's own table or rows), and host bounds on their values.  Fixed once made: the
+    tensors' contents may change from step to step, the tensors and the bounds not."""
 
     def __init__(self, q_begin: torch.Tensor, kv_len: torch.Tensor, max_q: int, max_kv: int, page_table: Optional[torch.Tensor] = None):
         assert q_begin.dtype == kv_len.dtype == torch.int32 and q_begin.is_contiguous() and kv_len.is_contiguous()
         assert q_begin.numel() == kv_len.numel() + 1
-        self.q_begin, self.kv_len, self.page_table = q_begin, kv_len, page_table
-        self.n, self.max_q, self.max_kv = int(kv_len.numel()), int(max_q), int(max_kv)
         stride = 0
         if page_table is not None:
-            assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == self.n
+            assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == kv_len.numel()
             assert page_table.shape[1] <= 1 or page_table.stride(1) == 1
-            stride = int(page_table.stride(0)) if self.n > 1 else int(page_table.shape[1])
+            stride = int(page_table.stride(0)) if kv_len.numel() > 1 else int(page_table.shape[1])
             assert stride >= int(page_table.shape[1])
-            assert self.max_kv >= 0
-        self._pages = 0 if page_table is None else int(page_table.shape[1])
-        self._struct = kvc_requests(self.n, self.max_q, self.max_kv, stride, q_begin.data_ptr(), kv_len.data_ptr(),
-                                    0 if page_table is None else page_table.data_ptr())
-        self._at = C.addressof(self._struct)
+            assert max_kv >= 0
+        made = kvc_requests(kv_len.numel(), int(max_q), int(max_kv), stride, q_begin.data_ptr(), kv_len.data_ptr(),
+                            0 if page_table is None else page_table.data_ptr())
         devs = {t.get_device() for t in (q_begin, kv_len, page_table) if t is not None}
-        self._dev = devs.pop() if len(devs) == 1 else -1
+        self.__dict__.update(q_begin=q_begin, kv_len=kv_len, page_table=page_table, n=int(kv_len.numel()), max_q=int(max_q),
+                             max_kv=int(max_kv), _pages=0 if page_table is None else int(page_table.shape[1]), _struct=made,
+                             _at=C.addressof(made), _dev=devs.pop() if len(devs) == 1 else -1)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"Requests.{name} is fixed; write into its tensors, or make another Requests")
 
     def struct(self) -> kvc_requests:
         return self._struct
@@ -767,16 +769,23 @@ def _heads(t: torch.Tensor, d: int, what: str) -> bytes:
 
 
 def _desc(c):
-    """(address of the descriptor of a Cache or QCache, its device), made again when its tensors or length changed."""
-    q8 = type(c) is QCache
-    key = (c.k.data_ptr(), c.v.data_ptr(), c.T, -1 if c.page_table is None else c.page_table.data_ptr()) + \
-        ((c.scale_k.data_ptr(), c.scale_v.data_ptr()) if q8 else ())
-    got = c.__dict__.get("_made")
-    if got is None or got[0] != key:
-        devs = {t.get_device() for t in (c.k, c.v, c.page_table) + ((c.scale_k, c.scale_v) if q8 else ()) if t is not None}
+    """(descriptor of a Cache or QCache, its address, its device): the structure is kept, its pointers set at every call."""
+    shape = (c.L, c.H, c.T, c.d, c.page, c.P, c.token_major, c.page_table is None)
+    made = c.__dict__.get("_made")
+    if made is None or made[0] != shape:
         s = c.struct()
-        got = c.__dict__["_made"] = (key, C.addressof(s), devs.pop() if len(devs) == 1 else -1, s)
-    return got
+        made = c.__dict__["_made"] = (shape, s, C.addressof(s), s.codes if type(c) is QCache else s)
+    _, s, at, rows = made
+    rows.k, rows.v = c.k.data_ptr(), c.v.data_ptr()
+    dev = c.k.get_device()
+    same = c.v.get_device() == dev
+    if c.page_table is not None:
+        rows.page_table = c.page_table.data_ptr()
+        same = same and c.page_table.get_device() == dev
+    if type(c) is QCache:
+        s.scale_k, s.scale_v = c.scale_k.data_ptr(), c.scale_v.data_ptr()
+        same = same and c.scale_k.get_device() == c.scale_v.get_device() == dev
+    return s, at, dev if same else -1
 
 
 def _here(what: str, stream, made, *tensors):
