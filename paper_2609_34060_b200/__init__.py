@@ -180,7 +180,15 @@ def version() -> str:
 # ---- descriptors over torch tensors ------------------------------------------------
 
 
-class Cache:
+class _Described:
+    """Base of the caches: setting an attribute drops the descriptor kept between calls."""
+
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_made", None)
+        object.__setattr__(self, name, value)
+
+
+class Cache(_Described):
     """A cache descriptor over torch tensors (which it keeps alive).
 
     contiguous: ``k``, ``v`` bf16 [L, H, T, d]; ``token_major=True``: [L, T, H, d] (each token with all its
@@ -246,7 +254,7 @@ class Cache:
         return Cache(k, v, T=0, page_table=torch.empty(0, dtype=torch.int32, device=k.device), token_major=token_major)
 
 
-class QCache:
+class QCache(_Described):
     """A cache held in 8 bits: ``k``, ``v`` float8_e4m3fn codes in the shapes of :class:`Cache`, ``scale_k``, ``scale_v``
     uint8 exponents of the same shapes without the channel axis (value = code * 2^(exponent - 127))."""
 
@@ -769,23 +777,21 @@ def _heads(t: torch.Tensor, d: int, what: str) -> bytes:
 
 
 def _desc(c):
-    """(descriptor of a Cache or QCache, its address, its device): the structure is kept, its pointers set at every call."""
-    shape = (c.L, c.H, c.T, c.d, c.page, c.P, c.token_major, c.page_table is None)
+    """(address of the descriptor of a Cache or QCache, its device): the structure is kept until an attribute of the
+    object is set, its pointers are set at every call."""
     made = c.__dict__.get("_made")
-    if made is None or made[0] != shape:
+    if made is None:
+        q8 = type(c) is QCache
         s = c.struct()
-        made = c.__dict__["_made"] = (shape, s, C.addressof(s), s.codes if type(c) is QCache else s)
-    _, s, at, rows = made
+        devs = {t.get_device() for t in (c.k, c.v, c.page_table) + ((c.scale_k, c.scale_v) if q8 else ()) if t is not None}
+        made = c.__dict__["_made"] = (C.addressof(s), devs.pop() if len(devs) == 1 else -1, s.codes if q8 else s, s if q8 else None)
+    rows, q = made[2], made[3]
     rows.k, rows.v = c.k.data_ptr(), c.v.data_ptr()
-    dev = c.k.get_device()
-    same = c.v.get_device() == dev
     if c.page_table is not None:
         rows.page_table = c.page_table.data_ptr()
-        same = same and c.page_table.get_device() == dev
-    if type(c) is QCache:
-        s.scale_k, s.scale_v = c.scale_k.data_ptr(), c.scale_v.data_ptr()
-        same = same and c.scale_k.get_device() == c.scale_v.get_device() == dev
-    return s, at, dev if same else -1
+    if q is not None:
+        q.scale_k, q.scale_v = c.scale_k.data_ptr(), c.scale_v.data_ptr()
+    return made
 
 
 def _here(what: str, stream, made, *tensors):
@@ -808,24 +814,24 @@ def _holds(req: Requests, c, what: str) -> None:
 def kvc_quantize(src: Cache, dst: QCache, stream=None) -> None:
     """dst = e4m3(src), one power-of-two scale per (layer, head, token)."""
     s, d = _desc(src), _desc(dst)
-    st = _here("kvc_quantize", stream, (s[2], d[2]))
-    _check(load().kvc_quantize(s[1], d[1], st), "kvc_quantize")
+    st = _here("kvc_quantize", stream, (s[1], d[1]))
+    _check(load().kvc_quantize(s[0], d[0], st), "kvc_quantize")
 
 
 def kvc_dequantize(src: QCache, dst: Cache, stream=None) -> None:
     """dst = bf16(code * 2^(exponent - 127))."""
     s, d = _desc(src), _desc(dst)
-    st = _here("kvc_dequantize", stream, (s[2], d[2]))
-    _check(load().kvc_dequantize(s[1], d[1], st), "kvc_dequantize")
+    st = _here("kvc_dequantize", stream, (s[1], d[1]))
+    _check(load().kvc_dequantize(s[0], d[0], st), "kvc_dequantize")
 
 
 def kvc_append(req: Requests, k_new: torch.Tensor, v_new: torch.Tensor, cache, layer: int, stream=None) -> None:
     """Write the new tokens' rows [rows, H, d] into `layer` of a Cache, or quantised into a QCache."""
     c, k, v = _desc(cache), _heads(k_new, cache.d, "k_new"), _heads(v_new, cache.d, "v_new")
-    st = _here("kvc_append", stream, (c[2], req._dev), k_new, v_new)
+    st = _here("kvc_append", stream, (c[1], req._dev), k_new, v_new)
     _holds(req, cache, "kvc_append")
     fn = load().kvc_append_q8 if type(cache) is QCache else load().kvc_append
-    _check(fn(req._at, k, v, int(layer), c[1], st), "kvc_append")
+    _check(fn(req._at, k, v, int(layer), c[0], st), "kvc_append")
 
 
 def kvc_attend_workspace_bytes(req: Requests, cache, n_heads: int) -> int:
@@ -836,12 +842,12 @@ def kvc_attend(req: Requests, q: torch.Tensor, cache, layer: int, out: torch.Ten
                scale: Optional[float] = None, causal: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
     """Attention of the new tokens' queries [rows, heads, d] over `layer` of a Cache or QCache (scale: 1 / sqrt(d))."""
     c, hq, ho = _desc(cache), _heads(q, cache.d, "q"), _heads(out, cache.d, "out")
-    st = _here("kvc_attend", stream, (c[2], req._dev), q, out, workspace, lse)
+    st = _here("kvc_attend", stream, (c[1], req._dev), q, out, workspace, lse)
     _holds(req, cache, "kvc_attend")
     if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
         raise KvcError(KVC_E_INVALID_ARG, "kvc_attend: lse must be float32 [rows, heads]")
     fn = load().kvc_attend_q8 if type(cache) is QCache else load().kvc_attend
-    _check(fn(req._at, hq, c[1], int(layer), cache.d ** -0.5 if scale is None else float(scale), bool(causal), ho,
+    _check(fn(req._at, hq, c[0], int(layer), cache.d ** -0.5 if scale is None else float(scale), bool(causal), ho,
               None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
               0 if workspace is None else workspace.numel() * workspace.element_size(), st), "kvc_attend")
 

@@ -139,14 +139,15 @@ def test_descriptors_follow_the_objects():
     """A cache's tensors may be replaced between calls; a Requests refuses it (its checks ran when it was made)."""
     mk = lambda: torch.zeros(1, 3, 2, 16, 64, dtype=torch.bfloat16)
     c = kvc.Cache.pool(mk(), mk())
-    at = lambda: (kvc._desc(c)[0].k, kvc._desc(c)[0].v, kvc._desc(c)[0].page_table, kvc._desc(c)[0].T)
+    held = lambda c, kind: kind.from_address(kvc._desc(c)[0])
+    at = lambda: tuple(getattr(held(c, kvc.kvc_cache), f) for f in ("k", "v", "page_table", "T"))
     assert at() == (c.k.data_ptr(), c.v.data_ptr(), c.page_table.data_ptr() or None, 0)
     c.v, c.page_table, c.T = mk(), torch.zeros(2, dtype=torch.int32), 32
     assert at() == (c.k.data_ptr(), c.v.data_ptr(), c.page_table.data_ptr(), 32)
     q = kvc.QCache.like(c)
     kvc._desc(q)
     q.k, q.scale_v = torch.zeros_like(q.k), torch.zeros_like(q.scale_v)
-    s = kvc._desc(q)[0]
+    s = held(q, kvc.kvc_qcache)
     assert (s.codes.k, s.codes.v, s.scale_k, s.scale_v) == tuple(t.data_ptr() for t in (q.k, q.v, q.scale_k, q.scale_v))
     r = kvc.Requests(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 1, 16)
     with pytest.raises(AttributeError):
