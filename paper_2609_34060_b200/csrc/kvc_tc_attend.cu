@@ -64,6 +64,7 @@ struct ChunkLaunch {
   TileGeo g;                               // of the raw tile
   int32_t blocks;
   int32_t min_rows;                        // requests with fewer rows belong to the other kernel
+  bool fine;                               // few units in many pieces: the join's small blocks
   UnitStart* starts;                       // [blocks]
   float* ml;                               // [blocks][2][256][2] maximum and sum of the rows of a block's two cut units
   float* part;                             // [blocks][2][256][d] their sums
@@ -790,14 +791,20 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
   }
 }
 
-// ---- join of the units that block borders cut; grid: x = border in front of block x + 1, y = 16 channels, a thread a row.
-// The first border inside a unit does its work: the pieces are slot 1 of the block before it and slot 0 of the blocks
-// whose parts begin inside the unit.
-template <int D>
-__global__ void __launch_bounds__(kUnitRows) attend_chunk_join_kernel(const __grid_constant__ ChunkLaunch p) {
+// ---- join of the units that block borders cut; grid: x = border in front of block x + 1, y = 32 rows (a lane a row) and
+// 8 CH channels (CH a warp).  The first border inside a unit does its work: the pieces are slot 1 of the block before it
+// and slot 0 of the blocks whose parts begin inside the unit.  The warps share the pieces' weights, and the loads of
+// several pieces are in flight at once.  Few units in many pieces (four a unit and more) take more and smaller blocks, CH = 4:
+// 427 rows over 3133 keys, 25 pieces a unit: 19 us in all, 40 with a thread a row and piece after piece.  Many
+// units in two or three pieces each take CH = D / 8 (2K tokens behind 8K 212 us, by small blocks 217).
+template <int D, int CH>
+__global__ void __launch_bounds__(256) attend_chunk_join_kernel(const __grid_constant__ ChunkLaunch p) {
+  constexpr int kJoinPieces = CH == 4 ? 64 : 16;                  // weights held at once
+  __shared__ float s_w[kJoinPieces][32], s_part[8][32];
   grid_dependents_launch();
   grid_dependency_wait();                                         // in every block, also those with nothing to join
-  const int lane = threadIdx.x & 31, row = threadIdx.x, ch = (int)blockIdx.y * 16;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row = (int)(blockIdx.y & 7) * 32 + lane, ch = ((int)(blockIdx.y >> 3) * 8 + warp) * CH;
   const int j = (int)blockIdx.x + 1;
   const UnitStart me = p.starts[j], before = p.starts[j - 1];
   if (me.b < 0 || me.t == 0) return;
@@ -805,7 +812,8 @@ __global__ void __launch_bounds__(kUnitRows) attend_chunk_join_kernel(const __gr
   if (same(before)) return;
   int q0, nq, kv;
   request_span(p.a.req, me.b, nullptr, q0, nq, kv);
-  const int r = me.u * kUnitRows + row;
+  const int r = me.u * kUnitRows + row, rows = nq * p.a.G;
+  if (r - lane >= rows) return;
   int pieces = 2;                                                 // blocks j - 1, j, ...
   for (bool go = true; go; pieces += 32) {
     const int k = j + pieces - 1 + lane;
@@ -816,42 +824,85 @@ __global__ void __launch_bounds__(kUnitRows) attend_chunk_join_kernel(const __gr
       go = false;
     }
   }
-  if (r >= nq * p.a.G) return;
   const float c = p.a.scale * kLog2e, minus_inf = __uint_as_float(0xff800000u);
   auto place = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0 ? 1 : 0)) * kUnitRows; };
-  float m = minus_inf, l = 0.f, acc[16];
+  auto held = [&](int i) { return *reinterpret_cast<const float2*>(p.ml + 2 * (place(i) + row)); };
+  constexpr int kAtOnce = CH == 4 ? 8 : 16 / CH;                                // pieces whose sums are in flight: before their weights are known
+  float x[kAtOnce][CH];
+  auto load = [&](int i0) {
 #pragma unroll
-  for (int q = 0; q < 16; ++q) acc[q] = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < pieces; ++i) {
-    const float2 v = *reinterpret_cast<const float2*>(p.ml + 2 * (place(i) + row));
-    if (v.y != 0.f) m = fmaxf(m, v.x);
-  }
-#pragma unroll 2
-  for (int i = 0; i < pieces; ++i) {
-    const float2 v = *reinterpret_cast<const float2*>(p.ml + 2 * (place(i) + row));
-    if (v.y == 0.f) continue;                                     // a piece that saw no key of the row wrote no sums of it
-    const float w = exp2f((v.x - m) * c);
-    l += w * v.y;
-    const float* o = p.part + place(i) * D + row;
+    for (int k = 0; k < kAtOnce; ++k) {
+      const float* o = p.part + place(i0 + k) * D + row + ch * kUnitRows;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) acc[q] += w * o[(ch + q) * kUnitRows];
+      for (int q = 0; q < CH; ++q) x[k][q] = i0 + k < pieces ? o[q * kUnitRows] : 0.f;
+    }
+  };
+  load(0);
+  float m = minus_inf;
+  float2 v[kJoinPieces / 8];
+  for (int i0 = (pieces - 1) / kJoinPieces * kJoinPieces; i0 >= 0; i0 -= kJoinPieces) {   // the first ones stay in v
+#pragma unroll
+    for (int k = 0; k < kJoinPieces / 8; ++k) v[k] = i0 + k * 8 + warp < pieces ? held(i0 + k * 8 + warp) : make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kJoinPieces / 8; ++k)
+      if (v[k].y != 0.f) m = fmaxf(m, v[k].x);
   }
+  s_part[warp][lane] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) m = fmaxf(m, s_part[w][lane]);
+  float sum = 0.f, acc[CH];
+#pragma unroll
+  for (int q = 0; q < CH; ++q) acc[q] = 0.f;
+  for (int i0 = 0; i0 < pieces; i0 += kJoinPieces) {
+    const int n = min(kJoinPieces, pieces - i0);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kJoinPieces / 8; ++k) {
+      const int i = k * 8 + warp;
+      if (i >= n) break;
+      if (i0 > 0) v[k] = held(i0 + i);
+      const bool none = v[k].y == 0.f;                            // a piece that saw no key of the row wrote no sums of it
+      const float w = none ? -1.f : exp2f((v[k].x - m) * c);
+      s_w[i][lane] = w;
+      if (!none) sum += w * v[k].y;
+    }
+    __syncthreads();
+    for (int i = 0; i < n; i += kAtOnce) {
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const float w = i + k < n ? s_w[i + k][lane] : -1.f;
+#pragma unroll
+        for (int q = 0; q < CH; ++q) acc[q] = w < 0.f ? acc[q] : fmaf(w, x[k][q], acc[q]);
+      }
+      if (i0 + i + kAtOnce < pieces) load(i0 + i + kAtOnce);
+    }
+  }
+  __syncthreads();
+  s_part[warp][lane] = sum;
+  __syncthreads();
+  if (r >= rows) return;
+  float l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) l += s_part[w][lane];
   const bool dead = l == 0.f;
   const float inv = dead ? 0.f : 1.f / l;
   const int64_t tok = q0 + r / p.a.G;
   const int head = me.h * p.a.G + r % p.a.G;
   __nv_bfloat16* dst = p.a.out.p + tok * p.a.out.s_row + (int64_t)head * p.a.out.s_head + ch;
 #pragma unroll
-  for (int q = 0; q < 16; ++q) acc[q] = dead ? 0.f : acc[q] * inv;
-  *reinterpret_cast<uint4*>(dst) = pack8(acc);
-  *reinterpret_cast<uint4*>(dst + 8) = pack8(acc + 8);
+  for (int q = 0; q < CH; ++q) acc[q] = dead ? 0.f : acc[q] * inv;
+  if constexpr (CH == 4)
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(acc[0], acc[1]), pack2(acc[2], acc[3]));
+  else
+#pragma unroll
+    for (int q = 0; q < CH; q += 8) *reinterpret_cast<uint4*>(dst + q) = pack8(acc + q);
   if (p.a.lse && ch == 0) p.a.lse[tok * (p.a.H * p.a.G) + head] = dead ? minus_inf : m * p.a.scale + log2f(l) * kLn2;
 }
 
+int64_t chunk_units(int n, int max_q, int G, int H) { return (int64_t)n * H * (((int64_t)max_q * G + kUnitRows - 1) / kUnitRows); }
 int64_t chunk_blocks(int n, int max_q, int max_kv, int G, int H) {
-  const int64_t units = (int64_t)n * H * (((int64_t)max_q * G + kUnitRows - 1) / kUnitRows);
-  const int64_t tiles = units * (max_kv <= 0 ? 1 : (max_kv + 127) / 128);
+  const int64_t tiles = chunk_units(n, max_q, G, H) * (max_kv <= 0 ? 1 : (max_kv + 127) / 128);
   const int sms = device_sm_count();
   return tiles < sms ? tiles : sms;
 }
@@ -869,7 +920,8 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
   }
   const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
   if (e != cudaSuccess || p.blocks < 2) return e;
-  return launch_after(attend_chunk_join_kernel<D>, dim3((unsigned)p.blocks - 1, D / 16), kUnitRows, 0, s, p);
+  if (p.fine) return launch_after(attend_chunk_join_kernel<D, 4>, dim3((unsigned)p.blocks - 1, 8 * (D / 32)), 256, 0, s, p);
+  return launch_after(attend_chunk_join_kernel<D, D / 8>, dim3((unsigned)p.blocks - 1, 8), 256, 0, s, p);
 }
 
 }  // namespace
@@ -913,6 +965,7 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   p.min_rows = plan.rc + 1;
   p.blocks = (int)chunk_blocks(a.req.n, a.req.max_q, a.req.max_kv, a.G, a.H);
   if (p.blocks <= 0) return KVC_E_CUDA;
+  p.fine = 4 * chunk_units(a.req.n, a.req.max_q, a.G, a.H) <= p.blocks;
   CUtensorMap mk, mv;
   bool ok;
   if (q8)
