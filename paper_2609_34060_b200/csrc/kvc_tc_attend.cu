@@ -791,9 +791,9 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
   }
 }
 
-// ---- join of the units that block borders cut; grid: x = border in front of block x + 1, y = 32 rows (a lane a row) and
-// 8 CH channels (CH a warp).  The first border inside a unit does its work: the pieces are slot 1 of the block before it
-// and slot 0 of the blocks whose parts begin inside the unit.  The warps share the pieces' weights, and the loads of
+// ---- join of the units that block borders cut; grid: x = border in front of block x + 1 (CH = 4: a unit), y = 32 rows (a
+// lane a row) and 8 CH channels (CH a warp).  The first border inside a unit does its work: the pieces are slot 1 of the
+// block before it and slot 0 of the blocks whose parts begin inside the unit.  The warps share the pieces' weights, and the loads of
 // several pieces are in flight at once.  Few units in many pieces (four a unit and more) take more and smaller blocks, CH = 4:
 // 427 rows over 3133 keys, 25 pieces a unit: 19 us in all, 40 with a thread a row and piece after piece.  Many
 // units in two or three pieces each take CH = D / 8 (2K tokens behind 8K 212 us, by small blocks 217).
@@ -805,25 +805,42 @@ __global__ void __launch_bounds__(256) attend_chunk_join_kernel(const __grid_con
   grid_dependency_wait();                                         // in every block, also those with nothing to join
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = (int)(blockIdx.y & 7) * 32 + lane, ch = ((int)(blockIdx.y >> 3) * 8 + warp) * CH;
-  const int j = (int)blockIdx.x + 1;
-  const UnitStart me = p.starts[j], before = p.starts[j - 1];
-  if (me.b < 0 || me.t == 0) return;
-  auto same = [&](const UnitStart& o) { return o.b == me.b && o.h == me.h && o.u == me.u && o.t > 0; };
-  if (same(before)) return;
+  UnitStart me;
+  int j, pieces;                                                  // blocks j - 1, j, ...
+  if constexpr (CH == 4) {                                        // x is a unit: the borders that lie inside it
+    const int units = (int)(((int64_t)p.a.req.max_q * p.a.G + kUnitRows - 1) / kUnitRows), bh = (int)blockIdx.x / units;
+    me = UnitStart{bh / p.a.H, bh % p.a.H, (int)blockIdx.x % units, 1};
+    j = p.blocks;
+    pieces = 1;
+    for (int k = 1 + lane; k < p.blocks + lane; k += 32) {
+      const UnitStart o = k < p.blocks ? p.starts[k] : UnitStart{-1, 0, 0, 0};
+      const unsigned in = __ballot_sync(0xffffffffu, o.b == me.b && o.h == me.h && o.u == me.u && o.t > 0);
+      if (in && j == p.blocks) j = k - lane + __ffs(in) - 1;
+      pieces += __popc(in);
+    }
+    if (pieces == 1) return;
+  } else {
+    j = (int)blockIdx.x + 1;
+    me = p.starts[j];
+    const UnitStart before = p.starts[j - 1];
+    if (me.b < 0 || me.t == 0) return;
+    auto same = [&](const UnitStart& o) { return o.b == me.b && o.h == me.h && o.u == me.u && o.t > 0; };
+    if (same(before)) return;
+    pieces = 2;
+    for (bool go = true; go; pieces += 32) {
+      const int k = j + pieces - 1 + lane;
+      const bool in = k < p.blocks && same(p.starts[k]);
+      const unsigned out = ~__ballot_sync(0xffffffffu, in);
+      if (out) {
+        pieces += __ffs(out) - 1 - 32;
+        go = false;
+      }
+    }
+  }
   int q0, nq, kv;
   request_span(p.a.req, me.b, nullptr, q0, nq, kv);
   const int r = me.u * kUnitRows + row, rows = nq * p.a.G;
   if (r - lane >= rows) return;
-  int pieces = 2;                                                 // blocks j - 1, j, ...
-  for (bool go = true; go; pieces += 32) {
-    const int k = j + pieces - 1 + lane;
-    const bool in = k < p.blocks && same(p.starts[k]);
-    const unsigned out = ~__ballot_sync(0xffffffffu, in);
-    if (out) {
-      pieces += __ffs(out) - 1 - 32;
-      go = false;
-    }
-  }
   const float c = p.a.scale * kLog2e, minus_inf = __uint_as_float(0xff800000u);
   auto place = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0 ? 1 : 0)) * kUnitRows; };
   auto held = [&](int i) { return *reinterpret_cast<const float2*>(p.ml + 2 * (place(i) + row)); };
@@ -920,7 +937,7 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
   }
   const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
   if (e != cudaSuccess || p.blocks < 2) return e;
-  if (p.fine) return launch_after(attend_chunk_join_kernel<D, 4>, dim3((unsigned)p.blocks - 1, 8 * (D / 32)), 256, 0, s, p);
+  if (p.fine) return launch_after(attend_chunk_join_kernel<D, 4>, dim3((unsigned)chunk_units(p.a.req.n, p.a.req.max_q, p.a.G, p.a.H), 8 * (D / 32)), 256, 0, s, p);
   return launch_after(attend_chunk_join_kernel<D, D / 8>, dim3((unsigned)p.blocks - 1, 8), 256, 0, s, p);
 }
 
