@@ -164,15 +164,15 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {   // inclusi
   return v;
 }
 // Key tiles of one head of 32 requests, each lane with a request of its own (whole warp): a lane adds up its request's
-// units, or, where one has many, the warp does, a lane a unit.
+// units, or, where few requests have many, the warp does, a lane a unit.
 __device__ __forceinline__ int64_t head_tiles(const ChunkLaunch& p, int nq, int kv, int lane) {
   const int units = units_of(p, nq);
   int64_t sum = 0;
-  if (__reduce_max_sync(0xffffffffu, units) <= 8) {
+  unsigned left = __ballot_sync(0xffffffffu, units > 0);
+  if (__reduce_max_sync(0xffffffffu, units) <= min(8, __popc(left))) {
     for (int u = 0; u < units; ++u) sum += unit_tiles(p.a, nq, kv, nq * p.a.G, u).all;
     return sum;
   }
-  unsigned left = __ballot_sync(0xffffffffu, units > 0);
   while (left) {
     const int o = __ffs(left) - 1;
     left &= left - 1;
@@ -326,6 +326,8 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
   }
   grid_dependency_wait();                                         // what follows reads what earlier kernels wrote
   grid_dependents_launch();                                       // the join's blocks may take the SMs that finish first
+  Walk walk;                                                      // warp 11: the block's part of the line
+  if (warp == 11) walk = line_start(p, lane, (int)blockIdx.x);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -547,7 +549,6 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
     bool ok = true;
     if (warp == 11) {
       // ---- the block's part of the line
-      Walk walk = line_start(p, lane, (int)blockIdx.x);
       if (lane == 0) p.starts[blockIdx.x] = walk.left > 0 ? UnitStart{walk.b, walk.h, walk.u, walk.t} : UnitStart{-1, 0, 0, 0};
       for (int i = 0; ok; ++i) {
         ok = wait_all(piece_empty + 8 * (i % kPieces), ((i / kPieces) & 1) ^ 1, abort_flag);
