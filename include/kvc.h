@@ -573,8 +573,9 @@ typedef struct kvc_heads {
  * [L, n_phys_pages, H, page_size].
  * The scale is a power of two, the smallest that brings the row's largest magnitude to at most 448 (e4m3's largest
  * number; never below 2^-127): e4m3 carries its own exponent, so a finer scale would buy no precision, and every value
- * of the cache is a bf16 number (magnitudes stop at 240 * 2^120, the largest such one): reading it back adds no rounding.  A row's error is that of e4m3: half a step, 2^-4 of
- * the value, or 2^-10 of the scale for values below 2^-6 of it.
+ * of the cache is a bf16 number (magnitudes stop at 240 * 2^120, the largest such one): reading it back adds no
+ * rounding.  A row's error is that of e4m3: half a step, 2^-4 of the value, or 2^-10 of the scale for values below 2^-6
+ * of it.
  */
 typedef struct kvc_qcache {
   kvc_cache codes;

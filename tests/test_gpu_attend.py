@@ -266,3 +266,15 @@ def test_offsets_past_32_bits():
             kvc.kvc_set_path(kvc.KVC_PATH_AUTO)
         small.check(out, lse)
     assert kvc.kvc_status_poll() == 0
+
+
+@pytest.mark.parametrize("loose", [False, True])
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_unit_in_many_pieces(d, q8, loose):
+    """One tile of rows over 79 tiles of keys, a piece a block, the last one out of sight of some rows; with a bound far
+    above the request's length the join is sized for many units."""
+    b = Built(Step(nq=[40], kv=[10007], H=1, G=4, d=d, q8=q8, seed=71))
+    if loose:
+        b.req = kvc.Requests(b.req.q_begin, b.req.kv_len, 8192, 10007, page_table=b.req.page_table)
+    b.check(*b.run())
