@@ -187,6 +187,9 @@ class _Described:
         self.__dict__.pop("_made", None)
         object.__setattr__(self, name, value)
 
+    def __getstate__(self):                       # copies and pickles make a descriptor of their own
+        return {k: v for k, v in self.__dict__.items() if k != "_made"}
+
 
 class Cache(_Described):
     """A cache descriptor over torch tensors (which it keeps alive).
@@ -334,6 +337,9 @@ class Requests:
 
     def __setattr__(self, name, value):
         raise AttributeError(f"Requests.{name} is fixed; write into its tensors, or make another Requests")
+
+    def __reduce__(self):
+        return Requests, (self.q_begin, self.kv_len, self.max_q, self.max_kv, self.page_table)
 
     def struct(self) -> kvc_requests:
         return self._struct

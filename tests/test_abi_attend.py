@@ -1,4 +1,5 @@
 """Refusals of kvc_append, kvc_attend, kvc_quantize and kvc_dequantize: argument checks before anything touches a device."""
+import copy
 import ctypes as C
 
 import pytest
@@ -152,3 +153,7 @@ def test_descriptors_follow_the_objects():
     r = kvc.Requests(torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 1, 16)
     with pytest.raises(AttributeError):
         r.kv_len = torch.ones(1, dtype=torch.int32)
+    two = copy.deepcopy((c, q, r))                # after calls too: descriptors hold pointers and are not copied
+    assert two[0].T == 32 and two[2].max_kv == 16 and two[2].kv_len.data_ptr() != r.kv_len.data_ptr()
+    assert held(two[0], kvc.kvc_cache).k == two[0].k.data_ptr() and held(c, kvc.kvc_cache).k == c.k.data_ptr()
+    assert two[2].struct().kv_len == two[2].kv_len.data_ptr()
