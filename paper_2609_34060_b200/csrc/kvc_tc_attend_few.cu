@@ -28,7 +28,8 @@
 //
 // Measured: 64 requests of 4K (lognormal), 32 / 8 heads, bf16 pages of 16: 201 us = 6.4 TB/s of 6.55 copied; eight
 // requests of 32K, 64 / 8 heads, 8-bit pages of 16: 111 us (100 with pages of 128: the copies of 2 KB boxes then bound it,
-// and 12 us are start and join); one request of 777 keys: 12 us, of which 3 are the join's.
+// and 12 us are start and join); one request of 777 keys: 11 us, of which 2 are the join's; one of 30K, 8 / 1 heads: 25 us
+// (31 with the join loading a piece's sums after its weights, eight at a time).
 //
 // Warps: 0-3 and 4-7 softmax (0-3 epilogue), 8 first products, 9 second products, 10 queries of the next pair, 12-15
 // loads: keys and values of even and odd tiles, with the exponents of 8-bit rows (a 16-token page is one small box, and
@@ -839,44 +840,57 @@ __global__ void __launch_bounds__(4 * D) attend_few_join_kernel(const __grid_con
   const float* ml = p.part + (int64_t)p.blocks * 2 * RC * D;
   // where block c left its piece: slot 1 holds a piece that begins with the pair, slot 0 one cut in front
   auto place = [&](int c) { return ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * RC; };
-  // maxima: a warp a row
-  if (warp < 4) {
-    const int row = (int)blockIdx.y * 4 + warp;
-    float m = minus_inf;
-    if (row < R)
-      for (int c = c0 + lane; c <= c1; c += 32) {
-        const float2 v = *reinterpret_cast<const float2*>(ml + 2 * (place(c) + row));
-        if (v.y != 0.f) m = fmaxf(m, v.x);
-      }
+  // sums of the first pieces are under way before their weights are known, and always kAtOnce of them
+  constexpr int kAtOnce = 16;
+  const int pieces = c1 + 1 - c0;
+  float x[kAtOnce];
+  auto load = [&](int i0) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) {
-      s_m[warp] = m;
-      s_l[warp] = 0.f;
-    }
+    for (int k = 0; k < kAtOnce; ++k) x[k] = r < R && i0 + k < pieces ? p.part[(place(c0 + i0 + k) + r) * D + ch] : 0.f;
+  };
+  load(0);
+  // maxima and weights: a warp a row, the first pieces' kept
+  const int mine = (int)blockIdx.y * 4 + warp;
+  auto held = [&](int i) {
+    return warp < 4 && mine < R && i < pieces ? *reinterpret_cast<const float2*>(ml + 2 * (place(c0 + i) + mine)) : make_float2(0.f, 0.f);
+  };
+  float2 v[kJoinPieces / 32];
+  float m = minus_inf;
+  for (int i0 = (pieces - 1) / kJoinPieces * kJoinPieces; i0 >= 0; i0 -= kJoinPieces) {
+#pragma unroll
+    for (int k = 0; k < kJoinPieces / 32; ++k) v[k] = held(i0 + k * 32 + lane);
+#pragma unroll
+    for (int k = 0; k < kJoinPieces / 32; ++k)
+      if (v[k].y != 0.f) m = fmaxf(m, v[k].x);
   }
-  float acc = 0.f;
-  for (int cb = c0; cb <= c1; cb += kJoinPieces) {
-    const int n = min(kJoinPieces, c1 + 1 - cb);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float acc = 0.f, all = 0.f;
+  for (int i0 = 0; i0 < pieces; i0 += kJoinPieces) {
+    const int n = min(kJoinPieces, pieces - i0);
     __syncthreads();
     if (warp < 4) {
-      const int row = (int)blockIdx.y * 4 + warp;
       float sum = 0.f;
-      if (row < R)
-        for (int k = lane; k < n; k += 32) {
-          const float2 v = *reinterpret_cast<const float2*>(ml + 2 * (place(cb + k) + row));
-          const float w = v.y == 0.f ? 0.f : exp2f(v.x - s_m[warp]);
-          s_w[warp][k] = w;
-          sum += w * v.y;
-        }
+#pragma unroll
+      for (int k = 0; k < kJoinPieces / 32; ++k) {
+        if (i0 > 0) v[k] = held(i0 + k * 32 + lane);
+        const float w = v[k].y == 0.f ? 0.f : exp2f(v[k].x - m);
+        s_w[warp][k * 32 + lane] = w;
+        sum += w * v[k].y;
+      }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (lane == 0) s_l[warp] += sum;
+      all += sum;
+      if (lane == 0) {
+        s_m[warp] = m;
+        s_l[warp] = all;
+      }
     }
     __syncthreads();
-    if (r < R) {
-#pragma unroll 8
-      for (int k = 0; k < n; ++k) acc += s_w[rr][k] * p.part[(place(cb + k) + r) * D + ch];
+    for (int k0 = 0; k0 < n; k0 += kAtOnce) {
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) acc += s_w[rr][k0 + k] * x[k];      // behind the last piece both are 0
+      if (i0 + k0 + kAtOnce < pieces) load(i0 + k0 + kAtOnce);
     }
   }
   if (r >= R) return;
