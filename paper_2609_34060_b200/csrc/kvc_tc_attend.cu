@@ -12,7 +12,7 @@
 // shared memory.  It is handed over in two parts (96 and 32 keys), so that most of the second product runs while the rest
 // is still being computed.
 //
-// Measured, 2048 tokens behind 8K, 32 / 8 heads of 128 (240 GFLOP): 220 us (1.09 PFLOP/s) in a short run, 238-250 us
+// Measured, 2048 tokens behind 8K, 32 / 8 heads of 128 (240 GFLOP): 212 us (1.13 PFLOP/s) in a short run, 238-250 us
 // once the power cap has set the clock.  What bounds it: a row tile's own chain, softmax (about 1750 cycles), the second
 // product's tail, the next first product, and the hand-overs between them (about 3200 a tile of keys; tensor cores busy
 // 63 % of it).  There is no tensor memory left for a second S.  Local memory would cost more than anything else (shared
