@@ -278,3 +278,17 @@ def test_a_unit_in_many_pieces(d, q8, loose):
     if loose:
         b.req = kvc.Requests(b.req.q_begin, b.req.kv_len, 8192, 10007, page_table=b.req.page_table)
     b.check(*b.run())
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 1), (128, 16)])
+def test_a_large_mixed_batch(d, G, q8):
+    """Enough key tiles by the call's bounds (40 requests x 2 heads x 28 tiles) that single tokens and chunks are served by
+    a kernel each, behind one another in one workspace."""
+    rng = random.Random(5)
+    nq = [rng.choice([1, 1, 1, 2, 0, 9]) for _ in range(38)] + [40, 1]
+    kv = [max(n, rng.randrange(0, 400)) for n in nq[:-2]] + [600, 3500]
+    b = Built(Step(nq=nq, kv=kv, H=2, G=G, d=d, q8=q8, spare=2, seed=81))
+    b.check(*b.run())
+    again = b.run()
+    assert all(torch.equal(x, y) for x, y in zip(again, b.run()))
