@@ -503,7 +503,8 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       const int r = y.u * kUnitRows + t * 128 + row;
       const bool live = r < y.rows;
       const int tok = r / p.a.G, head = y.h * p.a.G + r - tok * p.a.G;
-      const bool dead = m == minus_inf;                           // no key seen
+      // no key seen: decided by the sum, which a NaN logit makes NaN (maxima pass over NaN: m may still be minus infinity)
+      const bool dead = l == 0.f;
       const bool whole = y.whole;
       const int64_t slot = ((int64_t)blockIdx.x * 2 + (y.t0 > 0 ? 0 : 1)) * kUnitRows + t * 128 + row;
       const float inv = whole ? (dead ? 0.f : 1.f / l) : 1.f;
@@ -537,7 +538,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       }
       if (live && ok) {
         if (!whole)
-          *reinterpret_cast<float2*>(p.ml + 2 * slot) = make_float2(m, dead ? 0.f : l);
+          *reinterpret_cast<float2*>(p.ml + 2 * slot) = make_float2(m, l);
         else if (p.a.lse)
           p.a.lse[(int64_t)(y.q0 + tok) * (p.a.H * p.a.G) + head] = dead ? minus_inf : m * p.a.scale + log2f(l) * kLn2;
       }
@@ -880,7 +881,7 @@ __global__ void __launch_bounds__(256) attend_chunk_join_kernel(const __grid_con
       const int i = k * 8 + warp;
       if (i >= n) break;
       if (i0 > 0) v[k] = held(i0 + i);
-      const bool none = v[k].y == 0.f;                            // a piece that saw no key of the row wrote no sums of it
+      const bool none = v[k].y == 0.f;                            // a piece that saw no key of the row wrote no sums of it (one of NaN did)
       const float w = none ? -1.f : exp2f((v[k].x - m) * c);
       s_w[i][lane] = w;
       if (!none) sum += w * v[k].y;
