@@ -772,7 +772,7 @@ _HEADS = struct.Struct("@QiiQQ")      # kvc_heads
 
 def _heads(t: torch.Tensor, d: int, what: str) -> bytes:
     """A kvc_heads over bf16 [rows, heads, d] with contiguous channels."""
-    if t.dtype is not torch.bfloat16 or t.dim() != 3:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.dim() != 3:
         raise KvcError(KVC_E_INVALID_ARG, f"{what}: bf16 [rows, heads, d] expected")
     (rows, heads, dd), (s_row, s_head, s_ch) = t.shape, t.stride()
     if dd != d:
@@ -782,12 +782,15 @@ def _heads(t: torch.Tensor, d: int, what: str) -> bytes:
     return _HEADS.pack(t.data_ptr(), rows, heads, s_row if rows > 1 else 0, s_head if heads > 1 else 0)
 
 
-def _desc(c):
-    """(address of the descriptor of a Cache or QCache, its device): the structure is kept until an attribute of the
-    object is set, its pointers are set at every call."""
+def _desc(c, kind=None, what: str = "cache"):
+    """(address of the descriptor of a Cache or QCache, its device, ..., its kvc_qcache or None): the structure is kept until
+    an attribute of the object is set, its pointers are set at every call.  Addresses carry no type, so the class is
+    checked here: `kind`, or either."""
+    if not isinstance(c, _Described if kind is None else kind):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: a {'Cache or QCache' if kind is None else kind.__name__} expected, not {type(c).__name__}")
     made = c.__dict__.get("_made")
     if made is None:
-        q8 = type(c) is QCache
+        q8 = isinstance(c, QCache)
         s = c.struct()
         devs = {t.get_device() for t in (c.k, c.v, c.page_table) + ((c.scale_k, c.scale_v) if q8 else ()) if t is not None}
         made = c.__dict__["_made"] = (C.addressof(s), devs.pop() if len(devs) == 1 else -1, s.codes if q8 else s, s if q8 else None)
@@ -812,6 +815,12 @@ def _here(what: str, stream, made, *tensors):
     return torch._C._cuda_getCurrentRawStream(cur) if stream is None else _stream(stream)
 
 
+def _address(req: Requests, what: str) -> int:
+    if not isinstance(req, Requests):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: Requests expected, not {type(req).__name__}")
+    return req._at
+
+
 def _holds(req: Requests, c, what: str) -> None:
     if req.page_table is not None and c.page_table is not None and req.max_kv > req._pages * c.page:
         raise KvcError(KVC_E_SHAPE, what)
@@ -819,41 +828,41 @@ def _holds(req: Requests, c, what: str) -> None:
 
 def kvc_quantize(src: Cache, dst: QCache, stream=None) -> None:
     """dst = e4m3(src), one power-of-two scale per (layer, head, token)."""
-    s, d = _desc(src), _desc(dst)
+    s, d = _desc(src, Cache, "kvc_quantize: src"), _desc(dst, QCache, "kvc_quantize: dst")
     st = _here("kvc_quantize", stream, (s[1], d[1]))
     _check(load().kvc_quantize(s[0], d[0], st), "kvc_quantize")
 
 
 def kvc_dequantize(src: QCache, dst: Cache, stream=None) -> None:
     """dst = bf16(code * 2^(exponent - 127))."""
-    s, d = _desc(src), _desc(dst)
+    s, d = _desc(src, QCache, "kvc_dequantize: src"), _desc(dst, Cache, "kvc_dequantize: dst")
     st = _here("kvc_dequantize", stream, (s[1], d[1]))
     _check(load().kvc_dequantize(s[0], d[0], st), "kvc_dequantize")
 
 
 def kvc_append(req: Requests, k_new: torch.Tensor, v_new: torch.Tensor, cache, layer: int, stream=None) -> None:
     """Write the new tokens' rows [rows, H, d] into `layer` of a Cache, or quantised into a QCache."""
-    c, k, v = _desc(cache), _heads(k_new, cache.d, "k_new"), _heads(v_new, cache.d, "v_new")
+    at, c, k, v = _address(req, "kvc_append"), _desc(cache), _heads(k_new, cache.d, "k_new"), _heads(v_new, cache.d, "v_new")
     st = _here("kvc_append", stream, (c[1], req._dev), k_new, v_new)
     _holds(req, cache, "kvc_append")
-    fn = load().kvc_append_q8 if type(cache) is QCache else load().kvc_append
-    _check(fn(req._at, k, v, int(layer), c[0], st), "kvc_append")
+    fn = load().kvc_append if c[3] is None else load().kvc_append_q8
+    _check(fn(at, k, v, int(layer), c[0], st), "kvc_append")
 
 
 def kvc_attend_workspace_bytes(req: Requests, cache, n_heads: int) -> int:
-    return int(load().kvc_attend_workspace_bytes(req._at, int(n_heads), cache.H, cache.d))
+    return int(load().kvc_attend_workspace_bytes(_address(req, "kvc_attend_workspace_bytes"), int(n_heads), cache.H, cache.d))
 
 
 def kvc_attend(req: Requests, q: torch.Tensor, cache, layer: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
                scale: Optional[float] = None, causal: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
     """Attention of the new tokens' queries [rows, heads, d] over `layer` of a Cache or QCache (scale: 1 / sqrt(d))."""
-    c, hq, ho = _desc(cache), _heads(q, cache.d, "q"), _heads(out, cache.d, "out")
+    at, c, hq, ho = _address(req, "kvc_attend"), _desc(cache), _heads(q, cache.d, "q"), _heads(out, cache.d, "out")
     st = _here("kvc_attend", stream, (c[1], req._dev), q, out, workspace, lse)
     _holds(req, cache, "kvc_attend")
     if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
         raise KvcError(KVC_E_INVALID_ARG, "kvc_attend: lse must be float32 [rows, heads]")
-    fn = load().kvc_attend_q8 if type(cache) is QCache else load().kvc_attend
-    _check(fn(req._at, hq, c[0], int(layer), cache.d ** -0.5 if scale is None else float(scale), bool(causal), ho,
+    fn = load().kvc_attend if c[3] is None else load().kvc_attend_q8
+    _check(fn(at, hq, c[0], int(layer), cache.d ** -0.5 if scale is None else float(scale), bool(causal), ho,
               None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
               0 if workspace is None else workspace.numel() * workspace.element_size(), st), "kvc_attend")
 
