@@ -590,7 +590,8 @@ typedef struct kvc_qcache {
  *                   not count towards its row's scale.
  * kvc_dequantize -- dst = bf16(value) (exact but for numbers below bf16's subnormal step).
  * src and dst agree in L, H, T, d; layouts, strides and page tables may differ.  Pages that the tables do not name and
- * rows >= T are left as they were.  Errors as kvc_apply (KVC_E_ALIAS: the buffers overlap).
+ * rows >= T are left as they were.  Errors as kvc_apply (KVC_E_ALIAS: the buffers overlap, exponents among them; those
+ * of keys and values may lie between one another, or behind their row of codes, where no byte is shared).
  */
 int kvc_quantize(const kvc_cache *src, kvc_qcache *dst, void *stream);
 int kvc_dequantize(const kvc_qcache *src, kvc_cache *dst, void *stream);
@@ -620,6 +621,8 @@ int kvc_append_q8(const kvc_requests *req, const kvc_heads *k_new, const kvc_hea
  *            results over two parts of a context can be joined
  *   workspace DEVICE, kvc_attend_workspace_bytes(...) bytes, 256-byte aligned, written before it is read; calls that may
  *            overlap on the GPU need one each
+ *            out, lse and the workspace must lie apart from one another, from the exponents and from the request lists
+ *            (KVC_E_ALIAS)
  * Keys past kv_len are never used, whatever they hold (NaN included).  A NaN or infinity in a VALUE row below kv_len may
  * reach every row of its request, also those that the causal mask keeps from seeing that token.
  * Logits, maxima, sums and outputs are held in float32 until the output's rounding to bf16.  Probabilities meet the values

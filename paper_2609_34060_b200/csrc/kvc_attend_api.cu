@@ -27,6 +27,70 @@ int64_t cache_reach(const kvc_cache* c, const DevCache& d) {
   return last;
 }
 
+// The runs of bytes a cache's codes or exponents take: one of `width` bytes for every (layer, page, head, token).
+struct Runs {
+  uintptr_t at;
+  int64_t n[4], s[4], width;       // counts, distances in bytes
+  Extent all() const {
+    int64_t last = width;
+    for (int i = 0; i < 4; ++i) {
+      if (n[i] <= 0) return {at, at};
+      last += (n[i] - 1) * s[i];
+    }
+    return {at, at + (uintptr_t)last};
+  }
+};
+Runs runs_of(const void* p, const kvc_cache& c, int64_t s_layer, int64_t s_page, int64_t s_head, int64_t s_tok, int64_t width) {
+  const bool paged = c.layout == KVC_PAGED;
+  return {reinterpret_cast<uintptr_t>(p), {c.L, paged ? c.n_phys_pages : 1, c.H, paged ? c.page_size : c.T}, {s_layer, paged ? s_page : 0, s_head, s_tok}, width};
+}
+Runs exponent_runs(const uint8_t* p, const kvc_cache& c, const DevScale& e) { return runs_of(p, c, e.s_layer, e.s_page, e.s_head, e.s_tok, 1); }
+Runs code_runs(const void* p, const kvc_cache& c, const DevCache& d) { return runs_of(p, c, d.s_layer, d.s_page, d.s_head, d.s_tok, c.d); }
+
+// Whether two sets of runs share a byte.  Sets with the same distances may lie inside one another (keys' and values'
+// exponents side by side, exponents behind their row of codes): there the question is whether the distance of their
+// beginnings is a whole number of steps, level by level, give or take a run; otherwise overlapping extents decide.
+bool meet(const Runs& a, const Runs& b) {
+  if (!overlap(a.all(), b.all())) return false;
+  int order[4] = {0, 1, 2, 3}, live = 0;
+  for (int i = 0; i < 4; ++i) {
+    if (a.n[i] != b.n[i] || (a.n[i] > 1 && a.s[i] != b.s[i])) return true;
+    if (a.n[i] > 1) order[live++] = i;
+  }
+  for (int i = 1; i < live; ++i)                                  // smallest distance first
+    for (int j = i; j > 0 && a.s[order[j]] < a.s[order[j - 1]]; --j) {
+      const int t = order[j];
+      order[j] = order[j - 1];
+      order[j - 1] = t;
+    }
+  int64_t reach[5] = {a.width > b.width ? a.width : b.width};    // of the levels below
+  for (int i = 0; i < live; ++i) {
+    const int64_t s = a.s[order[i]];
+    if (s < reach[i]) return true;                                // levels that are not inside one another
+    reach[i + 1] = reach[i] + (a.n[order[i]] - 1) * s;
+  }
+  struct Search {
+    const int64_t *n, *s, *reach;
+    const int* order;
+    int64_t wa, wb;
+    bool at(int level, int64_t delta) const {                     // delta: b's position less a's
+      if (level == 0) return delta < wa && -delta < wb;
+      const int i = order[level - 1];
+      const int64_t q = delta / s[i];
+      for (int64_t t = q - 1; t <= q + 1; ++t)
+        if (t > -n[i] && t < n[i] && delta - t * s[i] < reach[level - 1] && t * s[i] - delta < reach[level - 1] && at(level - 1, delta - t * s[i])) return true;
+      return false;
+    }
+  };
+  return Search{a.n, a.s, reach, order, a.width, b.width}.at(live, (int64_t)(b.at - a.at));
+}
+// An 8-bit cache that is written: exponents apart from one another and from the codes.
+bool exponents_apart(const kvc_qcache* q, const DevCache& c, const DevScale& e) {
+  const Runs ek = exponent_runs(e.k, q->codes, e), ev = exponent_runs(e.v, q->codes, e);
+  const Runs ck = code_runs(q->codes.k, q->codes, c), cv = code_runs(q->codes.v, q->codes, c);
+  return !(meet(ek, ev) || meet(ek, ck) || meet(ek, cv) || meet(ev, ck) || meet(ev, cv));
+}
+
 int resolve_qcache(const kvc_qcache* q, DevCache* c, DevScale* e) {
   if (!q) return KVC_E_INVALID_ARG;
   const int rc = resolve_cache(&q->codes, c);
@@ -84,7 +148,8 @@ int resolve_heads(const kvc_heads* h, int d, DevHeads* out, Extent* ext) {
 }
 
 int append_common(const kvc_requests* req, const kvc_heads* kn, const kvc_heads* vn, int32_t layer, const kvc_cache* geo, AppendLaunch& a,
-                  int elem, void* stream) {
+                  const kvc_qcache* q8, void* stream) {
+  const int elem = q8 ? 1 : 2;
   int rc;
   Extent ek, ev;
   if (layer < 0 || layer >= geo->L) return KVC_E_INVALID_ARG;
@@ -96,6 +161,10 @@ int append_common(const kvc_requests* req, const kvc_heads* kn, const kvc_heads*
   const int64_t reach = cache_reach(geo, a.dst);
   const Extent ck = extent_of(geo->k, reach, elem), cv = extent_of(geo->v, reach, elem);
   if (overlap(ck, cv) || overlap(ck, ek) || overlap(ck, ev) || overlap(cv, ek) || overlap(cv, ev)) return KVC_E_ALIAS;
+  if (q8) {
+    const Extent sk = exponent_runs(a.e.k, *geo, a.e).all(), sv = exponent_runs(a.e.v, *geo, a.e).all();
+    if (!exponents_apart(q8, a.dst, a.e) || overlap(sk, ek) || overlap(sk, ev) || overlap(sv, ek) || overlap(sv, ev)) return KVC_E_ALIAS;
+  }
   a.H = geo->H;
   a.layer = layer;
   if (req->n == 0 || a.req.max_q == 0 || a.req.n_rows == 0) return KVC_OK;
@@ -117,6 +186,8 @@ int convert_common(const kvc_cache* bf, const kvc_qcache* q8, int to8, void* str
   const int64_t rb = cache_reach(bf, c.bf), rq = cache_reach(&g, c.q8);
   const Extent bk = extent_of(bf->k, rb, 2), bv = extent_of(bf->v, rb, 2), qk = extent_of(g.k, rq, 1), qv = extent_of(g.v, rq, 1);
   if (overlap(bk, qk) || overlap(bk, qv) || overlap(bv, qk) || overlap(bv, qv) || (to8 ? overlap(qk, qv) : overlap(bk, bv))) return KVC_E_ALIAS;
+  const Extent sk = exponent_runs(c.e.k, g, c.e).all(), sv = exponent_runs(c.e.v, g, c.e).all();
+  if (overlap(bk, sk) || overlap(bk, sv) || overlap(bv, sk) || overlap(bv, sv) || (to8 && !exponents_apart(q8, c.q8, c.e))) return KVC_E_ALIAS;
   if (bf->T == 0) return KVC_OK;
   c.L = bf->L;
   c.H = bf->H;
@@ -142,11 +213,25 @@ int attend_common(const kvc_requests* req, const kvc_heads* q, const kvc_cache* 
   const int64_t reach = cache_reach(geo, a.c);
   const Extent ck = extent_of(geo->k, reach, elem), cv = extent_of(geo->v, reach, elem);
   const Extent el = extent_of(lse, lse ? (int64_t)q->n_rows * q->n_heads : 0, 4);
-  if (overlap(eo, eq) || overlap(eo, ck) || overlap(eo, cv) || overlap(el, eo) || overlap(el, eq) || overlap(el, ck) || overlap(el, cv))
-    return KVC_E_ALIAS;
+  // what is read, and what is written: apart from that and from one another
+  const Extent none = {0, 0};
+  const bool q8 = a.e.k != nullptr;
+  const int64_t pages = geo->layout == KVC_PAGED ? ((int64_t)req->max_kv + geo->page_size - 1) / geo->page_size : 0;
+  const Extent reads[] = {eq, ck, cv, q8 ? exponent_runs(a.e.k, *geo, a.e).all() : none, q8 ? exponent_runs(a.e.v, *geo, a.e).all() : none,
+                          extent_of(req->q_begin, req->n > 0 ? (int64_t)req->n + 1 : 0, 4), extent_of(req->kv_len, req->n, 4),
+                          req->page_table && req->n > 0 ? extent_of(req->page_table, (int64_t)(req->n - 1) * req->table_stride + pages, 4)
+                                                        : extent_of(geo->page_table, geo->page_table ? pages : 0, 4)};
+  auto reads_meet = [&](const Extent& w) {
+    for (const Extent& r : reads)
+      if (overlap(w, r)) return true;
+    return false;
+  };
+  if (reads_meet(eo) || reads_meet(el) || overlap(el, eo)) return KVC_E_ALIAS;
   if (req->n == 0 || a.req.max_q == 0 || a.req.n_rows == 0) return KVC_OK;
   const size_t need = kvc_attend_workspace_bytes(req, q->n_heads, geo->H, geo->d);
   if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return KVC_E_WORKSPACE;
+  const Extent ew = extent_of(workspace, (int64_t)need, 1);
+  if (reads_meet(ew) || overlap(ew, eo) || overlap(ew, el)) return KVC_E_ALIAS;
   a.H = geo->H;
   a.G = q->n_heads / geo->H;
   a.layer = layer;
@@ -181,14 +266,14 @@ int kvc_append(const kvc_requests* req, const kvc_heads* k_new, const kvc_heads*
   AppendLaunch a;
   memset(&a, 0, sizeof(a));
   const int rc = resolve_cache(dst, &a.dst);
-  return rc != KVC_OK ? rc : append_common(req, k_new, v_new, layer, dst, a, 2, stream);
+  return rc != KVC_OK ? rc : append_common(req, k_new, v_new, layer, dst, a, nullptr, stream);
 }
 
 int kvc_append_q8(const kvc_requests* req, const kvc_heads* k_new, const kvc_heads* v_new, int32_t layer, kvc_qcache* dst, void* stream) {
   AppendLaunch a;
   memset(&a, 0, sizeof(a));
   const int rc = resolve_qcache(dst, &a.dst, &a.e);
-  return rc != KVC_OK ? rc : append_common(req, k_new, v_new, layer, &dst->codes, a, 1, stream);
+  return rc != KVC_OK ? rc : append_common(req, k_new, v_new, layer, &dst->codes, a, dst, stream);
 }
 
 size_t kvc_attend_workspace_bytes(const kvc_requests* req, int32_t n_heads, int32_t H, int32_t d) {
