@@ -625,7 +625,9 @@ int kvc_append_q8(const kvc_requests *req, const kvc_heads *k_new, const kvc_hea
  *            (KVC_E_ALIAS)
  * Keys past kv_len are never used, whatever they hold (NaN included).  A NaN or infinity in a VALUE row below kv_len may
  * reach every row of its request, also those that the causal mask keeps from seeing that token.
- * Logits, maxima, sums and outputs are held in float32 until the output's rounding to bf16.  Probabilities meet the values
+ * Logits, maxima, sums and outputs are held in float32 until the output's rounding to bf16.  Sums of values are held with
+ * probabilities of up to 2^16 times the final ones: they overflow, and outputs become infinite, where kv_len times the
+ * largest |V| passes 2^112 (5e33).  Probabilities meet the values
  * rounded to bf16 (2^-8 of themselves).  Over an 8-bit cache, where no request of the call has more than 32 rows (max_q
  * times query heads per KV head), and for single tokens in large calls that mix them with chunks, they meet the codes as
  * three e4m3 parts: 2^-12 of themselves, or 2^-24 of the row's largest where the value row's scale is the largest of the

@@ -24,9 +24,11 @@
 // slower, 234 -> 274 and 297 us on 2K tokens behind 8K: the warp's issue slots are what is short.
 //
 // m is a maximum of earlier tiles: a tile's own maximum is taken beside its exponentials, off the way from logits to
-// probabilities.  Exponentials above 1 cost nothing (bf16 and float32 have the same range, and no format's precision
-// depends on the scale); where one would pass 2^kJump the tile is done over with its own maximum.  A maximum grown by
-// more than 2^kLazy becomes m at the next tile: sums and accumulators are then rescaled, which the softmax warps do.
+// probabilities.  Exponentials above 1 cost no precision (bf16 and float32 have the same range), but P V is summed in
+// float32, and a sum that overflowed stays infinite whatever it is scaled by later: where one would pass 2^kJump the tile
+// is done over with its own maximum.  A maximum grown by more than 2^kLazy becomes m at the next tile: sums and
+// accumulators are then rescaled, which the softmax warps do.  (kJump = kLazy = 8, always done over: 250 us on 2K tokens
+// behind 8K, 244 so; 64 let values from 2^63 on overflow.)
 //
 // Rounding: P to bf16 (2^-8 of each term: what the tensor cores take), everything else float32.
 //
@@ -52,7 +54,7 @@ namespace {
 using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLazy = 8.f, kJump = 64.f; // log2 of the growth of a row's maximum that is let pass, and that a tile bears
+constexpr float kLazy = 8.f, kJump = 16.f; // log2 of the growth of a row's maximum that is let pass, and that a tile bears
 constexpr int kUnitRows = 256;
 
 struct alignas(16) UnitStart {             // where a block's part of the line begins; b < 0: it has none
