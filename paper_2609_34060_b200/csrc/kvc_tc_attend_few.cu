@@ -504,10 +504,12 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           for (int r = 0; r < RC; ++r) bars.half[1][r] = m[r];
           bars.half_e = eref;
         }
+        tc_fence_before();                                          // group 0 reads this group's accumulators
         named_bar_sync(3, 256);
       } else {
         named_bar_sync(4, 256);
         named_bar_sync(3, 256);
+        tc_fence_after();
         const bool had0 = last >= g0, had1 = g1 - g0 > 1 || !had0;  // which groups had tiles
         const uint32_t o0 = o_at, o1 = o_at + F::kPCols;
         const bool whole = x.t0 == 0 && x.t1 == x.nt;
