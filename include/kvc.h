@@ -629,9 +629,9 @@ int kvc_append_q8(const kvc_requests *req, const kvc_heads *k_new, const kvc_hea
  * probabilities of up to 2^16 times the final ones: they overflow, and outputs become infinite, where kv_len times the
  * largest |V| passes 2^112 (5e33).  Probabilities meet the values
  * rounded to bf16 (2^-8 of themselves).  Over an 8-bit cache, where no request of the call has more than 32 rows (max_q
- * times query heads per KV head), and for single tokens in large calls that mix them with chunks, they meet the codes as
- * three e4m3 parts: 2^-12 of themselves, or 2^-24 of the row's largest where the value row's scale is the largest of the
- * request (a step in the output of that scale: value rows 2^12 and more below the largest lose bits).
+ * times query heads per KV head), and for single tokens in large calls that mix them with chunks, the product of a
+ * probability and its value row's scale meets the codes as three e4m3 parts: 2^-12 of itself, or 2^-24 of the row's largest
+ * such product.
  * Results do not depend on the order in which blocks run, and equal calls give equal bits.
  */
 int kvc_attend(const kvc_requests *req, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale, int32_t causal,

@@ -22,8 +22,12 @@
 //     q 2^-b = t1 + t2 / 16   (b the row's exponent; bf16 has 8 significant bits, each part 4: exact but for channels
 //                              below 2^-15 of the row's largest, which are off by at most 2^-22 of it) ,
 // as separate columns of one product, K's scale multiplies the finished logit (a token's scale is its thread's), and
-// V's scale goes into the probability, split into three parts 16 apart (12 bits and a step of 2^-24 of the largest):
-//     p 2^(e_v - E) 64 = t1 + t2 / 16 + t3 / 256 ,   E the largest exponent of a value row so far .
+// V's scale e_v goes into the probability before that is split into three parts 16 apart,
+//     64 2^(s + e_v - Z) = t1 + t2 / 16 + t3 / 256   (s the logit to base 2, Z the row's largest s + e_v so far) ,
+// 12 bits and a step of 2^-24 of the row's largest term p 2^e_v.  The reference is the product's, not the largest exponent
+// alone: a large value row that a row of queries does not see, or hardly looks at, costs the others no bits.  The sum of
+// the probabilities has its own reference, the largest s, and its own exponentials (eight requests of 32K: 113.8 us, 113.4
+// with one exponential for both).
 // Sums and joins are float32.  Over bf16 caches P is rounded to bf16 as in the chunk kernel.
 //
 // Measured: 64 requests of 4K (lognormal), 32 / 8 heads, bf16 pages of 16: 202 us = 6.4 TB/s of 6.55 copied; eight
@@ -202,12 +206,20 @@ struct Few {
   static constexpr uint32_t kOCol = kSBufs * kQRows;
   static constexpr uint32_t kTmem = kOCol + 4 * kPCols <= 128 ? 128 : kOCol + 4 * kPCols <= 256 ? 256 : 512;
   static_assert(kOCol + 4 * kPCols <= 512, "tensor memory");
-  // p <= 2^kLazy; with 8-bit values 64 p has to stay below 448
-  static constexpr float kLazy = Q8 ? 2.f : 8.f;
+  // p <= 2^kLazy; with 8-bit values 64 2^(s + e_v - Z) <= 64 2^kLazyZ has to stay below 448
+  static constexpr float kLazy = 8.f, kLazyZ = 2.f;
 };
 
+// 8-bit caches: maxima of s + e_v; a warp's copy of Z - 6 (0 while there is none) and of what a new Z does to the sums;
+// group 1's Z - 6 of a finished piece
+template <bool Q8, int RC>
+struct FewScales {};
+template <int RC>
+struct alignas(16) FewScales<true, RC> {
+  float z[2][4][RC], z_keep[2][4][RC], red_z[2][4][RC], half_z[RC];
+};
 template <typename F>
-struct FewBars {
+struct FewBars : FewScales<F::E == 1, F::kRows> {
   uint64_t full[F::kSlots], empty[F::kSlots], s_full[F::kSBufs], s_free[F::kSBufs], p_ready[2], pv_done[2], q_full[2], q_empty[2], o_free[2];
   uint64_t e_full[F::kExpRing], e_empty[F::kExpRing];
   Walk start;
@@ -217,8 +229,7 @@ struct FewBars {
   float red[2][4][F::kRows];
   float qs[2][F::E == 1 ? F::kRows : 1];   // scales of the query rows (8-bit caches)
   float half[2][F::kRows];          // group 1's sums and maxima of a finished piece; then the weights of the two halves
-  int half_e;
-  int red_e[2][4], fail[2][4];
+  int fail[2][4];
 };
 
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
@@ -251,6 +262,12 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, float* v) {
   static_assert(N % 8 == 0, "columns");
 #pragma unroll
   for (int k = 0; k < N; k += 8) tmem_ld8(taddr + k, v + k);
+}
+// largest of a warp's values (NaN does not count)
+__device__ __forceinline__ float warp_max(float v) {
+  float m;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+  return m;
 }
 // 16-byte chunk of a token's row of probabilities under the row's swizzle
 template <int ROW>
@@ -340,11 +357,15 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       const int R = x.nq * p.a.G;
       const uint32_t o_at = lane_at + F::kOCol + ((piece & 1) * 2 + wg) * F::kPCols;
       float m[RC], l[RC];
-      int eref = -1000;                                             // 8-bit values: exponent their sums are held under
+      float z_lane = minus_inf;                                     // 8-bit values: Z - 6 of row `lane`, under which its sums are held
 #pragma unroll
       for (int r = 0; r < RC; ++r) {
         m[r] = minus_inf;
         l[r] = 0.f;
+      }
+      if constexpr (Q8) {
+        if (lane < RC) bars.z[wg][w4][lane] = 0.f;
+        __syncwarp();
       }
       wait(q_full + 8 * (piece & 1), (piece >> 1) & 1);
       const int g0 = g, g1 = g + x.t1 - x.t0;                       // the piece's tiles in the block's count
@@ -354,13 +375,12 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         const int i = x.t0 + g - g0;
         const int tok = i * 128 + tid4;
         const uint32_t use = (uint32_t)(g >> 1) & 1u;               // of buffer wg
-        float ek = 1.f;
-        int ev = 0;
+        float ek = 1.f, ev = 0.f;
         if (Q8) {
           const int es = g % F::kExpRing;
           wait(e_full + 8 * es, (g / F::kExpRing) & 1);
           ek = sexp[es * 256 + tid4];
-          ev = __float_as_int(sexp[es * 256 + 128 + tid4]);
+          ev = sexp[es * 256 + 128 + tid4];
           mbar_arrive(e_empty + 8 * es);
         }
         const int sb = g % F::kSBufs;
@@ -380,22 +400,27 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           for (int r = 0; r < RC; ++r)
             if (tok > lim + (p.a.causal ? r / p.a.G : 0) || r >= R) s[r] = minus_inf;
         }
-        const bool mine = tok < x.kv;                               // rows behind the last key hold anything
-        bool grow = Q8 && mine && ev > eref;
+        bool grow = false;
 #pragma unroll
         for (int r = 0; r < RC; ++r) grow |= s[r] - m[r] > F::kLazy;
+        if constexpr (Q8) {
+#pragma unroll
+          for (int r = 0; r < RC; r += 4) {
+            const float4 z = *reinterpret_cast<const float4*>(&bars.z[wg][w4][r]);
+            grow |= s[r] + (ev - z.x) > F::kLazyZ + 6.f || s[r + 1] + (ev - z.y) > F::kLazyZ + 6.f;
+            grow |= s[r + 2] + (ev - z.z) > F::kLazyZ + 6.f || s[r + 3] + (ev - z.w) > F::kLazyZ + 6.f;
+          }
+        }
         if (named_bar_or(1 + wg, 128, grow || !ok)) {
           float keep[RC];
 #pragma unroll
           for (int r = 0; r < RC; ++r) {
-            float v = s[r];
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+            const float v = warp_max(s[r]);
             if (lane == 0) bars.red[wg][w4][r] = v;
-          }
-          if (Q8) {
-            const int top = __reduce_max_sync(0xffffffffu, mine ? ev : -1000);
-            if (lane == 0) bars.red_e[wg][w4] = top;
+            if constexpr (Q8) {
+              const float z = warp_max(s[r] + ev);
+              if (lane == 0) bars.red_z[wg][w4][r] = z;
+            }
           }
           if (lane == 0) bars.fail[wg][w4] = !ok;
           named_bar_sync(1 + wg, 128);
@@ -403,11 +428,16 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
             stop = true;
             break;
           }
-          float oscale = 1.f;
-          if (Q8) {
-            const int top = max(eref, max(max(bars.red_e[wg][0], bars.red_e[wg][1]), max(bars.red_e[wg][2], bars.red_e[wg][3])));
-            oscale = eref == top ? 1.f : top - eref > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (top - eref)) << 23);
-            eref = top;
+          if constexpr (Q8) {
+            // a lane a row, in every warp alike
+            if (lane < RC) {
+              const int r = lane;
+              const float top = fmaxf(z_lane, fmaxf(fmaxf(bars.red_z[wg][0][r], bars.red_z[wg][1][r]), fmaxf(bars.red_z[wg][2][r], bars.red_z[wg][3][r])) - 6.f);
+              bars.z_keep[wg][w4][r] = top == z_lane || z_lane == minus_inf ? 1.f : exp2_fast(z_lane - top);
+              bars.z[wg][w4][r] = top == minus_inf ? 0.f : top;
+              z_lane = top;
+            }
+            __syncwarp();
           }
 #pragma unroll
           for (int r = 0; r < RC; ++r) {
@@ -426,7 +456,12 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
               tmem_ld8(o_at + k, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 8; ++j) o[j] *= keep[(k + j) % RC] * oscale;
+              for (int j = 0; j < 8; ++j) {
+                if constexpr (Q8)
+                  o[j] *= bars.z_keep[wg][w4][(k + j) % RC];
+                else
+                  o[j] *= keep[(k + j) % RC];
+              }
               tmem_st8(o_at + k, o);
             }
             tmem_st_wait();
@@ -435,8 +470,6 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         // probabilities; the buffer is free once the product that read it last is done
         wait(pv_done + 8 * wg, use ^ 1);
         uint8_t* row = sp + wg * F::kP + tid4 * F::kPRow;
-        float scale_v = 64.f;
-        if (Q8) scale_v = !mine || eref - ev > 120 ? 0.f : 64.f * __uint_as_float((uint32_t)(127 - (eref - ev)) << 23);
         uint32_t w[F::kPRow / 4];
 #pragma unroll
         for (int r = 0; r < RC; r += Q8 ? 4 : 2) {
@@ -446,9 +479,12 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
             e[j] = exp2_fast(s[r + j] - (m[r + j] == minus_inf ? 0.f : m[r + j]));
             l[r + j] += e[j];
           }
-          if (Q8) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] *= scale_v;
+          if constexpr (Q8) {
+            const float4 z = *reinterpret_cast<const float4*>(&bars.z[wg][w4][r]);
+            e[0] = exp2_fast(s[r] + (ev - z.x));
+            e[1] = exp2_fast(s[r + 1] + (ev - z.y));
+            e[2] = exp2_fast(s[r + 2] + (ev - z.z));
+            e[3] = exp2_fast(s[r + 3] + (ev - z.w));
 #pragma unroll
             for (int term = 0; term < 3; ++term) {
               const uint32_t lo = e4m3x2(e[0], e[1]), hi = e4m3x2(e[2], e[3]);
@@ -502,8 +538,9 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         if (tid4 == 0) {
 #pragma unroll
           for (int r = 0; r < RC; ++r) bars.half[1][r] = m[r];
-          bars.half_e = eref;
         }
+        if constexpr (Q8)
+          if (tid4 < RC) bars.half_z[tid4] = z_lane;                // warp 0: lane r has row r's
         tc_fence_before();                                          // group 0 reads this group's accumulators
         named_bar_sync(3, 256);
       } else {
@@ -526,10 +563,16 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
           float w0 = l0 == 0.f ? 0.f : exp2_fast(mr - top), w1 = l1 == 0.f ? 0.f : exp2_fast(m1 - top);
           const float sum = w0 * l0 + w1 * l1;
           const bool dead = sum == 0.f;
-          auto unit = [](int e) { return e < -900 ? 0.f : exponent_up((uint32_t)e) * 0.015625f; };
-          float scale = whole ? (dead ? 0.f : 1.f / sum) : 1.f;
-          w0 *= scale * (Q8 ? unit(eref) : 1.f);
-          w1 *= scale * (Q8 ? unit(bars.half_e) : 1.f);
+          const float scale = whole ? (dead ? 0.f : 1.f / sum) : 1.f;
+          if constexpr (Q8) {
+            // sums of codes are held under 2^(Z - 6): 2^(Z - 6 - 127 - top), whose exponent alone may leave float32's range
+            const float h0 = exp2_fast(0.5f * (z_lane - 127.f - top)), h1 = exp2_fast(0.5f * (bars.half_z[r] - 127.f - top));
+            w0 = h0 * scale * h0;
+            w1 = h1 * scale * h1;
+          } else {
+            w0 *= scale;
+            w1 *= scale;
+          }
           bars.half[0][r] = had0 && l0 != 0.f ? w0 : 0.f;
           bars.half[1][r] = had1 && l1 != 0.f ? w1 : 0.f;
           if (whole) {
@@ -605,7 +648,7 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
         if (!ok) return;
         float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = is_v ? __int_as_float(live[j] ? (int)bytes[j] : 0) : live[j] ? exponent_up(bytes[j]) : 1.f;
+        for (int j = 0; j < 4; ++j) v[j] = is_v ? (!live[j] ? 0.f : bytes[j] == 255u ? __uint_as_float(0x7fc00000u) : (float)bytes[j]) : live[j] ? exponent_up(bytes[j]) : 1.f;
         *reinterpret_cast<float4*>(sexp + es * 256 + is_v * 128 + lane * 4) = make_float4(v[0], v[1], v[2], v[3]);
         mbar_arrive(e_full + 8 * es);
       };
