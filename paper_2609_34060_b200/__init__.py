@@ -782,6 +782,23 @@ def _heads(t: torch.Tensor, d: int, what: str) -> bytes:
     return _HEADS.pack(t.data_ptr(), rows, heads, s_row if rows > 1 else 0, s_head if heads > 1 else 0)
 
 
+def _fits(c, q8: bool, what: str) -> None:
+    """The tensors hold what the descriptor will say they do, and the page table names a page for every token (attributes
+    may have been set since the object was made)."""
+    rows = c.L * c.H * (c.T if c.page_table is None else c.P * c.page)
+    dtype = torch.float8_e4m3fn if q8 else torch.bfloat16
+    for t, n, want in ((c.k, rows * c.d, dtype), (c.v, rows * c.d, dtype)) + (((c.scale_k, rows, torch.uint8), (c.scale_v, rows, torch.uint8)) if q8 else ()):
+        if t.dtype is not want or not t.is_contiguous():
+            raise KvcError(KVC_E_INVALID_ARG, f"{what}: contiguous {want} expected")
+        if t.numel() < n:
+            raise KvcError(KVC_E_SHAPE, f"{what}: a tensor of {t.numel()} elements for {n}")
+    if c.page_table is not None:
+        if c.page_table.dtype is not torch.int32 or not c.page_table.is_contiguous():
+            raise KvcError(KVC_E_INVALID_ARG, f"{what}: contiguous int32 page table expected")
+        if c.T > c.page_table.numel() * c.page:
+            raise KvcError(KVC_E_SHAPE, f"{what}: {c.page_table.numel()} pages of {c.page} for {c.T} tokens")
+
+
 def _desc(c, kind=None, what: str = "cache"):
     """(address of the descriptor of a Cache or QCache, its device, ..., its kvc_qcache or None): the structure is kept until
     an attribute of the object is set, its pointers are set at every call.  Addresses carry no type, so the class is
@@ -791,6 +808,7 @@ def _desc(c, kind=None, what: str = "cache"):
     made = c.__dict__.get("_made")
     if made is None:
         q8 = isinstance(c, QCache)
+        _fits(c, q8, what)
         s = c.struct()
         devs = {t.get_device() for t in (c.k, c.v, c.page_table) + ((c.scale_k, c.scale_v) if q8 else ()) if t is not None}
         made = c.__dict__["_made"] = (C.addressof(s), devs.pop() if len(devs) == 1 else -1, s.codes if q8 else s, s if q8 else None)
@@ -859,6 +877,8 @@ def kvc_attend(req: Requests, q: torch.Tensor, cache, layer: int, out: torch.Ten
     at, c, hq, ho = _address(req, "kvc_attend"), _desc(cache), _heads(q, cache.d, "q"), _heads(out, cache.d, "out")
     st = _here("kvc_attend", stream, (c[1], req._dev), q, out, workspace, lse)
     _holds(req, cache, "kvc_attend")
+    if workspace is not None and not workspace.is_contiguous():
+        raise KvcError(KVC_E_INVALID_ARG, "kvc_attend: a contiguous workspace expected")
     if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
         raise KvcError(KVC_E_INVALID_ARG, "kvc_attend: lse must be float32 [rows, heads]")
     fn = load().kvc_attend if c[3] is None else load().kvc_attend_q8
