@@ -545,7 +545,7 @@ int kvc_gate_weights(const double *dist_sq, int32_t n_anchors, double temperatur
  * A request whose numbers break these rules (a length above its bound, rows outside n_rows, a negative length) is
  * skipped, and KVC_FLAG_BAD_LENGTH is raised in the status word.  A page id outside the pool raises KVC_FLAG_BAD_PAGE;
  * kvc_append skips the row, kvc_attend takes the page's keys and values as zeros.  max_kv beyond what the table (or the
- * cache) holds: KVC_E_SHAPE.
+ * cache) holds: KVC_E_SHAPE; beyond 2^31 - 257: KVC_E_UNSUPPORTED.
  */
 typedef struct kvc_requests {
   int32_t n, max_q, max_kv, table_stride;

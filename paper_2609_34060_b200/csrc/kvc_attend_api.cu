@@ -114,6 +114,9 @@ int resolve_qcache(const kvc_qcache* q, DevCache* c, DevScale* e) {
   return KVC_OK;
 }
 
+// Positions are 32-bit integers, and the kernels step up to two tiles past the last one.
+constexpr int32_t kMaxTokens = 0x7fffffff - 256;
+
 int resolve_requests(const kvc_requests* r, const kvc_cache* c, int n_rows, DevRequests* out) {
   if (!r || r->n < 0 || r->max_q < 0 || r->max_kv < 0 || r->table_stride < 0 || n_rows < 0) return KVC_E_INVALID_ARG;
   if (r->n > 0 && (!r->q_begin || !r->kv_len)) return KVC_E_INVALID_ARG;
@@ -125,6 +128,7 @@ int resolve_requests(const kvc_requests* r, const kvc_cache* c, int n_rows, DevR
     return KVC_E_INVALID_ARG;
   }
   if (r->max_kv > cap) return KVC_E_SHAPE;
+  if (r->max_kv > kMaxTokens) return KVC_E_UNSUPPORTED;
   out->q_begin = r->q_begin;
   out->kv_len = r->kv_len;
   out->table = r->page_table;
@@ -182,7 +186,7 @@ int convert_common(const kvc_cache* bf, const kvc_qcache* q8, int to8, void* str
   if ((rc = resolve_cache(bf, &c.bf)) != KVC_OK || (rc = resolve_qcache(q8, &c.q8, &c.e)) != KVC_OK) return rc;
   const kvc_cache& g = q8->codes;
   if (bf->L != g.L || bf->H != g.H || bf->T != g.T || bf->d != g.d) return KVC_E_SHAPE;
-  if (g.H > 32767) return KVC_E_UNSUPPORTED;
+  if (g.H > 32767 || g.T > kMaxTokens) return KVC_E_UNSUPPORTED;
   const int64_t rb = cache_reach(bf, c.bf), rq = cache_reach(&g, c.q8);
   const Extent bk = extent_of(bf->k, rb, 2), bv = extent_of(bf->v, rb, 2), qk = extent_of(g.k, rq, 1), qv = extent_of(g.v, rq, 1);
   if (overlap(bk, qk) || overlap(bk, qv) || overlap(bv, qk) || overlap(bv, qv) || (to8 ? overlap(qk, qv) : overlap(bk, bv))) return KVC_E_ALIAS;
@@ -277,7 +281,7 @@ int kvc_append_q8(const kvc_requests* req, const kvc_heads* k_new, const kvc_hea
 }
 
 size_t kvc_attend_workspace_bytes(const kvc_requests* req, int32_t n_heads, int32_t H, int32_t d) {
-  if (!req || req->n <= 0 || req->max_q <= 0 || req->max_kv < 0 || H <= 0 || n_heads <= 0 || n_heads % H || (d != 64 && d != 128)) return 0;
+  if (!req || req->n <= 0 || req->max_q <= 0 || req->max_kv < 0 || req->max_kv > kMaxTokens || H <= 0 || n_heads <= 0 || n_heads % H || (d != 64 && d != 128)) return 0;
   return tc_attend_workspace_bytes(req->n, req->max_q, req->max_kv, n_heads / H, H, d);
 }
 
