@@ -96,8 +96,9 @@ __device__ __forceinline__ int own_page(const DevCache& c, int t, uint32_t* stat
 constexpr int kThreads = 256;
 
 // grid: x = token blocks, y = head x (K|V), z = layers (strided).  A thread keeps kUnroll rows in flight: two to quantise
-// (one: 296 us, four: 333), one to read back (two: 247), on the 8K and the 16K cache.  Measured: 253-258 us = 6.3 TB/s to
-// quantise the 8K cache (32 layers), 240-245 us = 5.8 TB/s to read back the 16K one, of 6.55 TB/s copied.
+// (one: 296 us, four: 333), one to read back (two: 247), on the 8K and the 16K cache.  Measured: 264 us = 6.1 TB/s to
+// quantise the 8K cache (32 layers; 253 us alone and cold under a profiler), 240 us = 5.9 TB/s to read back the 16K one,
+// of 6.55 TB/s copied.
 template <int D, bool TO8, int kUnroll>
 __global__ void __launch_bounds__(kThreads) convert_kernel(const __grid_constant__ ConvertLaunch p) {
   constexpr int LPR = D / 16, RPP = kThreads / LPR;

@@ -12,16 +12,18 @@
 // shared memory.  It is handed over in two parts (96 and 32 keys), so that most of the second product runs while the rest
 // is still being computed.
 //
-// Measured, 2048 tokens behind 8K, 32 / 8 heads of 128 (240 GFLOP): 212 us (1.13 PFLOP/s) in a short run, 238-250 us
+// Measured, 2048 tokens behind 8K, 32 / 8 heads of 128 (240 GFLOP): 212 us (1.13 PFLOP/s) in a short run, 245 us
 // once the power cap has set the clock.  What bounds it: a row tile's own chain, softmax (about 1750 cycles), the second
-// product's tail, the next first product, and the hand-overs between them (about 3200 a tile of keys; tensor cores busy
-// 63 % of it).  There is no tensor memory left for a second S.  Local memory would cost more than anything else (shared
+// product's tail, the next first product, and the hand-overs between them (about 3200 a tile of keys, in which the tensor
+// cores need 2048 for both row tiles; over the whole launch, start, epilogues and join included, they are busy 53 %).  A
+// second S of 128 columns finds no room; two of 64 would (P takes the lower half of S's columns), and are not tried.
+// Local memory would cost more than anything else (shared
 // memory takes all of L1: with 100 bytes of spills in the loop the kernel ran 310 us), and so does code that the
 // instruction cache does not hold (8-bit conversion unrolled whole: 277 us on the image context, in rounds 233).
 //
 // Exponentials stay on the special-function units (16 a cycle and SM, a tile's time of the tensor cores).  Moving a
 // quarter or half of them to the FMA pipe (rounding to a whole exponent and a degree-5 polynomial) made the kernel
-// slower, 234 -> 274 and 297 us on 2K tokens behind 8K: the warp's issue slots are what is short.
+// slower, 234 -> 274 and 297 us on 2K tokens behind 8K: the chain above got longer.
 //
 // m is a maximum of earlier tiles: a tile's own maximum is taken beside its exponentials, off the way from logits to
 // probabilities.  Exponentials above 1 cost no precision (bf16 and float32 have the same range), but P V is summed in
@@ -951,10 +953,15 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
 // others to this one (chunk = false: there are none).  Decided from the bounds alone: all requests within the few-rows
 // kernel's 32 rows take it; a batch of several requests with longer ones among them is served by both, single tokens by
 // the few-rows kernel; one long request by this kernel.  Both cost two more launches one behind the other, about 10 us,
-// and a tile of a single token costs this kernel about twice the other's time (0.02 against 0.01 us with all SMs at
-// work): about a thousand tiles pay for them.  The host knows the longest request only, and lengths about half of it on
-// average are the rule, so batches that could hold up to kBothTiles key tiles stay with this kernel alone (10 requests
-// of 8 heads, 1528 keys on average and 3056 at most: 36 us, by both 53; nine of 2 heads, 1500 keys on average: 35 and 50).
+// and a tile of a single token costs this kernel about twice the other's time.  The host knows the longest request only,
+// so batches that could hold up to kBothTiles key tiles by the bounds stay with this kernel alone.  Measured, this kernel
+// alone and both, us, 4 query heads of 128 per KV head, lengths to twice their mean, the rest single tokens:
+//     tiles by the bounds                     1152   1536   2304   3072    4096    4608    8192    16384   32256
+//     bf16, one request in ten of 50-400 rows 43 56  46 56  60 76  55 72   83 94   92 92   138 121 243 194 370 304
+//     bf16, one in two                        54 60  66 79  97 102 110 122 130 140 168 171 209 215 392 381 735 697
+//     8 bits, one in ten                      41 51  44 52  62 69  62 73   88 86   108 98  164 125 302 206 496 295
+//     8 bits, one in two                      61 68  80 90  111 112 131 143 161 165 193 193 267 261 508 454 848 737
+// The lines cross at about 4500 tiles; a batch between 2048 and 4096 is up to 17 us slower by both.
 constexpr int64_t kBothTiles = 2048;
 struct Plan {
   int rc;

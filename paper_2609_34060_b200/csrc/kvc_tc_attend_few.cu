@@ -30,8 +30,8 @@
 // with one exponential for both).
 // Sums and joins are float32.  Over bf16 caches P is rounded to bf16 as in the chunk kernel.
 //
-// Measured: 64 requests of 4K (lognormal), 32 / 8 heads, bf16 pages of 16: 202 us = 6.4 TB/s of 6.55 copied; eight
-// requests of 32K, 64 / 8 heads, 8-bit pages of 16: 111 us (100 with pages of 128: the copies of 2 KB boxes then bound it,
+// Measured: 64 requests of 4K (lognormal), 32 / 8 heads, bf16 pages of 16: 202-206 us = 6.3 TB/s of 6.55 copied; eight
+// requests of 32K, 64 / 8 heads, 8-bit pages of 16: 110-114 us (100 with pages of 128: the copies of 2 KB boxes then bound it,
 // and 12 us are start and join); one request of 777 keys: 11 us, of which 2 are the join's; one of 30K, 8 / 1 heads: 25 us
 // (31 with the join loading a piece's sums after its weights, eight at a time).
 //
