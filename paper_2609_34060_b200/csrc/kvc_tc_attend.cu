@@ -956,12 +956,12 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
 // and a tile of a single token costs this kernel about twice the other's time.  The host knows the longest request only,
 // so batches that could hold up to kBothTiles key tiles by the bounds stay with this kernel alone.  Measured, this kernel
 // alone and both, us, 4 query heads of 128 per KV head, lengths to twice their mean, the rest single tokens:
-//     tiles by the bounds                     1152   1536   2304   3072    4096    4608    8192    16384   32256
-//     bf16, one request in ten of 50-400 rows 43 56  46 56  60 76  55 72   83 94   92 92   138 121 243 194 370 304
-//     bf16, one in two                        54 60  66 79  97 102 110 122 130 140 168 171 209 215 392 381 735 697
-//     8 bits, one in ten                      41 51  44 52  62 69  62 73   88 86   108 98  164 125 302 206 496 295
-//     8 bits, one in two                      61 68  80 90  111 112 131 143 161 165 193 193 267 261 508 454 848 737
-// The lines cross at about 4500 tiles; a batch between 2048 and 4096 is up to 17 us slower by both.
+//     tiles by the bounds                     1152   1536   2304    4096    4608    8192    16384   32256
+//     bf16, one request in ten of 50-400 rows 43 56  46 56  60 76   83 94   92 92   138 121 243 194 370 304
+//     bf16, one in two                        54 60  66 79  97 102  130 140 168 171 209 215 392 381 735 697
+//     8 bits, one in ten                      41 51  44 52  62 69   88 86   108 98  164 125 302 206 496 295
+//     8 bits, one in two                      61 68  80 90  111 112 161 165 193 193 267 261 508 454 848 737
+// The lines cross at about 4500 tiles; a batch between 2048 and 4096 is up to 16 us slower by both.
 constexpr int64_t kBothTiles = 2048;
 struct Plan {
   int rc;
