@@ -590,7 +590,8 @@ typedef struct kvc_qcache {
  *                   not count towards its row's scale.
  * kvc_dequantize -- dst = bf16(value) (exact but for numbers below bf16's subnormal step).
  * src and dst agree in L, H, T, d; layouts, strides and page tables may differ.  Pages that the tables do not name and
- * rows >= T are left as they were.  Errors as kvc_apply (KVC_E_ALIAS: the buffers overlap, exponents among them; those
+ * rows >= T are left as they were; a table that is written through names no page twice.  Errors as kvc_apply
+ * (KVC_E_ALIAS: the buffers overlap, exponents among them; those
  * of keys and values may lie between one another, or behind their row of codes, where no byte is shared).
  */
 int kvc_quantize(const kvc_cache *src, kvc_qcache *dst, void *stream);
@@ -631,7 +632,8 @@ int kvc_append_q8(const kvc_requests *req, const kvc_heads *k_new, const kvc_hea
  * rounded to bf16 (2^-8 of themselves).  Over an 8-bit cache, where no request of the call has more than 32 rows (max_q
  * times query heads per KV head), and for single tokens in large calls that mix them with chunks, the product of a
  * probability and its value row's scale meets the codes as three e4m3 parts: 2^-12 of itself, or 2^-24 of the row's largest
- * such product.
+ * such product.  There a query meets the codes as two e4m3 parts: exact, but for channels below 2^-15 of the query's
+ * largest, which are off by up to 2^-22 of that.
  * Results do not depend on the order in which blocks run, and equal calls give equal bits.
  */
 int kvc_attend(const kvc_requests *req, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale, int32_t causal,
