@@ -645,6 +645,142 @@ int kvc_attend_q8(const kvc_requests *req, const kvc_heads *q, const kvc_qcache 
 size_t kvc_attend_workspace_bytes(const kvc_requests *req, int32_t n_heads, int32_t H, int32_t d);
 
 /*
+ * Drafted tokens: a small model proposes several continuations, one pass of the large model looks at all of them, some
+ * stay.  The proposals of a request are its new tokens (kvc_requests); they form a tree, a chain among trees being one
+ * draft behind the other.  A step of a serving program:
+ *     kvc_tree_build       masks and depths of the drafts from their parents, once a step
+ *     kvc_append_rotated   per layer: queries and keys turned to their positions, keys and values into the cache
+ *     kvc_attend_tree      per layer: every draft attends to the context and to the drafts it continues
+ *     kvc_verify           which drafts stay, and the token behind them, from the target's distributions
+ *     kvc_keep             the rows of those that stay moved together, in all layers
+ * (kvc_append_rotated and kvc_attend serve prompts and single tokens, which need no tree.)
+ *   words        32-bit words of a row's mask, at least ceil(max_q / 32)
+ *   n_rows       packed rows
+ *   parent       DEVICE int32 [n_rows]: place j' < j, within its request, of the new token that row j of the request
+ *                continues; -1: it continues the cache.  Anything else counts as -1 and raises KVC_FLAG_BAD_TREE.
+ *   mask         DEVICE uint32 [n_rows, words]: bit a of row j: it sees new token a of its request
+ *   depth        DEVICE int32 [n_rows]: how many new tokens a row has before it; its position is kv_len - n_q + depth
+ * A request's first row is usually its last accepted token (parent -1), which the cache does not hold yet.
+ */
+#define KVC_TREE_MAX_Q 1024
+typedef struct kvc_tree {
+  int32_t words, n_rows;
+  const int32_t *parent;
+  uint32_t *mask;
+  int32_t *depth;
+} kvc_tree;
+
+/*
+ * kvc_tree_build -- mask and depth of every row from the parents:
+ *     mask[j] = { j } and mask[parent[j]] ,  depth[j] = depth[parent[j]] + 1  (0 for parent -1) .
+ * All words of a row are written; rows outside every request are left as they were.  The lists, the parents and what is
+ * written lie apart (KVC_E_ALIAS).  max_q up to KVC_TREE_MAX_Q (KVC_E_UNSUPPORTED beyond); too few words: KVC_E_SHAPE.
+ */
+int kvc_tree_build(const kvc_requests *req, const kvc_tree *tree, void *stream);
+
+/*
+ * Rotary positions of new tokens.  New token j of request i has position
+ *     p = (pos_begin ? pos_begin[i] : 0) + kv_len[i] - n_q + (depth ? depth[row] : j)
+ * and is rotated, pair by pair, by the angle p f_k, k < rot_dim / 2:
+ *     (x, y) -> amplitude (x cos - y sin, x sin + y cos)
+ *   rope         pairing within the first rot_dim channels (KVC_ROPE_HALF: c with c + rot_dim / 2); theta gives
+ *                f_k = theta^(-2k / rot_dim); inv_freq (HOST float64 [rot_dim / 2]) overrides it: frequencies scaled for
+ *                long contexts, linearly or by parts, go in here
+ *   amplitude    factor on the rotated channels of queries and keys that goes with some scalings; 0 stands for 1
+ *   rot_dim      channels that are rotated, the first ones of every head; the others stay as they are.  A multiple of 16
+ *                (KVC_E_UNSUPPORTED otherwise), 0: all d
+ *   depth        DEVICE int32 [n_rows] or NULL
+ *   pos_begin    DEVICE int32 [n] or NULL: position of the cache's first token (an agent's prefix that is held elsewhere)
+ * Positions are exact, angles are reduced in float64, cos and sin rounded to float32: no precision is lost at far ones.
+ */
+typedef struct kvc_rotary {
+  kvc_rope rope;
+  double amplitude;
+  int32_t rot_dim, reserved;
+  const int32_t *depth;
+  const int32_t *pos_begin;
+} kvc_rotary;
+
+/*
+ * kvc_append_rotated -- kvc_append with the keys rotated on the way, and the queries of the same rows rotated beside them:
+ * q_out = bf16(Rot(q)), cache keys = bf16(Rot(k_new)), cache values = v_new.  kvc_append_rotated_q8: rotated keys and the
+ * values quantised as kvc_quantize would, from float32 (rounded once).
+ *   q, q_out     [n_rows, any number of heads, d], or both NULL; q_out may be q itself (in place), also where q, k_new and
+ *                v_new are slices of one projection's output
+ * Everything else as in kvc_append.  Queries are rotated whether or not their keys found a place.  KVC_E_ALIAS: what is
+ * written meets what is read.
+ */
+int kvc_append_rotated(const kvc_requests *req, const kvc_rotary *rot, const kvc_heads *q, kvc_heads *q_out, const kvc_heads *k_new,
+                       const kvc_heads *v_new, int32_t layer, kvc_cache *dst, void *stream);
+int kvc_append_rotated_q8(const kvc_requests *req, const kvc_rotary *rot, const kvc_heads *q, kvc_heads *q_out, const kvc_heads *k_new,
+                          const kvc_heads *v_new, int32_t layer, kvc_qcache *dst, void *stream);
+
+/*
+ * kvc_attend_tree -- kvc_attend for trees: new token j of a request sees the keys t < kv_len - n_q and those new tokens
+ * a <= j whose bits are set in its mask (bits beyond j are not looked at; the masks may be kvc_tree_build's or the caller's
+ * own).  A row that sees nothing gets zeros and minus infinity.  parent and depth of the tree are not used.  Workspace,
+ * rounding, limits and errors as in kvc_attend; max_q up to KVC_TREE_MAX_Q.
+ */
+int kvc_attend_tree(const kvc_requests *req, const kvc_tree *tree, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale,
+                    kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int kvc_attend_tree_q8(const kvc_requests *req, const kvc_tree *tree, const kvc_heads *q, const kvc_qcache *cache, int32_t layer, double scale,
+                       kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Probabilities: DEVICE float32 [n_rows, n], rows s_row elements apart (0: n), 4-byte aligned. */
+typedef struct kvc_probs {
+  const float *p;
+  int32_t n_rows, n;
+  int64_t s_row;
+} kvc_probs;
+
+/*
+ * kvc_verify -- which drafts of every request stay, and the next token, so that the tokens are distributed as the target's
+ * (rejection sampling from given random numbers).  Row r's distribution is that of the token behind row r.  The walk
+ * begins at the request's row 0, with P = target[row 0].  The current node's children are tried in their order; child c,
+ * drafted token x, is accepted where
+ *     u[c] q(x) < P(x) ,     q = draft[node] ,
+ * and becomes the node, with P = target[c].  Where it is rejected, P becomes max(P - q, 0), divided by its sum.  A node
+ * without a further child ends the walk: the next token is drawn from P by its distribution function,
+ *     next = min { x : sum_{y <= x} P(y) > u_next sum_y P(y) } .
+ *   parent       as in kvc_tree
+ *   token        DEVICE int32 [n_rows]: drafted tokens (of a request's row 0 not looked at)
+ *   target       distributions of the target; NaN and negative entries count as 0, sums need not be exactly 1
+ *   draft        distributions the children of every row were drawn from; same n and n_rows.  NULL: the drafts were chosen,
+ *                not drawn: child c is accepted where u[c] (1 - the probabilities of the siblings rejected before it) <
+ *                P(x), and a rejected token's probability becomes 0
+ *   u            DEVICE float32 [n_rows], u_next DEVICE float32 [n]: uniform in [0, 1)
+ *   kept         DEVICE int32 [n, kept_stride], kept_stride >= max_q: places of the accepted rows within the request, row 0
+ *                first, ascending; -1 behind them, up to max_q
+ *   n_kept       DEVICE int32 [n]: their number (0 only for a request without rows)
+ *   next         DEVICE int32 [n]: the next token; -1 for a request without rows
+ * Where a rejection leaves no residual (P <= q everywhere, as rounding may have it), the remaining siblings are rejected
+ * and the token is drawn from the node's own distribution.  A distribution without a positive finite sum gives -1 and
+ * KVC_FLAG_BAD_PROB.  A drafted token outside [0, n) is rejected and leaves P as it is; it, and a parent out of range,
+ * raises KVC_FLAG_BAD_TREE.  A request whose numbers break the rules of kvc_requests is answered like one without rows.
+ * Sums and comparisons are float64: results do not depend on the order of execution.  max_kv and the page table are not
+ * used, kv_len is (bounds).  max_q up to KVC_TREE_MAX_Q.
+ */
+int kvc_verify(const kvc_requests *req, const int32_t *parent, const int32_t *token, const kvc_probs *target, const kvc_probs *draft,
+               const float *u, const float *u_next, int32_t *kept, int32_t kept_stride, int32_t *n_kept, int32_t *next, void *stream);
+
+/*
+ * kvc_keep -- the rows of the accepted drafts moved together, in every layer and head, keys and values: row
+ * kv_len - n_q + kept[i][j] of request i goes to kv_len - n_q + j, j < n_kept[i]; codes and exponents of 8-bit caches
+ * alike.  Rows behind them stay as they are (the next step overwrites them).
+ *   kept         DEVICE int32 [n, kept_stride], ascending places below n_q, as kvc_verify leaves them
+ *   n_kept       DEVICE int32 [n]
+ *   kv_out       DEVICE int32 [n] or NULL: kv_len - n_q + n_kept, the length behind the step; not kv_len itself
+ * A list that is not ascending or leaves the request's rows, or a negative position, raises KVC_FLAG_BAD_TREE: nothing of
+ * that request is moved and kv_out gets kv_len.  A request whose numbers break the rules of kvc_requests is left, kv_out
+ * too.  A page id outside the pool raises KVC_FLAG_BAD_PAGE, its row is not moved.  Requests must not share the pages they
+ * move rows in; without a page table n == 1 (KVC_E_INVALID_ARG otherwise).  max_q up to KVC_TREE_MAX_Q.
+ */
+int kvc_keep(const kvc_requests *req, const int32_t *kept, int32_t kept_stride, const int32_t *n_kept, kvc_cache *cache, int32_t *kv_out,
+             void *stream);
+int kvc_keep_q8(const kvc_requests *req, const int32_t *kept, int32_t kept_stride, const int32_t *n_kept, kvc_qcache *cache,
+                int32_t *kv_out, void *stream);
+
+/*
  * Device-side anomalies never trap or hang: a kernel that meets a page id outside
  * [0, n_phys_pages) or whose bounded wait on an asynchronous copy runs out skips
  * that tile and ORs a bit into a per-device status word.
@@ -657,6 +793,8 @@ size_t kvc_attend_workspace_bytes(const kvc_requests *req, int32_t n_heads, int3
 #define KVC_FLAG_WAIT_EXPIRED 2u
 #define KVC_FLAG_NOT_CONVERGED 4u   /* eigensolver hit its sweep limit             */
 #define KVC_FLAG_BAD_LENGTH   8u    /* a request's rows or length outside its bounds */
+#define KVC_FLAG_BAD_TREE    16u    /* a draft's parent, token or place out of range */
+#define KVC_FLAG_BAD_PROB    32u    /* a distribution without a positive finite sum  */
 int kvc_status_poll(uint32_t *flags);
 int kvc_status_reset(void);
 

@@ -28,6 +28,8 @@ KVC_PATH_AUTO, KVC_PATH_GENERIC, KVC_PATH_TC, KVC_PATH_MIXED = 0, 1, 2, 3
 KVC_MAX_SEGMENTS, KVC_COORDS_TARGET, KVC_COORDS_SOURCE = 16, 0, 1
 KVC_GROUP_HEAD, KVC_GROUP_LAYER = 0, 1
 KVC_FLAG_BAD_PAGE, KVC_FLAG_WAIT_EXPIRED, KVC_FLAG_NOT_CONVERGED, KVC_FLAG_BAD_LENGTH = 1, 2, 4, 8
+KVC_FLAG_BAD_TREE, KVC_FLAG_BAD_PROB = 16, 32
+KVC_TREE_MAX_Q = 1024
 KVC_OK = 0
 (KVC_E_INVALID_ARG, KVC_E_SHAPE, KVC_E_UNSUPPORTED, KVC_E_ALIAS, KVC_E_CUDA, KVC_E_WORKSPACE, KVC_E_DEVICE_FLAG,
  KVC_E_TOO_LARGE) = (-1, -2, -3, -4, -5, -6, -7, -8)
@@ -40,6 +42,7 @@ EXPORTS = (
     "kvc_state_realign", "kvc_effective_rank", "kvc_fit_eigenvalues", "kvc_fit_solver", "kvc_group_fit_eigenvalues", "kvc_group_fit_solver", "kvc_selftest_wait_expiry", "kvc_apply_segmented", "kvc_state_update_segmented", "kvc_state_update_check", "kvc_state_update_chain",
     "kvc_chain_update_workspace_bytes", "kvc_chain_update_edge_stride", "kvc_chain_fused", "kvc_chain_workspace_bytes",
     "kvc_quantize", "kvc_dequantize", "kvc_append", "kvc_append_q8", "kvc_attend", "kvc_attend_q8", "kvc_attend_workspace_bytes",
+    "kvc_tree_build", "kvc_append_rotated", "kvc_append_rotated_q8", "kvc_attend_tree", "kvc_attend_tree_q8", "kvc_verify", "kvc_keep", "kvc_keep_q8",
 )
 
 
@@ -86,6 +89,19 @@ class kvc_requests(C.Structure):
 
 class kvc_heads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("n_rows", C.c_int32), ("n_heads", C.c_int32), ("s_row", C.c_int64), ("s_head", C.c_int64)]
+
+
+class kvc_tree(C.Structure):
+    _fields_ = [("words", C.c_int32), ("n_rows", C.c_int32), ("parent", C.c_void_p), ("mask", C.c_void_p), ("depth", C.c_void_p)]
+
+
+class kvc_rotary(C.Structure):
+    _fields_ = [("rope", kvc_rope), ("amplitude", C.c_double), ("rot_dim", C.c_int32), ("reserved", C.c_int32), ("depth", C.c_void_p),
+                ("pos_begin", C.c_void_p)]
+
+
+class kvc_probs(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("n_rows", C.c_int32), ("n", C.c_int32), ("s_row", C.c_int64)]
 
 
 _lib = None
@@ -149,6 +165,11 @@ def load(path: Optional[str] = None):
     lib.kvc_attend.argtypes = lib.kvc_attend_q8.argtypes = [vp, vp, vp, i32, C.c_double, i32, vp, vp, vp, sz, vp]
     lib.kvc_attend_workspace_bytes.argtypes = [vp, i32, i32, i32]
     lib.kvc_attend_workspace_bytes.restype = sz
+    lib.kvc_tree_build.argtypes = [vp, vp, vp]
+    lib.kvc_append_rotated.argtypes = lib.kvc_append_rotated_q8.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp]
+    lib.kvc_attend_tree.argtypes = lib.kvc_attend_tree_q8.argtypes = [vp, vp, vp, vp, i32, C.c_double, vp, vp, vp, sz, vp]
+    lib.kvc_verify.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.kvc_keep.argtypes = lib.kvc_keep_q8.argtypes = [vp, vp, i32, vp, vp, vp, vp]
     lib.kvc_status_poll.argtypes = [C.POINTER(C.c_uint32)]
     lib.kvc_status_reset.argtypes = []
     lib.kvc_set_path.argtypes = [i32]
@@ -345,6 +366,51 @@ class Requests:
         return self._struct
 
 
+class _Fixed:
+    """Base of the descriptors of device lists: the tensors' contents may change from step to step, the tensors not."""
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed; write into its tensors, or make another {type(self).__name__}")
+
+
+def _list(t, what: str, dtype=torch.int32) -> int:
+    """Address of a contiguous device list."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_contiguous():
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: contiguous {dtype} expected")
+    return t.data_ptr()
+
+
+def _device_of(*tensors) -> int:
+    devs = {t.get_device() for t in tensors if t is not None}
+    return devs.pop() if len(devs) == 1 else -1
+
+
+class Tree(_Fixed):
+    """A step's drafted tokens: ``parent`` int32 [rows] (place of the new token a row continues within its request, -1: the
+    cache), ``mask`` int32 [rows, words] (32 new tokens a word) and ``depth`` int32 [rows], which :func:`kvc_tree_build`
+    fills; all on the GPU.  ``max_q``: bound on the new tokens of a request, as in :class:`Requests`."""
+
+    def __init__(self, parent: torch.Tensor, max_q: int, mask: Optional[torch.Tensor] = None, depth: Optional[torch.Tensor] = None):
+        _list(parent, "parent")
+        rows, words = int(parent.numel()), max(1, (int(max_q) + 31) // 32)
+        if mask is None:
+            mask = torch.zeros(rows, words, dtype=torch.int32, device=parent.device)
+        if depth is None:
+            depth = torch.zeros(rows, dtype=torch.int32, device=parent.device)
+        _list(mask, "mask"), _list(depth, "depth")
+        if parent.dim() != 1 or mask.dim() != 2 or mask.shape[0] != rows or mask.shape[1] < words or depth.shape != parent.shape:
+            raise KvcError(KVC_E_SHAPE, f"parent [rows], mask [rows, {words} or more] and depth [rows] expected")
+        made = kvc_tree(int(mask.shape[1]), rows, parent.data_ptr(), mask.data_ptr(), depth.data_ptr())
+        self.__dict__.update(parent=parent, mask=mask, depth=depth, max_q=int(max_q), _struct=made, _at=C.addressof(made),
+                             _dev=_device_of(parent, mask, depth))
+
+    def __reduce__(self):
+        return Tree, (self.parent, self.max_q, self.mask, self.depth)
+
+    def struct(self) -> kvc_tree:
+        return self._struct
+
+
 class State:
     """Rank-r state over torch tensors.  Per (layer, head): coeff fp32 [L,H,n_cov,r], basis fp32|bf16
     [L,H,r,d].  Per layer (``grouping=KVC_GROUP_LAYER``): coeff [L,n_cov,r], basis [L,r,H*d]."""
@@ -457,6 +523,66 @@ class Rope:
         s.theta, s.pairing = self.theta, self.pairing
         s.inv_freq = None if self._tab is None else C.cast(self._tab, C.c_void_p)
         return s
+
+
+def scaled_frequencies(theta: float, rot_dim: int, factor: float = 1.0, original: Optional[int] = None, slow: float = 1.0,
+                       fast: float = 32.0) -> List[float]:
+    """Frequencies theta^(-2k / rot_dim) for contexts ``factor`` times longer than the model was trained on.  ``original``
+    None: linearly, f / factor.  Otherwise by parts (YaRN, arXiv 2309.00071, section 3.2): a pair that turns at least ``fast``
+    times over the ``original`` tokens keeps its frequency, one that turns at most ``slow`` times is divided by the factor,
+    in between a mix linear in the number of turns."""
+    import math
+    f = [float(theta) ** (-2.0 * k / rot_dim) for k in range(rot_dim // 2)]
+    if original is None:
+        return [x / factor for x in f]
+    keep = [min(1.0, max(0.0, (original * x / (2 * math.pi) - slow) / (fast - slow))) for x in f]
+    return [x * (w + (1.0 - w) / factor) for x, w in zip(f, keep)]
+
+
+class Rotary(_Fixed):
+    """How new tokens are turned to their positions: ``rope`` (theta and pairing, or a table of rot_dim / 2 frequencies, see
+    :func:`scaled_frequencies`), the number of channels that are rotated (``rot_dim``; None: all), a factor on them
+    (``amplitude``), and on the GPU ``depth`` int32 [rows] (None: a chain) and ``pos_begin`` int32 [requests], the position of
+    a cache's first token (None: 0).  Fixed once made."""
+
+    def __init__(self, rope: Rope, rot_dim: Optional[int] = None, amplitude: float = 1.0, depth: Optional[torch.Tensor] = None,
+                 pos_begin: Optional[torch.Tensor] = None):
+        if not isinstance(rope, Rope):
+            raise KvcError(KVC_E_INVALID_ARG, f"Rotary: Rope expected, not {type(rope).__name__}")
+        if amplitude == 0.0:
+            raise KvcError(KVC_E_INVALID_ARG, "Rotary: an amplitude of 0")
+        for t in (depth, pos_begin):
+            if t is not None:
+                _list(t, "depth, pos_begin")
+        made = kvc_rotary(rope.struct(), float(amplitude), int(rot_dim or 0), 0, None if depth is None else depth.data_ptr(),
+                          None if pos_begin is None else pos_begin.data_ptr())
+        # one table per width is worked out here, not at every call
+        tables = {}
+        table = None if rope._tab is None else list(rope._tab)
+        self.__dict__.update(rope=rope, rot_dim=int(rot_dim or 0), amplitude=float(amplitude), depth=depth, pos_begin=pos_begin, _struct=made,
+                             _at=C.addressof(made), _table=table, _tables=tables, _dev=_device_of(depth, pos_begin))
+
+    def __reduce__(self):
+        return Rotary, (self.rope, self.rot_dim or None, self.amplitude, self.depth, self.pos_begin)
+
+    def struct(self) -> kvc_rotary:
+        return self._struct
+
+    def _for(self, d: int, rows: int, n: int) -> int:
+        """Address of the descriptor for heads of d channels."""
+        made = self._tables.get(d)
+        if made is None:
+            rot = self.rot_dim or d
+            if self._table is not None and 2 * len(self._table) != rot:
+                raise KvcError(KVC_E_SHAPE, f"Rotary: {len(self._table)} frequencies for {rot} channels")
+            f = self._table if self._table is not None else [self.rope.theta ** (-2.0 * k / rot) if self.rope.theta > 0 else float("nan") for k in range(rot // 2)]
+            tab = (C.c_double * max(1, len(f)))(*f)
+            s = kvc_rotary.from_buffer_copy(self._struct)
+            s.rope.inv_freq = C.cast(tab, C.c_void_p)
+            made = self._tables[d] = (C.addressof(s), s, tab)
+        if (self.depth is not None and self.depth.numel() < rows) or (self.pos_begin is not None and self.pos_begin.numel() < n):
+            raise KvcError(KVC_E_SHAPE, "Rotary: depth [rows] and pos_begin [requests] expected")
+        return made[0]
 
 
 def _stream(stream) -> int:
@@ -885,6 +1011,104 @@ def kvc_attend(req: Requests, q: torch.Tensor, cache, layer: int, out: torch.Ten
     _check(fn(at, hq, c[0], int(layer), cache.d ** -0.5 if scale is None else float(scale), bool(causal), ho,
               None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(),
               0 if workspace is None else workspace.numel() * workspace.element_size(), st), "kvc_attend")
+
+
+def kvc_tree_build(req: Requests, tree: Tree, stream=None) -> None:
+    """Masks and depths of a step's drafted tokens from their parents."""
+    at, t = _address(req, "kvc_tree_build"), _tree(tree, "kvc_tree_build")
+    st = _here("kvc_tree_build", stream, (req._dev, tree._dev))
+    _check(load().kvc_tree_build(at, t, st), "kvc_tree_build")
+
+
+def _tree(tree, what: str) -> int:
+    if not isinstance(tree, Tree):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: Tree expected, not {type(tree).__name__}")
+    return tree._at
+
+
+def kvc_append_rotated(req: Requests, rotary: Rotary, k_new: torch.Tensor, v_new: torch.Tensor, cache, layer: int, q: Optional[torch.Tensor] = None,
+                       q_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Keys of the new tokens [rows, H, d] turned to their positions and written, with their values, into `layer` of a Cache
+    or QCache; queries [rows, heads, d] of the same rows turned beside them (`q_out` may be `q`)."""
+    what = "kvc_append_rotated"
+    if not isinstance(rotary, Rotary):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: Rotary expected, not {type(rotary).__name__}")
+    if (q is None) != (q_out is None):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: q and q_out go together")
+    at, c, k, v = _address(req, what), _desc(cache), _heads(k_new, cache.d, "k_new"), _heads(v_new, cache.d, "v_new")
+    hq, ho = (None, None) if q is None else (_heads(q, cache.d, "q"), _heads(q_out, cache.d, "q_out"))
+    st = _here(what, stream, (c[1], req._dev), k_new, v_new, q, q_out, rotary.depth, rotary.pos_begin)
+    _holds(req, cache, what)
+    fn = load().kvc_append_rotated if c[3] is None else load().kvc_append_rotated_q8
+    _check(fn(at, rotary._for(cache.d, k_new.shape[0], req.n), hq, ho, k, v, int(layer), c[0], st), what)
+
+
+def kvc_attend_tree(req: Requests, tree: Tree, q: torch.Tensor, cache, layer: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of a tree of drafted tokens: every row sees its request's context and the new tokens of its mask.
+    Workspace: kvc_attend_workspace_bytes."""
+    what = "kvc_attend_tree"
+    at, t, c, hq, ho = _address(req, what), _tree(tree, what), _desc(cache), _heads(q, cache.d, "q"), _heads(out, cache.d, "out")
+    st = _here(what, stream, (c[1], req._dev, tree._dev), q, out, workspace, lse)
+    _holds(req, cache, what)
+    if workspace is not None and not workspace.is_contiguous():
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: a contiguous workspace expected")
+    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: lse must be float32 [rows, heads]")
+    fn = load().kvc_attend_tree if c[3] is None else load().kvc_attend_tree_q8
+    _check(fn(at, t, hq, c[0], int(layer), cache.d ** -0.5 if scale is None else float(scale), ho, None if lse is None else lse.data_ptr(),
+              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(), st), what)
+
+
+_PROBS = struct.Struct("@QiiQ")       # kvc_probs
+
+
+def _probs(t: torch.Tensor, what: str) -> bytes:
+    """A kvc_probs over float32 [rows, n] with contiguous entries."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.dim() != 2:
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: float32 [rows, n] expected")
+    (rows, n), (s_row, s_at) = t.shape, t.stride()
+    if (n > 1 and s_at != 1) or (rows > 1 and s_row < n):
+        raise KvcError(KVC_E_UNSUPPORTED, f"{what}: contiguous entries and no broadcast rows expected")
+    return _PROBS.pack(t.data_ptr(), rows, n, s_row if rows > 1 else 0)
+
+
+def _kept_lists(req: Requests, kept: torch.Tensor, what: str, *ones):
+    """The lists a request each: kept [n, max_q or more], the others [n]."""
+    at = _list(kept, f"{what}: kept")
+    if kept.dim() != 2 or kept.shape[0] != req.n or kept.shape[1] < req.max_q or any(t is not None and tuple(t.shape) != (req.n,) for t in ones):
+        raise KvcError(KVC_E_SHAPE, f"{what}: kept [requests, max_q or more] and lists of {req.n} expected")
+    return at, int(kept.shape[1])
+
+
+def kvc_verify(req: Requests, parent: torch.Tensor, token: torch.Tensor, target: torch.Tensor, u: torch.Tensor, u_next: torch.Tensor,
+               kept: torch.Tensor, n_kept: torch.Tensor, next_token: torch.Tensor, draft: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Which drafted tokens stay (`kept` int32 [n, max_q], `n_kept` int32 [n]) and the token behind them (`next_token` int32
+    [n]), from the target's distributions float32 [rows, vocabulary], those the drafts were drawn from (None: they were
+    chosen) and uniform random numbers `u` [rows], `u_next` [n]."""
+    what = "kvc_verify"
+    at, pt, pd = _address(req, what), _probs(target, "target"), None if draft is None else _probs(draft, "draft")
+    a_kept, stride = _kept_lists(req, kept, what, n_kept, next_token, u_next)
+    rows = (target.shape[0],)
+    if parent.shape != rows or token.shape != rows or u.shape != rows:
+        raise KvcError(KVC_E_SHAPE, f"{what}: parent, token and u [rows] expected")
+    args = (_list(parent, "parent"), _list(token, "token"), pt, pd, _list(u, "u", torch.float32), _list(u_next, "u_next", torch.float32), a_kept, stride,
+            _list(n_kept, "n_kept"), _list(next_token, "next_token"))
+    st = _here(what, stream, (req._dev,), parent, token, target, draft, u, u_next, kept, n_kept, next_token)
+    _check(load().kvc_verify(at, *args, st), what)
+
+
+def kvc_keep(req: Requests, kept: torch.Tensor, n_kept: torch.Tensor, cache, kv_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The rows of the accepted drafts moved together in every layer of a Cache or QCache; `kv_out` int32 [n]: the lengths
+    behind the step."""
+    what = "kvc_keep"
+    at, c = _address(req, what), _desc(cache)
+    a_kept, stride = _kept_lists(req, kept, what, n_kept, kv_out)
+    a_n, a_out = _list(n_kept, "n_kept"), None if kv_out is None else _list(kv_out, "kv_out")
+    st = _here(what, stream, (c[1], req._dev), kept, n_kept, kv_out)
+    _holds(req, cache, what)
+    fn = load().kvc_keep if c[3] is None else load().kvc_keep_q8
+    _check(fn(at, a_kept, stride, a_n, c[0], a_out, st), what)
 
 
 def kvc_status_poll() -> int:

@@ -57,6 +57,8 @@ struct AttendLaunch {
   float scale;
   uint32_t* status;
   float* part;                 // workspace
+  const uint32_t* mask;        // trees of drafted tokens: [n_rows, words], else nullptr (causal is set with it)
+  int32_t words;
 };
 
 // Request b's packed rows and cache length; false (and the flag) when its numbers break the bounds the launch was sized by.
@@ -84,6 +86,22 @@ __device__ __forceinline__ int request_page(const DevRequests& r, const DevCache
 }
 // whether a cache is paged (the table itself may come from the requests)
 __host__ __device__ __forceinline__ bool is_paged(const DevCache& c) { return c.n_phys > 0; }
+
+// element offset of row (l, h, t)
+__device__ __forceinline__ int64_t row_off(const DevCache& c, int l, int h, int t, int page) {
+  const int64_t o = (int64_t)l * c.s_layer + (int64_t)h * c.s_head;
+  return is_paged(c) ? o + (int64_t)page * c.s_page + (int64_t)(t & c.page_mask) * c.s_tok : o + (int64_t)t * c.s_tok;
+}
+__device__ __forceinline__ int64_t exp_off(const DevScale& e, const DevCache& c, int l, int h, int t, int page) {
+  const int64_t o = (int64_t)l * e.s_layer + (int64_t)h * e.s_head;
+  return is_paged(c) ? o + (int64_t)page * e.s_page + (int64_t)(t & c.page_mask) * e.s_tok : o + (int64_t)t * e.s_tok;
+}
+
+// 32 bits of a row's mask over the request's new tokens, from new token `rel` on; tokens of the context (rel < 0) are seen.
+// `row`: the row's words, nullptr: nothing seen.
+__device__ __forceinline__ uint32_t seen_word(const uint32_t* row, int words, int i) {
+  return row == nullptr ? 0u : i < 0 ? 0xffffffffu : i < words ? __ldg(row + i) : 0u;
+}
 
 // ---- e4m3 rows under a power-of-two scale
 // Exponent byte of a row from its largest finite magnitude: the smallest b with amax <= 448 * 2^(b - 127), at least 0.

@@ -1,155 +1,14 @@
-// C ABI of kvc_append, kvc_attend, kvc_quantize and kvc_dequantize: argument checks, descriptor resolution, dispatch.
+// C ABI of kvc_append, kvc_attend, kvc_attend_tree, kvc_quantize and kvc_dequantize: argument checks, descriptor resolution, dispatch.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <string.h>
 
-#include "kvc_attend.h"
+#include "kvc_attend_args.h"
 #include "kvc_launch.h"
 #include "kvc_tc.h"
 
 namespace kvc {
 namespace {
-
-struct Extent {
-  uintptr_t lo, hi;
-};
-Extent extent_of(const void* p, int64_t last_elem, int elem) {
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  return {lo, lo + (uintptr_t)last_elem * elem};
-}
-bool overlap(const Extent& a, const Extent& b) { return a.lo < b.hi && b.lo < a.hi; }
-
-// elements a cache's K (or V) buffer reaches
-int64_t cache_reach(const kvc_cache* c, const DevCache& d) {
-  int64_t last = (int64_t)(c->L - 1) * d.s_layer + (int64_t)(c->H - 1) * d.s_head + c->d;
-  last += is_paged(d) ? (int64_t)(c->n_phys_pages - 1) * d.s_page + (int64_t)(c->page_size - 1) * d.s_tok
-                      : (int64_t)(c->T > 0 ? c->T - 1 : 0) * d.s_tok;
-  return last;
-}
-
-// The runs of bytes a cache's codes or exponents take: one of `width` bytes for every (layer, page, head, token).
-struct Runs {
-  uintptr_t at;
-  int64_t n[4], s[4], width;       // counts, distances in bytes
-  Extent all() const {
-    int64_t last = width;
-    for (int i = 0; i < 4; ++i) {
-      if (n[i] <= 0) return {at, at};
-      last += (n[i] - 1) * s[i];
-    }
-    return {at, at + (uintptr_t)last};
-  }
-};
-Runs runs_of(const void* p, const kvc_cache& c, int64_t s_layer, int64_t s_page, int64_t s_head, int64_t s_tok, int64_t width) {
-  const bool paged = c.layout == KVC_PAGED;
-  return {reinterpret_cast<uintptr_t>(p), {c.L, paged ? c.n_phys_pages : 1, c.H, paged ? c.page_size : c.T}, {s_layer, paged ? s_page : 0, s_head, s_tok}, width};
-}
-Runs exponent_runs(const uint8_t* p, const kvc_cache& c, const DevScale& e) { return runs_of(p, c, e.s_layer, e.s_page, e.s_head, e.s_tok, 1); }
-Runs code_runs(const void* p, const kvc_cache& c, const DevCache& d) { return runs_of(p, c, d.s_layer, d.s_page, d.s_head, d.s_tok, c.d); }
-
-// Whether two sets of runs share a byte.  Sets with the same distances may lie inside one another (keys' and values'
-// exponents side by side, exponents behind their row of codes): there the question is whether the distance of their
-// beginnings is a whole number of steps, level by level, give or take a run; otherwise overlapping extents decide.
-bool meet(const Runs& a, const Runs& b) {
-  if (!overlap(a.all(), b.all())) return false;
-  int order[4] = {0, 1, 2, 3}, live = 0;
-  for (int i = 0; i < 4; ++i) {
-    if (a.n[i] != b.n[i] || (a.n[i] > 1 && a.s[i] != b.s[i])) return true;
-    if (a.n[i] > 1) order[live++] = i;
-  }
-  for (int i = 1; i < live; ++i)                                  // smallest distance first
-    for (int j = i; j > 0 && a.s[order[j]] < a.s[order[j - 1]]; --j) {
-      const int t = order[j];
-      order[j] = order[j - 1];
-      order[j - 1] = t;
-    }
-  int64_t reach[5] = {a.width > b.width ? a.width : b.width};    // of the levels below
-  for (int i = 0; i < live; ++i) {
-    const int64_t s = a.s[order[i]];
-    if (s < reach[i]) return true;                                // levels that are not inside one another
-    reach[i + 1] = reach[i] + (a.n[order[i]] - 1) * s;
-  }
-  struct Search {
-    const int64_t *n, *s, *reach;
-    const int* order;
-    int64_t wa, wb;
-    bool at(int level, int64_t delta) const {                     // delta: b's position less a's
-      if (level == 0) return delta < wa && -delta < wb;
-      const int i = order[level - 1];
-      const int64_t q = delta / s[i];
-      for (int64_t t = q - 1; t <= q + 1; ++t)
-        if (t > -n[i] && t < n[i] && delta - t * s[i] < reach[level - 1] && t * s[i] - delta < reach[level - 1] && at(level - 1, delta - t * s[i])) return true;
-      return false;
-    }
-  };
-  return Search{a.n, a.s, reach, order, a.width, b.width}.at(live, (int64_t)(b.at - a.at));
-}
-// An 8-bit cache that is written: exponents apart from one another and from the codes.
-bool exponents_apart(const kvc_qcache* q, const DevCache& c, const DevScale& e) {
-  const Runs ek = exponent_runs(e.k, q->codes, e), ev = exponent_runs(e.v, q->codes, e);
-  const Runs ck = code_runs(q->codes.k, q->codes, c), cv = code_runs(q->codes.v, q->codes, c);
-  return !(meet(ek, ev) || meet(ek, ck) || meet(ek, cv) || meet(ev, ck) || meet(ev, cv));
-}
-
-int resolve_qcache(const kvc_qcache* q, DevCache* c, DevScale* e) {
-  if (!q) return KVC_E_INVALID_ARG;
-  const int rc = resolve_cache(&q->codes, c);
-  if (rc != KVC_OK) return rc;
-  if (!q->scale_k || !q->scale_v) return KVC_E_INVALID_ARG;
-  if (q->e_layer < 0 || q->e_page < 0 || q->e_head < 0 || q->e_tok < 0) return KVC_E_INVALID_ARG;
-  if ((c->s_tok | c->s_head | c->s_layer | c->s_page) & 15) return KVC_E_UNSUPPORTED;   // 16-byte rows of codes
-  const kvc_cache& g = q->codes;
-  e->k = q->scale_k;
-  e->v = q->scale_v;
-  e->s_tok = q->e_tok ? q->e_tok : 1;
-  if (g.layout == KVC_CONTIG) {
-    e->s_head = q->e_head ? q->e_head : (int64_t)g.T * e->s_tok;
-    e->s_layer = q->e_layer ? q->e_layer : (int64_t)g.H * e->s_head;
-    e->s_page = 0;
-  } else {
-    e->s_head = q->e_head ? q->e_head : (int64_t)g.page_size * e->s_tok;
-    e->s_page = q->e_page ? q->e_page : (int64_t)g.H * e->s_head;
-    e->s_layer = q->e_layer ? q->e_layer : (int64_t)g.n_phys_pages * e->s_page;
-  }
-  return KVC_OK;
-}
-
-// Positions are 32-bit integers, and the kernels step up to two tiles past the last one.
-constexpr int32_t kMaxTokens = 0x7fffffff - 256;
-
-int resolve_requests(const kvc_requests* r, const kvc_cache* c, int n_rows, DevRequests* out) {
-  if (!r || r->n < 0 || r->max_q < 0 || r->max_kv < 0 || r->table_stride < 0 || n_rows < 0) return KVC_E_INVALID_ARG;
-  if (r->n > 0 && (!r->q_begin || !r->kv_len)) return KVC_E_INVALID_ARG;
-  int64_t cap = c->T;
-  if (r->page_table) {
-    if (c->layout != KVC_PAGED) return KVC_E_INVALID_ARG;
-    cap = (int64_t)r->table_stride * c->page_size;
-  } else if (c->layout == KVC_PAGED && !c->page_table && r->max_kv > 0) {
-    return KVC_E_INVALID_ARG;
-  }
-  if (r->max_kv > cap) return KVC_E_SHAPE;
-  if (r->max_kv > kMaxTokens) return KVC_E_UNSUPPORTED;
-  out->q_begin = r->q_begin;
-  out->kv_len = r->kv_len;
-  out->table = r->page_table;
-  out->table_stride = r->table_stride;
-  out->n = r->n;
-  out->max_q = r->max_q;
-  out->max_kv = r->max_kv;
-  out->n_rows = n_rows;
-  return KVC_OK;
-}
-
-int resolve_heads(const kvc_heads* h, int d, DevHeads* out, Extent* ext) {
-  if (!h || h->n_rows < 0 || h->n_heads <= 0 || h->s_row < 0 || h->s_head < 0) return KVC_E_INVALID_ARG;
-  if (!h->data && h->n_rows > 0) return KVC_E_INVALID_ARG;
-  out->p = reinterpret_cast<__nv_bfloat16*>(h->data);
-  out->s_head = h->s_head ? h->s_head : d;
-  out->s_row = h->s_row ? h->s_row : (int64_t)h->n_heads * out->s_head;
-  if (((out->s_head | out->s_row) & 7) || (reinterpret_cast<uintptr_t>(h->data) & 15)) return KVC_E_UNSUPPORTED;
-  *ext = extent_of(h->data, h->n_rows > 0 ? (int64_t)(h->n_rows - 1) * out->s_row + (int64_t)(h->n_heads - 1) * out->s_head + d : 0, 2);
-  return KVC_OK;
-}
 
 int append_common(const kvc_requests* req, const kvc_heads* kn, const kvc_heads* vn, int32_t layer, const kvc_cache* geo, AppendLaunch& a,
                   const kvc_qcache* q8, void* stream) {
@@ -204,7 +63,8 @@ int convert_common(const kvc_cache* bf, const kvc_qcache* q8, int to8, void* str
 }
 
 int attend_common(const kvc_requests* req, const kvc_heads* q, const kvc_cache* geo, int32_t layer, double scale, int32_t causal,
-                  kvc_heads* out, float* lse, void* workspace, size_t workspace_bytes, AttendLaunch& a, int elem, void* stream) {
+                  kvc_heads* out, float* lse, void* workspace, size_t workspace_bytes, AttendLaunch& a, int elem, void* stream,
+                  const kvc_tree* tree = nullptr) {
   int rc;
   Extent eq, eo;
   if (layer < 0 || layer >= geo->L || !(scale > 0.0) || !isfinite(scale) || !((float)scale > 0.f) || !isfinite((float)scale)) return KVC_E_INVALID_ARG;
@@ -213,6 +73,9 @@ int attend_common(const kvc_requests* req, const kvc_heads* q, const kvc_cache* 
   if (q->n_heads / geo->H > 64 || geo->H > 65535) return KVC_E_UNSUPPORTED;
   if ((rc = resolve_requests(req, geo, q->n_rows, &a.req)) != KVC_OK) return rc;
   if (reinterpret_cast<uintptr_t>(lse) & 3) return KVC_E_UNSUPPORTED;
+  if (tree && (rc = check_tree(tree, req)) != KVC_OK) return rc;
+  if (tree && tree->n_rows != q->n_rows) return KVC_E_SHAPE;
+  if (tree && tree->n_rows > 0 && !tree->mask) return KVC_E_INVALID_ARG;
   if ((int64_t)req->max_q * (q->n_heads / geo->H) >= (int64_t)1 << 30) return KVC_E_UNSUPPORTED;
   const int64_t reach = cache_reach(geo, a.c);
   const Extent ck = extent_of(geo->k, reach, elem), cv = extent_of(geo->v, reach, elem);
@@ -224,7 +87,8 @@ int attend_common(const kvc_requests* req, const kvc_heads* q, const kvc_cache* 
   const Extent reads[] = {eq, ck, cv, q8 ? exponent_runs(a.e.k, *geo, a.e).all() : none, q8 ? exponent_runs(a.e.v, *geo, a.e).all() : none,
                           extent_of(req->q_begin, req->n > 0 ? (int64_t)req->n + 1 : 0, 4), extent_of(req->kv_len, req->n, 4),
                           req->page_table && req->n > 0 ? extent_of(req->page_table, (int64_t)(req->n - 1) * req->table_stride + pages, 4)
-                                                        : extent_of(geo->page_table, geo->page_table ? pages : 0, 4)};
+                                                        : extent_of(geo->page_table, geo->page_table ? pages : 0, 4),
+                          tree ? extent_of(tree->mask, (int64_t)tree->n_rows * tree->words, 4) : none};
   auto reads_meet = [&](const Extent& w) {
     for (const Extent& r : reads)
       if (overlap(w, r)) return true;
@@ -243,6 +107,8 @@ int attend_common(const kvc_requests* req, const kvc_heads* q, const kvc_cache* 
   a.scale = (float)scale;
   a.lse = lse;
   a.part = reinterpret_cast<float*>(workspace);
+  a.mask = tree ? tree->mask : nullptr;
+  a.words = tree ? tree->words : 0;
   if (!(a.status = status_word_ptr())) return KVC_E_CUDA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (path_force() != KVC_PATH_GENERIC) {
@@ -299,6 +165,24 @@ int kvc_attend_q8(const kvc_requests* req, const kvc_heads* q, const kvc_qcache*
   memset(&a, 0, sizeof(a));
   const int rc = resolve_qcache(cache, &a.c, &a.e);
   return rc != KVC_OK ? rc : attend_common(req, q, &cache->codes, layer, scale, causal, out, lse, workspace, workspace_bytes, a, 1, stream);
+}
+
+int kvc_attend_tree(const kvc_requests* req, const kvc_tree* tree, const kvc_heads* q, const kvc_cache* cache, int32_t layer, double scale,
+                    kvc_heads* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  AttendLaunch a;
+  memset(&a, 0, sizeof(a));
+  if (!tree) return KVC_E_INVALID_ARG;
+  const int rc = resolve_cache(cache, &a.c);
+  return rc != KVC_OK ? rc : attend_common(req, q, cache, layer, scale, 1, out, lse, workspace, workspace_bytes, a, 2, stream, tree);
+}
+
+int kvc_attend_tree_q8(const kvc_requests* req, const kvc_tree* tree, const kvc_heads* q, const kvc_qcache* cache, int32_t layer, double scale,
+                       kvc_heads* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  AttendLaunch a;
+  memset(&a, 0, sizeof(a));
+  if (!tree) return KVC_E_INVALID_ARG;
+  const int rc = resolve_qcache(cache, &a.c, &a.e);
+  return rc != KVC_OK ? rc : attend_common(req, q, &cache->codes, layer, scale, 1, out, lse, workspace, workspace_bytes, a, 1, stream, tree);
 }
 
 }  // extern "C"

@@ -90,7 +90,10 @@ __global__ void __launch_bounds__(128) attend_generic_kernel(const __grid_consta
           float s = 0.f;
 #pragma unroll 8
           for (int c = 0; c < D; ++c) s = fmaf(qs[warp * 4 + k][c], ks[lane][c], s);
-          s = t0 + lane <= lim[k] ? s * p.scale : minus_inf;
+          const int t = t0 + lane, fresh = t - (kv - nq);          // place among the new tokens
+          bool sees = t <= lim[k];
+          if (p.mask && fresh >= 0 && sees) sees = (p.mask[(int64_t)(q0 + (rb + warp * 4 + k) / p.G) * p.words + (fresh >> 5)] >> (fresh & 31)) & 1u;
+          s = sees ? s * p.scale : minus_inf;
           float mx = s;
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -107,6 +110,7 @@ __global__ void __launch_bounds__(128) attend_generic_kernel(const __grid_consta
           const int n = min(kKeys, lim[k] - t0 + 1);       // a hidden key's value is not touched, whatever it holds
           for (int j = 0; j < n; ++j) {
             const float w = __shfl_sync(0xffffffffu, e, j);
+            if (p.mask && w == 0.f) continue;              // nor one that a tree's mask hides
 #pragma unroll
             for (int c = 0; c < C; ++c) acc[k][c] = fmaf(w, vs[j][c * 32 + lane], acc[k][c]);
           }

@@ -76,15 +76,6 @@ __device__ __forceinline__ void decode16(const uint4& c, uint32_t b, uint4& lo, 
   hi = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
-// element offset of row (l, h, t); -1 when the table names no page
-__device__ __forceinline__ int64_t row_off(const DevCache& c, int l, int h, int t, int page) {
-  const int64_t o = (int64_t)l * c.s_layer + (int64_t)h * c.s_head;
-  return is_paged(c) ? o + (int64_t)page * c.s_page + (int64_t)(t & c.page_mask) * c.s_tok : o + (int64_t)t * c.s_tok;
-}
-__device__ __forceinline__ int64_t exp_off(const DevScale& e, const DevCache& c, int l, int h, int t, int page) {
-  const int64_t o = (int64_t)l * e.s_layer + (int64_t)h * e.s_head;
-  return is_paged(c) ? o + (int64_t)page * e.s_page + (int64_t)(t & c.page_mask) * e.s_tok : o + (int64_t)t * e.s_tok;
-}
 __device__ __forceinline__ int own_page(const DevCache& c, int t, uint32_t* status) {
   if (!is_paged(c)) return 0;
   const int p = c.page_table[t >> c.page_shift];

@@ -282,7 +282,8 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return d;
 }
 
-template <int D, bool Q8>
+// kTree: the new tokens of a request form a tree; a row sees the context and those new tokens whose bits are set in its mask.
+template <int D, bool Q8, bool kTree>
 __global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1)
 attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using SH = Shape<D, Q8>;
@@ -386,15 +387,31 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       const Piece& y = bars.piece[piece % kPieces];
       const int n = y.n[t], kv = y.kv, first = y.t0 * 128;
       int lim = -1;
+      const uint32_t* mask = nullptr;                             // kTree: the row's words
+      const int fresh = kv - y.nq;                                // first new token
       {
         const int r = y.u * kUnitRows + t * 128 + row;
-        if (r < y.rows) lim = p.a.causal ? kv - y.nq + r / p.a.G : kv - 1;
+        if (r < y.rows) {
+          lim = p.a.causal ? kv - y.nq + r / p.a.G : kv - 1;
+          if (kTree) mask = p.a.mask + (int64_t)(y.q0 + r / p.a.G) * p.a.words;
+        }
       }
       const int lowest = __reduce_min_sync(0xffffffffu, lim);     // of the warp's rows
       float m = minus_inf, l = 0.f;
       float late = minus_inf;                                     // a maximum that m is to follow
       for (int it = 0; it < n; ++it) {
         const uint32_t par = (uint32_t)(count + it) & 1u;
+        uint32_t sees[4];                                         // kTree: bits of the tile's keys, fetched while the product runs
+        if (kTree && first + it * 128 + 127 >= fresh) {
+          const int rel = first + it * 128 - fresh;
+          uint32_t lo = seen_word(mask, p.a.words, rel >> 5);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t hi = seen_word(mask, p.a.words, (rel >> 5) + w + 1);
+            sees[w] = __funnelshift_r(lo, hi, rel & 31);
+            lo = hi;
+          }
+        }
         if (!wait(s_full + 8 * t, par)) break;
         tc_fence_after();
         float s[128];
@@ -405,6 +422,10 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         if (lowest < t0 + 127) {
 #pragma unroll
           for (int k = 0; k < 128; ++k) s[k] = t0 + k <= lim ? s[k] : minus_inf;
+        }
+        if (kTree && t0 + 127 >= fresh) {
+#pragma unroll
+          for (int k = 0; k < 128; ++k) s[k] = (sees[k >> 5] >> (k & 31)) & 1u ? s[k] : minus_inf;
         }
         const f32x2 c2 = f2_pack(c, c);
         f32x2 mc2, sum2[2];
@@ -931,17 +952,17 @@ int64_t chunk_blocks(int n, int max_q, int max_kv, int G, int H) {
 }
 size_t chunk_starts_bytes(int64_t blocks) { return ((size_t)blocks * sizeof(UnitStart) + 255) / 256 * 256; }
 
-template <int D, bool Q8>
+template <int D, bool Q8, bool kTree>
 cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
   using SH = Shape<D, Q8>;
   static DeviceOnce once;
   int dev;
   if (once.pending(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(attend_chunk_kernel<D, Q8>, cudaFuncAttributeMaxDynamicSharedMemorySize, SH::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(attend_chunk_kernel<D, Q8, kTree>, cudaFuncAttributeMaxDynamicSharedMemorySize, SH::kSmem);
     if (e != cudaSuccess) return e;
     once.mark(dev);
   }
-  const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
+  const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8, kTree>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
   if (e != cudaSuccess || p.blocks < 2) return e;
   if (p.fine) return launch_after(attend_chunk_join_kernel<D, 4>, dim3((unsigned)chunk_units(p.a.req.n, p.a.req.max_q, p.a.G, p.a.H), 8 * (D / 32)), 256, 0, s, p);
   return launch_after(attend_chunk_join_kernel<D, D / 8>, dim3((unsigned)p.blocks - 1, 8), 256, 0, s, p);
@@ -1012,10 +1033,12 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   p.ml = reinterpret_cast<float*>(ws + chunk_starts_bytes(p.blocks));
   p.part = p.ml + (int64_t)p.blocks * 2 * kUnitRows * 2;
   cudaError_t e;
-  if (d == 128)
-    e = q8 ? launch_chunk<128, true>(p, mk, mv, s) : launch_chunk<128, false>(p, mk, mv, s);
-  else
-    e = q8 ? launch_chunk<64, true>(p, mk, mv, s) : launch_chunk<64, false>(p, mk, mv, s);
+#define KVC_CHUNK(D, Q, T) \
+  if (d == D && q8 == Q && (a.mask != nullptr) == T) e = launch_chunk<D, Q, T>(p, mk, mv, s);
+  e = cudaErrorInvalidValue;
+  KVC_CHUNK(128, false, false) KVC_CHUNK(128, true, false) KVC_CHUNK(64, false, false) KVC_CHUNK(64, true, false)
+  KVC_CHUNK(128, false, true) KVC_CHUNK(128, true, true) KVC_CHUNK(64, false, true) KVC_CHUNK(64, true, true)
+#undef KVC_CHUNK
   return e == cudaSuccess ? KVC_OK : KVC_E_CUDA;
 }
 

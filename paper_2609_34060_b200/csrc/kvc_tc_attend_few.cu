@@ -281,7 +281,9 @@ static_assert(sizeof(FewBars<Few<128, true, 8>>) + Few<128, true, 8>::kSmem <= 2
 static_assert(sizeof(FewBars<Few<128, true, 16>>) + Few<128, true, 16>::kSmem <= 232448, "shared memory");
 static_assert(sizeof(FewBars<Few<128, true, 32>>) + Few<128, true, 32>::kSmem <= 232448, "shared memory");
 
-template <int D, bool Q8, int RC>
+// kTree: a request's new tokens (at most RC, so that a row's mask is one word) form a tree; a row sees the context and those
+// new tokens whose bits are set in its mask.
+template <int D, bool Q8, int RC, bool kTree>
 __global__ void __launch_bounds__(Few<D, Q8, RC>::kThreads, 1)
 attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using F = Few<D, Q8, RC>;
@@ -357,6 +359,8 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
       const int R = x.nq * p.a.G;
       const uint32_t o_at = lane_at + F::kOCol + ((piece & 1) * 2 + wg) * F::kPCols;
       float m[RC], l[RC];
+      uint32_t mask_lane = 0;                                       // kTree: mask of row `lane`
+      if (kTree && lane < R) mask_lane = __ldg(p.a.mask + (int64_t)(x.q0 + lane / p.a.G) * p.a.words);
       float z_lane = minus_inf;                                     // 8-bit values: Z - 6 of row `lane`, under which its sums are held
 #pragma unroll
       for (int r = 0; r < RC; ++r) {
@@ -399,6 +403,14 @@ attend_few_kernel(const __grid_constant__ FewLaunch p, const __grid_constant__ C
 #pragma unroll
           for (int r = 0; r < RC; ++r)
             if (tok > lim + (p.a.causal ? r / p.a.G : 0) || r >= R) s[r] = minus_inf;
+          if (kTree) {
+            const int fresh = tok - lim;                            // the key's place among the new tokens
+#pragma unroll
+            for (int r = 0; r < RC; ++r) {
+              const uint32_t mask = __shfl_sync(0xffffffffu, mask_lane, r);
+              if (fresh >= 0 && !((mask >> (fresh & 31)) & 1u)) s[r] = minus_inf;
+            }
+          }
         }
         bool grow = false;
 #pragma unroll
@@ -947,17 +959,17 @@ __global__ void __launch_bounds__(4 * D) attend_few_join_kernel(const __grid_con
   if (p.a.lse && ch == 0) p.a.lse[row * (p.a.H * p.a.G) + head] = dead ? minus_inf : (s_m[rr] + log2f(l)) * kLn2;
 }
 
-template <int D, bool Q8, int RC>
+template <int D, bool Q8, int RC, bool kTree>
 cudaError_t launch(const FewLaunch& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
   using F = Few<D, Q8, RC>;
   static DeviceOnce once;
   int dev;
   if (once.pending(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(attend_few_kernel<D, Q8, RC>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(attend_few_kernel<D, Q8, RC, kTree>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem);
     if (e != cudaSuccess) return e;
     once.mark(dev);
   }
-  const cudaError_t e = launch_after(attend_few_kernel<D, Q8, RC>, dim3((unsigned)p.blocks), F::kThreads, F::kSmem, s, p, mk, mv);
+  const cudaError_t e = launch_after(attend_few_kernel<D, Q8, RC, kTree>, dim3((unsigned)p.blocks), F::kThreads, F::kSmem, s, p, mk, mv);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)p.a.req.max_q * p.a.G;
   const dim3 g((unsigned)((int64_t)p.a.req.n * p.a.H), (unsigned)(((rows < RC ? rows : RC) + 3) / 4));
@@ -987,7 +999,7 @@ cudaError_t launch_attend_few(const AttendLaunch& a, const tc::TileGeo& g, const
   const bool q8 = a.e.k != nullptr;
   if (p.blocks <= 0) return cudaErrorInvalidConfiguration;
 #define KVC_FEW(D, Q, R) \
-  if (d == D && q8 == Q && rc == R) return launch<D, Q, R>(p, mk, mv, s);
+  if (d == D && q8 == Q && rc == R) return a.mask ? launch<D, Q, R, true>(p, mk, mv, s) : launch<D, Q, R, false>(p, mk, mv, s);
   KVC_FEW(128, false, 8) KVC_FEW(64, false, 8) KVC_FEW(128, false, 16) KVC_FEW(128, false, 32) KVC_FEW(64, false, 16) KVC_FEW(64, false, 32)
   KVC_FEW(128, true, 8) KVC_FEW(128, true, 16) KVC_FEW(128, true, 32) KVC_FEW(64, true, 8) KVC_FEW(64, true, 16) KVC_FEW(64, true, 32)
 #undef KVC_FEW

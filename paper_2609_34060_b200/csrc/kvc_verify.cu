@@ -1,0 +1,358 @@
+// kvc_verify: which drafted tokens stay, and the next token, by rejection sampling from given random numbers.
+//
+// With P the distribution at the current node (the target's at first) and q the one its children were drawn from, child c
+// with token x stays where u q(x) < P(x); otherwise P <- max(P - q, 0) / Z.  After any number of rejections
+//     P = max(A p - B q, 0) ,   A = B = 1 and divided by Z, B one more at each ( max(max(a, 0) / Z - q, 0) = max(a / Z - q, 0) ) ,
+// so nothing of a distribution is stored: a sum or a draw is one pass over p and q.  A rejection alone needs no pass; a
+// further sibling needs Z, and the draw at the end one pass more for the sum (its last part is read twice, from L2).
+//
+// Bound: the bytes of the distributions that are passed over (V values each), and for few requests the chain lists -> gathers
+// -> pass -> draw.  The gathers of all rows, p and q at their tokens, are made at once before the walk.
+//
+// A cluster of blocks shares a request.  Every block walks the tree by itself (all of them come to the same decisions from
+// the same numbers), sums its part of the vocabulary, and the parts' sums meet in distributed shared memory.  Blocks, warps
+// and lanes hold ascending parts, so the draw finds its place from prefix sums: block, warp, 128 entries, lane, entry.
+// Sums are float64, in a fixed order.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+
+#include "kvc_draft.h"
+#include "kvc_launch.h"
+#include "kvc_tc_attend.cuh"
+
+namespace kvc {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 512, kWarps = kThreads / 32, kCluster = 8;
+constexpr int kStep = 128;                 // entries a warp takes at a time
+
+// P(x) from the node's two distributions; NaN and negative entries count as 0
+__device__ __forceinline__ double residual(float p, float q, double A, double B) { return fmax((double)p * A - (double)q * B, 0.0); }
+
+struct Node {                              // where the walk is
+  int node, asked, gone;                   // the node's row, the row tried last, rejected tokens (drafts chosen)
+  bool spent;                              // no residual left: no further child, the draw is from p itself
+  bool normal;                             // A and B hold the last rejection's division
+  double A, B, left;
+};
+
+template <bool kDraft, bool kWide>
+__global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant__ VerifyLaunch p) {
+  __shared__ float s_p[KVC_TREE_MAX_Q], s_q[KVC_TREE_MAX_Q], s_u[KVC_TREE_MAX_Q];
+  __shared__ int s_token[KVC_TREE_MAX_Q], s_gone[KVC_TREE_MAX_Q];
+  __shared__ int16_t s_parent[KVC_TREE_MAX_Q], s_path[KVC_TREE_MAX_Q];
+  __shared__ double s_warp[kWarps], s_block[2][kCluster];
+  __shared__ Node s_at;
+  __shared__ int s_more, s_kept;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int b = (int)(blockIdx.x / blocks);
+  tc::grid_dependency_wait();
+  tc::grid_dependents_launch();
+  const float u_next = p.u_next[b];
+  int q0, nq, kv;
+  request_span(p.req, b, tid == 0 && rank == 0 ? p.status : nullptr, q0, nq, kv);
+  if (nq == 0) {
+    if (rank == 0) {
+      for (int j = tid; j < p.req.max_q; j += kThreads) p.kept[(int64_t)b * p.stride + j] = -1;
+      if (tid == 0) {
+        p.n_kept[b] = 0;
+        p.next[b] = -1;
+      }
+    }
+    return;                                // the same for the whole cluster
+  }
+  // what the walk may ask for
+  for (int j = tid; j < nq; j += kThreads) {
+    int a = j == 0 ? -1 : p.parent[q0 + j];
+    const int x = j == 0 ? 0 : p.token[q0 + j];
+    s_u[j] = j == 0 ? 0.f : p.u[q0 + j];
+    const bool known = (unsigned)x < (unsigned)p.vocab;
+    if (a < -1 || a >= j || !known) {
+      if (rank == 0) atomicOr(p.status, KVC_FLAG_BAD_TREE);
+      a = -1;
+    }
+    s_parent[j] = (int16_t)a;
+    s_token[j] = x;
+    s_p[j] = a >= 0 ? p.target[(int64_t)(q0 + a) * p.s_target + x] : 0.f;
+    if (kDraft) s_q[j] = a >= 0 ? p.draft[(int64_t)(q0 + a) * p.s_draft + x] : 0.f;
+  }
+  if (tid == 0) {
+    s_at = Node{0, 0, 0, false, true, 1.0, 0.0, 1.0};
+    s_path[0] = 0;
+    s_kept = 1;
+  }
+  cluster.sync();                          // every block of the cluster runs: its shared memory may be written
+
+  // the vocabulary: blocks, warps, steps of 128 entries
+  const int64_t per_block = (((int64_t)p.vocab + blocks - 1) / blocks + kStep - 1) / kStep * kStep;
+  const int64_t lo_block = per_block * rank, hi_block = min((int64_t)p.vocab, lo_block + per_block);
+  const int per_warp = (int)((per_block + kWarps * kStep - 1) / (kWarps * kStep) * kStep);
+  auto warp_range = [&](int w, int64_t& lo, int64_t& hi) {
+    lo = lo_block + (int64_t)w * per_warp;
+    hi = min(hi_block, lo + per_warp);
+  };
+  // four entries of P from `at` on (at a multiple of 4; behind hi: 0)
+  struct Four {
+    float p[4], q[4];
+  };
+  auto fetch = [&](const float* pt, const float* pd, int64_t at, int64_t hi, Four& x) {
+    if (kWide && at + 4 <= hi) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(pt + at));
+      x.p[0] = v.x, x.p[1] = v.y, x.p[2] = v.z, x.p[3] = v.w;
+      if (kDraft) {
+        const float4 w = __ldg(reinterpret_cast<const float4*>(pd + at));
+        x.q[0] = w.x, x.q[1] = w.y, x.q[2] = w.z, x.q[3] = w.w;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x.p[k] = at + k < hi ? __ldg(pt + at + k) : 0.f;
+        if (kDraft) x.q[k] = at + k < hi ? __ldg(pd + at + k) : 0.f;
+      }
+    }
+  };
+  auto value = [&](const Four& x, int k, int64_t at, double A, double B, int gone) {
+    if (!kDraft) {
+      for (int g = 0; g < gone; ++g)
+        if (s_gone[g] == at + k) return 0.0;
+    }
+    return residual(x.p[k], kDraft ? x.q[k] : 0.f, A, B);
+  };
+  int passes = 0;
+  // sum of P over the vocabulary, the same in all threads of the cluster
+  auto sum_all = [&](int node, double A, double B, int gone) {
+    const float* pt = p.target + (int64_t)(q0 + node) * p.s_target;
+    const float* pd = kDraft ? p.draft + (int64_t)(q0 + node) * p.s_draft : nullptr;
+    int64_t lo, hi;
+    warp_range(warp, lo, hi);
+    double sum = 0.0;
+    constexpr int kAhead = 4;              // loads in flight
+    for (int64_t at = lo + lane * 4; at < hi; at += kAhead * kStep) {
+      Four x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) fetch(pt, pd, at + i * kStep, hi, x[i]);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        double s = 0.0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s += value(x[i], k, at + i * kStep, A, B, gone);
+        sum += s;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    __syncthreads();                       // s_warp of the pass before has been read
+    if (lane == 0) s_warp[warp] = sum;
+    __syncthreads();
+    double* mine = s_block[passes & 1];
+    ++passes;
+    if (tid < blocks) {
+      double all = 0.0;
+      for (int w = 0; w < kWarps; ++w) all += s_warp[w];
+      *cluster.map_shared_rank(mine + rank, tid) = all;
+    }
+    cluster.sync();                        // the parts lie in two buffers in turn: nobody writes one that is still read
+    double total = 0.0;
+    for (int c = 0; c < blocks; ++c) total += mine[c];
+    return total;
+  };
+
+  for (;;) {
+    if (warp == 0) {
+      Node n = s_at;
+      int kept = s_kept;
+      bool more = false;                   // a sibling waits for the sum
+      for (int c0 = n.asked + 1; c0 < nq && !n.spent;) {
+        const int c = c0 + lane;
+        const unsigned hit = __ballot_sync(0xffffffffu, c < nq && s_parent[c] == n.node);
+        if (!hit) {
+          c0 += 32;
+          continue;
+        }
+        const int child = c0 + __ffs(hit) - 1;
+        if (!n.normal) {
+          more = true;
+          break;
+        }
+        n.asked = child;
+        c0 = child + 1;
+        bool yes;
+        bool fresh = true;
+        const double px = (double)s_p[child];
+        if (kDraft) {
+          yes = (double)s_u[child] * (double)s_q[child] < residual(s_p[child], s_q[child], n.A, n.B);
+        } else {
+          for (int g = 0; g < n.gone; ++g) fresh = fresh && s_gone[g] != s_token[child];
+          yes = fresh && (double)s_u[child] * n.left < px;
+        }
+        if (yes) {
+          if (lane == 0) s_path[kept] = (int16_t)child;
+          ++kept;
+          n.node = child;
+          n.A = 1.0;
+          n.B = 0.0;
+          n.left = 1.0;
+          n.gone = 0;
+        } else if (kDraft) {
+          n.B += 1.0;
+          n.normal = false;
+        } else if (fresh) {
+          n.left -= fmax(px, 0.0);
+          __syncwarp();
+          if (lane == 0) s_gone[n.gone] = s_token[child];
+          __syncwarp();
+          ++n.gone;
+        }
+      }
+      if (lane == 0) {
+        s_at = n;
+        s_kept = kept;
+        s_more = more;
+      }
+    }
+    __syncthreads();
+    if (!s_more) break;
+    const Node n = s_at;
+    const double z = sum_all(n.node, n.A, n.B, n.gone);
+    __syncthreads();
+    if (tid == 0) {
+      const bool some = z > 0.0 && z < __longlong_as_double(0x7ff0000000000000ll);
+      s_at.spent = !some;
+      s_at.normal = true;
+      s_at.A = some ? n.A / z : 1.0;
+      s_at.B = some ? n.B / z : 0.0;
+    }
+    __syncthreads();
+  }
+
+  Node n = s_at;
+  const double infinite = __longlong_as_double(0x7ff0000000000000ll);
+  double total = sum_all(n.node, n.A, n.B, n.gone);
+  if (!(total > 0.0 && total < infinite) && (n.B != 0.0 || n.gone > 0)) {
+    n.A = 1.0;
+    n.B = 0.0;
+    n.gone = 0;
+    total = sum_all(n.node, n.A, n.B, n.gone);
+  }
+  if (rank == 0) {
+    const int kept = s_kept;
+    for (int j = tid; j < p.req.max_q; j += kThreads) p.kept[(int64_t)b * p.stride + j] = j < kept ? s_path[j] : -1;
+    if (tid == 0) p.n_kept[b] = kept;
+  }
+  if (!(total > 0.0 && total < infinite)) {
+    if (rank == 0 && tid == 0) {
+      p.next[b] = -1;
+      atomicOr(p.status, KVC_FLAG_BAD_PROB);
+    }
+    return;
+  }
+  // the draw: the first part whose end lies beyond the threshold; where rounding leaves none, the last that has anything
+  const double threshold = (double)u_next * total;
+  auto find = [&](const double* parts, int count, double& before) {
+    double run = before;
+    int last = -1;
+    double at_last = before;
+    for (int i = 0; i < count; ++i) {
+      if (parts[i] > 0.0) {
+        last = i;
+        at_last = run;
+      }
+      run += parts[i];
+      if (run > threshold && last == i) break;
+    }
+    before = at_last;
+    return last;
+  };
+  double before = 0.0;
+  const int block = find(s_block[(passes - 1) & 1], blocks, before);
+  if (block != rank) return;
+  const int in = find(s_warp, kWarps, before);
+  if (in != warp) return;
+  const float* pt = p.target + (int64_t)(q0 + n.node) * p.s_target;
+  const float* pd = kDraft ? p.draft + (int64_t)(q0 + n.node) * p.s_draft : nullptr;
+  int64_t lo, hi;
+  warp_range(warp, lo, hi);
+  int64_t found = -1;                      // lane's last positive entry so far
+  constexpr int kAhead = 4;
+  for (int64_t base = lo; base < hi; base += kAhead * kStep) {
+    Four x[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fetch(pt, pd, base + i * kStep + lane * 4, hi, x[i]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t at = base + i * kStep + lane * 4;
+      double v[4], own = 0.0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = value(x[i], k, at, n.A, n.B, n.gone);
+        own += v[k];
+      }
+      double incl = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const double t = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += t;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, own > 0.0 && before + incl > threshold);
+      if (hit) {
+        if (lane == __ffs(hit) - 1) {
+          double run = before + (incl - own);
+          int pick = 0;
+#pragma unroll
+          for (int k = 3; k >= 0; --k) pick = v[k] > 0.0 ? k : pick;   // the first positive one, at least
+          bool done = false;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            run += v[k];
+            if (!done && v[k] > 0.0) {
+              pick = k;
+              done = run > threshold;
+            }
+          }
+          p.next[b] = (int)(at + pick);
+        }
+        return;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (v[k] > 0.0) found = at + k;
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) found = max(found, __shfl_xor_sync(0xffffffffu, found, o));
+  if (lane == 0) p.next[b] = (int)found;
+}
+
+template <bool kDraft, bool kWide>
+cudaError_t launch(const VerifyLaunch& v, cudaStream_t s) {
+  const int blocks = v.vocab <= 4096 ? 1 : kCluster;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim = {(unsigned)blocks, 1, 1};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((int64_t)v.req.n * blocks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, verify_kernel<kDraft, kWide>, v);
+}
+
+}  // namespace
+
+cudaError_t launch_verify(const VerifyLaunch& v, cudaStream_t s) {
+  // 16-byte loads where every row begins on 16 bytes
+  const bool wide = ((reinterpret_cast<uintptr_t>(v.target) | (uintptr_t)(v.s_target * 4)) & 15) == 0 &&
+                    (!v.draft || ((reinterpret_cast<uintptr_t>(v.draft) | (uintptr_t)(v.s_draft * 4)) & 15) == 0);
+  if (v.draft) return wide ? launch<true, true>(v, s) : launch<true, false>(v, s);
+  return wide ? launch<false, true>(v, s) : launch<false, false>(v, s);
+}
+
+}  // namespace kvc
