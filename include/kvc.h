@@ -719,7 +719,9 @@ int kvc_append_rotated_q8(const kvc_requests *req, const kvc_rotary *rot, const 
  * kvc_attend_tree -- kvc_attend for trees: new token j of a request sees the keys t < kv_len - n_q and those new tokens
  * a <= j whose bits are set in its mask (bits beyond j are not looked at; the masks may be kvc_tree_build's or the caller's
  * own).  A row that sees nothing gets zeros and minus infinity.  parent and depth of the tree are not used.  Workspace,
- * rounding, limits and errors as in kvc_attend; max_q up to KVC_TREE_MAX_Q.
+ * rounding, limits and errors as in kvc_attend; max_q up to KVC_TREE_MAX_Q.  One thing differs: over an 8-bit cache, where
+ * max_q times query heads per KV head is 33 to 128, a query meets the codes as two e4m3 parts whose sum is off by at most
+ * 2^-17 of the query's largest channel in each of the others (exact in those above 2^-10 of it).
  */
 int kvc_attend_tree(const kvc_requests *req, const kvc_tree *tree, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale,
                     kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);

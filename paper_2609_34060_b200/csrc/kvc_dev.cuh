@@ -240,6 +240,7 @@ __device__ __forceinline__ f32x2 f2_sub(f32x2 a, f32x2 b) {
   asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+__device__ __forceinline__ void f2_scale(f32x2& v, float a) { v = f2_mul(v, f2_pack(a, a)); }
 // the two bf16 halves of a word as a pair of float32 (low half first)
 __device__ __forceinline__ f32x2 f2_from_bf16x2(uint32_t w) { return f2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 // pair -> bf16x2 word, round to nearest even (one packed conversion)

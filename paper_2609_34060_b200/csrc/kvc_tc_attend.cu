@@ -74,15 +74,21 @@ struct ChunkLaunch {
   float* part;                             // [blocks][2][256][d] their sums
 };
 
-template <int D, bool Q8>
+template <int D, bool Q8, bool kSplit>
 struct Shape {
   static constexpr int kTile = 128 * D * 2;                       // bytes of a bf16 tile
   static constexpr int kRaw = 128 * D;
-  static constexpr int kSlots = Q8 ? 4 : (D == 128 ? 5 : 8);
-  static constexpr int kRawSlots = Q8 ? 2 : 1;
+  static constexpr bool kDirect = Q8 && kSplit;                   // keys as codes into the first product: slots of their own
+  static constexpr int kQTiles = kSplit ? 1 : 2;
+  static constexpr int kSlots = kDirect ? 2 : Q8 ? 4 : D == 128 ? (kSplit ? 6 : 5) : 8;
+  static constexpr int kRawSlots = kDirect ? 3 : Q8 ? 2 : 1;
+  static constexpr int kKeySlots = kDirect ? 4 : 1;
+  static constexpr int kScales = kDirect ? 4 : 1;                 // tiles whose keys' scales are held
+
   static constexpr int kThreads = Q8 ? 512 : 384;
-  static constexpr int kRegs = Q8 ? 184 : 208;                    // of the softmax warps; the others keep 72 or 88
-  static constexpr int kSmem = 1024 + 2 * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0);
+  static constexpr int kRegs = kDirect ? 152 : Q8 ? 184 : 208;    // of the softmax warps
+  static constexpr int kRegsOthers = kDirect ? 104 : Q8 ? 72 : 88;
+  static constexpr int kSmem = 1024 + kQTiles * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0) + (kDirect ? kKeySlots * kRaw + kScales * 512 : 0);
 };
 
 // Key tiles of unit u of a request (at least one, so that rows without keys are answered too), and of its two row tiles.
@@ -118,6 +124,7 @@ struct Walk {
   int64_t left;
   int b, h, u, t;
   int known, q0, nq, kv, units;
+  template <bool kSplit>
   __device__ __forceinline__ bool next(const ChunkLaunch& p, Piece& x) {
     if (left <= 0) return false;
     for (;; ++b) {
@@ -143,6 +150,10 @@ struct Walk {
     x.n[0] = max(0, min(c.row[0], t1) - t);
     x.n[1] = max(0, min(c.row[1], t1) - t);
     x.n_all = max(x.n[0], x.n[1]);
+    if (kSplit) {
+      x.n[0] = (x.n_all + 1) / 2;
+      x.n[1] = x.n_all / 2;
+    }
     left -= t1 - t;
     t = 0;
     if (++u == units) {
@@ -244,14 +255,28 @@ __device__ __forceinline__ Walk line_start(const ChunkLaunch& p, int lane, int c
   return w;
 }
 
-template <int NS, int NR>
+template <int NS, int NR, int NK = 1, int NE = 1>
 struct Bars {
   uint64_t q_full[2], s_full[2], p_ready[2][2], o_done[2];
-  uint64_t full[NS], empty[NS], raw_full[NR], raw_empty[NR], piece_full[kPieces], piece_empty[kPieces];
+  uint64_t full[NS], empty[NS], raw_full[NR], raw_empty[NR], key_full[NK], key_empty[NK], scale_full[NE], scale_empty[NE], piece_full[kPieces], piece_empty[kPieces];
   Piece piece[kPieces];
   uint32_t tmem;
   int abort_flag;
 };
+
+template <bool kSplit>
+struct Halves {};
+template <>
+struct Halves<true> {
+  float half[2][128];                      // of a row, by either half of the block
+};
+
+template <int D, bool Q8, bool kSplit>
+using BarsOf = Bars<Shape<D, Q8, kSplit>::kSlots, Shape<D, Q8, kSplit>::kRawSlots, Shape<D, Q8, kSplit>::kKeySlots, Shape<D, Q8, kSplit>::kScales>;
+static_assert(sizeof(BarsOf<128, false, true>) + sizeof(Halves<true>) + Shape<128, false, true>::kSmem <= 232448, "shared memory");
+static_assert(sizeof(BarsOf<128, true, true>) + sizeof(Halves<true>) + Shape<128, true, true>::kSmem <= 232448, "shared memory");
+static_assert(sizeof(BarsOf<128, false, false>) + Shape<128, false, false>::kSmem <= 232448, "shared memory");
+static_assert(sizeof(BarsOf<128, true, false>) + Shape<128, true, false>::kSmem <= 232448, "shared memory");
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
@@ -283,21 +308,29 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 }
 
 // kTree: the new tokens of a request form a tree; a row sees the context and those new tokens whose bits are set in its mask.
-template <int D, bool Q8, bool kTree>
-__global__ void __launch_bounds__(Shape<D, Q8>::kThreads, 1)
+// kSplit: no request has more than 128 rows.  The two halves of the block then share one row tile and take its key tiles in
+// turn, each with a maximum, sums and accumulators of its own, which meet at the end of a piece: a row tile's chain is
+// longer than its products, and without a second row tile nothing would run beside it.
+template <int D, bool Q8, bool kTree, bool kSplit>
+__global__ void __launch_bounds__(Shape<D, Q8, kSplit>::kThreads, 1)
 attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  using SH = Shape<D, Q8>;
+  using SH = Shape<D, Q8, kSplit>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ Bars<SH::kSlots, SH::kRawSlots> bars;
+  __shared__ BarsOf<D, Q8, kSplit> bars;
+  __shared__ Halves<kSplit> meet;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* sq = smem;                                             // [2][part][128 rows][128 B]
-  uint8_t* skv = smem + 2 * SH::kTile;
+  uint8_t* skv = smem + SH::kQTiles * SH::kTile;
   uint8_t* sraw = skv + SH::kSlots * SH::kTile;
+  uint8_t* skey = sraw + SH::kRawSlots * SH::kRaw;                // kDirect
+  float* sscale = reinterpret_cast<float*>(skey + SH::kKeySlots * SH::kRaw);   // [kScales][128]
+  constexpr bool kDirect = SH::kDirect;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort_flag = &bars.abort_flag;
   const uint32_t q_full = smem_u32(bars.q_full), s_full = smem_u32(bars.s_full), p_ready = smem_u32(bars.p_ready), o_done = smem_u32(bars.o_done);
   const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), rfull = smem_u32(bars.raw_full), rempty = smem_u32(bars.raw_empty);
   const uint32_t piece_full = smem_u32(bars.piece_full), piece_empty = smem_u32(bars.piece_empty);
+  const uint32_t key_full = smem_u32(bars.key_full), key_empty = smem_u32(bars.key_empty), scale_full = smem_u32(bars.scale_full), scale_empty = smem_u32(bars.scale_empty);
   if (tid == 0) {
     for (int t = 0; t < 2; ++t) {
       mbar_init(q_full + 8 * t, 128);
@@ -313,6 +346,14 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
     for (int s = 0; s < SH::kRawSlots; ++s) {
       mbar_init(rfull + 8 * s, 1);
       mbar_init(rempty + 8 * s, 128);
+    }
+    for (int s = 0; s < SH::kKeySlots; ++s) {
+      mbar_init(key_full + 8 * s, 1);
+      mbar_init(key_empty + 8 * s, 1);
+    }
+    for (int s = 0; s < SH::kScales; ++s) {
+      mbar_init(scale_full + 8 * s, 128);
+      mbar_init(scale_empty + 8 * s, 128);
     }
     for (int s = 0; s < kPieces; ++s) {
       mbar_init(piece_full + 8 * s, 1);
@@ -348,25 +389,73 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
 
   if (warp < 8) {
     regs_inc<SH::kRegs>();
-    const int t = warp >> 2, row = tid & 127;
-    const float c = p.a.scale * kLog2e, minus_inf = __uint_as_float(0xff800000u);
+    const int t = warp >> 2, row = tid & 127, tile_row = kSplit ? 0 : t * 128;
+    const float c_all = p.a.scale * kLog2e, minus_inf = __uint_as_float(0xff800000u);
     const uint32_t lane_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t s_at = lane_at + t * 128, o_at = lane_at + 256 + t * D;
     const uint32_t pr = p_ready + 16 * t;
-    int count = 0;                                                // products of this row tile so far
+    int count = 0;                                                // products of this row tile (kSplit: of this half) so far
+    int count_other = 0;                                          // kSplit: of the other half
     int g = 0;                                                    // key tiles of the block so far
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && wait_all(bar, parity, abort_flag); };
     // queries of a piece's row tile, a thread its row, all loads in flight at once; 8-bit caches: channels 1 and 2 of
     // every four change places, as their keys do
-    auto load_q = [&](const Piece& y) {
-      const int r = y.u * kUnitRows + t * 128 + row, tok = r / p.a.G;
+    float q_scale = 1.f;                                          // kDirect: of the row's codes, in the piece whose queries were loaded last
+    auto load_q = [&](const Piece& y) {                           // kSplit: the first half's threads, for both
+      const int r = y.u * kUnitRows + tile_row + row, tok = r / p.a.G;
       const bool live = r < y.rows;
       const uint4* src = reinterpret_cast<const uint4*>(p.a.q.p + (live ? (int64_t)(y.q0 + tok) * p.a.q.s_row + (int64_t)(y.h * p.a.G + r - tok * p.a.G) * p.a.q.s_head : 0));
-      uint8_t* dst = sq + t * SH::kTile + (row >> 3) * 1024 + (row & 7) * 128;
+      uint8_t* dst = sq + (kSplit ? 0 : t * SH::kTile) + (row >> 3) * 1024 + (row & 7) * 128;
       uint4 v[D / 8];
 #pragma unroll
       for (int j = 0; j < D / 8; ++j) v[j] = live ? __ldg(src + j) : make_uint4(0, 0, 0, 0);
+      if constexpr (kDirect) {
+        // codes of the row under its power of two, and of what they leave: q 2^-b = t1 + t2, both into one sum
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j) {
+          const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) most = __vmaxu2(most, w[i] & 0x7fff7fffu);
+        }
+        const float top = __uint_as_float(max(most & 0xffffu, most >> 16) << 16);
+        const uint32_t b = top < __uint_as_float(0x7f800000u) ? row_exponent(top) : 127u;
+        q_scale = exponent_up(b);
+        if (t == 1) return;
+        const float down = exponent_down(b), nan = __uint_as_float(0x7fc00000u);
+        uint8_t* to = sq + row * D;
+#pragma unroll
+        for (int j = 0; j < D / 8; j += 2) {
+          float x[16];
+          unpack8(v[j], x);
+          unpack8(v[j + 1], x + 8);
+#pragma unroll
+          for (int term = 0; term < 2; ++term) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float lo = x[2 * i], hi = x[2 * i + 1];
+              if (term == 0) {
+                lo *= down;
+                hi *= down;
+                if (!(fabsf(lo) < __uint_as_float(0x7f800000u))) lo = nan;   // infinities give NaN logits
+                if (!(fabsf(hi) < __uint_as_float(0x7f800000u))) hi = nan;
+              }
+              const uint32_t code = e4m3x2(lo, hi);
+              const float2 back = e4m3x2_to_float2(code);
+              w[i >> 1] = (i & 1) ? w[i >> 1] | (code << 16) : code;
+              x[2 * i] = lo - back.x;
+              x[2 * i + 1] = hi - back.y;
+            }
+            const int chunk = D == 128 ? (j >> 1) ^ (row & 7) : (j >> 1) ^ ((row >> 1) & 3);
+            *reinterpret_cast<uint4*>(to + term * 128 * D + (chunk << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        fence_proxy_async();
+        mbar_arrive(q_full);
+        return;
+      }
 #pragma unroll
       for (int j = 0; j < D / 8; ++j) {
         if (Q8) v[j] = make_uint4(__byte_perm(v[j].x, v[j].y, 0x5410), __byte_perm(v[j].x, v[j].y, 0x7632), __byte_perm(v[j].z, v[j].w, 0x5410), __byte_perm(v[j].z, v[j].w, 0x7632));
@@ -379,31 +468,35 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       if (!ok || !(ok = piece_wait(i))) return false;
       const Piece& y = bars.piece[i % kPieces];
       if (y.b < 0) return false;
-      if (y.n[t] > 0) load_q(y);                                  // only then: the products wait for no others
+      if (y.n[t] > 0 && (kDirect || !(kSplit && t == 1))) load_q(y);           // only then: the products wait for no others
       return true;
     };
     bool more = next_piece(0);
     for (int piece = 0; more; ++piece) {
       const Piece& y = bars.piece[piece % kPieces];
       const int n = y.n[t], kv = y.kv, first = y.t0 * 128;
-      int lim = -1;
+      int lim = kSplit ? 0x7fffffff : -1;                         // kSplit: rows behind the last one see what they like (nobody reads them)
       const uint32_t* mask = nullptr;                             // kTree: the row's words
       const int fresh = kv - y.nq;                                // first new token
       {
-        const int r = y.u * kUnitRows + t * 128 + row;
+        const int r = y.u * kUnitRows + tile_row + row;
         if (r < y.rows) {
           lim = p.a.causal ? kv - y.nq + r / p.a.G : kv - 1;
           if (kTree) mask = p.a.mask + (int64_t)(y.q0 + r / p.a.G) * p.a.words;
         }
       }
       const int lowest = __reduce_min_sync(0xffffffffu, lim);     // of the warp's rows
+      const bool idle = kSplit && lowest == 0x7fffffff;           // a warp without rows hands on whatever its lanes hold
+      const float c = kDirect ? c_all * q_scale : c_all;          // kDirect: logits are those of the codes
       float m = minus_inf, l = 0.f;
+      float mc = minus_inf;                                       // kDirect: the maximum, times c
       float late = minus_inf;                                     // a maximum that m is to follow
       for (int it = 0; it < n; ++it) {
         const uint32_t par = (uint32_t)(count + it) & 1u;
         uint32_t sees[4];                                         // kTree: bits of the tile's keys, fetched while the product runs
-        if (kTree && first + it * 128 + 127 >= fresh) {
-          const int rel = first + it * 128 - fresh;
+        const int kt = kSplit ? 2 * it + t : it, t0 = first + kt * 128;
+        if (kTree && t0 + 127 >= fresh) {
+          const int rel = t0 - fresh;
           uint32_t lo = seen_word(mask, p.a.words, rel >> 5);
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
@@ -414,11 +507,133 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         }
         if (!wait(s_full + 8 * t, par)) break;
         tc_fence_after();
+        // stale value rows behind the last key: P is zero there, but zero times a stale NaN would not be
+        auto clear_stale = [&]() {
+          if (Q8 || kv >= t0 + 128) return;
+          const int use = 2 * (g + kt) + 1, vs = use % SH::kSlots;
+          if (wait(full + 8 * vs, (use / SH::kSlots) & 1) && t0 + row >= kv) {
+            uint8_t* v = skv + vs * SH::kTile + (row >> 3) * gs + (row & 7) * 128;
+#pragma unroll
+            for (int ch = 0; ch < D / 8; ++ch) *reinterpret_cast<uint4*>(v + (ch >> 3) * ps + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
+        };
+        if (kSplit && idle) {
+          clear_stale();
+          if constexpr (kDirect) {
+            const int es = (g + kt) % SH::kScales;
+            if (!wait(scale_full + 8 * es, ((g + kt) / SH::kScales) & 1)) break;
+            mbar_arrive(scale_empty + 8 * es);
+          }
+          tc_fence_before();
+          mbar_arrive(pr);
+          mbar_arrive(pr + 8);
+          continue;
+        }
+        if constexpr (kDirect) {
+          // 32 logits at a time, the next ones on their way: all of a tile in registers beside the rest found no room (300
+          // bytes of spills: 159 us on four requests of 27K), and the instruction cache holds a short loop (64 at a time:
+          // 118 us).  The maximum is taken before the probabilities; where a later part's is far above, the probabilities
+          // before it, which lie over their logits by then, are scaled: by a power of two, so that bf16 loses nothing.  mc is
+          // the maximum in steps of 2.
+          const int es = (g + kt) % SH::kScales;
+          if (!wait(scale_full + 8 * es, ((g + kt) / SH::kScales) & 1)) break;
+          const float4* ks = reinterpret_cast<const float4*>(sscale + es * 128);
+          const bool hidden = lowest < t0 + 127 || (kTree && t0 + 127 >= fresh);
+          if (!(kTree && t0 + 127 >= fresh)) sees[0] = sees[1] = sees[2] = sees[3] = 0xffffffffu;
+          const f32x2 c2 = f2_pack(c, c);
+          f32x2 sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+          constexpr int W = 32;                                   // 16: 128 us
+          float next[W];
+          tmem_ld32(s_at, next);
+#pragma unroll 1
+          for (int q = 0; q < 128; q += W) {
+            float s[W];
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < W; k += 4) {                      // the keys' scales
+              const float4 e = ks[(q + k) >> 2];
+              f2_unpack(f2_mul(f2_pack(next[k], next[k + 1]), f2_pack(e.x, e.y)), s[k], s[k + 1]);
+              f2_unpack(f2_mul(f2_pack(next[k + 2], next[k + 3]), f2_pack(e.z, e.w)), s[k + 2], s[k + 3]);
+            }
+            if (q + W < 128) tmem_ld32(s_at + q + W, next);
+            if (hidden) {
+              const int last = lim - t0 - q;                      // of the part's keys
+              uint32_t bits = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1u;
+              bits &= (q < 32 ? sees[0] : q < 64 ? sees[1] : q < 96 ? sees[2] : sees[3]) >> (q & 31);
+#pragma unroll
+              for (int k = 0; k < W; ++k) s[k] = (bits >> k) & 1u ? s[k] : minus_inf;
+            }
+            float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+            for (int k = 4; k < W - 4; k += 8) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mx[j] = max3(mx[j], s[k + 2 * j], s[k + 2 * j + 1]);
+            }
+            const float top = max3(max3(mx[0], s[W - 4], s[W - 3]), max3(mx[1], s[W - 2], s[W - 1]), fmaxf(mx[2], mx[3]));
+            const float up = top * c - mc;                        // NaN where neither is there yet
+            const bool grow = up > kLazy;
+            if (__any_sync(0xffffffffu, grow)) {
+              const float to = !grow ? mc : mc == minus_inf ? top * c : mc + ceilf(up);
+              const float keep = grow ? exp2_fast(mc - to) : 1.f;
+              mc = to;
+              l *= keep;
+              f2_scale(sum2[0], keep);
+              f2_scale(sum2[1], keep);
+              tmem_ld_wait();
+#pragma unroll 1
+              for (int k = 0; k < q / 2; k += 8) {
+                uint32_t w[8];
+                tmem_ld8(s_at + k, reinterpret_cast<float*>(w));
+                tmem_ld_wait();
+                const uint32_t two = pack2(keep, keep);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = mul_bf16x2(w[j], two);
+                tmem_st8(s_at + k, w);
+              }
+              if (it > 0) {                                       // the sums so far, once the product that wrote them last is done
+                wait(o_done + 8 * t, par ^ 1);
+                tc_fence_after();
+#pragma unroll 1
+                for (int k = 0; k < D; k += 8) {
+                  float o[8];
+                  tmem_ld8(o_at + k, o);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) o[j] *= keep;
+                  tmem_st8(o_at + k, reinterpret_cast<const uint32_t*>(o));
+                }
+              }
+              tmem_st_wait();
+            }
+            const float at = mc == minus_inf ? 0.f : mc;
+            const f32x2 mc2 = f2_pack(-at, -at);
+            uint32_t w[W / 2];
+#pragma unroll
+            for (int k = 0; k < W / 2; ++k) {
+              float a, b;
+              f2_unpack(f2_fma(f2_pack(s[2 * k], s[2 * k + 1]), c2, mc2), a, b);
+              const f32x2 e = f2_pack(exp2_fast(a), exp2_fast(b));
+              sum2[k & 1] = f2_add(sum2[k & 1], e);
+              w[k] = f2_to_bf16x2(e);
+            }
+            tmem_st16(s_at + q / 2, w);                     // over logits that have been read
+            if (q + W == 96 || q + W == 128) {                    // behind 96 and behind all 128 keys
+              tmem_st_wait();
+              tc_fence_before();
+              mbar_arrive(pr + (q + W == 96 ? 0 : 8));
+            }
+          }
+          mbar_arrive(scale_empty + 8 * es);
+          float a, b;
+          f2_unpack(f2_add(sum2[0], sum2[1]), a, b);
+          l += a + b;
+          continue;
+        }
         float s[128];
 #pragma unroll
         for (int k = 0; k < 4; ++k) tmem_ld32(s_at + 32 * k, s + 32 * k);
         tmem_ld_wait();
-        const int t0 = first + it * 128;
         if (lowest < t0 + 127) {
 #pragma unroll
           for (int k = 0; k < 128; ++k) s[k] = t0 + k <= lim ? s[k] : minus_inf;
@@ -477,8 +692,8 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
               m = to;
             }
           }
-          const float mc = m == minus_inf ? 0.f : m * c;
-          mc2 = f2_pack(-mc, -mc);
+          const float at = m == minus_inf ? 0.f : m * c;
+          mc2 = f2_pack(-at, -at);
           sum2[0] = sum2[1] = f2_pack(0.f, 0.f);
 #pragma unroll
           for (int j = 0; j < 4; ++j) mx[j] = s[j];
@@ -498,16 +713,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           if (!__any_sync(0xffffffffu, grow)) break;
         }
         late = (top - m) * c > kLazy ? top : minus_inf;
-        // stale value rows behind the last key: P is zero there, but zero times a stale NaN would not be
-        if (!Q8 && kv < t0 + 128) {
-          const int use = 2 * (g + it) + 1, vs = use % SH::kSlots;
-          if (wait(full + 8 * vs, (use / SH::kSlots) & 1) && t0 + row >= kv) {
-            uint8_t* v = skv + vs * SH::kTile + (row >> 3) * gs + (row & 7) * 128;
-#pragma unroll
-            for (int ch = 0; ch < D / 8; ++ch) *reinterpret_cast<uint4*>(v + (ch >> 3) * ps + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
-          }
-          fence_proxy_async();
-        }
+        clear_stale();
         tmem_st_wait();
         tc_fence_before();
         mbar_arrive(pr);
@@ -522,26 +728,63 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       // the next piece's queries go in while the last products run: this tile's logits are all there
       g += y.n_all;
       count += n;
+      if constexpr (kSplit) {
+        // ... and the other half's: they are the last of this piece until new queries are there
+        count_other += y.n[t ^ 1];
+        if (t == 0 && y.n[1] > 0) wait(s_full + 8, (uint32_t)(count_other - 1) & 1u);
+      }
       more = next_piece(piece + 1);
       if (n > 0) wait(o_done + 8 * t, (uint32_t)(count - 1) & 1u);
       tc_fence_after();
-      const int r = y.u * kUnitRows + t * 128 + row;
+      const int r = y.u * kUnitRows + tile_row + row;
       const bool live = r < y.rows;
       const int tok = r / p.a.G, head = y.h * p.a.G + r - tok * p.a.G;
+      if (kDirect) m = mc / c_all;
+      float keep = 1.f, other = 0.f;                              // kSplit: weights of this half's sums and of the other's
+      const int n_other = kSplit ? y.n[t ^ 1] : 0;
+      if constexpr (kSplit) {
+        float2 o;                                                 // the other half's maximum, then its sum
+        meet.half[t][row] = m;
+        tc_fence_before();
+        named_bar_sync(1, 256);
+        tc_fence_after();
+        o.x = meet.half[t ^ 1][row];
+        named_bar_sync(1, 256);
+        meet.half[t][row] = l;
+        named_bar_sync(1, 256);
+        o.y = meet.half[t ^ 1][row];
+        const float top = o.y == 0.f ? m : l == 0.f ? o.x : fmaxf(m, o.x);
+        keep = l == 0.f ? 0.f : exp2_fast((m - top) * c_all);
+        other = o.y == 0.f ? 0.f : exp2_fast((o.x - top) * c_all);
+        l = keep * l + other * o.y;
+        m = top;
+      }
       // no key seen: decided by the sum, which a NaN logit makes NaN (maxima pass over NaN: m may still be minus infinity)
       const bool dead = l == 0.f;
       const bool whole = y.whole;
-      const int64_t slot = ((int64_t)blockIdx.x * 2 + (y.t0 > 0 ? 0 : 1)) * kUnitRows + t * 128 + row;
+      const int64_t slot = ((int64_t)blockIdx.x * 2 + (y.t0 > 0 ? 0 : 1)) * kUnitRows + tile_row + row;
       const float inv = whole ? (dead ? 0.f : 1.f / l) : 1.f;
       __nv_bfloat16* dst = p.a.out.p + (int64_t)(y.q0 + tok) * p.a.out.s_row + (int64_t)head * p.a.out.s_head;
       // partial sums lie channel by channel: a warp's rows are neighbours
-      float* pdst = p.part + (slot - row - t * 128) * D + t * 128 + row;
+      float* pdst = p.part + (slot - row - tile_row) * D + tile_row + row;
+      const uint32_t o_other = lane_at + 256 + (t ^ 1) * D;
+      const int k_begin = kSplit ? t * (D / 2) : 0, k_end = kSplit ? k_begin + D / 2 : D;   // kSplit: half of the channels each
 #pragma unroll 1
-      for (int k = 0; k < D; k += 16) {
+      for (int k = k_begin; k < k_end; k += 16) {
         float o[16];
         if (n > 0) {
           tmem_ld16(o_at + k, o);
           tmem_ld_wait();
+        }
+        if constexpr (kSplit) {
+          float v[16];
+          if (n_other > 0) {
+            tmem_ld16(o_other + k, v);
+            tmem_ld_wait();
+          }
+          // a half that saw no key of the row gets no weight, whatever its accumulators hold
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[j] = (keep == 0.f ? 0.f : o[j] * keep) + (other == 0.f ? 0.f : v[j] * other);
         }
         if (!live || !ok) continue;
 #pragma unroll
@@ -556,22 +799,28 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         }
         if (whole) {
           store32(dst + k, pack8(o), pack8(o + 8));
-        } else if (n > 0) {
+        } else if (n + n_other > 0) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) pdst[(k + j) * kUnitRows] = o[j];
         }
       }
-      if (live && ok) {
+      if (live && ok && (!kSplit || t == 0)) {
         if (!whole)
           *reinterpret_cast<float2*>(p.ml + 2 * slot) = make_float2(m, l);
         else if (p.a.lse)
           p.a.lse[(int64_t)(y.q0 + tok) * (p.a.H * p.a.G) + head] = dead ? minus_inf : m * p.a.scale + log2f(l) * kLn2;
       }
+      if constexpr (kSplit) {
+        tc_fence_before();
+        // both have read both: the next piece's products may overwrite them.  Where a wait failed anywhere all of them
+        // stop, so that nobody is left at a barrier.
+        if (named_bar_or(2, 256, !ok || !more)) more = false;
+      }
       tc_fence_before();
       piece_done(piece);
     }
   } else {
-    regs_dec<Q8 ? 72 : 88>();
+    regs_dec<SH::kRegsOthers>();
     bool ok = true;
     if (warp == 11) {
       // ---- the block's part of the line
@@ -579,7 +828,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       for (int i = 0; ok; ++i) {
         ok = wait_all(piece_empty + 8 * (i % kPieces), ((i / kPieces) & 1) ^ 1, abort_flag);
         Piece x;
-        const bool more = walk.next(p, x);
+        const bool more = walk.next<kSplit>(p, x);
         if (!more) x.b = -1;
         if (ok && lane == 0) {
           bars.piece[i % kPieces] = x;
@@ -590,19 +839,22 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
     } else if (warp == 8 || warp == 10) {
       // ---- loads of the keys (8) and the values (10); the ring's slots alternate between them.  (A 16-token page is a box
       // of its own, about 140 cycles each: one warp for both was the bound.)
-      const uint32_t ring = smem_u32(Q8 ? sraw : skv);
+      // kDirect: keys have a ring of their own
+      const bool keys = kDirect && warp == 8;
+      const uint32_t ring = smem_u32(keys ? skey : Q8 ? sraw : skv);
       const uint32_t bytes = Q8 ? SH::kRaw : SH::kTile;
-      constexpr int NS = Q8 ? SH::kRawSlots : SH::kSlots;
-      const uint32_t fb = Q8 ? rfull : full, eb = Q8 ? rempty : empty;
+      const int NS = keys ? SH::kKeySlots : Q8 ? SH::kRawSlots : SH::kSlots;
+      const uint32_t fb = keys ? key_full : Q8 ? rfull : full, eb = keys ? key_empty : Q8 ? rempty : empty;
       const CUtensorMap* map = warp == 8 ? &map_k : &map_v;
-      int use = warp == 8 ? 0 : 1;
+      constexpr int kUses = kDirect ? 1 : 2;
+      int use = warp == 8 || kDirect ? 0 : 1;
       for (int i = 0; ok && (ok = piece_wait(i)); ++i) {
         const Piece x = bars.piece[i % kPieces];
         piece_done(i);
         if (x.b < 0) break;
         const int n = x.n_all;
         int ahead = n > 0 ? tile_entry(p.a, p.g, x.b, x.t0 * 128, min(128, x.kv - x.t0 * 128), lane) : 0;
-        for (int it = 0; it < n; ++it, use += 2) {
+        for (int it = 0; it < n; ++it, use += kUses) {
           const int t0 = (x.t0 + it) * 128, rows = min(128, x.kv - t0), entry = ahead;
           if (it + 1 < n) ahead = tile_entry(p.a, p.g, x.b, t0 + 128, min(128, x.kv - t0 - 128), lane);
           const int slot = use % NS;
@@ -632,7 +884,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       };
       auto score = [&](int t, int slot) {                         // S_t = Q_t K^T
         tc_fence_after();
-        const uint64_t kd = k_desc + (uint32_t)(slot * (SH::kTile >> 4)), qd = q_desc + (uint32_t)(t * (SH::kTile >> 4));
+        const uint64_t kd = k_desc + (uint32_t)(slot * (SH::kTile >> 4)), qd = q_desc + (uint32_t)(kSplit ? 0 : t * (SH::kTile >> 4));
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k)
@@ -640,76 +892,140 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           umma_commit(s_full + 8 * t);
         }
       };
-      for (int piece = 0; ok && (ok = piece_wait(piece)); ++piece) {
-        const Piece& y = bars.piece[piece % kPieces];
-        const int b = y.b, n_all = y.n_all, n[2] = {y.n[0], y.n[1]};
-        piece_done(piece);
-        if (b < 0) break;
-        if (n_all > 0) {
-          wait(full + 8 * slot, phase);
+      if constexpr (kSplit) {
+        // key tile i: use 2 i of the ring its keys, 2 i + 1 its values (kDirect: use i of either ring); S_t, P_t and O_t
+        // belong to the tiles of parity t
+        int use = 0;                                              // tiles before the piece
+        auto at = [&](int u) { return u % SH::kSlots; };
+        auto loaded = [&](int u) { return wait(full + 8 * at(u), (uint32_t)(u / SH::kSlots) & 1u); };
+        auto first_product = [&](int t, int i) {                  // S_t over key tile i
+          if constexpr (kDirect) {
+            const int ks = (use + i) % SH::kKeySlots;
+            if (!wait(key_full + 8 * ks, (uint32_t)((use + i) / SH::kKeySlots) & 1u)) return false;
+            tc_fence_after();
+            constexpr uint32_t idesc = idesc_e4m3(128, 128, 0, 0);
+            constexpr uint32_t swizzle = D == 128 ? 2 : 4;
+            const uint64_t qd = operand_desc(smem_u32(sq), 16, 8 * D, swizzle), kd = operand_desc(smem_u32(skey), 16, (uint32_t)p.g.gs, swizzle) + (uint32_t)(ks * (SH::kRaw >> 4));
+            if (elect_one()) {
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-            if (n[t] > 0 && wait(q_full + 8 * t, (uint32_t)queries[t]++ & 1u)) score(t, slot);
-          release(slot);
-          next();
-        }
-        for (int it = 0; it < n_all && ok; ++it) {
-          const int vs = slot, ks = slot + 1 == SH::kSlots ? 0 : slot + 1;
-          const uint32_t vphase = phase, kphase = ks == 0 ? phase ^ 1 : phase;
-          const bool more = it + 1 < n_all;
-          if (!wait(full + 8 * vs, vphase)) break;
-          if (more && !wait(full + 8 * ks, kphase)) break;
-          const uint64_t vd = v_desc + (uint32_t)(vs * (SH::kTile >> 4)), kd = k_desc + (uint32_t)(ks * (SH::kTile >> 4));
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (!ok || it >= n[t]) continue;
-            const uint32_t par = (uint32_t)(count[t] + it) & 1u;
-            const bool again = it + 1 < n[t];
-            const uint64_t qd = q_desc + (uint32_t)(t * (SH::kTile >> 4));
+              for (int k = 0; k < 2 * (D / 32); ++k) {
+                const int term = k / (D / 32), step = k % (D / 32);
+                umma_f8(tmem + t * 128, qd + (term * (128 * D / 16) + step * 2), kd + step * 2, idesc, k > 0);
+              }
+              umma_commit(s_full + 8 * t);
+              umma_commit(key_empty + 8 * ks);
+            }
+          } else {
+            const int ku = 2 * (use + i);
+            if (!loaded(ku)) return false;
+            score(t, at(ku));
+            release(at(ku));
+          }
+          return true;
+        };
+        for (int piece = 0; ok && (ok = piece_wait(piece)); ++piece) {
+          const Piece& y = bars.piece[piece % kPieces];
+          const int b = y.b, n_all = y.n_all;
+          piece_done(piece);
+          if (b < 0) break;
+          if (n_all > 0 && !wait(q_full, (uint32_t)queries[0]++ & 1u)) break;
+          for (int i = 0; i < 2 && i < n_all; ++i)
+            if (!first_product(i, i)) break;
+          for (int i = 0; i < n_all && ok; ++i) {
+            const int t = i & 1, vu = kDirect ? use + i : 2 * (use + i) + 1, vs = at(vu);
+            const uint32_t par = (uint32_t)count[t]++ & 1u;
+            if (!loaded(vu)) break;
+            const uint64_t vd = v_desc + (uint32_t)(vs * (SH::kTile >> 4));
             if (!wait(p_ready + 16 * t, par)) break;
             tc_fence_after();
-            if (elect_one()) {                                    // O_t += P_t V, keys 0 .. 95
+            if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, it > 0 || k > 0);
+              for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, i > 1 || k > 0);
             }
             if (!wait(p_ready + 16 * t + 8, par)) break;
             tc_fence_after();
-            if (elect_one()) {                                    // keys 96 .. 127, then the next S_t over them
+            if (elect_one()) {
 #pragma unroll
               for (int k = 6; k < 8; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, 1);
               umma_commit(o_done + 8 * t);
-              if (again) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                  umma_bf16(tmem + t * 128, qd + ((k >> 2) * 1024 + (k & 3) * 2), kd + ((k >> 2) * k_part + (k & 3) * 2), idesc_s, k > 0);
-                umma_commit(s_full + 8 * t);
-              }
             }
+            release(vs);
+            if (i + 2 < n_all && !first_product(t, i + 2)) break;
           }
-          if (!ok) break;
-          release(vs);
-          next();
-          if (more) {
-            release(ks);
+          use += n_all;
+        }
+      } else {
+        for (int piece = 0; ok && (ok = piece_wait(piece)); ++piece) {
+          const Piece& y = bars.piece[piece % kPieces];
+          const int b = y.b, n_all = y.n_all, n[2] = {y.n[0], y.n[1]};
+          piece_done(piece);
+          if (b < 0) break;
+          if (n_all > 0) {
+            wait(full + 8 * slot, phase);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              if (n[t] > 0 && wait(q_full + 8 * t, (uint32_t)queries[t]++ & 1u)) score(t, slot);
+            release(slot);
             next();
           }
+          for (int it = 0; it < n_all && ok; ++it) {
+            const int vs = slot, ks = slot + 1 == SH::kSlots ? 0 : slot + 1;
+            const uint32_t vphase = phase, kphase = ks == 0 ? phase ^ 1 : phase;
+            const bool more = it + 1 < n_all;
+            if (!wait(full + 8 * vs, vphase)) break;
+            if (more && !wait(full + 8 * ks, kphase)) break;
+            const uint64_t vd = v_desc + (uint32_t)(vs * (SH::kTile >> 4)), kd = k_desc + (uint32_t)(ks * (SH::kTile >> 4));
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (!ok || it >= n[t]) continue;
+              const uint32_t par = (uint32_t)(count[t] + it) & 1u;
+              const bool again = it + 1 < n[t];
+              const uint64_t qd = q_desc + (uint32_t)(t * (SH::kTile >> 4));
+              if (!wait(p_ready + 16 * t, par)) break;
+              tc_fence_after();
+              if (elect_one()) {                                    // O_t += P_t V, keys 0 .. 95
+#pragma unroll
+                for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, it > 0 || k > 0);
+              }
+              if (!wait(p_ready + 16 * t + 8, par)) break;
+              tc_fence_after();
+              if (elect_one()) {                                    // keys 96 .. 127, then the next S_t over them
+#pragma unroll
+                for (int k = 6; k < 8; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, 1);
+                umma_commit(o_done + 8 * t);
+                if (again) {
+#pragma unroll
+                  for (int k = 0; k < D / 16; ++k)
+                    umma_bf16(tmem + t * 128, qd + ((k >> 2) * 1024 + (k & 3) * 2), kd + ((k >> 2) * k_part + (k & 3) * 2), idesc_s, k > 0);
+                  umma_commit(s_full + 8 * t);
+                }
+              }
+            }
+            if (!ok) break;
+            release(vs);
+            next();
+            if (more) {
+              release(ks);
+              next();
+            }
+          }
+          count[0] += n[0];
+          count[1] += n[1];
         }
-        count[0] += n[0];
-        count[1] += n[1];
       }
     } else if (Q8 && warp >= 12) {
       // ---- 8-bit tiles to bf16: a thread a token row, channels in the order (0, 2, 1, 3) of every four
       const int r = tid & 127;
       constexpr int CH = D / 16;                                  // 16-byte chunks of a raw row
       const uint32_t sw = D == 128 ? (uint32_t)(r & 7) : (uint32_t)((r >> 1) & 3);
-      int rs = 0, rphase = 0, slot = 0, phase = 0;
+      int rs = 0, rphase = 0, slot = 0, phase = 0, scales = 0;
       Piece x{};
-      auto exponents = [&](int tt, uint32_t& ek, uint32_t& ev) {
+      auto page_of = [&](int tt) { return p.g.paged && tt < x.kv ? request_page(p.a.req, p.a.c, x.b, tt, nullptr) : 0; };
+      auto exponents = [&](int tt, int page, uint32_t& ek, uint32_t& ev) {
         ek = ev = 127;
         if (tt >= x.kv) return;
         int64_t o = (int64_t)p.a.layer * p.a.e.s_layer + (int64_t)x.h * p.a.e.s_head;
         if (p.g.paged) {
-          const int page = request_page(p.a.req, p.a.c, x.b, tt, nullptr);
           if (page < 0) return;
           o += (int64_t)page * p.a.e.s_page + (int64_t)(tt & p.a.c.page_mask) * p.a.e.s_tok;
         } else {
@@ -724,13 +1040,26 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         if (x.b < 0) break;
         const int n = x.n_all;
         uint32_t ek, ev, nk, nv;
-        exponents(x.t0 * 128 + r, ek, ev);
+        exponents(x.t0 * 128 + r, page_of(x.t0 * 128 + r), ek, ev);
+        int page = kDirect ? page_of(n > 1 ? x.t0 * 128 + 128 + r : x.kv) : 0;
         for (int it = 0; it < n && ok; ++it) {
-          const int tt = (x.t0 + it) * 128 + r;
-          exponents(it + 1 < n ? tt + 128 : x.kv, nk, nv);
+          const int tt = (x.t0 + it) * 128 + r, next = it + 1 < n ? tt + 128 : x.kv;
+          // kDirect: page ids two tiles ahead, so that their exponents are asked for without a wait
+          if (!kDirect) page = page_of(next);
+          exponents(next, page, nk, nv);
+          if (kDirect) page = page_of(it + 2 < n ? tt + 256 : x.kv);
           const bool valid = tt < x.kv;
+          if constexpr (kDirect) {
+            // the keys' scales go to the softmax; the values alone are converted
+            const int es = scales % SH::kScales;
+            ok = wait_all(scale_empty + 8 * es, ((scales / SH::kScales) & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            sscale[es * 128 + r] = exponent_up(ek);
+            mbar_arrive(scale_full + 8 * es);
+            ++scales;
+          }
 #pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) {
+          for (int kv = kDirect ? 1 : 0; kv < 2; ++kv) {
             ok = wait_all(rfull + 8 * rs, rphase, abort_flag) && wait_all(empty + 8 * slot, phase ^ 1, abort_flag);
             if (!ok) break;
             const uint8_t* in = sraw + rs * SH::kRaw + r * D;
@@ -952,17 +1281,17 @@ int64_t chunk_blocks(int n, int max_q, int max_kv, int G, int H) {
 }
 size_t chunk_starts_bytes(int64_t blocks) { return ((size_t)blocks * sizeof(UnitStart) + 255) / 256 * 256; }
 
-template <int D, bool Q8, bool kTree>
+template <int D, bool Q8, bool kTree, bool kSplit>
 cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
-  using SH = Shape<D, Q8>;
+  using SH = Shape<D, Q8, kSplit>;
   static DeviceOnce once;
   int dev;
   if (once.pending(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(attend_chunk_kernel<D, Q8, kTree>, cudaFuncAttributeMaxDynamicSharedMemorySize, SH::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(attend_chunk_kernel<D, Q8, kTree, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, SH::kSmem);
     if (e != cudaSuccess) return e;
     once.mark(dev);
   }
-  const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8, kTree>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
+  const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8, kTree, kSplit>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
   if (e != cudaSuccess || p.blocks < 2) return e;
   if (p.fine) return launch_after(attend_chunk_join_kernel<D, 4>, dim3((unsigned)chunk_units(p.a.req.n, p.a.req.max_q, p.a.G, p.a.H), 8 * (D / 32)), 256, 0, s, p);
   return launch_after(attend_chunk_join_kernel<D, D / 8>, dim3((unsigned)p.blocks - 1, 8), 256, 0, s, p);
@@ -988,15 +1317,15 @@ struct Plan {
   int rc;
   bool chunk;
 };
-static Plan attend_plan(int n, int max_q, int max_kv, int G, int H) {
+static Plan attend_plan(int n, int max_q, int max_kv, int G, int H, bool split) {
   const int64_t rows = (int64_t)max_q * G;
   if (const int rc = few_capacity(rows)) return {rc, false};
-  const bool both = n > 1 && (int64_t)n * H * ((max_kv + 127) / 128) > kBothTiles;
+  const bool both = !split && n > 1 && (int64_t)n * H * ((max_kv + 127) / 128) > kBothTiles;
   return {both ? few_capacity(G) : 0, true};
 }
 
 size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d) {
-  const Plan p = attend_plan(n, max_q, max_kv, G, H);
+  const Plan p = attend_plan(n, max_q, max_kv, G, H, false);      // what any call needs: one that splits needs no more
   size_t bytes = p.rc ? (few_workspace_bytes(n, max_kv, H, d, p.rc) + 255) / 256 * 256 : 0;
   if (p.chunk) {
     const int64_t blocks = chunk_blocks(n, max_q, max_kv, G, H);
@@ -1008,7 +1337,8 @@ size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int
 int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   (void)L;
   const bool q8 = a.e.k != nullptr;
-  const Plan plan = attend_plan(a.req.n, a.req.max_q, a.req.max_kv, a.G, a.H);
+  const bool split = a.mask && (int64_t)a.req.max_q * a.G <= 128;
+  const Plan plan = attend_plan(a.req.n, a.req.max_q, a.req.max_kv, a.G, a.H, split);
   ChunkLaunch p;
   p.a = a;
   p.min_rows = plan.rc + 1;
@@ -1033,11 +1363,12 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   p.ml = reinterpret_cast<float*>(ws + chunk_starts_bytes(p.blocks));
   p.part = p.ml + (int64_t)p.blocks * 2 * kUnitRows * 2;
   cudaError_t e;
-#define KVC_CHUNK(D, Q, T) \
-  if (d == D && q8 == Q && (a.mask != nullptr) == T) e = launch_chunk<D, Q, T>(p, mk, mv, s);
+#define KVC_CHUNK(D, Q, T, S) \
+  if (d == D && q8 == Q && (a.mask != nullptr) == T && split == S) e = launch_chunk<D, Q, T, S>(p, mk, mv, s);
   e = cudaErrorInvalidValue;
-  KVC_CHUNK(128, false, false) KVC_CHUNK(128, true, false) KVC_CHUNK(64, false, false) KVC_CHUNK(64, true, false)
-  KVC_CHUNK(128, false, true) KVC_CHUNK(128, true, true) KVC_CHUNK(64, false, true) KVC_CHUNK(64, true, true)
+  KVC_CHUNK(128, false, false, false) KVC_CHUNK(128, true, false, false) KVC_CHUNK(64, false, false, false) KVC_CHUNK(64, true, false, false)
+  KVC_CHUNK(128, false, true, false) KVC_CHUNK(128, true, true, false) KVC_CHUNK(64, false, true, false) KVC_CHUNK(64, true, true, false)
+  KVC_CHUNK(128, false, true, true) KVC_CHUNK(128, true, true, true) KVC_CHUNK(64, false, true, true) KVC_CHUNK(64, true, true, true)
 #undef KVC_CHUNK
   return e == cudaSuccess ? KVC_OK : KVC_E_CUDA;
 }

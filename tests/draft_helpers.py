@@ -74,6 +74,11 @@ class TreeBuilt(Built):
                         assert np.all(o[r, a] == 0) and s[r, a] == -np.inf
                         continue
                     ds = (st.d + 8) * 2.0 ** -24 * self.scale * big
+                    if st.q8:
+                        # queries meet the codes as two e4m3 parts of q 2^-b, whose largest channel is above 224: what the
+                        # second leaves is at most half its smallest step, 2^-10, in every channel
+                        qr = f64(self.q_cpu[r, a])
+                        ds += self.scale * 2.0 ** -10 * np.abs(qr).max() / 224.0 * np.abs(k).sum(-1).max()
                     rel = 2.0 ** -8 + 2 * ds + len(keys) * 2.0 ** -23 + 2.0 ** -21
                     tol = 2.0 ** -8 * np.abs(ref) + 1.01 * rel * absv + 1e-30
                     if st.q8:
