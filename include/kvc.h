@@ -746,7 +746,7 @@ typedef struct kvc_probs {
  *     next = min { x : sum_{y <= x} P(y) > u_next sum_y P(y) } .
  *   parent       as in kvc_tree
  *   token        DEVICE int32 [n_rows]: drafted tokens (of a request's row 0 not looked at)
- *   target       distributions of the target; NaN and negative entries count as 0, sums need not be exactly 1
+ *   target       distributions of the target; NaN and negative entries count as 0 (in draft too), sums need not be exactly 1
  *   draft        distributions the children of every row were drawn from; same n and n_rows.  NULL: the drafts were chosen,
  *                not drawn: child c is accepted where u[c] (1 - the probabilities of the siblings rejected before it) <
  *                P(x), and a rejected token's probability becomes 0

@@ -43,6 +43,8 @@ def _clean(p):
 def verify(parent, token, target, draft, u, u_next):
     """One request (lists and float64 [rows, n]) -> (kept places, next token)."""
     n = target.shape[1]
+    if draft is not None:
+        draft = _clean(draft)
     node, kept, P, spent, left, gone = 0, [0], _clean(target[0]), False, 1.0, []
     for c in range(1, len(parent)):
         if parent[c] != node or spent or not 0 <= token[c] < n:

@@ -11,7 +11,8 @@
 //
 // A cluster of blocks shares a request.  Every block walks the tree by itself (all of them come to the same decisions from
 // the same numbers), sums its part of the vocabulary, and the parts' sums meet in distributed shared memory.  Blocks, warps
-// and lanes hold ascending parts, so the draw finds its place from prefix sums: block, warp, 128 entries, lane, entry.
+// and lanes hold ascending parts, so the draw finds its place from prefix sums: block, warp, then a run of entries a thread
+// over the warp's part.
 // Sums are float64, in a fixed order.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -25,11 +26,21 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kCluster = 8;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kCluster = 8;
+constexpr int kRowBytes = 24;              // of shared memory for a row of the request
 constexpr int kStep = 128;                 // entries a warp takes at a time
 
+// A non-negative float as a double, by moving its bits (the conversion unit takes 16 a cycle and SM, four times fewer than
+// the integer pipe; subnormal floats come out as other numbers below 2^-126).
+__device__ __forceinline__ double widen(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return __hiloint2double((int)((u >> 3) + 0x38000000u), (int)(u << 29));
+}
 // P(x) from the node's two distributions; NaN and negative entries count as 0
-__device__ __forceinline__ double residual(float p, float q, double A, double B) { return fmax((double)p * A - (double)q * B, 0.0); }
+__device__ __forceinline__ double residual(float p, float q, double A, double B) {
+  const double v = widen(p) * A - (q > 0.f ? widen(q) : 0.0) * B;
+  return p > 0.f && v > 0.0 ? v : 0.0;
+}
 
 struct Node {                              // where the walk is
   int node, asked, gone;                   // the node's row, the row tried last, rejected tokens (drafts chosen)
@@ -39,10 +50,14 @@ struct Node {                              // where the walk is
 };
 
 template <bool kDraft, bool kWide>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant__ VerifyLaunch p) {
-  __shared__ float s_p[KVC_TREE_MAX_Q], s_q[KVC_TREE_MAX_Q], s_u[KVC_TREE_MAX_Q];
-  __shared__ int s_token[KVC_TREE_MAX_Q], s_gone[KVC_TREE_MAX_Q];
-  __shared__ int16_t s_parent[KVC_TREE_MAX_Q], s_path[KVC_TREE_MAX_Q];
+__global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_constant__ VerifyLaunch p) {
+  extern __shared__ float s_p[];           // [max_q] each: p and q of the drafted tokens, u, tokens, rejected tokens, parents, path
+  float* s_q = s_p + p.req.max_q;
+  float* s_u = s_q + p.req.max_q;
+  int* s_token = reinterpret_cast<int*>(s_u + p.req.max_q);
+  int* s_gone = s_token + p.req.max_q;
+  int16_t* s_parent = reinterpret_cast<int16_t*>(s_gone + p.req.max_q);
+  int16_t* s_path = s_parent + p.req.max_q;
   __shared__ double s_warp[kWarps], s_block[2][kCluster];
   __shared__ Node s_at;
   __shared__ int s_more, s_kept;
@@ -120,7 +135,8 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
       for (int g = 0; g < gone; ++g)
         if (s_gone[g] == at + k) return 0.0;
     }
-    return residual(x.p[k], kDraft ? x.q[k] : 0.f, A, B);
+    if (!kDraft) return x.p[k] > 0.f ? widen(x.p[k]) : 0.0;
+    return residual(x.p[k], x.q[k], A, B);
   };
   int passes = 0;
   // sum of P over the vocabulary, the same in all threads of the cluster
@@ -130,7 +146,8 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
     int64_t lo, hi;
     warp_range(warp, lo, hi);
     double sum = 0.0;
-    constexpr int kAhead = 4;              // loads in flight
+    float top = 0.f;
+    constexpr int kAhead = kDraft ? 2 : 4;   // loads in flight (two rows, or one)
     for (int64_t at = lo + lane * 4; at < hi; at += kAhead * kStep) {
       Four x[kAhead];
 #pragma unroll
@@ -139,10 +156,14 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
       for (int i = 0; i < kAhead; ++i) {
         double s = 0.0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s += value(x[i], k, at + i * kStep, A, B, gone);
+        for (int k = 0; k < 4; ++k) {
+          s += value(x[i], k, at + i * kStep, A, B, gone);
+          top = fmaxf(top, x[i].p[k]);
+        }
         sum += s;
       }
     }
+    if (top > 3.4028235e38f) sum = __longlong_as_double(0x7ff0000000000000ll);   // no sum with an infinity in it
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     __syncthreads();                       // s_warp of the pass before has been read
@@ -184,7 +205,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
         bool fresh = true;
         const double px = (double)s_p[child];
         if (kDraft) {
-          yes = (double)s_u[child] * (double)s_q[child] < residual(s_p[child], s_q[child], n.A, n.B);
+          yes = (double)s_u[child] * (double)fmaxf(s_q[child], 0.f) < residual(s_p[child], s_q[child], n.A, n.B);
         } else {
           for (int g = 0; g < n.gone; ++g) fresh = fresh && s_gone[g] != s_token[child];
           yes = fresh && (double)s_u[child] * n.left < px;
@@ -270,62 +291,56 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const __grid_constant_
   double before = 0.0;
   const int block = find(s_block[(passes - 1) & 1], blocks, before);
   if (block != rank) return;
-  const int in = find(s_warp, kWarps, before);
-  if (in != warp) return;
+  // the warp's part once more, by the whole block: a thread a run of entries, one scan over the threads
+  const int part = find(s_warp, kWarps, before);
   const float* pt = p.target + (int64_t)(q0 + n.node) * p.s_target;
   const float* pd = kDraft ? p.draft + (int64_t)(q0 + n.node) * p.s_draft : nullptr;
   int64_t lo, hi;
-  warp_range(warp, lo, hi);
-  int64_t found = -1;                      // lane's last positive entry so far
-  constexpr int kAhead = 4;
-  for (int64_t base = lo; base < hi; base += kAhead * kStep) {
-    Four x[kAhead];
+  warp_range(part, lo, hi);
+  const int run = (per_warp + 4 * kThreads - 1) / (4 * kThreads) * 4;
+  const int64_t begin = lo + (int64_t)tid * run, end = min(hi, begin + run);
+  double own = 0.0;
+  for (int64_t at = begin; at < end; at += 4) {
+    Four x;
+    fetch(pt, pd, at, end, x);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) fetch(pt, pd, base + i * kStep + lane * 4, hi, x[i]);
+    for (int k = 0; k < 4; ++k) own += value(x, k, at, n.A, n.B, n.gone);
+  }
+  double incl = own;
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int64_t at = base + i * kStep + lane * 4;
-      double v[4], own = 0.0;
+  for (int o = 1; o < 32; o <<= 1) {
+    const double t = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += t;
+  }
+  __syncthreads();                         // s_warp has been read
+  if (lane == 31) s_warp[warp] = incl;
+  if (tid == 0) {
+    s_more = kThreads;                     // the first thread whose run ends beyond the threshold
+    s_kept = -1;                           // the last one with anything
+  }
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) before += s_warp[w];
+  if (own > 0.0) {
+    if (before + incl > threshold) atomicMin(&s_more, tid);
+    atomicMax(&s_kept, tid);
+  }
+  __syncthreads();
+  if (tid != (s_more < kThreads ? s_more : s_kept)) return;
+  double sum = before + (incl - own);
+  int64_t next = -1;
+  for (int64_t at = begin; at < end && !(next >= 0 && sum > threshold); at += 4) {
+    Four x;
+    fetch(pt, pd, at, end, x);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k] = value(x[i], k, at, n.A, n.B, n.gone);
-        own += v[k];
+    for (int k = 0; k < 4; ++k) {
+      const double v = value(x, k, at, n.A, n.B, n.gone);
+      if (v > 0.0 && !(next >= 0 && sum > threshold)) {
+        next = at + k;
+        sum += v;
       }
-      double incl = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const double t = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += t;
-      }
-      const unsigned hit = __ballot_sync(0xffffffffu, own > 0.0 && before + incl > threshold);
-      if (hit) {
-        if (lane == __ffs(hit) - 1) {
-          double run = before + (incl - own);
-          int pick = 0;
-#pragma unroll
-          for (int k = 3; k >= 0; --k) pick = v[k] > 0.0 ? k : pick;   // the first positive one, at least
-          bool done = false;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            run += v[k];
-            if (!done && v[k] > 0.0) {
-              pick = k;
-              done = run > threshold;
-            }
-          }
-          p.next[b] = (int)(at + pick);
-        }
-        return;
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (v[k] > 0.0) found = at + k;
-      before += __shfl_sync(0xffffffffu, incl, 31);
     }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) found = max(found, __shfl_xor_sync(0xffffffffu, found, o));
-  if (lane == 0) p.next[b] = (int)found;
+  p.next[b] = (int)next;
 }
 
 template <bool kDraft, bool kWide>
@@ -339,6 +354,7 @@ cudaError_t launch(const VerifyLaunch& v, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)v.req.n * blocks));
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = (size_t)(v.req.max_q > 0 ? v.req.max_q : 1) * kRowBytes;
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = 2;

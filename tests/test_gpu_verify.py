@@ -129,6 +129,8 @@ def test_nan_negative_and_empty_distributions(drawn):
     c = Case([5] * 9, 6000, seed=9, drawn=drawn)
     c.target[:, ::7] = float("nan")
     c.target[:, 1::7] = -1.0
+    c.draft[:, 2::7] = float("nan")
+    c.draft[:, 3::7] = -0.5
     c.run().check()
     assert c.flags == 0
     c.target[:] = 0.0
