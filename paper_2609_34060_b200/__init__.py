@@ -170,6 +170,7 @@ def load(path: Optional[str] = None):
     lib.kvc_attend_tree.argtypes = lib.kvc_attend_tree_q8.argtypes = [vp, vp, vp, vp, i32, C.c_double, vp, vp, vp, sz, vp]
     lib.kvc_verify.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     lib.kvc_keep.argtypes = lib.kvc_keep_q8.argtypes = [vp, vp, i32, vp, vp, vp, vp]
+    lib.kvc_block_append_rotated.argtypes = lib.kvc_block_attend_tree.argtypes = lib.kvc_block_verify.argtypes = lib.kvc_block_keep.argtypes = [vp]
     lib.kvc_status_poll.argtypes = [C.POINTER(C.c_uint32)]
     lib.kvc_status_reset.argtypes = []
     lib.kvc_set_path.argtypes = [i32]
@@ -375,9 +376,9 @@ class _Fixed:
 
 def _list(t, what: str, dtype=torch.int32) -> int:
     """Address of a contiguous device list."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_contiguous():
-        raise KvcError(KVC_E_INVALID_ARG, f"{what}: contiguous {dtype} expected")
-    return t.data_ptr()
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous():
+        return t.data_ptr()
+    raise KvcError(KVC_E_INVALID_ARG, f"{what}: contiguous {dtype} expected")
 
 
 def _device_of(*tensors) -> int:
@@ -560,7 +561,8 @@ class Rotary(_Fixed):
         tables = {}
         table = None if rope._tab is None else list(rope._tab)
         self.__dict__.update(rope=rope, rot_dim=int(rot_dim or 0), amplitude=float(amplitude), depth=depth, pos_begin=pos_begin, _struct=made,
-                             _at=C.addressof(made), _table=table, _tables=tables, _dev=_device_of(depth, pos_begin))
+                             _at=C.addressof(made), _table=table, _tables=tables, _rows=-1 if depth is None else depth.numel(),
+                             _requests=-1 if pos_begin is None else pos_begin.numel(), _dev=None if depth is None and pos_begin is None else _device_of(depth, pos_begin))
 
     def __reduce__(self):
         return Rotary, (self.rope, self.rot_dim or None, self.amplitude, self.depth, self.pos_begin)
@@ -568,7 +570,7 @@ class Rotary(_Fixed):
     def struct(self) -> kvc_rotary:
         return self._struct
 
-    def _for(self, d: int, rows: int, n: int) -> int:
+    def _for(self, d: int) -> int:
         """Address of the descriptor for heads of d channels."""
         made = self._tables.get(d)
         if made is None:
@@ -580,8 +582,6 @@ class Rotary(_Fixed):
             s = kvc_rotary.from_buffer_copy(self._struct)
             s.rope.inv_freq = C.cast(tab, C.c_void_p)
             made = self._tables[d] = (C.addressof(s), s, tab)
-        if (self.depth is not None and self.depth.numel() < rows) or (self.pos_begin is not None and self.pos_begin.numel() < n):
-            raise KvcError(KVC_E_SHAPE, "Rotary: depth [rows] and pos_begin [requests] expected")
         return made[0]
 
 
@@ -1013,6 +1013,38 @@ def kvc_attend(req: Requests, q: torch.Tensor, cache, layer: int, out: torch.Ten
               0 if workspace is None else workspace.numel() * workspace.element_size(), st), "kvc_attend")
 
 
+def _pack(*args) -> bytes:
+    """An argument block of the calls below (``csrc/marshal.cpp``).  The module takes this function's place at the first
+    call; no Python stands in for it."""
+    global _pack
+    try:
+        from . import _marshal
+    except ImportError as e:
+        raise RuntimeError("_marshal.so not found: build it with `python -m paper_2609_34060_b200.build`") from e
+    _marshal.setup(KvcError, torch.bfloat16, torch.float32, torch.int32)
+    _pack = _marshal.pack
+    return _pack(*args)
+
+
+def _tree(tree, what: str) -> int:
+    if not isinstance(tree, Tree):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: Tree expected, not {type(tree).__name__}")
+    return tree._at
+
+
+def _kept_lists(req: Requests, kept: torch.Tensor, what: str, *ones) -> int:
+    """The lists a request each: kept [n, max_q or more], the others [n]; kept's row length."""
+    if not isinstance(kept, torch.Tensor):
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: kept: contiguous int32 expected")
+    n = (req.n,)
+    good = kept.dim() == 2 and kept.shape[0] == req.n and kept.shape[1] >= req.max_q
+    for t in ones:
+        good = good and (t is None or t.shape == n)
+    if not good:
+        raise KvcError(KVC_E_SHAPE, f"{what}: kept [requests, max_q or more] and lists of {req.n} expected")
+    return kept.shape[1]
+
+
 def kvc_tree_build(req: Requests, tree: Tree, stream=None) -> None:
     """Masks and depths of a step's drafted tokens from their parents."""
     at, t = _address(req, "kvc_tree_build"), _tree(tree, "kvc_tree_build")
@@ -1020,10 +1052,9 @@ def kvc_tree_build(req: Requests, tree: Tree, stream=None) -> None:
     _check(load().kvc_tree_build(at, t, st), "kvc_tree_build")
 
 
-def _tree(tree, what: str) -> int:
-    if not isinstance(tree, Tree):
-        raise KvcError(KVC_E_INVALID_ARG, f"{what}: Tree expected, not {type(tree).__name__}")
-    return tree._at
+_ROTATED_NAMES, _TREE_NAMES = ("q", "q_out", "k_new", "v_new"), ("lse", "workspace", "q", "out")
+_VERIFY_NAMES = ("parent", "token", "u", "u_next", "kept", "n_kept", "next_token", "target", "draft")
+_KEEP_NAMES = ("kept", "n_kept", "kv_out")
 
 
 def kvc_append_rotated(req: Requests, rotary: Rotary, k_new: torch.Tensor, v_new: torch.Tensor, cache, layer: int, q: Optional[torch.Tensor] = None,
@@ -1035,12 +1066,12 @@ def kvc_append_rotated(req: Requests, rotary: Rotary, k_new: torch.Tensor, v_new
         raise KvcError(KVC_E_INVALID_ARG, f"{what}: Rotary expected, not {type(rotary).__name__}")
     if (q is None) != (q_out is None):
         raise KvcError(KVC_E_INVALID_ARG, f"{what}: q and q_out go together")
-    at, c, k, v = _address(req, what), _desc(cache), _heads(k_new, cache.d, "k_new"), _heads(v_new, cache.d, "v_new")
-    hq, ho = (None, None) if q is None else (_heads(q, cache.d, "q"), _heads(q_out, cache.d, "q_out"))
-    st = _here(what, stream, (c[1], req._dev), k_new, v_new, q, q_out, rotary.depth, rotary.pos_begin)
+    at, c = _address(req, what), _desc(cache)
+    st = _here(what, stream, (c[1], req._dev) if rotary._dev is None else (c[1], req._dev, rotary._dev))
     _holds(req, cache, what)
-    fn = load().kvc_append_rotated if c[3] is None else load().kvc_append_rotated_q8
-    _check(fn(at, rotary._for(cache.d, k_new.shape[0], req.n), hq, ho, k, v, int(layer), c[0], st), what)
+    block = _pack("PPPPHHHHiiiii", what, _ROTATED_NAMES, req._dev, cache.d, at, rotary._for(cache.d), c[0], st, q, q_out, k_new, v_new, layer,
+                  c[3] is not None, q is not None, rotary._rows, rotary._requests)
+    _check(load().kvc_block_append_rotated(block), what)
 
 
 def kvc_attend_tree(req: Requests, tree: Tree, q: torch.Tensor, cache, layer: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
@@ -1048,37 +1079,14 @@ def kvc_attend_tree(req: Requests, tree: Tree, q: torch.Tensor, cache, layer: in
     """Attention of a tree of drafted tokens: every row sees its request's context and the new tokens of its mask.
     Workspace: kvc_attend_workspace_bytes."""
     what = "kvc_attend_tree"
-    at, t, c, hq, ho = _address(req, what), _tree(tree, what), _desc(cache), _heads(q, cache.d, "q"), _heads(out, cache.d, "out")
-    st = _here(what, stream, (c[1], req._dev, tree._dev), q, out, workspace, lse)
+    at, t, c = _address(req, what), _tree(tree, what), _desc(cache)
+    st = _here(what, stream, (c[1], req._dev, tree._dev))
     _holds(req, cache, what)
-    if workspace is not None and not workspace.is_contiguous():
-        raise KvcError(KVC_E_INVALID_ARG, f"{what}: a contiguous workspace expected")
-    if lse is not None and (lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
+    if lse is not None and lse.shape != q.shape[:2]:
         raise KvcError(KVC_E_INVALID_ARG, f"{what}: lse must be float32 [rows, heads]")
-    fn = load().kvc_attend_tree if c[3] is None else load().kvc_attend_tree_q8
-    _check(fn(at, t, hq, c[0], int(layer), cache.d ** -0.5 if scale is None else float(scale), ho, None if lse is None else lse.data_ptr(),
-              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(), st), what)
-
-
-_PROBS = struct.Struct("@QiiQ")       # kvc_probs
-
-
-def _probs(t: torch.Tensor, what: str) -> bytes:
-    """A kvc_probs over float32 [rows, n] with contiguous entries."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.dim() != 2:
-        raise KvcError(KVC_E_INVALID_ARG, f"{what}: float32 [rows, n] expected")
-    (rows, n), (s_row, s_at) = t.shape, t.stride()
-    if (n > 1 and s_at != 1) or (rows > 1 and s_row < n):
-        raise KvcError(KVC_E_UNSUPPORTED, f"{what}: contiguous entries and no broadcast rows expected")
-    return _PROBS.pack(t.data_ptr(), rows, n, s_row if rows > 1 else 0)
-
-
-def _kept_lists(req: Requests, kept: torch.Tensor, what: str, *ones):
-    """The lists a request each: kept [n, max_q or more], the others [n]."""
-    at = _list(kept, f"{what}: kept")
-    if kept.dim() != 2 or kept.shape[0] != req.n or kept.shape[1] < req.max_q or any(t is not None and tuple(t.shape) != (req.n,) for t in ones):
-        raise KvcError(KVC_E_SHAPE, f"{what}: kept [requests, max_q or more] and lists of {req.n} expected")
-    return at, int(kept.shape[1])
+    block = _pack("PPPFAPPdHHii", what, _TREE_NAMES, req._dev, cache.d, at, t, c[0], lse, workspace, 0 if workspace is None else workspace.nbytes, st,
+                  cache.d ** -0.5 if scale is None else scale, q, out, layer, c[3] is not None)
+    _check(load().kvc_block_attend_tree(block), what)
 
 
 def kvc_verify(req: Requests, parent: torch.Tensor, token: torch.Tensor, target: torch.Tensor, u: torch.Tensor, u_next: torch.Tensor,
@@ -1087,28 +1095,25 @@ def kvc_verify(req: Requests, parent: torch.Tensor, token: torch.Tensor, target:
     [n]), from the target's distributions float32 [rows, vocabulary], those the drafts were drawn from (None: they were
     chosen) and uniform random numbers `u` [rows], `u_next` [n]."""
     what = "kvc_verify"
-    at, pt, pd = _address(req, what), _probs(target, "target"), None if draft is None else _probs(draft, "draft")
-    a_kept, stride = _kept_lists(req, kept, what, n_kept, next_token, u_next)
-    rows = (target.shape[0],)
+    at, stride = _address(req, what), _kept_lists(req, kept, what, n_kept, next_token, u_next)
+    st = _here(what, stream, (req._dev,))
+    block = _pack("PIIFFIIIPppii", what, _VERIFY_NAMES, req._dev, 0, at, parent, token, u, u_next, kept, n_kept, next_token, st, target, draft, stride,
+                  draft is not None)
+    rows = target.shape[:1]
     if parent.shape != rows or token.shape != rows or u.shape != rows:
         raise KvcError(KVC_E_SHAPE, f"{what}: parent, token and u [rows] expected")
-    args = (_list(parent, "parent"), _list(token, "token"), pt, pd, _list(u, "u", torch.float32), _list(u_next, "u_next", torch.float32), a_kept, stride,
-            _list(n_kept, "n_kept"), _list(next_token, "next_token"))
-    st = _here(what, stream, (req._dev,), parent, token, target, draft, u, u_next, kept, n_kept, next_token)
-    _check(load().kvc_verify(at, *args, st), what)
+    _check(load().kvc_block_verify(block), what)
 
 
 def kvc_keep(req: Requests, kept: torch.Tensor, n_kept: torch.Tensor, cache, kv_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """The rows of the accepted drafts moved together in every layer of a Cache or QCache; `kv_out` int32 [n]: the lengths
     behind the step."""
     what = "kvc_keep"
-    at, c = _address(req, what), _desc(cache)
-    a_kept, stride = _kept_lists(req, kept, what, n_kept, kv_out)
-    a_n, a_out = _list(n_kept, "n_kept"), None if kv_out is None else _list(kv_out, "kv_out")
-    st = _here(what, stream, (c[1], req._dev), kept, n_kept, kv_out)
+    at, c, stride = _address(req, what), _desc(cache), _kept_lists(req, kept, what, n_kept, kv_out)
+    st = _here(what, stream, (c[1], req._dev))
     _holds(req, cache, what)
-    fn = load().kvc_keep if c[3] is None else load().kvc_keep_q8
-    _check(fn(at, a_kept, stride, a_n, c[0], a_out, st), what)
+    block = _pack("PIIPIPii", what, _KEEP_NAMES, req._dev, 0, at, kept, n_kept, c[0], kv_out, st, stride, c[3] is not None)
+    _check(load().kvc_block_keep(block), what)
 
 
 def kvc_status_poll() -> int:

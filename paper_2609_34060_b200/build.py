@@ -1,8 +1,9 @@
 """In-tree build of the CUDA library (libkvc.so) for sm_100a with nvcc.
 
 ``python -m paper_2609_34060_b200.build`` compiles every ``csrc/*.cu`` and links
-them into ``paper_2609_34060_b200/libkvc.so``.  The shared object sits beside
-the sources (it is git-ignored but travels with a snapshot of the tree).
+them into ``paper_2609_34060_b200/libkvc.so``, and ``csrc/marshal.cpp`` into
+``_marshal.so`` (the Python binding's argument blocks).  The shared objects sit beside
+the sources (they are git-ignored but travel with a snapshot of the tree).
 """
 from __future__ import annotations
 
@@ -11,11 +12,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libkvc.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -46,11 +49,11 @@ def _stamp(paths) -> str:
 
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) -> str:
     srcs = sources()
-    deps = srcs + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
+    deps = srcs + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh", ".cpp"))]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "kvc.h"))
     stamp = _stamp(deps)
     stamp_file = os.path.join(OBJ, "stamp")
-    if not force and os.path.exists(LIB) and os.path.exists(stamp_file) and open(stamp_file).read() == stamp:
+    if not force and os.path.exists(LIB) and os.path.exists(MARSHAL) and os.path.exists(stamp_file) and open(stamp_file).read() == stamp:
         return LIB
     os.makedirs(OBJ, exist_ok=True)
     nvcc = _nvcc()
@@ -63,6 +66,8 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
             print(" ".join(cmd))
         procs.append((s, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(o)
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL]
+    procs.append((cmd[-3], subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = False
     for s, p in procs:
         out, _ = p.communicate()

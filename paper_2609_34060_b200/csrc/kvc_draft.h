@@ -53,6 +53,51 @@ struct KeepLaunch {
   uint32_t* status;
 };
 
+// A call's arguments in one piece, as the Python binding hands them over (one argument costs it a third of nine).
+struct AppendRotatedCall {
+  const kvc_requests* req;
+  const kvc_rotary* rot;
+  void* cache;                 // kvc_cache or kvc_qcache
+  void* stream;
+  kvc_heads q, q_out, k_new, v_new;
+  int32_t layer, q8, has_q;
+  int32_t n_depth, n_pos;      // entries that depth and pos_begin hold; -1: there are none
+};
+struct AttendTreeCall {
+  const kvc_requests* req;
+  const kvc_tree* tree;
+  const void* cache;
+  float* lse;
+  void* workspace;
+  uint64_t workspace_bytes;
+  void* stream;
+  double scale;
+  kvc_heads q, out;
+  int32_t layer, q8;
+};
+struct VerifyCall {
+  const kvc_requests* req;
+  const int32_t* parent;
+  const int32_t* token;
+  const float* u;
+  const float* u_next;
+  int32_t* kept;
+  int32_t* n_kept;
+  int32_t* next;
+  void* stream;
+  kvc_probs target, draft;
+  int32_t stride, has_draft;
+};
+struct KeepCall {
+  const kvc_requests* req;
+  const int32_t* kept;
+  const int32_t* n_kept;
+  void* cache;
+  int32_t* kv_out;
+  void* stream;
+  int32_t stride, q8;
+};
+
 cudaError_t launch_tree_build(const TreeLaunch& t, cudaStream_t s);
 cudaError_t launch_append_rotated(const RotateLaunch& r, int d, cudaStream_t s);
 cudaError_t launch_verify(const VerifyLaunch& v, cudaStream_t s);

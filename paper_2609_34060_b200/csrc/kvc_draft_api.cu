@@ -225,4 +225,30 @@ int kvc_keep_q8(const kvc_requests* req, const int32_t* kept, int32_t kept_strid
   return rc != KVC_OK ? rc : keep_common(req, kept, kept_stride, n_kept, &cache->codes, cache, kv_out, a, stream);
 }
 
+// The same calls from one block of arguments (not part of kvc.h: the Python binding's way in).
+int kvc_block_append_rotated(const AppendRotatedCall* c) {
+  AppendRotatedCall x;
+  memcpy(&x, c, sizeof(x) - 4);                                   // the block ends with its last number
+  if ((x.n_depth >= 0 && x.n_depth < x.k_new.n_rows) || (x.n_pos >= 0 && x.n_pos < x.req->n)) return KVC_E_SHAPE;
+  const kvc_heads* q = x.has_q ? &x.q : nullptr;
+  kvc_heads* out = x.has_q ? &x.q_out : nullptr;
+  return x.q8 ? kvc_append_rotated_q8(x.req, x.rot, q, out, &x.k_new, &x.v_new, x.layer, reinterpret_cast<kvc_qcache*>(x.cache), x.stream)
+              : kvc_append_rotated(x.req, x.rot, q, out, &x.k_new, &x.v_new, x.layer, reinterpret_cast<kvc_cache*>(x.cache), x.stream);
+}
+int kvc_block_attend_tree(const AttendTreeCall* c) {
+  AttendTreeCall x = *c;
+  return x.q8 ? kvc_attend_tree_q8(x.req, x.tree, &x.q, reinterpret_cast<const kvc_qcache*>(x.cache), x.layer, x.scale, &x.out, x.lse, x.workspace,
+                                   (size_t)x.workspace_bytes, x.stream)
+              : kvc_attend_tree(x.req, x.tree, &x.q, reinterpret_cast<const kvc_cache*>(x.cache), x.layer, x.scale, &x.out, x.lse, x.workspace,
+                                (size_t)x.workspace_bytes, x.stream);
+}
+int kvc_block_verify(const VerifyCall* c) {
+  return kvc_verify(c->req, c->parent, c->token, &c->target, c->has_draft ? &c->draft : nullptr, c->u, c->u_next, c->kept, c->stride, c->n_kept, c->next,
+                    c->stream);
+}
+int kvc_block_keep(const KeepCall* c) {
+  return c->q8 ? kvc_keep_q8(c->req, c->kept, c->stride, c->n_kept, reinterpret_cast<kvc_qcache*>(c->cache), c->kv_out, c->stream)
+               : kvc_keep(c->req, c->kept, c->stride, c->n_kept, reinterpret_cast<kvc_cache*>(c->cache), c->kv_out, c->stream);
+}
+
 }  // extern "C"

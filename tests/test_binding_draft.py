@@ -1,6 +1,7 @@
 """What the binding checks before it hands addresses on: classes, types, shapes, strides.  (A stand-in for the library.)"""
 import copy
 import pickle
+import struct
 
 import pytest
 import torch
@@ -36,6 +37,21 @@ def refused(code, *calls):
         assert e.value.code == code, i
 
 
+def test_blocks():
+    """Argument blocks: what lies where, and what is no argument."""
+    q, p = z(3, 4, 64), torch.zeros(5, 9, dtype=torch.float32)
+    b = kvc._pack("PHpIii", "x", ("q", "p", "i"), -1, 64, 7, q[:, 1:3], p[1:3, :6], None, -2, 3)
+    want = struct.pack("@QQiiQQQiiQQii", 7, q.data_ptr() + 128, 3, 2, 256, 64, p.data_ptr() + 36, 2, 6, 9, 0, -2, 3)
+    assert b == want
+    assert len(kvc._pack("Hp", "x", ("q", "p"), -1, 64, z(1, 1, 64), torch.zeros(1, 1))) == 32 + 24
+    with pytest.raises(OverflowError):
+        kvc._pack("i", "x", (), -1, 0, 1 << 31)
+    with pytest.raises(TypeError):
+        kvc._pack("PP", "x", (), -1, 0, 1)
+    refused(-1, lambda: kvc._pack("H", "x", ("q",), 0, 64, q), lambda: kvc._pack("H", "x", ("q",), -1, 64, object()),
+            lambda: kvc._pack("A", "x", (), -1, 0, q[:, ::2]), lambda: kvc._pack("F", "x", (), -1, 0, z(3)))
+
+
 def test_tree(fake):
     refused(-1, lambda: kvc.Tree([0, 1], 3), lambda: kvc.Tree(z(3, dtype=torch.int64), 3), lambda: kvc.Tree(z(6, dtype=I32)[::2], 3),
             lambda: kvc.Tree(z(3, dtype=I32), 3, mask=z(3, 1, dtype=torch.uint8)))
@@ -54,12 +70,21 @@ def test_tree(fake):
 def test_rotary():
     refused(-1, lambda: kvc.Rotary(1e4), lambda: kvc.Rotary(kvc.Rope(1e4), amplitude=0.0), lambda: kvc.Rotary(kvc.Rope(1e4), depth=z(3, dtype=torch.int64)))
     r = kvc.Rotary(kvc.Rope(1e4, inv_freq=[1.0] * 16))
-    refused(-2, lambda: r._for(64, 1, 1), lambda: kvc.Rotary(kvc.Rope(1e4), depth=z(3, dtype=I32))._for(64, 4, 1),
-            lambda: kvc.Rotary(kvc.Rope(1e4), pos_begin=z(3, dtype=I32))._for(64, 1, 4))
-    kvc.Rotary(kvc.Rope(1e4, inv_freq=[1.0] * 16), rot_dim=32)._for(64, 1, 1)
+    refused(-2, lambda: r._for(64))
+    kvc.Rotary(kvc.Rope(1e4, inv_freq=[1.0] * 16), rot_dim=32)._for(64)
     assert copy.deepcopy(kvc.Rotary(kvc.Rope(1e4), rot_dim=32, amplitude=1.5)).struct().amplitude == 1.5
     with pytest.raises(AttributeError):
         r.depth = None
+
+
+def test_lists_of_positions_that_are_too_short(monkeypatch):
+    """The library itself: refused before it looks at a device."""
+    monkeypatch.setattr(kvc, "_here", lambda what, stream, made, *tensors: 0)
+    c, q8, req, tree, _ = objects()
+    k = z(3, 2, 64)
+    for cache in (c, q8):
+        for rot in (kvc.Rotary(kvc.Rope(1e4), depth=z(2, dtype=I32)), kvc.Rotary(kvc.Rope(1e4), pos_begin=z(0, dtype=I32))):
+            refused(-2, lambda: kvc.kvc_append_rotated(req, rot, k, k.clone(), cache, 0))
 
 
 def test_scaled_frequencies():
@@ -77,7 +102,7 @@ def test_append_rotated(fake):
     k, q = z(3, 2, 64), z(3, 4, 64)
     kvc.kvc_append_rotated(req, rot, k, k, c, 0, q=q, q_out=q)
     kvc.kvc_append_rotated(req, rot, k, k, q8, 0)
-    assert fake.calls == ["kvc_append_rotated", "kvc_append_rotated_q8"]
+    assert fake.calls == ["kvc_block_append_rotated"] * 2
     refused(-1, lambda: kvc.kvc_append_rotated(req, kvc.Rope(1e4), k, k, c, 0), lambda: kvc.kvc_append_rotated(rot, req, k, k, c, 0),
             lambda: kvc.kvc_append_rotated(req, rot, k, k, c, 0, q=q), lambda: kvc.kvc_append_rotated(req, rot, k, k, c, 0, q_out=q),
             lambda: kvc.kvc_append_rotated(req, rot, k.float(), k, c, 0), lambda: kvc.kvc_append_rotated(req, rot, k, k, k, 0))
@@ -91,7 +116,7 @@ def test_attend_tree(fake):
     q = z(3, 4, 64)
     kvc.kvc_attend_tree(req, tree, q, c, 0, q.clone())
     kvc.kvc_attend_tree(req, tree, q, q8, 0, q.clone(), lse=z(3, 4, dtype=torch.float32))
-    assert fake.calls == ["kvc_attend_tree", "kvc_attend_tree_q8"]
+    assert fake.calls == ["kvc_block_attend_tree"] * 2
     refused(-1, lambda: kvc.kvc_attend_tree(req, None, q, c, 0, q.clone()), lambda: kvc.kvc_attend_tree(tree, req, q, c, 0, q.clone()),
             lambda: kvc.kvc_attend_tree(req, tree, q, tree, 0, q.clone()), lambda: kvc.kvc_attend_tree(req, tree, q, c, 0, q.clone(), lse=z(3, 4)),
             lambda: kvc.kvc_attend_tree(req, tree, q, c, 0, q.clone(), workspace=z(8, 8)[:, ::2]))
@@ -105,7 +130,7 @@ def test_verify(fake):
     call = lambda **kw: kvc.kvc_verify(req, **{**good, **kw})
     call()
     call(draft=f(3, 16)[:, :10], kept=i(1, 7))
-    assert fake.calls == ["kvc_verify"] * 2
+    assert fake.calls == ["kvc_block_verify"] * 2
     refused(-1, lambda: call(target=z(3, 10)), lambda: call(draft=f(3, 10).double()), lambda: call(parent=f(3)), lambda: call(u=f(3).double()),
             lambda: call(token=i(6)[::2]), lambda: call(kept=f(1, 3)), lambda: kvc.kvc_verify(tree, **good), lambda: call(n_kept=f(1)), lambda: call(u_next=i(1)))
     refused(-2, lambda: call(parent=i(4)), lambda: call(token=i(2)), lambda: call(u=f(4)), lambda: call(kept=i(1, 2)), lambda: call(kept=i(2, 3)),
@@ -119,7 +144,7 @@ def test_keep(fake):
     i = lambda *s: z(*s, dtype=I32)
     kvc.kvc_keep(req, i(1, 3), i(1), c, i(1))
     kvc.kvc_keep(req, i(1, 5), i(1), q8)
-    assert fake.calls == ["kvc_keep", "kvc_keep_q8"]
+    assert fake.calls == ["kvc_block_keep"] * 2
     refused(-1, lambda: kvc.kvc_keep(req, i(1, 3).long(), i(1), c), lambda: kvc.kvc_keep(req, i(1, 3), i(1).long(), c), lambda: kvc.kvc_keep(req, i(1, 3), i(1), req),
             lambda: kvc.kvc_keep(c, i(1, 3), i(1), c), lambda: kvc.kvc_keep(req, i(1, 6)[:, ::2], i(1), c))
     refused(-2, lambda: kvc.kvc_keep(req, i(1, 2), i(1), c), lambda: kvc.kvc_keep(req, i(2, 3), i(1), c), lambda: kvc.kvc_keep(req, i(1, 3), i(2), c),
