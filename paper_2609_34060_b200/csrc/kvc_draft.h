@@ -18,7 +18,7 @@ struct RotateLaunch {
   DevHeads q, qo, kn, vn;
   DevCache dst;
   DevScale e;
-  int32_t Hq, H, layer, rot, pairing;
+  int32_t Hq, H, layer, rot, pairing, tokens;   // tokens a block
   float amplitude;
   const int32_t* depth;
   const int32_t* pos_begin;
