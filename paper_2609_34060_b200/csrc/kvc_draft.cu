@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(256) tree_build_kernel(const __grid_constant__
   }
 }
 
-constexpr int kKeepThreads = 256, kRowsAtOnce = 32, kInFlight = 8;
+constexpr int kKeepThreads = 128, kRowsAtOnce = 32, kInFlight = 4;
 
 // A thread owns 16 bytes of a row in one (layer, head, K|V) and moves them for the request's accepted rows in their order,
 // kInFlight loads and then as many stores.  Places are ascending, so a row's new place is never one that a later row is
@@ -60,7 +60,8 @@ constexpr int kKeepThreads = 256, kRowsAtOnce = 32, kInFlight = 8;
 template <int D, bool Q8>
 __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constant__ KeepLaunch p) {
   constexpr int CH = D * (Q8 ? 1 : 2) / 16;
-  __shared__ int64_t s_src[kRowsAtOnce], s_dst[kRowsAtOnce], s_esrc[kRowsAtOnce], s_edst[kRowsAtOnce];
+  __shared__ int64_t s_src[kRowsAtOnce], s_dst[kRowsAtOnce], s_esrc[kRowsAtOnce], s_edst[kRowsAtOnce];   // of the rows that move
+  __shared__ int s_n;
   grid_dependency_wait();
   grid_dependents_launch();
   const int tid = threadIdx.x;
@@ -77,7 +78,8 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
     const int32_t* kept = p.kept + (int64_t)b * p.stride;
     const bool first_block = blockIdx.x == 0 && tid == 0;
     const int nk = p.n_kept[b];
-    int place = tid < p.req.max_q ? kept[tid] : 0;              // asked for before the lengths are there
+    // the first places and the ones before them, asked for before the lengths are there
+    const int place = tid < p.req.max_q ? kept[tid] : 0, place_before = tid > 0 && tid < p.req.max_q ? kept[tid - 1] : -1;
     int q0, nq, kv;
     const bool valid = request_span(p.req, b, first_block ? p.status : nullptr, q0, nq, kv);
     const int first = kv - nq;
@@ -85,7 +87,7 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
     if (!bad) {
       for (int j = tid; j < nk; j += kKeepThreads) {
         const int a = j == tid ? place : kept[j];
-        bad |= a >= nq || a <= (j > 0 ? kept[j - 1] : -1);
+        bad |= a >= nq || a <= (j == tid ? place_before : kept[j - 1]);
       }
     }
     bad = __syncthreads_or(bad);
@@ -95,39 +97,42 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
     }
     if (bad || !valid) continue;
     for (int j0 = 0; j0 < nk; j0 += kRowsAtOnce) {
-      const int n = min(kRowsAtOnce, nk - j0);
       if (j0 > 0) __syncthreads();
-      if (tid < n) {
-        const int j = j0 + tid, a = j0 == 0 ? place : kept[j];
-        int64_t src = -1;
+      if (tid < kRowsAtOnce) {                                   // one warp
+        const int j = j0 + tid, a = j >= nk ? j : j0 == 0 ? place : kept[j];
+        int ps = -1, pd = -1;
         if (a != j) {
-          const int ps = is_paged(p.c) ? request_page(p.req, p.c, b, first + a, p.status) : 0;
-          const int pd = is_paged(p.c) ? request_page(p.req, p.c, b, first + j, p.status) : 0;
-          if (ps >= 0 && pd >= 0) {
-            src = row_off(p.c, 0, 0, first + a, ps);
-            s_dst[tid] = row_off(p.c, 0, 0, first + j, pd);
-            if (Q8) {
-              s_esrc[tid] = exp_off(p.e, p.c, 0, 0, first + a, ps);
-              s_edst[tid] = exp_off(p.e, p.c, 0, 0, first + j, pd);
-            }
+          ps = is_paged(p.c) ? request_page(p.req, p.c, b, first + a, p.status) : 0;
+          pd = is_paged(p.c) ? request_page(p.req, p.c, b, first + j, p.status) : 0;
+        }
+        const bool moves = ps >= 0 && pd >= 0;
+        const unsigned all = __ballot_sync(0xffffffffu, moves);
+        if (moves) {
+          const int at = __popc(all & ((1u << tid) - 1u));
+          s_src[at] = row_off(p.c, 0, 0, first + a, ps);
+          s_dst[at] = row_off(p.c, 0, 0, first + j, pd);
+          if (Q8) {
+            s_esrc[at] = exp_off(p.e, p.c, 0, 0, first + a, ps);
+            s_edst[at] = exp_off(p.e, p.c, 0, 0, first + j, pd);
           }
         }
-        s_src[tid] = src;
+        if (tid == 0) s_n = __popc(all);
       }
       __syncthreads();
+      const int n = s_n;
       if (live) {
         for (int k0 = 0; k0 < n; k0 += kInFlight) {
           uint4 x[kInFlight];
           uint8_t e[kInFlight];
 #pragma unroll
           for (int k = 0; k < kInFlight; ++k) {
-            if (k0 + k >= n || s_src[k0 + k] < 0) continue;
+            if (k0 + k >= n) continue;
             x[k] = *reinterpret_cast<const uint4*>(rows + s_src[k0 + k] * (Q8 ? 1 : 2));
             if (exponent) e[k] = exps[s_esrc[k0 + k]];
           }
 #pragma unroll
           for (int k = 0; k < kInFlight; ++k) {
-            if (k0 + k >= n || s_src[k0 + k] < 0) continue;
+            if (k0 + k >= n) continue;
             *reinterpret_cast<uint4*>(rows + s_dst[k0 + k] * (Q8 ? 1 : 2)) = x[k];
             if (exponent) exps[s_edst[k0 + k]] = e[k];
           }
