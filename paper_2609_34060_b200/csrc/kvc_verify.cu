@@ -26,7 +26,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kCluster = 8;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 16;
 constexpr int kRowBytes = 24;              // of shared memory for a row of the request
 constexpr int kStep = 128;                 // entries a warp takes at a time
 
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
   int* s_gone = s_token + p.req.max_q;
   int16_t* s_parent = reinterpret_cast<int16_t*>(s_gone + p.req.max_q);
   int16_t* s_path = s_parent + p.req.max_q;
-  __shared__ double s_warp[kWarps], s_block[2][kCluster];
+  __shared__ double s_warp[kWarps], s_block[2][kMaxCluster];
   __shared__ Node s_at;
   __shared__ int s_more, s_kept;
   cg::cluster_group cluster = cg::this_cluster();
@@ -114,11 +114,12 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
   struct Four {
     float p[4], q[4];
   };
-  auto fetch = [&](const float* pt, const float* pd, int64_t at, int64_t hi, Four& x) {
+  auto fetch = [&](const float* pt, const float* pd, int64_t at, int64_t hi, Four& x) {   // pd == nullptr: P is p's
+    x.q[0] = x.q[1] = x.q[2] = x.q[3] = 0.f;
     if (kWide && at + 4 <= hi) {
       const float4 v = __ldg(reinterpret_cast<const float4*>(pt + at));
       x.p[0] = v.x, x.p[1] = v.y, x.p[2] = v.z, x.p[3] = v.w;
-      if (kDraft) {
+      if (kDraft && pd) {
         const float4 w = __ldg(reinterpret_cast<const float4*>(pd + at));
         x.q[0] = w.x, x.q[1] = w.y, x.q[2] = w.z, x.q[3] = w.w;
       }
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         x.p[k] = at + k < hi ? __ldg(pt + at + k) : 0.f;
-        if (kDraft) x.q[k] = at + k < hi ? __ldg(pd + at + k) : 0.f;
+        if (kDraft && pd) x.q[k] = at + k < hi ? __ldg(pd + at + k) : 0.f;
       }
     }
   };
@@ -142,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
   // sum of P over the vocabulary, the same in all threads of the cluster
   auto sum_all = [&](int node, double A, double B, int gone) {
     const float* pt = p.target + (int64_t)(q0 + node) * p.s_target;
-    const float* pd = kDraft ? p.draft + (int64_t)(q0 + node) * p.s_draft : nullptr;
+    const float* pd = kDraft && B != 0.0 ? p.draft + (int64_t)(q0 + node) * p.s_draft : nullptr;
     int64_t lo, hi;
     warp_range(warp, lo, hi);
     double sum = 0.0;
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
   // the warp's part once more, by the whole block: a thread a run of entries, one scan over the threads
   const int part = find(s_warp, kWarps, before);
   const float* pt = p.target + (int64_t)(q0 + n.node) * p.s_target;
-  const float* pd = kDraft ? p.draft + (int64_t)(q0 + n.node) * p.s_draft : nullptr;
+  const float* pd = kDraft && n.B != 0.0 ? p.draft + (int64_t)(q0 + n.node) * p.s_draft : nullptr;
   int64_t lo, hi;
   warp_range(part, lo, hi);
   const int run = (per_warp + 4 * kThreads - 1) / (4 * kThreads) * 4;
@@ -345,7 +346,17 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
 
 template <bool kDraft, bool kWide>
 cudaError_t launch(const VerifyLaunch& v, cudaStream_t s) {
-  const int blocks = v.vocab <= 4096 ? 1 : kCluster;
+  // A small vocabulary is one block's.  Else eight blocks a request (four fit on an SM: 74 requests at once), or, while all
+  // requests are resident with them, sixteen: 4 / 16 trees over 128000 entries 20 / 27 us with eight, 15 / 20 with sixteen;
+  // 64 trees 42 and 45.
+  const int blocks = v.vocab <= 4096 ? 1 : v.req.n <= 32 ? kMaxCluster : kMaxCluster / 2;
+  static DeviceOnce once;
+  int dev;
+  if (once.pending(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(verify_kernel<kDraft, kWide>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    once.mark(dev);
+  }
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;

@@ -66,7 +66,7 @@ class Case:
 @pytest.mark.parametrize("drawn", [True, False], ids=["drawn", "chosen"])
 @pytest.mark.parametrize("nq,V,kind", [([1], 1, "tree"), ([4], 3, "tree"), ([6], 1000, "chain"), ([5, 0, 9, 1], 127, "tree"), ([12] * 20, 50, "tree"),
                                        ([8, 16], 4096, "tree"), ([8, 3], 4097, "chain"), ([10] * 5, 32000, "tree"), ([7, 7], 50001, "tree"),
-                                       ([200, 90], 600, "tree"), ([3], 131072, "tree")])
+                                       ([200, 90], 600, "tree"), ([3], 131072, "tree"), ([5] * 40, 6001, "tree")])
 def test_against_the_oracle(nq, V, kind, drawn):
     for seed in range(3):
         c = Case(nq, V, kind, drawn, seed=seed, sharp=1.0 + 2 * seed, near=(1.0, 0.2, 3.0)[seed])
