@@ -88,7 +88,7 @@ struct Shape {
   static constexpr int kThreads = Q8 ? 512 : 384;
   static constexpr int kRegs = kDirect ? 152 : Q8 ? 184 : 208;    // of the softmax warps
   static constexpr int kRegsOthers = kDirect ? 104 : Q8 ? 72 : 88;
-  static constexpr int kSmem = 1024 + kQTiles * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0) + (kDirect ? kKeySlots * kRaw + kScales * 512 : 0);
+  static constexpr int kSmem = 1024 + kQTiles * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0) + (kDirect ? kKeySlots * kRaw + kScales * 512 + 8192 : 0);
 };
 
 // Key tiles of unit u of a request (at least one, so that rows without keys are answered too), and of its two row tiles.
@@ -257,7 +257,7 @@ __device__ __forceinline__ Walk line_start(const ChunkLaunch& p, int lane, int c
 
 template <int NS, int NR, int NK = 1, int NE = 1>
 struct Bars {
-  uint64_t q_full[2], s_full[2], p_ready[2][2], o_done[2];
+  uint64_t q_full[2], s_full[2], p_ready[2][2], o_done[2], o_most[2];   // o_most: the first 96 keys' product (kDirect)
   uint64_t full[NS], empty[NS], raw_full[NR], raw_empty[NR], key_full[NK], key_empty[NK], scale_full[NE], scale_empty[NE], piece_full[kPieces], piece_empty[kPieces];
   Piece piece[kPieces];
   uint32_t tmem;
@@ -324,10 +324,11 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
   uint8_t* sraw = skv + SH::kSlots * SH::kTile;
   uint8_t* skey = sraw + SH::kRawSlots * SH::kRaw;                // kDirect
   float* sscale = reinterpret_cast<float*>(skey + SH::kKeySlots * SH::kRaw);   // [kScales][128]
+  float* stwin = sscale + SH::kScales * 128;                      // [2][16][64] sums on their way from a row's second lane to its first
   constexpr bool kDirect = SH::kDirect;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort_flag = &bars.abort_flag;
-  const uint32_t q_full = smem_u32(bars.q_full), s_full = smem_u32(bars.s_full), p_ready = smem_u32(bars.p_ready), o_done = smem_u32(bars.o_done);
+  const uint32_t q_full = smem_u32(bars.q_full), s_full = smem_u32(bars.s_full), p_ready = smem_u32(bars.p_ready), o_done = smem_u32(bars.o_done), o_most = smem_u32(bars.o_most);
   const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), rfull = smem_u32(bars.raw_full), rempty = smem_u32(bars.raw_empty);
   const uint32_t piece_full = smem_u32(bars.piece_full), piece_empty = smem_u32(bars.piece_empty);
   const uint32_t key_full = smem_u32(bars.key_full), key_empty = smem_u32(bars.key_empty), scale_full = smem_u32(bars.scale_full), scale_empty = smem_u32(bars.scale_empty);
@@ -338,6 +339,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       mbar_init(p_ready + 16 * t, 128);
       mbar_init(p_ready + 16 * t + 8, 128);
       mbar_init(o_done + 8 * t, 1);
+      mbar_init(o_most + 8 * t, 1);
     }
     for (int s = 0; s < SH::kSlots; ++s) {
       mbar_init(full + 8 * s, Q8 ? 128 : 1);
@@ -402,8 +404,11 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
     // queries of a piece's row tile, a thread its row, all loads in flight at once; 8-bit caches: channels 1 and 2 of
     // every four change places, as their keys do
     float q_scale = 1.f;                                          // kDirect: of the row's codes, in the piece whose queries were loaded last
+    // kDirect, at most 64 rows: a row has two lanes, which take half of a tile's keys each (their probabilities of the other
+    // half are zeros), so that all eight warps work
+    auto row_of = [&](const Piece& y) { return y.u * kUnitRows + tile_row + (kDirect && y.rows <= 64 ? row & 63 : row); };
     auto load_q = [&](const Piece& y) {                           // kSplit: the first half's threads, for both
-      const int r = y.u * kUnitRows + tile_row + row, tok = r / p.a.G;
+      const int r = row_of(y), tok = r / p.a.G;
       const bool live = r < y.rows;
       const uint4* src = reinterpret_cast<const uint4*>(p.a.q.p + (live ? (int64_t)(y.q0 + tok) * p.a.q.s_row + (int64_t)(y.h * p.a.G + r - tok * p.a.G) * p.a.q.s_head : 0));
       uint8_t* dst = sq + (kSplit ? 0 : t * SH::kTile) + (row >> 3) * 1024 + (row & 7) * 128;
@@ -479,7 +484,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       const uint32_t* mask = nullptr;                             // kTree: the row's words
       const int fresh = kv - y.nq;                                // first new token
       {
-        const int r = y.u * kUnitRows + tile_row + row;
+        const int r = row_of(y);
         if (r < y.rows) {
           lim = p.a.causal ? kv - y.nq + r / p.a.G : kv - 1;
           if (kTree) mask = p.a.mask + (int64_t)(y.q0 + r / p.a.G) * p.a.words;
@@ -488,6 +493,8 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       const int lowest = __reduce_min_sync(0xffffffffu, lim);     // of the warp's rows
       const bool idle = kSplit && lowest == 0x7fffffff;           // a warp without rows hands on whatever its lanes hold
       const float c = kDirect ? c_all * q_scale : c_all;          // kDirect: logits are those of the codes
+      const bool twin = kDirect && y.rows <= 64, second = twin && row >= 64;
+      const int key0 = second ? 64 : 0, key1 = twin && !second ? 64 : 128;   // the lane's keys of a tile
       float m = minus_inf, l = 0.f;
       float mc = minus_inf;                                       // kDirect: the maximum, times c
       float late = minus_inf;                                     // a maximum that m is to follow
@@ -545,9 +552,9 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           f32x2 sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
           constexpr int W = 32;                                   // 16: 128 us
           float next[W];
-          tmem_ld32(s_at, next);
+          tmem_ld32(s_at + key0, next);
 #pragma unroll 1
-          for (int q = 0; q < 128; q += W) {
+          for (int q = key0; q < key1; q += W) {
             float s[W];
             tmem_ld_wait();
 #pragma unroll
@@ -556,7 +563,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
               f2_unpack(f2_mul(f2_pack(next[k], next[k + 1]), f2_pack(e.x, e.y)), s[k], s[k + 1]);
               f2_unpack(f2_mul(f2_pack(next[k + 2], next[k + 3]), f2_pack(e.z, e.w)), s[k + 2], s[k + 3]);
             }
-            if (q + W < 128) tmem_ld32(s_at + q + W, next);
+            if (q + W < key1) tmem_ld32(s_at + q + W, next);
             if (hidden) {
               const int last = lim - t0 - q;                      // of the part's keys
               uint32_t bits = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1u;
@@ -581,8 +588,11 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
               f2_scale(sum2[0], keep);
               f2_scale(sum2[1], keep);
               tmem_ld_wait();
+              // The first 96 probabilities may be in their product by the last part: then the sums are scaled behind that
+              // one, otherwise the probabilities before this part and the sums before this tile.
+              const bool late = !twin && q == 128 - W;
 #pragma unroll 1
-              for (int k = 0; k < q / 2; k += 8) {
+              for (int k = key0 / 2; k < q / 2 && !late; k += 8) {
                 uint32_t w[8];
                 tmem_ld8(s_at + k, reinterpret_cast<float*>(w));
                 tmem_ld_wait();
@@ -591,8 +601,8 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
                 for (int j = 0; j < 8; ++j) w[j] = mul_bf16x2(w[j], two);
                 tmem_st8(s_at + k, w);
               }
-              if (it > 0) {                                       // the sums so far, once the product that wrote them last is done
-                wait(o_done + 8 * t, par ^ 1);
+              if (it > 0 || late) {                               // the sums so far, once the product that wrote them last is done
+                wait(late ? o_most + 8 * t : o_done + 8 * t, late ? par : par ^ 1);
                 tc_fence_after();
 #pragma unroll 1
                 for (int k = 0; k < D; k += 8) {
@@ -618,11 +628,22 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
               w[k] = f2_to_bf16x2(e);
             }
             tmem_st16(s_at + q / 2, w);                     // over logits that have been read
-            if (q + W == 96 || q + W == 128) {                    // behind 96 and behind all 128 keys
+            if (!twin && (q + W == 96 || q + W == 128)) {         // behind 96 and behind all 128 keys
               tmem_st_wait();
               tc_fence_before();
               mbar_arrive(pr + (q + W == 96 ? 0 : 8));
             }
+          }
+          if (twin) {                                             // nothing of the other lane's keys
+            uint32_t none[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) none[k] = 0;
+            tmem_st16(s_at + 32 - key0 / 2, none);
+            tmem_st16(s_at + 48 - key0 / 2, none);
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(pr);
+            mbar_arrive(pr + 8);
           }
           mbar_arrive(scale_empty + 8 * es);
           float a, b;
@@ -736,27 +757,38 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       more = next_piece(piece + 1);
       if (n > 0) wait(o_done + 8 * t, (uint32_t)(count - 1) & 1u);
       tc_fence_after();
-      const int r = y.u * kUnitRows + tile_row + row;
+      const int r = row_of(y);
       const bool live = r < y.rows;
       const int tok = r / p.a.G, head = y.h * p.a.G + r - tok * p.a.G;
       if (kDirect) m = mc / c_all;
       float keep = 1.f, other = 0.f;                              // kSplit: weights of this half's sums and of the other's
       const int n_other = kSplit ? y.n[t ^ 1] : 0;
       if constexpr (kSplit) {
-        float2 o;                                                 // the other half's maximum, then its sum
+        // maxima and then sums of the others that have the row: the other half, and the row's other lane in both
+        float om[3], ol[3] = {0.f, 0.f, 0.f};
         meet.half[t][row] = m;
         tc_fence_before();
         named_bar_sync(1, 256);
         tc_fence_after();
-        o.x = meet.half[t ^ 1][row];
+        om[0] = meet.half[t ^ 1][row];
+        om[1] = meet.half[t][row ^ 64];
+        om[2] = meet.half[t ^ 1][row ^ 64];
         named_bar_sync(1, 256);
         meet.half[t][row] = l;
         named_bar_sync(1, 256);
-        o.y = meet.half[t ^ 1][row];
-        const float top = o.y == 0.f ? m : l == 0.f ? o.x : fmaxf(m, o.x);
-        keep = l == 0.f ? 0.f : exp2_fast((m - top) * c_all);
-        other = o.y == 0.f ? 0.f : exp2_fast((o.x - top) * c_all);
-        l = keep * l + other * o.y;
+        ol[0] = meet.half[t ^ 1][row];
+        if (twin) {
+          ol[1] = meet.half[t][row ^ 64];
+          ol[2] = meet.half[t ^ 1][row ^ 64];
+        }
+        float top = l == 0.f ? minus_inf : m;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) top = ol[k] == 0.f ? top : fmaxf(top, om[k]);
+        auto weight = [&](float m_, float l_) { return l_ == 0.f ? 0.f : exp2_fast((m_ - top) * c_all); };
+        keep = weight(m, l);
+        other = weight(om[0], ol[0]);
+        l = keep * l + other * ol[0];
+        if (twin) l += weight(om[1], ol[1]) * ol[1] + weight(om[2], ol[2]) * ol[2];
         m = top;
       }
       // no key seen: decided by the sum, which a NaN logit makes NaN (maxima pass over NaN: m may still be minus infinity)
@@ -785,8 +817,21 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           // a half that saw no key of the row gets no weight, whatever its accumulators hold
 #pragma unroll
           for (int j = 0; j < 16; ++j) o[j] = (keep == 0.f ? 0.f : o[j] * keep) + (other == 0.f ? 0.f : v[j] * other);
+          if (twin) {
+            float* at = stwin + t * 1024 + (row & 63);
+            if (second) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) at[j * 64] = o[j];
+            }
+            named_bar_sync(3 + t, 128);
+            if (!second) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] += at[j * 64];
+            }
+            named_bar_sync(3 + t, 128);                           // before the next channels
+          }
         }
-        if (!live || !ok) continue;
+        if (!live || !ok || second) continue;
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] = dead ? 0.f : o[j] * inv;
         if (Q8) {                                                 // channels back in their places
@@ -804,7 +849,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           for (int j = 0; j < 16; ++j) pdst[(k + j) * kUnitRows] = o[j];
         }
       }
-      if (live && ok && (!kSplit || t == 0)) {
+      if (live && ok && !second && (!kSplit || t == 0)) {
         if (!whole)
           *reinterpret_cast<float2*>(p.ml + 2 * slot) = make_float2(m, l);
         else if (p.a.lse)
@@ -941,6 +986,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             if (elect_one()) {
 #pragma unroll
               for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, i > 1 || k > 0);
+              if (kDirect) umma_commit(o_most + 8 * t);
             }
             if (!wait(p_ready + 16 * t + 8, par)) break;
             tc_fence_after();

@@ -38,6 +38,27 @@ def test_trees(i, q8):
     b.check_tree(out, lse)
 
 
+@pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nq,kv,G", [([12], [3000], 4), ([16, 9, 2], [2500, 64, 1900], 4), ([25, 32, 7], [1800, 140, 2200], 4), ([128], [1000], 1), ([5, 5], [129, 63], 13)])
+def test_one_row_tile(nq, kv, G, d, q8):
+    """33 to 128 rows, units cut into pieces and whole ones, lengths on and off the tiles' halves."""
+    b = TreeBuilt(Step(nq, kv, G=G, d=d, q8=q8, seed=sum(kv)))
+    out, lse = b.run_tree()
+    b.check_tree(out, lse)
+    again, lse2 = b.run_tree()
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
+@pytest.mark.parametrize("ramp", [60.0, -60.0, 400.0])
+@pytest.mark.parametrize("m", [10, 30])
+def test_rising_and_falling_logits(m, ramp, q8):
+    """Keys that grow or shrink with their position: maxima move inside tiles, far above what came before."""
+    b = TreeBuilt(Step([m], [700], G=4, q8=q8, ramp=ramp, seed=m))
+    b.check_tree(*b.run_tree())
+
+
 @pytest.mark.parametrize("nq,kv,G", [([6, 3], [90, 200], 4), ([70], [300], 2)])
 @pytest.mark.parametrize("q8", [False, True], ids=["bf16", "q8"])
 def test_a_chain_is_causal_attention(nq, kv, G, q8):
