@@ -720,7 +720,7 @@ int kvc_append_rotated_q8(const kvc_requests *req, const kvc_rotary *rot, const 
  * a <= j whose bits are set in its mask (bits beyond j are not looked at; the masks may be kvc_tree_build's or the caller's
  * own).  A row that sees nothing gets zeros and minus infinity.  parent and depth of the tree are not used.  Workspace,
  * rounding, limits and errors as in kvc_attend; max_q up to KVC_TREE_MAX_Q.  One thing differs: over an 8-bit cache, where
- * max_q times query heads per KV head is 33 to 128, a query meets the codes as two e4m3 parts whose sum is off by at most
+ * max_q times query heads per KV head is 17 to 128, a query meets the codes as two e4m3 parts whose sum is off by at most
  * 2^-17 of the query's largest channel in each of the others (exact in those above 2^-10 of it).
  */
 int kvc_attend_tree(const kvc_requests *req, const kvc_tree *tree, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale,

@@ -58,6 +58,10 @@ using namespace tc;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f, kJump = 16.f; // log2 of the growth of a row's maximum that is let pass, and that a tile bears
 constexpr int kUnitRows = 256;
+// rows a cut unit's partial result has room for
+constexpr int slot_rows(bool split) { return split ? 128 : kUnitRows; }
+// trees whose requests have more rows than this and at most 128 share a row tile between the halves of a block (kSplit below)
+constexpr int kSplitAbove = 16, kSplitRows = 128;
 
 struct alignas(16) UnitStart {             // where a block's part of the line begins; b < 0: it has none
   int32_t b, h, u, t;
@@ -794,7 +798,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       // no key seen: decided by the sum, which a NaN logit makes NaN (maxima pass over NaN: m may still be minus infinity)
       const bool dead = l == 0.f;
       const bool whole = y.whole;
-      const int64_t slot = ((int64_t)blockIdx.x * 2 + (y.t0 > 0 ? 0 : 1)) * kUnitRows + tile_row + row;
+      const int64_t slot = ((int64_t)blockIdx.x * 2 + (y.t0 > 0 ? 0 : 1)) * slot_rows(kSplit) + tile_row + row;
       const float inv = whole ? (dead ? 0.f : 1.f / l) : 1.f;
       __nv_bfloat16* dst = p.a.out.p + (int64_t)(y.q0 + tok) * p.a.out.s_row + (int64_t)head * p.a.out.s_head;
       // partial sums lie channel by channel: a warp's rows are neighbours
@@ -846,7 +850,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           store32(dst + k, pack8(o), pack8(o + 8));
         } else if (n + n_other > 0) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) pdst[(k + j) * kUnitRows] = o[j];
+          for (int j = 0; j < 16; ++j) pdst[(k + j) * slot_rows(kSplit)] = o[j];
         }
       }
       if (live && ok && !second && (!kSplit || t == 0)) {
@@ -1199,14 +1203,15 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
 // several pieces are in flight at once.  Few units in many pieces (four a unit and more) take more and smaller blocks, CH = 4:
 // 427 rows over 3133 keys, 25 pieces a unit: 19 us in all, 40 with a thread a row and piece after piece.  Many
 // units in two or three pieces each take CH = D / 8 (2K tokens behind 8K 212 us, by small blocks 217).
-template <int D, int CH>
+template <int D, int CH, int kSlotRows>
 __global__ void __launch_bounds__(256) attend_chunk_join_kernel(const __grid_constant__ ChunkLaunch p) {
   constexpr int kJoinPieces = CH == 4 ? 64 : 16;                  // weights held at once
   __shared__ float s_w[kJoinPieces][32], s_part[8][32];
   grid_dependents_launch();
   grid_dependency_wait();                                         // in every block, also those with nothing to join
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row = (int)(blockIdx.y & 7) * 32 + lane, ch = ((int)(blockIdx.y >> 3) * 8 + warp) * CH;
+  constexpr int kRowBlocks = kSlotRows / 32;
+  const int row = (int)(blockIdx.y % kRowBlocks) * 32 + lane, ch = ((int)(blockIdx.y / kRowBlocks) * 8 + warp) * CH;
   UnitStart me;
   int j, pieces;                                                  // blocks j - 1, j, ...
   if constexpr (CH == 4) {                                        // x is a unit: the borders that lie inside it
@@ -1244,16 +1249,16 @@ __global__ void __launch_bounds__(256) attend_chunk_join_kernel(const __grid_con
   const int r = me.u * kUnitRows + row, rows = nq * p.a.G;
   if (r - lane >= rows) return;
   const float c = p.a.scale * kLog2e, minus_inf = __uint_as_float(0xff800000u);
-  auto place = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0 ? 1 : 0)) * kUnitRows; };
+  auto place = [&](int i) { return ((int64_t)(j - 1 + i) * 2 + (i == 0 ? 1 : 0)) * kSlotRows; };
   auto held = [&](int i) { return *reinterpret_cast<const float2*>(p.ml + 2 * (place(i) + row)); };
   constexpr int kAtOnce = CH == 4 ? 8 : 16 / CH;                                // pieces whose sums are in flight: before their weights are known
   float x[kAtOnce][CH];
   auto load = [&](int i0) {
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const float* o = p.part + place(i0 + k) * D + row + ch * kUnitRows;
+      const float* o = p.part + place(i0 + k) * D + row + ch * kSlotRows;
 #pragma unroll
-      for (int q = 0; q < CH; ++q) x[k][q] = i0 + k < pieces ? o[q * kUnitRows] : 0.f;
+      for (int q = 0; q < CH; ++q) x[k][q] = i0 + k < pieces ? o[q * kSlotRows] : 0.f;
     }
   };
   load(0);
@@ -1339,8 +1344,10 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
   }
   const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8, kTree, kSplit>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
   if (e != cudaSuccess || p.blocks < 2) return e;
-  if (p.fine) return launch_after(attend_chunk_join_kernel<D, 4>, dim3((unsigned)chunk_units(p.a.req.n, p.a.req.max_q, p.a.G, p.a.H), 8 * (D / 32)), 256, 0, s, p);
-  return launch_after(attend_chunk_join_kernel<D, D / 8>, dim3((unsigned)p.blocks - 1, 8), 256, 0, s, p);
+  constexpr int kSlotRows = slot_rows(kSplit), kRowBlocks = kSlotRows / 32;
+  if (p.fine)
+    return launch_after(attend_chunk_join_kernel<D, 4, kSlotRows>, dim3((unsigned)chunk_units(p.a.req.n, p.a.req.max_q, p.a.G, p.a.H), kRowBlocks * (D / 32)), 256, 0, s, p);
+  return launch_after(attend_chunk_join_kernel<D, D / 8, kSlotRows>, dim3((unsigned)p.blocks - 1, kRowBlocks), 256, 0, s, p);
 }
 
 }  // namespace
@@ -1363,19 +1370,26 @@ struct Plan {
   int rc;
   bool chunk;
 };
+// Trees (split): 17 to 128 rows go to this kernel alone, whose block then works on one row tile.  Measured, us, the few-rows
+// kernel and this one, 4 query heads of 128 a KV head: 24 requests of 4K, 32 rows, bf16 115 and 89, 8 bits 208 and 129; of 600
+// keys 67 and 38, 94 and 54; 16 rows of 4K 88 and 85, 103 and 128.  (Chains without a tree stay where they were.)
+static bool split_rows(int64_t rows) { return rows > kSplitAbove && rows <= kSplitRows; }
 static Plan attend_plan(int n, int max_q, int max_kv, int G, int H, bool split) {
   const int64_t rows = (int64_t)max_q * G;
-  if (const int rc = few_capacity(rows)) return {rc, false};
+  if (const int rc = split ? 0 : few_capacity(rows)) return {rc, false};
   const bool both = !split && n > 1 && (int64_t)n * H * ((max_kv + 127) / 128) > kBothTiles;
   return {both ? few_capacity(G) : 0, true};
 }
 
 size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d) {
-  const Plan p = attend_plan(n, max_q, max_kv, G, H, false);      // what any call needs: one that splits needs no more
+  // with a tree or without one
+  const Plan p = attend_plan(n, max_q, max_kv, G, H, false);
+  const int64_t rows = (int64_t)max_q * G;
   size_t bytes = p.rc ? (few_workspace_bytes(n, max_kv, H, d, p.rc) + 255) / 256 * 256 : 0;
-  if (p.chunk) {
+  if (p.chunk || split_rows(rows)) {
     const int64_t blocks = chunk_blocks(n, max_q, max_kv, G, H);
-    bytes += chunk_starts_bytes(blocks) + (size_t)(blocks * 2 * kUnitRows * (d + 2) * 4);
+    const size_t chunk = chunk_starts_bytes(blocks) + (size_t)(blocks * 2 * slot_rows(!p.chunk) * (d + 2) * 4);
+    bytes = p.chunk ? bytes + chunk : chunk > bytes ? chunk : bytes;
   }
   return bytes;
 }
@@ -1383,7 +1397,7 @@ size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int
 int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   (void)L;
   const bool q8 = a.e.k != nullptr;
-  const bool split = a.mask && (int64_t)a.req.max_q * a.G <= 128;
+  const bool split = a.mask && split_rows((int64_t)a.req.max_q * a.G);
   const Plan plan = attend_plan(a.req.n, a.req.max_q, a.req.max_kv, a.G, a.H, split);
   ChunkLaunch p;
   p.a = a;
@@ -1407,7 +1421,7 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   if (!plan.chunk) return KVC_OK;
   p.starts = reinterpret_cast<UnitStart*>(ws);
   p.ml = reinterpret_cast<float*>(ws + chunk_starts_bytes(p.blocks));
-  p.part = p.ml + (int64_t)p.blocks * 2 * kUnitRows * 2;
+  p.part = p.ml + (int64_t)p.blocks * 2 * slot_rows(split) * 2;
   cudaError_t e;
 #define KVC_CHUNK(D, Q, T, S) \
   if (d == D && q8 == Q && (a.mask != nullptr) == T && split == S) e = launch_chunk<D, Q, T, S>(p, mk, mv, s);
