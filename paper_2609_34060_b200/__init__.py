@@ -1032,17 +1032,11 @@ def _tree(tree, what: str) -> int:
     return tree._at
 
 
-def _kept_lists(req: Requests, kept: torch.Tensor, what: str, *ones) -> int:
-    """The lists a request each: kept [n, max_q or more], the others [n]; kept's row length."""
-    if not isinstance(kept, torch.Tensor):
-        raise KvcError(KVC_E_INVALID_ARG, f"{what}: kept: contiguous int32 expected")
-    n = (req.n,)
-    good = kept.dim() == 2 and kept.shape[0] == req.n and kept.shape[1] >= req.max_q
-    for t in ones:
-        good = good and (t is None or t.shape == n)
-    if not good:
-        raise KvcError(KVC_E_SHAPE, f"{what}: kept [requests, max_q or more] and lists of {req.n} expected")
-    return kept.shape[1]
+def _describe(c):
+    """A cache whose descriptor is there (made at its first use, dropped when an attribute of it is set)."""
+    if not isinstance(c, _Described) or "_made" not in c.__dict__:
+        _desc(c)
+    return c
 
 
 def kvc_tree_build(req: Requests, tree: Tree, stream=None) -> None:
@@ -1052,9 +1046,9 @@ def kvc_tree_build(req: Requests, tree: Tree, stream=None) -> None:
     _check(load().kvc_tree_build(at, t, st), "kvc_tree_build")
 
 
-_ROTATED_NAMES, _TREE_NAMES = ("q", "q_out", "k_new", "v_new"), ("lse", "workspace", "q", "out")
-_VERIFY_NAMES = ("parent", "token", "u", "u_next", "kept", "n_kept", "next_token", "target", "draft")
-_KEEP_NAMES = ("kept", "n_kept", "kv_out")
+_ROTATED_NAMES, _TREE_NAMES = ("cache", "q", "q_out", "k_new", "v_new"), ("cache", "lse", "workspace", "q", "out")
+_VERIFY_NAMES = ("target", "draft", "parent", "token", "u", "u_next", "kept", "n_kept", "next_token")
+_KEEP_NAMES = ("kept", "n_kept", "cache", "kv_out")
 
 
 def kvc_append_rotated(req: Requests, rotary: Rotary, k_new: torch.Tensor, v_new: torch.Tensor, cache, layer: int, q: Optional[torch.Tensor] = None,
@@ -1066,11 +1060,12 @@ def kvc_append_rotated(req: Requests, rotary: Rotary, k_new: torch.Tensor, v_new
         raise KvcError(KVC_E_INVALID_ARG, f"{what}: Rotary expected, not {type(rotary).__name__}")
     if (q is None) != (q_out is None):
         raise KvcError(KVC_E_INVALID_ARG, f"{what}: q and q_out go together")
-    at, c = _address(req, what), _desc(cache)
-    st = _here(what, stream, (c[1], req._dev) if rotary._dev is None else (c[1], req._dev, rotary._dev))
+    at, dev = _address(req, what), req._dev
+    _describe(cache)
+    st = _here(what, stream, (dev,) if rotary._dev is None else (dev, rotary._dev))
     _holds(req, cache, what)
-    block = _pack("PPPPHHHHiiiii", what, _ROTATED_NAMES, req._dev, cache.d, at, rotary._for(cache.d), c[0], st, q, q_out, k_new, v_new, layer,
-                  c[3] is not None, q is not None, rotary._rows, rotary._requests)
+    block = _pack("PPCPHHHHiiii", _ROTATED_NAMES, dev, cache.d, 0, 0, at, rotary._for(cache.d), cache, st, q, q_out, k_new, v_new, layer, q is not None,
+                  rotary._rows, rotary._requests)
     _check(load().kvc_block_append_rotated(block), what)
 
 
@@ -1079,13 +1074,14 @@ def kvc_attend_tree(req: Requests, tree: Tree, q: torch.Tensor, cache, layer: in
     """Attention of a tree of drafted tokens: every row sees its request's context and the new tokens of its mask.
     Workspace: kvc_attend_workspace_bytes."""
     what = "kvc_attend_tree"
-    at, t, c = _address(req, what), _tree(tree, what), _desc(cache)
-    st = _here(what, stream, (c[1], req._dev, tree._dev))
+    at, t, dev = _address(req, what), _tree(tree, what), req._dev
+    _describe(cache)
+    st = _here(what, stream, (dev, tree._dev))
     _holds(req, cache, what)
     if lse is not None and lse.shape != q.shape[:2]:
         raise KvcError(KVC_E_INVALID_ARG, f"{what}: lse must be float32 [rows, heads]")
-    block = _pack("PPPFAPPdHHii", what, _TREE_NAMES, req._dev, cache.d, at, t, c[0], lse, workspace, 0 if workspace is None else workspace.nbytes, st,
-                  cache.d ** -0.5 if scale is None else scale, q, out, layer, c[3] is not None)
+    block = _pack("PPCFAPPdHHP", _TREE_NAMES, dev, cache.d, 0, 0, at, t, cache, lse, workspace, 0 if workspace is None else workspace.nbytes, st,
+                  cache.d ** -0.5 if scale is None else scale, q, out, layer)
     _check(load().kvc_block_attend_tree(block), what)
 
 
@@ -1095,13 +1091,9 @@ def kvc_verify(req: Requests, parent: torch.Tensor, token: torch.Tensor, target:
     [n]), from the target's distributions float32 [rows, vocabulary], those the drafts were drawn from (None: they were
     chosen) and uniform random numbers `u` [rows], `u_next` [n]."""
     what = "kvc_verify"
-    at, stride = _address(req, what), _kept_lists(req, kept, what, n_kept, next_token, u_next)
-    st = _here(what, stream, (req._dev,))
-    block = _pack("PIIFFIIIPppii", what, _VERIFY_NAMES, req._dev, 0, at, parent, token, u, u_next, kept, n_kept, next_token, st, target, draft, stride,
-                  draft is not None)
-    rows = target.shape[:1]
-    if parent.shape != rows or token.shape != rows or u.shape != rows:
-        raise KvcError(KVC_E_SHAPE, f"{what}: parent, token and u [rows] expected")
+    at, dev = _address(req, what), req._dev
+    block = _pack("PpprrfuKnnPP", _VERIFY_NAMES, dev, 0, req.n, req.max_q, at, target, draft, parent, token, u, u_next, kept, n_kept, next_token,
+                  _here(what, stream, (dev,)), draft is not None)
     _check(load().kvc_block_verify(block), what)
 
 
@@ -1109,10 +1101,10 @@ def kvc_keep(req: Requests, kept: torch.Tensor, n_kept: torch.Tensor, cache, kv_
     """The rows of the accepted drafts moved together in every layer of a Cache or QCache; `kv_out` int32 [n]: the lengths
     behind the step."""
     what = "kvc_keep"
-    at, c, stride = _address(req, what), _desc(cache), _kept_lists(req, kept, what, n_kept, kv_out)
-    st = _here(what, stream, (c[1], req._dev))
+    at, dev = _address(req, what), req._dev
+    _describe(cache)
     _holds(req, cache, what)
-    block = _pack("PIIPIPii", what, _KEEP_NAMES, req._dev, 0, at, kept, n_kept, c[0], kv_out, st, stride, c[3] is not None)
+    block = _pack("PKnCnP", _KEEP_NAMES, dev, 0, req.n, req.max_q, at, kept, n_kept, cache, kv_out, _here(what, stream, (dev,)))
     _check(load().kvc_block_keep(block), what)
 
 

@@ -18,7 +18,7 @@ struct RotateLaunch {
   DevHeads q, qo, kn, vn;
   DevCache dst;
   DevScale e;
-  int32_t Hq, H, layer, rot, pairing, tokens;   // tokens a block
+  int32_t Hq, H, layer, rot, pairing;
   float amplitude;
   const int32_t* depth;
   const int32_t* pos_begin;
@@ -57,45 +57,49 @@ struct KeepLaunch {
 struct AppendRotatedCall {
   const kvc_requests* req;
   const kvc_rotary* rot;
-  void* cache;                 // kvc_cache or kvc_qcache
+  void* cache;                 // kvc_cache or, with q8, kvc_qcache
+  int64_t q8;
   void* stream;
   kvc_heads q, q_out, k_new, v_new;
-  int32_t layer, q8, has_q;
+  int32_t layer, has_q;
   int32_t n_depth, n_pos;      // entries that depth and pos_begin hold; -1: there are none
 };
 struct AttendTreeCall {
   const kvc_requests* req;
   const kvc_tree* tree;
   const void* cache;
+  int64_t q8;
   float* lse;
   void* workspace;
   uint64_t workspace_bytes;
   void* stream;
   double scale;
   kvc_heads q, out;
-  int32_t layer, q8;
+  int64_t layer;
 };
 struct VerifyCall {
   const kvc_requests* req;
+  kvc_probs target, draft;
   const int32_t* parent;
   const int32_t* token;
   const float* u;
   const float* u_next;
   int32_t* kept;
+  int64_t stride;              // of kept
   int32_t* n_kept;
   int32_t* next;
   void* stream;
-  kvc_probs target, draft;
-  int32_t stride, has_draft;
+  int64_t has_draft;
 };
 struct KeepCall {
   const kvc_requests* req;
   const int32_t* kept;
+  int64_t stride;
   const int32_t* n_kept;
   void* cache;
+  int64_t q8;
   int32_t* kv_out;
   void* stream;
-  int32_t stride, q8;
 };
 
 cudaError_t launch_tree_build(const TreeLaunch& t, cudaStream_t s);

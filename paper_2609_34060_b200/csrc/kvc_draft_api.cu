@@ -227,8 +227,7 @@ int kvc_keep_q8(const kvc_requests* req, const int32_t* kept, int32_t kept_strid
 
 // The same calls from one block of arguments (not part of kvc.h: the Python binding's way in).
 int kvc_block_append_rotated(const AppendRotatedCall* c) {
-  AppendRotatedCall x;
-  memcpy(&x, c, sizeof(x) - 4);                                   // the block ends with its last number
+  AppendRotatedCall x = *c;
   if ((x.n_depth >= 0 && x.n_depth < x.k_new.n_rows) || (x.n_pos >= 0 && x.n_pos < x.req->n)) return KVC_E_SHAPE;
   const kvc_heads* q = x.has_q ? &x.q : nullptr;
   kvc_heads* out = x.has_q ? &x.q_out : nullptr;
@@ -237,18 +236,19 @@ int kvc_block_append_rotated(const AppendRotatedCall* c) {
 }
 int kvc_block_attend_tree(const AttendTreeCall* c) {
   AttendTreeCall x = *c;
-  return x.q8 ? kvc_attend_tree_q8(x.req, x.tree, &x.q, reinterpret_cast<const kvc_qcache*>(x.cache), x.layer, x.scale, &x.out, x.lse, x.workspace,
+  if (x.layer != (int32_t)x.layer) return KVC_E_INVALID_ARG;
+  return x.q8 ? kvc_attend_tree_q8(x.req, x.tree, &x.q, reinterpret_cast<const kvc_qcache*>(x.cache), (int32_t)x.layer, x.scale, &x.out, x.lse, x.workspace,
                                    (size_t)x.workspace_bytes, x.stream)
-              : kvc_attend_tree(x.req, x.tree, &x.q, reinterpret_cast<const kvc_cache*>(x.cache), x.layer, x.scale, &x.out, x.lse, x.workspace,
+              : kvc_attend_tree(x.req, x.tree, &x.q, reinterpret_cast<const kvc_cache*>(x.cache), (int32_t)x.layer, x.scale, &x.out, x.lse, x.workspace,
                                 (size_t)x.workspace_bytes, x.stream);
 }
 int kvc_block_verify(const VerifyCall* c) {
-  return kvc_verify(c->req, c->parent, c->token, &c->target, c->has_draft ? &c->draft : nullptr, c->u, c->u_next, c->kept, c->stride, c->n_kept, c->next,
+  return kvc_verify(c->req, c->parent, c->token, &c->target, c->has_draft ? &c->draft : nullptr, c->u, c->u_next, c->kept, (int32_t)c->stride, c->n_kept, c->next,
                     c->stream);
 }
 int kvc_block_keep(const KeepCall* c) {
-  return c->q8 ? kvc_keep_q8(c->req, c->kept, c->stride, c->n_kept, reinterpret_cast<kvc_qcache*>(c->cache), c->kv_out, c->stream)
-               : kvc_keep(c->req, c->kept, c->stride, c->n_kept, reinterpret_cast<kvc_cache*>(c->cache), c->kv_out, c->stream);
+  return c->q8 ? kvc_keep_q8(c->req, c->kept, (int32_t)c->stride, c->n_kept, reinterpret_cast<kvc_qcache*>(c->cache), c->kv_out, c->stream)
+               : kvc_keep(c->req, c->kept, (int32_t)c->stride, c->n_kept, reinterpret_cast<kvc_cache*>(c->cache), c->kv_out, c->stream);
 }
 
 }  // extern "C"

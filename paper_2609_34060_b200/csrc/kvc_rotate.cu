@@ -44,23 +44,23 @@ __device__ __forceinline__ void encode16(float* x, uint32_t& b, uint2& lo, uint2
   hi = make_uint2(e4m3x2(x[8], x[9]) | (e4m3x2(x[10], x[11]) << 16), e4m3x2(x[12], x[13]) | (e4m3x2(x[14], x[15]) << 16));
 }
 
-constexpr int kMaxTokens = 8, kUnroll = 2;
+constexpr int kUnroll = 2;
 
-// grid: x = tiles of p.tokens tokens of a request, y = requests (strided)
-template <int D, bool Q8>
+// grid: x = tiles of TOKENS tokens of a request, y = requests (strided)
+template <int D, bool Q8, int TOKENS>
 __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_constant__ RotateLaunch p) {
   constexpr int LPR = D / 16;
-  __shared__ float s_cos[kMaxTokens][kMaxHalfD], s_sin[kMaxTokens][kMaxHalfD];
-  __shared__ int64_t s_off[kMaxTokens], s_exp[kMaxTokens];        // of the tokens' rows in the layer, head 0; -1: none
+  __shared__ float s_cos[TOKENS][kMaxHalfD], s_sin[TOKENS][kMaxHalfD];
+  __shared__ int64_t s_off[TOKENS], s_exp[TOKENS];        // of the tokens' rows in the layer, head 0; -1: none
   tc::grid_dependency_wait();
   tc::grid_dependents_launch();
-  const int tid = threadIdx.x, step = (int)blockDim.x, j0 = (int)blockIdx.x * p.tokens;
+  const int tid = threadIdx.x, step = (int)blockDim.x, j0 = (int)blockIdx.x * TOKENS;
   const int heads = p.Hq + 2 * p.H, half = p.rot / 2;
   for (int b = blockIdx.y; b < p.req.n; b += gridDim.y) {
     int q0, nq, kv;
     request_span(p.req, b, tid == 0 && j0 == 0 ? p.status : nullptr, q0, nq, kv);
     if (j0 >= nq) continue;
-    const int nt = min(p.tokens, nq - j0), items = nt * heads * LPR, lane = tid % LPR;   // step is a multiple of LPR
+    const int nt = min(TOKENS, nq - j0), items = nt * heads * LPR, lane = tid % LPR;   // step is a multiple of LPR
     // 16 channels of a row a lane, in two chunks
     const bool turns = lane * 16 < p.rot, far = turns && p.pairing == KVC_ROPE_HALF;
     const int ch0 = far ? 8 * lane : 16 * lane, ch1 = far ? half + 8 * lane : 16 * lane + 8;
@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
     auto load = [&](int i0) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const int i = i0 + u * step + tid, r = i / LPR, tk = r / heads, head = r - tk * heads;
+        const int i = i0 + u * step + tid, r = i / LPR, tk = TOKENS == 1 ? 0 : r / heads, head = r - tk * heads;
         lo[u] = hi[u] = make_uint4(0, 0, 0, 0);
         if (i >= items) continue;
         const bool is_q = head < p.Hq, is_k = head < p.Hq + p.H;
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
     load(0);
     // while the first rows are on their way: angles, and where the tokens' rows go
     for (int i = tid; i < nt * half; i += step) {
-      const int tk = i / half, k = i - tk * half, j = j0 + tk;
+      const int tk = TOKENS == 1 ? 0 : i / half, k = i - tk * half, j = j0 + tk;
       const double pos = (double)((int64_t)(p.pos_begin ? p.pos_begin[b] : 0) + (kv - nq) + (p.depth ? p.depth[q0 + j] : j));
       const double rounds = pos * p.turns[k];
       float sn, cs;
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
       if (i0 > 0) load(i0);
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const int i = i0 + u * step + tid, r = i / LPR, tk = min(r / heads, nt - 1), head = i < items ? r - tk * heads : -1;
+        const int i = i0 + u * step + tid, r = i / LPR, tk = TOKENS == 1 ? 0 : min(r / heads, nt - 1), head = i < items ? r - tk * heads : -1;
         const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.H;
         float x[16];
         unpack8(lo[u], x);
@@ -145,17 +145,17 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
 
 }  // namespace
 
-cudaError_t launch_append_rotated(const RotateLaunch& launch, int d, cudaStream_t s) {
+cudaError_t launch_append_rotated(const RotateLaunch& r, int d, cudaStream_t s) {
   // prompts: tiles of several tokens, whose rows stream through a block; few tokens: a block each, as many threads as it has work
-  RotateLaunch r = launch;
-  r.tokens = r.req.max_q >= 64 ? kMaxTokens : 1;
-  const int64_t each = ((int64_t)r.tokens * (r.Hq + 2 * r.H) * (d / 16) + kUnroll - 1) / kUnroll;
+  const int tokens = r.req.max_q >= 64 ? 8 : 1;
+  const int64_t each = ((int64_t)tokens * (r.Hq + 2 * r.H) * (d / 16) + kUnroll - 1) / kUnroll;
   const int threads = each < kMaxHalfD ? kMaxHalfD : each > 256 ? 256 : (int)((each + 31) / 32 * 32);
-  const dim3 g((unsigned)((r.req.max_q + r.tokens - 1) / r.tokens), (unsigned)(r.req.n < 65535 ? r.req.n : 65535));
+  const dim3 g((unsigned)((r.req.max_q + tokens - 1) / tokens), (unsigned)(r.req.n < 65535 ? r.req.n : 65535));
   const bool q8 = r.e.k != nullptr;
-#define KVC_ROTATE(D, Q) \
-  if (d == D && q8 == Q) return tc::launch_after(append_rotated_kernel<D, Q>, g, threads, 0, s, r);
-  KVC_ROTATE(128, false) KVC_ROTATE(128, true) KVC_ROTATE(64, false) KVC_ROTATE(64, true)
+#define KVC_ROTATE(D, Q, T) \
+  if (d == D && q8 == Q && tokens == T) return tc::launch_after(append_rotated_kernel<D, Q, T>, g, threads, 0, s, r);
+  KVC_ROTATE(128, false, 1) KVC_ROTATE(128, true, 1) KVC_ROTATE(64, false, 1) KVC_ROTATE(64, true, 1)
+  KVC_ROTATE(128, false, 8) KVC_ROTATE(128, true, 8) KVC_ROTATE(64, false, 8) KVC_ROTATE(64, true, 8)
 #undef KVC_ROTATE
   return cudaErrorInvalidValue;
 }

@@ -1,11 +1,15 @@
 // Argument blocks of the Python binding: tensors checked and written out as the structures the library takes.
 //
-// pack(codes, what, names, device, d, *args) -> bytes.  One argument a code, written one behind the other:
-//   P  a whole number (an address), 8 bytes        i  a whole number, 4 bytes        d  a float, 8 bytes
-//   H  kvc_heads of a bf16 tensor [rows, heads, d] p  kvc_probs of a float32 tensor [rows, n]
-//   I  address of a contiguous int32 tensor        F  of a contiguous float32 tensor A  of any contiguous tensor
-// H, p, I, F and A take None too (zeros).  Every tensor has to live on `device`.  Wrong ones raise KvcError with the name of
-// the argument.  Done in Python the same costs a call of four tensors 5 us, which is more than its kernel takes.
+// pack(codes, names, device, d, n, max_q, *args) -> bytes.  One argument a code, written one behind the other:
+//   P  a whole number (an address), 8 bytes         i  a whole number, 4 bytes         d  a float, 8 bytes
+//   C  address of the descriptor of a Cache or QCache (its pointers set from its tensors) and, 8 bytes, whether it is a QCache
+//   H  kvc_heads of a bf16 tensor [rows, heads, d]  p  kvc_probs of a float32 tensor [rows, entries]
+//   r  address of an int32 tensor of the probabilities' rows, f  of a float32 one
+//   n  address of an int32 tensor of n entries, u  of a float32 one
+//   K  address of an int32 tensor [n, max_q or more] and, 8 bytes, its row length
+//   F  address of a float32 tensor, A  of any tensor
+// H, p, n, F and A take None too (zeros).  Lists are contiguous, and every tensor lives on `device`.  Wrong ones raise KvcError
+// with the name of the argument.  Done in Python the same costs a call of four tensors 5 us, more than its kernel takes.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -16,6 +20,7 @@
 namespace {
 
 PyObject *g_error, *g_bf16, *g_f32, *g_i32;                       // KvcError and the types, from setup()
+PyObject *s_made, *s_k, *s_v, *s_scale_k, *s_scale_v, *s_page_table;
 PyObject *s_shape, *s_stride, *s_dtype, *s_data_ptr, *s_get_device, *s_is_contiguous;
 
 bool refuse(int code, PyObject* names, Py_ssize_t i, const char* why) {
@@ -70,15 +75,48 @@ bool contiguous(PyObject* t) {
   return ok;
 }
 
+// Sets one pointer of a descriptor from the object's tensor; false with an error set.
+bool set_pointer(PyObject* c, PyObject* name, void* to, bool may_be_none) {
+  PyObject* t = PyObject_GetAttr(c, name);
+  if (!t) return false;
+  int64_t at = 0;
+  const bool ok = (may_be_none && t == Py_None) || number_of(t, s_data_ptr, &at);
+  if (ok && t != Py_None) memcpy(to, &at, 8);
+  Py_DECREF(t);
+  return ok;
+}
+// `made`: (address of the descriptor, device, its rows, its kvc_qcache or None), kept in the object by the binding
+bool describe(PyObject* c, int64_t device, PyObject* names, Py_ssize_t name, int64_t* out) {
+  PyObject* made = PyObject_GetAttr(c, s_made);
+  if (!made || !PyTuple_Check(made) || PyTuple_GET_SIZE(made) != 4) {
+    Py_XDECREF(made);
+    return refuse(KVC_E_INVALID_ARG, names, name, "a Cache or QCache expected");
+  }
+  const int64_t at = PyLong_AsLongLong(PyTuple_GET_ITEM(made, 0)), where = PyLong_AsLongLong(PyTuple_GET_ITEM(made, 1));
+  const bool q8 = PyTuple_GET_ITEM(made, 3) != Py_None;
+  Py_DECREF(made);                                                // the object holds it
+  if (PyErr_Occurred()) return false;
+  if (where != device) return refuse(KVC_E_INVALID_ARG, names, name, "tensors on the current CUDA device expected");
+  kvc_qcache* q = reinterpret_cast<kvc_qcache*>(at);
+  kvc_cache* rows = q8 ? &q->codes : reinterpret_cast<kvc_cache*>(at);
+  if (!set_pointer(c, s_k, &rows->k, false) || !set_pointer(c, s_v, &rows->v, false) || !set_pointer(c, s_page_table, &rows->page_table, true)) return false;
+  if (q8 && (!set_pointer(c, s_scale_k, &q->scale_k, false) || !set_pointer(c, s_scale_v, &q->scale_v, false))) return false;
+  out[0] = at;
+  out[1] = q8;
+  return true;
+}
+
 PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  if (nargs < 5) return PyErr_Format(PyExc_TypeError, "pack(codes, what, names, device, d, ...)");
+  constexpr Py_ssize_t kHead = 6;
+  if (nargs < kHead) return PyErr_Format(PyExc_TypeError, "pack(codes, names, device, d, n, max_q, ...)");
   Py_ssize_t n = 0;
   const char* codes = PyUnicode_AsUTF8AndSize(args[0], &n);
-  if (!codes || !PyTuple_Check(args[2])) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_TypeError, "names: a tuple");
-  if (nargs != 5 + n || n > 64) return PyErr_Format(PyExc_TypeError, "an argument a code, 64 at most");
-  PyObject* names = args[2];
-  const int64_t device = PyLong_AsLongLong(args[3]), d = PyLong_AsLongLong(args[4]);
+  if (!codes || !PyTuple_Check(args[1])) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_TypeError, "names: a tuple");
+  if (nargs != kHead + n || n > 64) return PyErr_Format(PyExc_TypeError, "an argument a code, 64 at most");
+  PyObject* names = args[1];
+  const int64_t device = PyLong_AsLongLong(args[2]), d = PyLong_AsLongLong(args[3]), requests = PyLong_AsLongLong(args[4]), max_q = PyLong_AsLongLong(args[5]);
   if (PyErr_Occurred()) return nullptr;
+  int64_t rows = -1;                                              // of the probabilities
   unsigned char block[64 * sizeof(kvc_heads)];
   size_t at = 0;
   Py_ssize_t tensor = 0;                                          // among the tensors: its name
@@ -87,7 +125,7 @@ PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     at += bytes;
   };
   for (Py_ssize_t i = 0; i < n; ++i) {
-    PyObject* x = args[5 + i];
+    PyObject* x = args[kHead + i];
     const char code = codes[i];
     if (code == 'P' || code == 'i') {
       const long long v = PyLong_AsLongLong(x);
@@ -108,12 +146,18 @@ PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       continue;
     }
     const Py_ssize_t name = tensor++;
+    if (code == 'C') {
+      int64_t made[2];
+      if (!describe(x, device, names, name, made)) return nullptr;
+      put(made, 16);
+      continue;
+    }
     kvc_heads h;
     kvc_probs p;
     memset(&h, 0, sizeof(h));
     memset(&p, 0, sizeof(p));
-    int64_t address = 0;
-    if (x != Py_None) {
+    int64_t address = 0, length = 0;
+    if (x != Py_None || code == 'K' || code == 'r' || code == 'f' || code == 'u') {
       int64_t shape[3], stride[3], where = 0;
       if (code == 'H') {
         if (!sizes(x, shape, stride, 3) || !is_type(x, g_bf16)) return refuse(KVC_E_INVALID_ARG, names, name, "bf16 [rows, heads, d] expected"), nullptr;
@@ -133,9 +177,21 @@ PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         p.n_rows = (int32_t)shape[0];
         p.n = (int32_t)shape[1];
         p.s_row = shape[0] > 1 ? stride[0] : 0;
-      } else if ((code != 'A' && !is_type(x, code == 'I' ? g_i32 : g_f32)) || !contiguous(x)) {
-        return refuse(KVC_E_INVALID_ARG, names, name, code == 'I' ? "contiguous int32 expected" : code == 'F' ? "contiguous float32 expected" : "a contiguous tensor expected"), nullptr;
+        if (rows < 0) rows = shape[0];
+      } else if (code == 'K') {
+        if (!sizes(x, shape, stride, 2) || !is_type(x, g_i32) || !contiguous(x)) return refuse(KVC_E_INVALID_ARG, names, name, "contiguous int32 [requests, max_q or more] expected"), nullptr;
+        if (shape[0] != requests || shape[1] < max_q || shape[1] > INT32_MAX) return refuse(KVC_E_SHAPE, names, name, "[requests, max_q or more] expected"), nullptr;
+      } else if (code == 'n' || code == 'u' || code == 'r' || code == 'f') {
+        const bool whole = code == 'n' || code == 'r';
+        if (!is_type(x, whole ? g_i32 : g_f32) || !contiguous(x)) return refuse(KVC_E_INVALID_ARG, names, name, whole ? "contiguous int32 expected" : "contiguous float32 expected"), nullptr;
+        PyObject* a = PyObject_GetAttr(x, s_shape);
+        const bool one = numbers(a, shape, 1);
+        Py_XDECREF(a);
+        if (!one || shape[0] != (code == 'n' || code == 'u' ? requests : rows)) return refuse(KVC_E_SHAPE, names, name, code == 'n' || code == 'u' ? "[requests] expected" : "[rows] expected"), nullptr;
+      } else if ((code == 'F' && !is_type(x, g_f32)) || !contiguous(x)) {
+        return refuse(KVC_E_INVALID_ARG, names, name, code == 'F' ? "contiguous float32 expected" : "a contiguous tensor expected"), nullptr;
       }
+      if (code == 'K') length = shape[1];
       if (!number_of(x, s_data_ptr, &address) || !number_of(x, s_get_device, &where)) return refuse(KVC_E_INVALID_ARG, names, name, "a tensor expected"), nullptr;
       if (where != device) return refuse(KVC_E_INVALID_ARG, names, name, "tensors on the current CUDA device expected"), nullptr;
     }
@@ -147,6 +203,7 @@ PyObject* pack(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       put(&p, sizeof(p));
     } else {
       put(&address, 8);
+      if (code == 'K') put(&length, 8);
     }
   }
   return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(block), (Py_ssize_t)at);
@@ -175,7 +232,7 @@ PyMODINIT_FUNC PyInit__marshal(void) {
   struct {
     PyObject** to;
     const char* name;
-  } const names[] = {{&s_shape, "shape"}, {&s_stride, "stride"}, {&s_dtype, "dtype"}, {&s_data_ptr, "data_ptr"}, {&s_get_device, "get_device"}, {&s_is_contiguous, "is_contiguous"}};
+  } const names[] = {{&s_shape, "shape"}, {&s_made, "_made"}, {&s_k, "k"}, {&s_v, "v"}, {&s_scale_k, "scale_k"}, {&s_scale_v, "scale_v"}, {&s_page_table, "page_table"}, {&s_stride, "stride"}, {&s_dtype, "dtype"}, {&s_data_ptr, "data_ptr"}, {&s_get_device, "get_device"}, {&s_is_contiguous, "is_contiguous"}};
   for (const auto& x : names)
     if (!(*x.to = PyUnicode_InternFromString(x.name))) return nullptr;
   return PyModule_Create(&module);

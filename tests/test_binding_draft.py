@@ -39,17 +39,25 @@ def refused(code, *calls):
 
 def test_blocks():
     """Argument blocks: what lies where, and what is no argument."""
-    q, p = z(3, 4, 64), torch.zeros(5, 9, dtype=torch.float32)
-    b = kvc._pack("PHpIii", "x", ("q", "p", "i"), -1, 64, 7, q[:, 1:3], p[1:3, :6], None, -2, 3)
-    want = struct.pack("@QQiiQQQiiQQii", 7, q.data_ptr() + 128, 3, 2, 256, 64, p.data_ptr() + 36, 2, 6, 9, 0, -2, 3)
-    assert b == want
-    assert len(kvc._pack("Hp", "x", ("q", "p"), -1, 64, z(1, 1, 64), torch.zeros(1, 1))) == 32 + 24
+    q, p, k = z(3, 4, 64), torch.zeros(5, 9), z(2, 6, dtype=I32)
+    pack = lambda codes, names, *args: kvc._pack(codes, names, -1, 64, 2, 5, *args)
+    b = pack("PHpnKii", ("q", "p", "n", "k"), 7, q[:, 1:3], p[1:3, :6], None, k, -2, 3)
+    assert b == struct.pack("@QQiiQQQiiQQQQii", 7, q.data_ptr() + 128, 3, 2, 256, 64, p.data_ptr() + 36, 2, 6, 9, 0, k.data_ptr(), 6, -2, 3)
+    assert len(pack("Hp", ("q", "p"), z(1, 1, 64), torch.zeros(1, 1))) == 32 + 24
+    c, q8, *_ = objects()
+    for x in (c, q8):
+        made = kvc._desc(x)
+        for name in ("k", "v") + (("scale_k", "scale_v") if x is q8 else ()):
+            x.__dict__[name] = getattr(x, name).clone()                 # tensors that moved: the descriptor follows
+        assert pack("C", ("c",), x) == struct.pack("@QQ", made[0], x is q8) and made[2].k == x.k.data_ptr() and made[2].v == x.v.data_ptr()
+        assert x is c or (made[3].scale_k, made[3].scale_v) == (x.scale_k.data_ptr(), x.scale_v.data_ptr())
     with pytest.raises(OverflowError):
-        kvc._pack("i", "x", (), -1, 0, 1 << 31)
+        pack("i", (), 1 << 31)
     with pytest.raises(TypeError):
-        kvc._pack("PP", "x", (), -1, 0, 1)
-    refused(-1, lambda: kvc._pack("H", "x", ("q",), 0, 64, q), lambda: kvc._pack("H", "x", ("q",), -1, 64, object()),
-            lambda: kvc._pack("A", "x", (), -1, 0, q[:, ::2]), lambda: kvc._pack("F", "x", (), -1, 0, z(3)))
+        pack("PP", (), 1)
+    refused(-1, lambda: kvc._pack("H", ("q",), 0, 64, 0, 0, q), lambda: pack("H", ("q",), object()), lambda: pack("A", (), q[:, ::2]), lambda: pack("F", (), z(3)),
+            lambda: pack("C", ("c",), q), lambda: pack("K", ("k",), None), lambda: pack("u", ("u",), None))
+    refused(-2, lambda: pack("n", ("n",), z(3, dtype=I32)), lambda: pack("K", ("k",), z(2, 4, dtype=I32)), lambda: pack("pr", ("p", "r"), p, z(4, dtype=I32)))
 
 
 def test_tree(fake):
