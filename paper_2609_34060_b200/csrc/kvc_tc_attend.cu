@@ -693,6 +693,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         // second where the tile's own is too far above it (a piece's first tile among them: m = -inf)
         bool grow = late > m;
         float to = late, top;
+        bool look = kSplit && it == 0;                            // the first tile: its maximum first, and the probabilities once
 #pragma unroll 1
         for (;;) {
           if (__any_sync(0xffffffffu, grow)) {
@@ -729,13 +730,16 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           }
           mx[0] = max3(mx[0], s[124], s[125]);
           mx[1] = max3(mx[1], s[126], s[127]);
-          quarter(0);
-          quarter(32);
-          quarter(64);
+          if (!kSplit || !look) {
+            quarter(0);
+            quarter(32);
+            quarter(64);
+          }
           top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-          grow = (top - m) * c > kJump;
+          grow = kSplit && look ? top > m : (top - m) * c > kJump;
           to = top;
-          if (!__any_sync(0xffffffffu, grow)) break;
+          if (!(kSplit && look) && !__any_sync(0xffffffffu, grow)) break;
+          look = false;
         }
         late = (top - m) * c > kLazy ? top : minus_inf;
         clear_stale();
