@@ -50,12 +50,15 @@ constexpr int kUnroll = 2;
 template <int D, bool Q8, int TOKENS>
 __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_constant__ RotateLaunch p) {
   constexpr int LPR = D / 16;
-  __shared__ float s_cos[TOKENS][kMaxHalfD], s_sin[TOKENS][kMaxHalfD];
+  __shared__ alignas(16) float s_cos[TOKENS][kMaxHalfD], s_sin[TOKENS][kMaxHalfD];
   __shared__ int64_t s_off[TOKENS], s_exp[TOKENS];        // of the tokens' rows in the layer, head 0; -1: none
   tc::grid_dependency_wait();
   tc::grid_dependents_launch();
   const int tid = threadIdx.x, step = (int)blockDim.x, j0 = (int)blockIdx.x * TOKENS;
   const int heads = p.Hq + 2 * p.H, half = p.rot / 2;
+  // r / heads for a row r of the tile: quotients below 8 with steps of at least 2^-18 between them, off by less than 2^-20
+  const float each = 1.f / (float)heads;
+  auto token_of = [&](int r) { return TOKENS == 1 ? 0 : (int)(((float)r + 0.5f) * each); };
   for (int b = blockIdx.y; b < p.req.n; b += gridDim.y) {
     int q0, nq, kv;
     request_span(p.req, b, tid == 0 && j0 == 0 ? p.status : nullptr, q0, nq, kv);
@@ -68,7 +71,7 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
     auto load = [&](int i0) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const int i = i0 + u * step + tid, r = i / LPR, tk = TOKENS == 1 ? 0 : r / heads, head = r - tk * heads;
+        const int i = i0 + u * step + tid, r = i / LPR, tk = token_of(r), head = r - tk * heads;
         lo[u] = hi[u] = make_uint4(0, 0, 0, 0);
         if (i >= items) continue;
         const bool is_q = head < p.Hq, is_k = head < p.Hq + p.H;
@@ -102,13 +105,18 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
       if (i0 > 0) load(i0);
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const int i = i0 + u * step + tid, r = i / LPR, tk = TOKENS == 1 ? 0 : min(r / heads, nt - 1), head = i < items ? r - tk * heads : -1;
+        const int i = i0 + u * step + tid, r = i / LPR, tk = min(token_of(r), nt - 1), head = i < items ? r - tk * heads : -1;
         const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.H;
         float x[16];
         unpack8(lo[u], x);
         unpack8(hi[u], x + 8);
         if (turns && !is_v) {
-          rope16(x, &s_cos[tk][8 * lane], &s_sin[tk][8 * lane], p.pairing);
+          float cs[8], sn[8];
+          *reinterpret_cast<float4*>(cs) = *reinterpret_cast<const float4*>(&s_cos[tk][8 * lane]);
+          *reinterpret_cast<float4*>(cs + 4) = *reinterpret_cast<const float4*>(&s_cos[tk][8 * lane + 4]);
+          *reinterpret_cast<float4*>(sn) = *reinterpret_cast<const float4*>(&s_sin[tk][8 * lane]);
+          *reinterpret_cast<float4*>(sn + 4) = *reinterpret_cast<const float4*>(&s_sin[tk][8 * lane + 4]);
+          rope16(x, cs, sn, p.pairing);
           if (!Q8 || is_q) {
             lo[u] = pack8(x);
             hi[u] = pack8(x + 8);
