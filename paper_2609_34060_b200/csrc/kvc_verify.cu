@@ -29,6 +29,7 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 16;
 constexpr int kRowBytes = 24;              // of shared memory for a row of the request
 constexpr int kStep = 128;                 // entries a warp takes at a time
+constexpr int kList = 512;                 // entries of a warp's part that are kept from one pass over a node to the next
 
 // A non-negative float as a double, by moving its bits (the conversion unit takes 16 a cycle and SM, four times fewer than
 // the integer pipe; subnormal floats come out as other numbers below 2^-126).
@@ -44,6 +45,7 @@ __device__ __forceinline__ double residual(float p, float q, double A, double B)
 
 struct Node {                              // where the walk is
   int node, asked, gone;                   // the node's row, the row tried last, rejected tokens (drafts chosen)
+  bool listed;                             // the node's entries with P > 0 are in shared memory
   bool spent;                              // no residual left: no further child, the draw is from p itself
   bool normal;                             // A and B hold the last rejection's division
   double A, B, left;
@@ -58,6 +60,10 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
   int* s_gone = s_token + p.req.max_q;
   int16_t* s_parent = reinterpret_cast<int16_t*>(s_gone + p.req.max_q);
   int16_t* s_path = s_parent + p.req.max_q;
+  // entries (p, q) with P > 0 of every warp's part, where they fit: P > 0 never comes back, so the passes behind a node's
+  // first rejection go over these alone
+  float2* s_list = reinterpret_cast<float2*>(s_p + (p.req.max_q * kRowBytes / 4 + 3) / 4 * 4) + (threadIdx.x >> 5) * kList;
+  __shared__ int s_count[kWarps];          // of them; -1: too many
   __shared__ double s_warp[kWarps], s_block[2][kMaxCluster];
   __shared__ Node s_at;
   __shared__ int s_more, s_kept;
@@ -96,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     if (kDraft) s_q[j] = a >= 0 ? p.draft[(int64_t)(q0 + a) * p.s_draft + x] : 0.f;
   }
   if (tid == 0) {
-    s_at = Node{0, 0, 0, false, true, 1.0, 0.0, 1.0};
+    s_at = Node{0, 0, 0, false, false, true, 1.0, 0.0, 1.0};
     s_path[0] = 0;
     s_kept = 1;
   }
@@ -140,28 +146,55 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     return residual(x.p[k], x.q[k], A, B);
   };
   int passes = 0;
-  // sum of P over the vocabulary, the same in all threads of the cluster
-  auto sum_all = [&](int node, double A, double B, int gone) {
+  // sum of P over the vocabulary, the same in all threads of the cluster; list: fill the lists, or go over them (listed)
+  auto sum_all = [&](int node, double A, double B, int gone, bool list, bool listed) {
     const float* pt = p.target + (int64_t)(q0 + node) * p.s_target;
     const float* pd = kDraft && B != 0.0 ? p.draft + (int64_t)(q0 + node) * p.s_draft : nullptr;
     int64_t lo, hi;
     warp_range(warp, lo, hi);
     double sum = 0.0;
     float top = 0.f;
-    constexpr int kAhead = kDraft ? 2 : 4;   // loads in flight (two rows, or one)
-    for (int64_t at = lo + lane * 4; at < hi; at += kAhead * kStep) {
-      Four x[kAhead];
+    if (kDraft && listed && s_count[warp] >= 0) {
+      const int n = s_count[warp];
+      for (int i = lane; i < n; i += 32) sum += residual(s_list[i].x, s_list[i].y, A, B);
+    } else if (kDraft && list) {
+      int n = 0;
+      for (int64_t base = lo; base < hi; base += 2 * kStep) {
+        Four x[2];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) fetch(pt, pd, at + i * kStep, hi, x[i]);
+        for (int i = 0; i < 2; ++i) fetch(pt, pd, base + i * kStep + lane * 4, hi, x[i]);
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        double s = 0.0;
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          s += value(x[i], k, at + i * kStep, A, B, gone);
-          top = fmaxf(top, x[i].p[k]);
+          for (int k = 0; k < 4; ++k) {
+            const double v = residual(x[i].p[k], x[i].q[k], A, B);
+            sum += v;
+            top = fmaxf(top, x[i].p[k]);
+            const unsigned some = __ballot_sync(0xffffffffu, v > 0.0);
+            const int at = n + __popc(some & ((1u << lane) - 1u));
+            if (v > 0.0 && at < kList) s_list[at] = make_float2(x[i].p[k], x[i].q[k]);
+            n += __popc(some);
+          }
         }
-        sum += s;
+      }
+      if (lane == 0) s_count[warp] = n <= kList ? n : -1;
+      __syncwarp();
+    } else {
+      constexpr int kAhead = kDraft ? 2 : 4;   // loads in flight (two rows, or one)
+      for (int64_t at = lo + lane * 4; at < hi; at += kAhead * kStep) {
+        Four x[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fetch(pt, pd, at + i * kStep, hi, x[i]);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          double s = 0.0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            s += value(x[i], k, at + i * kStep, A, B, gone);
+            top = fmaxf(top, x[i].p[k]);
+          }
+          sum += s;
+        }
       }
     }
     if (top > 3.4028235e38f) sum = __longlong_as_double(0x7ff0000000000000ll);   // no sum with an infinity in it
@@ -219,6 +252,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
           n.B = 0.0;
           n.left = 1.0;
           n.gone = 0;
+          n.listed = false;
         } else if (kDraft) {
           n.B += 1.0;
           n.normal = false;
@@ -239,11 +273,12 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
     __syncthreads();
     if (!s_more) break;
     const Node n = s_at;
-    const double z = sum_all(n.node, n.A, n.B, n.gone);
+    const double z = sum_all(n.node, n.A, n.B, n.gone, !n.listed, n.listed);
     __syncthreads();
     if (tid == 0) {
       const bool some = z > 0.0 && z < __longlong_as_double(0x7ff0000000000000ll);
       s_at.spent = !some;
+      s_at.listed = true;
       s_at.normal = true;
       s_at.A = some ? n.A / z : 1.0;
       s_at.B = some ? n.B / z : 0.0;
@@ -253,12 +288,12 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
 
   Node n = s_at;
   const double infinite = __longlong_as_double(0x7ff0000000000000ll);
-  double total = sum_all(n.node, n.A, n.B, n.gone);
+  double total = sum_all(n.node, n.A, n.B, n.gone, false, n.listed && n.B != 0.0);
   if (!(total > 0.0 && total < infinite) && (n.B != 0.0 || n.gone > 0)) {
     n.A = 1.0;
     n.B = 0.0;
     n.gone = 0;
-    total = sum_all(n.node, n.A, n.B, n.gone);
+    total = sum_all(n.node, n.A, n.B, n.gone, false, false);
   }
   if (rank == 0) {
     const int kept = s_kept;
@@ -344,16 +379,20 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
   p.next[b] = (int)next;
 }
 
+int dynamic_bytes(int max_q, bool draft) { return (max_q * kRowBytes + 15) / 16 * 16 + 16 + (draft ? kWarps * kList * 8 : 0); }
+
 template <bool kDraft, bool kWide>
 cudaError_t launch(const VerifyLaunch& v, cudaStream_t s) {
   // A small vocabulary is one block's.  Else eight blocks a request (four fit on an SM: 74 requests at once), or, while all
   // requests are resident with them, sixteen: 4 / 16 trees over 128000 entries 20 / 27 us with eight, 15 / 20 with sixteen;
-  // 64 trees 42 and 45.
+  // 64 trees 42 and 45.  (All before the lists: with them 13 / 17 and, with eight blocks, 33 us; lists of 1024 entries leave
+  // room for three blocks on an SM, 34 us.)
   const int blocks = v.vocab <= 4096 ? 1 : v.req.n <= 32 ? kMaxCluster : kMaxCluster / 2;
   static DeviceOnce once;
   int dev;
   if (once.pending(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(verify_kernel<kDraft, kWide>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    cudaError_t e = cudaFuncSetAttribute(verify_kernel<kDraft, kWide>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(verify_kernel<kDraft, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynamic_bytes(KVC_TREE_MAX_Q, kDraft));
     if (e != cudaSuccess) return e;
     once.mark(dev);
   }
@@ -365,7 +404,7 @@ cudaError_t launch(const VerifyLaunch& v, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)v.req.n * blocks));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)(v.req.max_q > 0 ? v.req.max_q : 1) * kRowBytes;
+  cfg.dynamicSmemBytes = (size_t)dynamic_bytes(v.req.max_q, kDraft);
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = 2;
