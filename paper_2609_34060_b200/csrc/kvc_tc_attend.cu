@@ -90,8 +90,8 @@ struct Shape {
   static constexpr int kScales = kDirect ? 4 : 1;                 // tiles whose keys' scales are held
 
   static constexpr int kThreads = Q8 ? 512 : 384;
-  static constexpr int kRegs = kDirect ? 152 : Q8 ? 184 : 208;    // of the softmax warps
-  static constexpr int kRegsOthers = kDirect ? 104 : Q8 ? 72 : 88;
+  static constexpr int kRegs = kDirect ? 168 : Q8 ? 184 : 208;    // of the softmax warps (kDirect, four agents of 27K: 152: 123 us, 168: 119, 184: 122)
+  static constexpr int kRegsOthers = kDirect ? 88 : Q8 ? 72 : 88;
   static constexpr int kSmem = 1024 + kQTiles * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0) + (kDirect ? kKeySlots * kRaw + kScales * 512 + 8192 : 0);
 };
 
@@ -516,6 +516,8 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             lo = hi;
           }
         }
+        // the scales of the tile's keys, there before its logits
+        if (kDirect && !wait(scale_full + 8 * ((g + kt) % SH::kScales), ((g + kt) / SH::kScales) & 1)) break;
         if (!wait(s_full + 8 * t, par)) break;
         tc_fence_after();
         // stale value rows behind the last key: P is zero there, but zero times a stale NaN would not be
@@ -531,11 +533,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         };
         if (kSplit && idle) {
           clear_stale();
-          if constexpr (kDirect) {
-            const int es = (g + kt) % SH::kScales;
-            if (!wait(scale_full + 8 * es, ((g + kt) / SH::kScales) & 1)) break;
-            mbar_arrive(scale_empty + 8 * es);
-          }
+          if (kDirect) mbar_arrive(scale_empty + 8 * ((g + kt) % SH::kScales));
           tc_fence_before();
           mbar_arrive(pr);
           mbar_arrive(pr + 8);
@@ -548,7 +546,6 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           // before it, which lie over their logits by then, are scaled: by a power of two, so that bf16 loses nothing.  mc is
           // the maximum in steps of 2.
           const int es = (g + kt) % SH::kScales;
-          if (!wait(scale_full + 8 * es, ((g + kt) / SH::kScales) & 1)) break;
           const float4* ks = reinterpret_cast<const float4*>(sscale + es * 128);
           const bool hidden = lowest < t0 + 127 || (kTree && t0 + 127 >= fresh);
           if (!(kTree && t0 + 127 >= fresh)) sees[0] = sees[1] = sees[2] = sees[3] = 0xffffffffu;
