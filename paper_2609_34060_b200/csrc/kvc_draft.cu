@@ -14,7 +14,8 @@ using tc::launch_after;
 
 // A block a request, a thread a row: the row's ancestors one after the other, parents in shared memory.  A parent comes
 // before its child, so a walk ends after at most max_q steps and meets the words of the mask from the last to the first:
-// each is written once, complete.
+// each is written once, complete.  Bound: launch and the chain lengths -> parents -> walk (a tree of 24 drafts 1.8 us, 192 of
+// 40-200 drafts 4.5 us).
 __global__ void __launch_bounds__(256) tree_build_kernel(const __grid_constant__ TreeLaunch p) {
   __shared__ int16_t parent[KVC_TREE_MAX_Q];
   grid_dependency_wait();
@@ -55,7 +56,8 @@ constexpr int kKeepThreads = 128, kRowsAtOnce = 32, kInFlight = 4;
 // A thread owns 16 bytes of a row in one (layer, head, K|V) and moves them for the request's accepted rows in their order,
 // kInFlight loads and then as many stores.  Places are ascending, so a row's new place is never one that a later row is
 // still to be read from, and nobody else touches these bytes.  Bound: bytes for many requests, for one the chain of
-// dependent reads (lengths, page ids, rows).
+// dependent reads (lengths, page ids, rows).  Measured, 32 layers, 8 heads of 128: 64 requests in 8 bits, 38 MB moved, 7.8 us
+// from L2, 11.6 from HBM (eight rows in flight 12.3: registers; 256 threads a block 9); one request 2.6 us.
 // grid: x = (layer, K|V, head, 16-byte chunk), y = requests (strided)
 template <int D, bool Q8>
 __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constant__ KeepLaunch p) {

@@ -2,8 +2,13 @@
 //
 //     (x, y) -> a (x cos - y sin, x sin + y cos) ,  angle = p f_k ,
 // over the first `rot` channels of a head.  Bound: the bytes of the rows, read once and written once.  A block has all
-// heads of a token, or of eight: they share the angles, which its threads work out while the first rows are on their way.  An angle is p f_k / 2 pi turns, less the whole ones, in float64 (position 2^20: off by 2e-10 of a turn), cos and
-// sin of the rest in float32.
+// heads of a token, or of eight: they share the angles, which its threads work out while the first rows are on their way.
+// An angle is p f_k / 2 pi turns, less the whole ones, in float64 (position 2^20: off by 2e-10 of a turn), cos and sin of
+// the rest in float32.
+//
+// Measured: five prompts of 1500-2500 tokens, 28 / 4 heads of 128 into bf16 pages (167 MB): 32 us, 5.2 TB/s of 6.5 copied
+// (a block a token 36, four 37, 32 tokens 57; streaming loads and stores no better); 32 trees of 9-63 drafts 6.8 us, 64
+// single tokens into 8-bit pages 3.2 us, where launch and the chain lists -> pages -> rows bound it.
 //
 // Layout of the work: d / 16 neighbouring lanes hold one row, 16 channels each: two 16-byte chunks that hold pairs, half a
 // rotated width apart (KVC_ROPE_HALF) or side by side.  Eight bits: the row's largest magnitude over its lanes, exponents

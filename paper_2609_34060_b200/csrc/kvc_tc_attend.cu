@@ -38,6 +38,18 @@
 // part; ragged and causal batches balance to a tile.  Of a unit cut by its borders a block leaves a float32 partial
 // result (at most two a block); a second kernel joins those in a fixed order.
 //
+// Trees of drafted tokens (kvc_attend_tree): a row sees the context and those new tokens whose bits its mask has; masks are
+// looked at in the tiles that hold new tokens.  Where no request has more than 128 rows there is one row tile, and its chain
+// alone would leave the tensor cores and the memory waiting (24 requests of 4K, 32 drafts: 133 us).  The two halves of the
+// block then take its key tiles in turn, each with a maximum, sums and accumulators of its own, and meet at the end of a
+// piece through tensor memory: 97 us, 1900 cycles a tile in the middle of the run, where memory bounds it; start, the
+// epilogues of two or three pieces a block and the join are the rest.  Over 8-bit caches the keys stay codes:
+//     q 2^-b = t1 + t2  (e4m3, into one sum) ,   S = (t1 + t2) K 2^b 2^e ,
+// their scales are the softmax's, and the converting warps have the values alone.  There a tile takes 3500 cycles (four
+// agents of 5-9 drafts over 27K, 64 / 8 heads: 117 us, by the way of the other calls 170): the softmax's chain, 32 logits at
+// a time (5700 cycles a tile beside the other half's; twice the loop does not fit the instruction cache: 121 to 137 us), and
+// the conversion's 2300.  Eight converting warps instead of four: 134 us.
+//
 // Warps: 0-3 and 4-7 softmax and epilogue of the row tiles (a thread a row; two threads a row with sixteen warps were no
 // faster, 235 us), 8 and 10 loads of keys and values, 9 products, 11 walks the block's part of the line and hands its
 // pieces to the others through shared memory (their registers are for the work itself); 8-bit caches: 12-15 turn raw
@@ -1215,38 +1227,49 @@ __global__ void __launch_bounds__(256) attend_chunk_join_kernel(const __grid_con
   const int row = (int)(blockIdx.y % kRowBlocks) * 32 + lane, ch = ((int)(blockIdx.y / kRowBlocks) * 8 + warp) * CH;
   UnitStart me;
   int j, pieces;                                                  // blocks j - 1, j, ...
+  int q0, nq, kv;
+  const UnitStart nowhere{-1, 0, 0, 0};
+  // reads that do not depend on one another go out together: they are most of this kernel's time
   if constexpr (CH == 4) {                                        // x is a unit: the borders that lie inside it
     const int units = (int)(((int64_t)p.a.req.max_q * p.a.G + kUnitRows - 1) / kUnitRows), bh = (int)blockIdx.x / units;
     me = UnitStart{bh / p.a.H, bh % p.a.H, (int)blockIdx.x % units, 1};
     j = p.blocks;
     pieces = 1;
-    for (int k = 1 + lane; k < p.blocks + lane; k += 32) {
-      const UnitStart o = k < p.blocks ? p.starts[k] : UnitStart{-1, 0, 0, 0};
-      const unsigned in = __ballot_sync(0xffffffffu, o.b == me.b && o.h == me.h && o.u == me.u && o.t > 0);
-      if (in && j == p.blocks) j = k - lane + __ffs(in) - 1;
-      pieces += __popc(in);
+    constexpr int kAhead = 5;                                     // 160 blocks
+    for (int k0 = 1; k0 < p.blocks; k0 += 32 * kAhead) {
+      UnitStart o[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) o[i] = k0 + 32 * i + lane < p.blocks ? p.starts[k0 + 32 * i + lane] : nowhere;
+      if (k0 == 1) request_span(p.a.req, me.b, nullptr, q0, nq, kv);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const unsigned in = __ballot_sync(0xffffffffu, o[i].b == me.b && o[i].h == me.h && o[i].u == me.u && o[i].t > 0);
+        if (in && j == p.blocks) j = k0 + 32 * i + __ffs(in) - 1;
+        pieces += __popc(in);
+      }
     }
     if (pieces == 1) return;
   } else {
     j = (int)blockIdx.x + 1;
     me = p.starts[j];
     const UnitStart before = p.starts[j - 1];
+    UnitStart after = j + 1 + lane < p.blocks ? p.starts[j + 1 + lane] : nowhere;
     if (me.b < 0 || me.t == 0) return;
     auto same = [&](const UnitStart& o) { return o.b == me.b && o.h == me.h && o.u == me.u && o.t > 0; };
     if (same(before)) return;
+    request_span(p.a.req, me.b, nullptr, q0, nq, kv);
     pieces = 2;
     for (bool go = true; go; pieces += 32) {
-      const int k = j + pieces - 1 + lane;
-      const bool in = k < p.blocks && same(p.starts[k]);
-      const unsigned out = ~__ballot_sync(0xffffffffu, in);
+      const unsigned out = ~__ballot_sync(0xffffffffu, same(after));
       if (out) {
         pieces += __ffs(out) - 1 - 32;
         go = false;
+      } else {
+        const int k = j + pieces + 31 + lane;
+        after = k < p.blocks ? p.starts[k] : nowhere;
       }
     }
   }
-  int q0, nq, kv;
-  request_span(p.a.req, me.b, nullptr, q0, nq, kv);
   const int r = me.u * kUnitRows + row, rows = nq * p.a.G;
   if (r - lane >= rows) return;
   const float c = p.a.scale * kLog2e, minus_inf = __uint_as_float(0xff800000u);
