@@ -1078,10 +1078,10 @@ def kvc_attend_tree(req: Requests, tree: Tree, q: torch.Tensor, cache, layer: in
     _describe(cache)
     st = _here(what, stream, (dev, tree._dev))
     _holds(req, cache, what)
-    if lse is not None and lse.shape != q.shape[:2]:
-        raise KvcError(KVC_E_INVALID_ARG, f"{what}: lse must be float32 [rows, heads]")
     block = _pack("PPCFAPPdHHP", _TREE_NAMES, dev, cache.d, 0, 0, at, t, cache, lse, workspace, 0 if workspace is None else workspace.nbytes, st,
                   cache.d ** -0.5 if scale is None else scale, q, out, layer)
+    if lse is not None and lse.shape != q.shape[:2]:
+        raise KvcError(KVC_E_INVALID_ARG, f"{what}: lse must be float32 [rows, heads]")
     _check(load().kvc_block_attend_tree(block), what)
 
 

@@ -159,7 +159,8 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
 }  // namespace
 
 cudaError_t launch_append_rotated(const RotateLaunch& r, int d, cudaStream_t s) {
-  // prompts: tiles of several tokens, whose rows stream through a block; few tokens: a block each, as many threads as it has work
+  // prompts: tiles of eight tokens, whose rows stream through a block (five prompts of 1500-2500 tokens 32 us, a block a token
+  // 36); few tokens: a block each, as many threads as it has work (32 trees of 9-63 drafts 8.1 us a call, in tiles of four 9.5)
   const int tokens = r.req.max_q >= 64 ? 8 : 1;
   const int64_t each = ((int64_t)tokens * (r.Hq + 2 * r.H) * (d / 16) + kUnroll - 1) / kUnroll;
   const int threads = each < kMaxHalfD ? kMaxHalfD : each > 256 ? 256 : (int)((each + 31) / 32 * 32);

@@ -493,6 +493,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       return true;
     };
     bool more = next_piece(0);
+    if constexpr (kSplit) more = !named_bar_or(2, 256, !more);   // both halves, or neither
     for (int piece = 0; more; ++piece) {
       const Piece& y = bars.piece[piece % kPieces];
       const int n = y.n[t], kv = y.kv, first = y.t0 * 128;
