@@ -216,7 +216,8 @@ __device__ __forceinline__ int64_t head_tiles(const ChunkLaunch& p, int nq, int 
   }
   return sum;
 }
-// The start of block c's part of the line (whole warp); up to 32 requests are looked at once.
+// The start of block c's part of the line (whole warp); up to 32 requests are looked at once.  kSplit: a request is one unit.
+template <bool kSplit>
 __device__ __forceinline__ Walk line_start(const ChunkLaunch& p, int lane, int c) {
   const int n = p.a.req.n;
   int q0 = 0, nq = 0, kv = 0;
@@ -224,7 +225,7 @@ __device__ __forceinline__ Walk line_start(const ChunkLaunch& p, int lane, int c
   auto look = [&](int b0, uint32_t* status) {                     // requests b0 .. b0 + 31
     q0 = nq = kv = 0;
     if (b0 + lane < n) request_span(p.a.req, b0 + lane, status, q0, nq, kv);
-    each = head_tiles(p, nq, kv, lane);
+    each = !kSplit ? head_tiles(p, nq, kv, lane) : units_of(p, nq) > 0 ? unit_tiles(p.a, nq, kv, nq * p.a.G, 0).all : 0;
     incl = warp_scan(each * p.a.H, lane);
   };
   for (int b0 = 0; b0 < n; b0 += 32) {
@@ -253,6 +254,11 @@ __device__ __forceinline__ Walk line_start(const ChunkLaunch& p, int lane, int c
     int64_t off = lo - before - (__shfl_sync(0xffffffffu, incl, l) - head * p.a.H);
     w.h = (int)divide(off, head);
     off -= w.h * head;
+    if constexpr (kSplit) {
+      w.t = (int)off;
+      w.left = divide(total * (c + 1), blocks) - lo;
+      return w;
+    }
     for (int u0 = 0; u0 < w.units; u0 += 32) {
       const int mine = u0 + lane < w.units ? unit_tiles(p.a, w.nq, w.kv, w.nq * p.a.G, u0 + lane).all : 0;
       const int sum = (int)warp_scan(mine, lane);
@@ -391,7 +397,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
   grid_dependency_wait();                                         // what follows reads what earlier kernels wrote
   grid_dependents_launch();                                       // the join's blocks may take the SMs that finish first
   Walk walk;                                                      // warp 11: the block's part of the line
-  if (warp == 11) walk = line_start(p, lane, (int)blockIdx.x);
+  if (warp == 11) walk = line_start<kSplit>(p, lane, (int)blockIdx.x);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
