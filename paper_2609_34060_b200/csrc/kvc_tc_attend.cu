@@ -830,14 +830,12 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         float o[16];
         if (n > 0) {
           tmem_ld16(o_at + k, o);
-          tmem_ld_wait();
+          if (!kSplit) tmem_ld_wait();
         }
         if constexpr (kSplit) {
           float v[16];
-          if (n_other > 0) {
-            tmem_ld16(o_other + k, v);
-            tmem_ld_wait();
-          }
+          if (n_other > 0) tmem_ld16(o_other + k, v);
+          tmem_ld_wait();
           // a half that saw no key of the row gets no weight, whatever its accumulators hold
 #pragma unroll
           for (int j = 0; j < 16; ++j) o[j] = (keep == 0.f ? 0.f : o[j] * keep) + (other == 0.f ? 0.f : v[j] * other);
