@@ -45,10 +45,16 @@
 // piece through tensor memory: 97 us, 1900 cycles a tile in the middle of the run, where memory bounds it; start, the
 // epilogues of two or three pieces a block and the join are the rest.  Over 8-bit caches the keys stay codes:
 //     q 2^-b = t1 + t2  (e4m3, into one sum) ,   S = (t1 + t2) K 2^b 2^e ,
-// their scales are the softmax's, and the converting warps have the values alone.  There a tile takes 3500 cycles (four
-// agents of 5-9 drafts over 27K, 64 / 8 heads: 117 us, by the way of the other calls 170): the softmax's chain, 32 logits at
-// a time (5700 cycles a tile beside the other half's; twice the loop does not fit the instruction cache: 121 to 137 us), and
-// the conversion's 2300.  Eight converting warps instead of four: 134 us.
+// their scales are the softmax's, and the converting warps have the values alone.  32 values' rows (a converting warp's)
+// become f16 where their scales allow it, and the probabilities that meet them as well: one instruction makes two codes a
+// pair, where bf16 takes five.  They allow it between 2^-15 and 2^-1: every code is then exact, and what f16 cuts off a
+// probability, 2^-25 of the largest, weighs with a value of 224 no more than bf16's rounding of an output that the smallest
+// rows make (2^-9 of 2^-7).  Everything else goes as bf16, 32 keys at a time, into the same sums.
+// Measured, four agents of 5-9 drafts over 27K, 64 / 8 heads: 104 us (by the way of the other calls 170, values in bf16 alone
+// 109).  The softmax's chain bounds it, 32 logits at a time, and with it the instruction cache that it shares with the
+// conversion: the loop twice as long takes 140 us, with the masks of a tile inside it 110, with the next logits asked for
+// ahead (copies between registers) 122, the conversion in four rounds instead of unrolled 115.  Eight converting warps
+// instead of four: 134 us.
 //
 // Warps: 0-3 and 4-7 softmax and epilogue of the row tiles (a thread a row; two threads a row with sixteen warps were no
 // faster, 235 us), 8 and 10 loads of keys and values, 9 products, 11 walks the block's part of the line and hands its
@@ -102,9 +108,9 @@ struct Shape {
   static constexpr int kScales = kDirect ? 4 : 1;                 // tiles whose keys' scales are held
 
   static constexpr int kThreads = Q8 ? 512 : 384;
-  static constexpr int kRegs = kDirect ? 168 : Q8 ? 184 : 208;    // of the softmax warps (kDirect, four agents of 27K: 152: 123 us, 168: 119, 184: 122)
+  static constexpr int kRegs = kDirect ? 168 : Q8 ? 184 : 208;    // of the softmax warps (kDirect, four agents of 27K: 152: 107 us, 168 and 184: 104)
   static constexpr int kRegsOthers = kDirect ? 88 : Q8 ? 72 : 88;
-  static constexpr int kSmem = 1024 + kQTiles * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0) + (kDirect ? kKeySlots * kRaw + kScales * 512 + 8192 : 0);
+  static constexpr int kSmem = 1024 + kQTiles * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0) + (kDirect ? kKeySlots * kRaw + kScales * 512 + 512 + 8192 : 0);
 };
 
 // Key tiles of unit u of a request (at least one, so that rows without keys are answered too), and of its two row tiles.
@@ -282,6 +288,7 @@ struct Bars {
   uint64_t q_full[2], s_full[2], p_ready[2][2], o_done[2], o_most[2];   // o_most: the first 96 keys' product (kDirect)
   uint64_t full[NS], empty[NS], raw_full[NR], raw_empty[NR], key_full[NK], key_empty[NK], scale_full[NE], scale_empty[NE], piece_full[kPieces], piece_empty[kPieces];
   Piece piece[kPieces];
+  uint32_t part_f16[NE], value_f16[NS];    // kDirect: a byte for every 32 keys, whether P and V are f16 there (else bf16)
   uint32_t tmem;
   int abort_flag;
 };
@@ -328,6 +335,22 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t to_f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+// two e4m3 codes as an f16 pair: exact, a NaN stays one
+__device__ __forceinline__ uint32_t codes_to_f16x2(uint32_t two) {
+  uint32_t d;
+  asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(d) : "r"(two));
+  return d;
+}
 
 // kTree: the new tokens of a request form a tree; a row sees the context and those new tokens whose bits are set in its mask.
 // kSplit: no request has more than 128 rows.  The two halves of the block then share one row tile and take its key tiles in
@@ -346,7 +369,8 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
   uint8_t* sraw = skv + SH::kSlots * SH::kTile;
   uint8_t* skey = sraw + SH::kRawSlots * SH::kRaw;                // kDirect
   float* sscale = reinterpret_cast<float*>(skey + SH::kKeySlots * SH::kRaw);   // [kScales][128]
-  float* stwin = sscale + SH::kScales * 128;                      // [2][16][64] sums on their way from a row's second lane to its first
+  float* sone = sscale + SH::kScales * 128;                       // [128] ones: the scales of logits that have been scaled
+  float* stwin = sone + 128;                                      // [2][16][64] sums on their way from a row's second lane to its first
   constexpr bool kDirect = SH::kDirect;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort_flag = &bars.abort_flag;
@@ -386,6 +410,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
     bars.abort_flag = 0;
     fence_barrier_init();
   }
+  if (kDirect && tid >= 64 && tid < 192) sone[tid - 64] = 1.f;
   if (tid == 32) {
     prefetch_map(&map_k);
     prefetch_map(&map_v);
@@ -559,37 +584,49 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           continue;
         }
         if constexpr (kDirect) {
-          // 32 logits at a time, the next ones on their way: all of a tile in registers beside the rest found no room (300
-          // bytes of spills: 159 us on four requests of 27K), and the instruction cache holds a short loop (64 at a time:
-          // 118 us).  The maximum is taken before the probabilities; where a later part's is far above, the probabilities
-          // before it, which lie over their logits by then, are scaled: by a power of two, so that bf16 loses nothing.  mc is
-          // the maximum in steps of 2.
+          // 32 logits at a time: all of a tile in registers beside the rest found no room (300 bytes of spills: 159 us on four
+          // requests of 27K), and the instruction cache holds a short loop.  The maximum is taken before the probabilities;
+          // where a later part's is far above, the probabilities before it, which lie over their logits by then, are scaled:
+          // by a power of two, so that bf16 loses nothing, and f16 half a step of its subnormals.  mc is the maximum in steps
+          // of 2.
           const int es = (g + kt) % SH::kScales;
           const float4* ks = reinterpret_cast<const float4*>(sscale + es * 128);
+          const uint32_t types = *reinterpret_cast<const volatile uint32_t*>(&bars.part_f16[es]);
           const bool hidden = lowest < t0 + 127 || (kTree && t0 + 127 >= fresh);
           if (!(kTree && t0 + 127 >= fresh)) sees[0] = sees[1] = sees[2] = sees[3] = 0xffffffffu;
           const f32x2 c2 = f2_pack(c, c);
           f32x2 sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
-          constexpr int W = 32;                                   // 16: 128 us
-          float next[W];
-          tmem_ld32(s_at + key0, next);
+          if (hidden) {
+            // masked tiles: their logits are scaled and masked in place, beside scales of one (masking the parts in the loop
+            // below would put cold code between its instructions)
 #pragma unroll 1
-          for (int q = key0; q < key1; q += W) {
-            float s[W];
-            tmem_ld_wait();
-#pragma unroll
-            for (int k = 0; k < W; k += 4) {                      // the keys' scales
-              const float4 e = ks[(q + k) >> 2];
-              f2_unpack(f2_mul(f2_pack(next[k], next[k + 1]), f2_pack(e.x, e.y)), s[k], s[k + 1]);
-              f2_unpack(f2_mul(f2_pack(next[k + 2], next[k + 3]), f2_pack(e.z, e.w)), s[k + 2], s[k + 3]);
-            }
-            if (q + W < key1) tmem_ld32(s_at + q + W, next);
-            if (hidden) {
-              const int last = lim - t0 - q;                      // of the part's keys
+            for (int q = key0; q < key1; q += 8) {
+              float s[8];
+              tmem_ld8(s_at + q, s);
+              tmem_ld_wait();
+              const int last = lim - t0 - q;
               uint32_t bits = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1u;
               bits &= (q < 32 ? sees[0] : q < 64 ? sees[1] : q < 96 ? sees[2] : sees[3]) >> (q & 31);
 #pragma unroll
-              for (int k = 0; k < W; ++k) s[k] = (bits >> k) & 1u ? s[k] : minus_inf;
+              for (int k = 0; k < 8; ++k) s[k] = (bits >> k) & 1u ? s[k] * sscale[es * 128 + q + k] : minus_inf;
+              tmem_st8(s_at + q, reinterpret_cast<const uint32_t*>(s));
+            }
+            tmem_st_wait();
+            ks = reinterpret_cast<const float4*>(sone);
+          }
+          constexpr int W = 32;
+#pragma unroll 1
+          for (int q = key0; q < key1; q += W) {
+            float s[W];
+            float4 e[W / 4];                                      // the keys' scales
+            tmem_ld32(s_at + q, s);
+#pragma unroll
+            for (int k = 0; k < W / 4; ++k) e[k] = ks[(q >> 2) + k];
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < W; k += 4) {
+              f2_unpack(f2_mul(f2_pack(s[k], s[k + 1]), f2_pack(e[k >> 2].x, e[k >> 2].y)), s[k], s[k + 1]);
+              f2_unpack(f2_mul(f2_pack(s[k + 2], s[k + 3]), f2_pack(e[k >> 2].z, e[k >> 2].w)), s[k + 2], s[k + 3]);
             }
             float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
@@ -616,9 +653,17 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
                 uint32_t w[8];
                 tmem_ld8(s_at + k, reinterpret_cast<float*>(w));
                 tmem_ld_wait();
-                const uint32_t two = pack2(keep, keep);
+                if ((types >> (k >> 4 << 3)) & 1u) {
+                  // in two steps: f16 ends at 2^-24, and probabilities may stand 2^kLazy above the old maximum
+                  const float first = fmaxf(keep, 0x1p-12f), then = keep < 0x1p-12f ? keep * 0x1p12f : 1.f;
+                  const uint32_t one = to_f16x2(first, first), two = to_f16x2(then, then);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = mul_bf16x2(w[j], two);
+                  for (int j = 0; j < 8; ++j) w[j] = mul_f16x2(mul_f16x2(w[j], one), two);
+                } else {
+                  const uint32_t two = pack2(keep, keep);
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) w[j] = mul_bf16x2(w[j], two);
+                }
                 tmem_st8(s_at + k, w);
               }
               if (it > 0 || late) {                               // the sums so far, once the product that wrote them last is done
@@ -639,14 +684,21 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             const float at = mc == minus_inf ? 0.f : mc;
             const f32x2 mc2 = f2_pack(-at, -at);
             uint32_t w[W / 2];
+            auto probabilities = [&](auto to_pair) {
 #pragma unroll
-            for (int k = 0; k < W / 2; ++k) {
-              float a, b;
-              f2_unpack(f2_fma(f2_pack(s[2 * k], s[2 * k + 1]), c2, mc2), a, b);
-              const f32x2 e = f2_pack(exp2_fast(a), exp2_fast(b));
-              sum2[k & 1] = f2_add(sum2[k & 1], e);
-              w[k] = f2_to_bf16x2(e);
-            }
+              for (int k = 0; k < W / 2; ++k) {
+                float a, b;
+                f2_unpack(f2_fma(f2_pack(s[2 * k], s[2 * k + 1]), c2, mc2), a, b);
+                a = exp2_fast(a);
+                b = exp2_fast(b);
+                sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(a, b));
+                w[k] = to_pair(a, b);
+              }
+            };
+            if ((types >> (q >> 5 << 3)) & 1u)
+              probabilities([](float a, float b) { return to_f16x2(a, b); });
+            else
+              probabilities([](float a, float b) { return pack2(a, b); });
             tmem_st16(s_at + q / 2, w);                     // over logits that have been read
             if (!twin && (q + W == 96 || q + W == 128)) {         // behind 96 and behind all 128 keys
               tmem_st_wait();
@@ -856,7 +908,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         if (!live || !ok || second) continue;
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] = dead ? 0.f : o[j] * inv;
-        if (Q8) {                                                 // channels back in their places
+        if (Q8 && !kDirect) {                                     // channels back in their places
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
             const float v = o[j + 1];
@@ -1003,18 +1055,20 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             const uint32_t par = (uint32_t)count[t]++ & 1u;
             if (!loaded(vu)) break;
             const uint64_t vd = v_desc + (uint32_t)(vs * (SH::kTile >> 4));
+            const uint32_t types = kDirect ? *reinterpret_cast<const volatile uint32_t*>(&bars.value_f16[vs]) : 0u;
+            auto idesc = [&](int k) { return kDirect && ((types >> (k >> 1 << 3)) & 1u) ? idesc_f16(idesc_o) : idesc_o; };
             if (!wait(p_ready + 16 * t, par)) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, i > 1 || k > 0);
+              for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc(k), i > 1 || k > 0);
               if (kDirect) umma_commit(o_most + 8 * t);
             }
             if (!wait(p_ready + 16 * t + 8, par)) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-              for (int k = 6; k < 8; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, 1);
+              for (int k = 6; k < 8; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc(k), 1);
               umma_commit(o_done + 8 * t);
             }
             release(vs);
@@ -1117,12 +1171,15 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           exponents(next, page, nk, nv);
           if (kDirect) page = page_of(it + 2 < n ? tt + 256 : x.kv);
           const bool valid = tt < x.kv;
+          bool f16 = false;                                       // of the warp's rows: f16 takes their values (2^-15 <= scale <= 2^-1)
           if constexpr (kDirect) {
             // the keys' scales go to the softmax; the values alone are converted
             const int es = scales % SH::kScales;
             ok = wait_all(scale_empty + 8 * es, ((scales / SH::kScales) & 1) ^ 1, abort_flag);
             if (!ok) break;
             sscale[es * 128 + r] = exponent_up(ek);
+            f16 = __all_sync(0xffffffffu, valid && ev - 112u <= 14u);
+            if (lane == 0) reinterpret_cast<volatile uint8_t*>(&bars.part_f16[es])[warp - 12] = f16;
             mbar_arrive(scale_full + 8 * es);
             ++scales;
           }
@@ -1134,6 +1191,32 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             uint8_t* out = skv + slot * SH::kTile + (r >> 3) * 1024 + (r & 7) * 128;
             // 2^120 2^(e - 127), in one factor where bf16 holds it; exponent 255 reads as NaN
             const uint32_t e = kv ? ev : ek;
+            if (kDirect && lane == 0) reinterpret_cast<volatile uint8_t*>(&bars.value_f16[slot])[warp - 12] = f16;
+            if (kDirect && f16) {
+              const uint32_t two = to_f16x2(exponent_up(e), exponent_up(e));
+              uint4 raw[2];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + ((j ^ sw) << 4));
+#pragma unroll
+              for (int c0 = 0; c0 < CH; c0 += 2) {
+                const uint4 now[2] = {raw[0], raw[1]};
+                if (c0 + 2 < CH) {
+#pragma unroll
+                  for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + (((c0 + 2 + j) ^ sw) << 4));
+                }
+#pragma unroll
+                for (int jj = 0; jj < 2; ++jj) {
+                  const uint32_t w[4] = {now[jj].x, now[jj].y, now[jj].z, now[jj].w};
+                  uint32_t o[8];
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) o[j] = mul_f16x2(codes_to_f16x2(j & 1 ? w[j >> 1] >> 16 : w[j >> 1]), two);
+                  const int ch = c0 + jj, j0 = (2 * ch) & 7;
+                  uint8_t* q = out + (ch >> 2) * 16384;
+                  *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                  *reinterpret_cast<uint4*>(q + (((j0 + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+              }
+            } else {
             const uint32_t f1 = e == 255u ? 0x7fc0u : e > 134u ? 254u << 7 : (e + 120u) << 7;
             const uint32_t scale = f1 | (f1 << 16);
             uint32_t nan = 0;
@@ -1161,6 +1244,14 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
               }
 #pragma unroll
               for (int j = 0; j < 8; ++j) o[j] = mul_bf16x2(o[j], scale);
+              if (kDirect) {                                      // there in their order
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                  const uint32_t even = o[j], odd = o[j + 1];
+                  o[j] = __byte_perm(even, odd, 0x5410);
+                  o[j + 1] = __byte_perm(even, odd, 0x7632);
+                }
+              }
               uint8_t* q = out + (ch >> 2) * 16384;
               const int j0 = (2 * ch) & 7;
               *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
@@ -1178,9 +1269,10 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
                   const float2 lo = e4m3x2_to_float2(w[j] & 0xffffu), hi = e4m3x2_to_float2(w[j] >> 16);
                   const int at = 2 * ch + (j >> 1);
                   *reinterpret_cast<uint2*>(out + (at >> 3) * 16384 + (((at & 7) ^ (r & 7)) << 4) + (j & 1) * 8) =
-                      make_uint2(pack2(lo.x * s, hi.x * s), pack2(lo.y * s, hi.y * s));
+                      kDirect ? make_uint2(pack2(lo.x * s, lo.y * s), pack2(hi.x * s, hi.y * s)) : make_uint2(pack2(lo.x * s, hi.x * s), pack2(lo.y * s, hi.y * s));
                 }
               }
+            }
             }
             fence_proxy_async();
             mbar_arrive(full + 8 * slot);
