@@ -50,8 +50,8 @@
 // pair, where bf16 takes five.  They allow it between 2^-15 and 2^-1: every code is then exact, and what f16 cuts off a
 // probability, 2^-25 of the largest, weighs with a value of 224 no more than bf16's rounding of an output that the smallest
 // rows make (2^-9 of 2^-7).  Everything else goes as bf16, 32 keys at a time, into the same sums.
-// Measured, four agents of 5-9 drafts over 27K, 64 / 8 heads: 104 us (by the way of the other calls 170, values in bf16 alone
-// 109).  The softmax's chain bounds it, 32 logits at a time, and with it the instruction cache that it shares with the
+// Measured, four agents of 5-9 drafts over 27K, 64 / 8 heads: 104 us, 115 where no row's scale allows f16 (by the way of the
+// other calls 170).  The softmax's chain bounds it, 32 logits at a time, and with it the instruction cache that it shares with the
 // conversion: the loop twice as long takes 140 us, with the masks of a tile inside it 110, with the next logits asked for
 // ahead (copies between registers) 122, the conversion in four rounds instead of unrolled 115.  Eight converting warps
 // instead of four: 134 us.
@@ -1193,6 +1193,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             const uint32_t e = kv ? ev : ek;
             if (kDirect && lane == 0) reinterpret_cast<volatile uint8_t*>(&bars.value_f16[slot])[warp - 12] = f16;
             if (kDirect && f16) {
+              // unrolled whole, short as it is: four requests of 12 drafts over 27K 102 us, in rounds of four chunks 108
               const uint32_t two = to_f16x2(exponent_up(e), exponent_up(e));
               uint4 raw[2];
 #pragma unroll
@@ -1217,62 +1218,62 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
                 }
               }
             } else {
-            const uint32_t f1 = e == 255u ? 0x7fc0u : e > 134u ? 254u << 7 : (e + 120u) << 7;
-            const uint32_t scale = f1 | (f1 << 16);
-            uint32_t nan = 0;
-            // two chunks a round, the next round's on their way: unrolled whole, this code and the softmax's displace each
-            // other in the instruction cache
-            uint4 raw[2];
+              const uint32_t f1 = e == 255u ? 0x7fc0u : e > 134u ? 254u << 7 : (e + 120u) << 7;
+              const uint32_t scale = f1 | (f1 << 16);
+              uint32_t nan = 0;
+              // two chunks a round, the next round's on their way: unrolled whole, this code and the softmax's displace each
+              // other in the instruction cache
+              uint4 raw[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + ((j ^ sw) << 4));
+              for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + ((j ^ sw) << 4));
 #pragma unroll 1
-            for (int c0 = 0; c0 < CH; c0 += 2) {
-             const uint4 now[2] = {raw[0], raw[1]};
-             if (c0 + 2 < CH) {
+              for (int c0 = 0; c0 < CH; c0 += 2) {
+               const uint4 now[2] = {raw[0], raw[1]};
+               if (c0 + 2 < CH) {
 #pragma unroll
-               for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + (((c0 + 2 + j) ^ sw) << 4));
-             }
+                 for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + (((c0 + 2 + j) ^ sw) << 4));
+               }
 #pragma unroll
-             for (int jj = 0; jj < 2; ++jj) {
-              const int ch = c0 + jj;
-              const uint32_t w[4] = {valid ? now[jj].x : 0u, valid ? now[jj].y : 0u, valid ? now[jj].z : 0u, valid ? now[jj].w : 0u};
-              uint32_t o[8];
+               for (int jj = 0; jj < 2; ++jj) {
+                const int ch = c0 + jj;
+                const uint32_t w[4] = {valid ? now[jj].x : 0u, valid ? now[jj].y : 0u, valid ? now[jj].z : 0u, valid ? now[jj].w : 0u};
+                uint32_t o[8];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                spread_codes(w[j], o[2 * j], o[2 * j + 1]);
-                nan |= (w[j] & 0x7f7f7f7fu) + 0x01010101u;
-              }
-#pragma unroll
-              for (int j = 0; j < 8; ++j) o[j] = mul_bf16x2(o[j], scale);
-              if (kDirect) {                                      // there in their order
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                  const uint32_t even = o[j], odd = o[j + 1];
-                  o[j] = __byte_perm(even, odd, 0x5410);
-                  o[j + 1] = __byte_perm(even, odd, 0x7632);
-                }
-              }
-              uint8_t* q = out + (ch >> 2) * 16384;
-              const int j0 = (2 * ch) & 7;
-              *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-              *reinterpret_cast<uint4*>(q + (((j0 + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
-             }
-            }
-            if (((nan & 0x80808080u) != 0 || e > 134u) && valid) {
-              // a NaN code in the row, or a scale beyond one factor: the plain way
-              const float s = exponent_up(e);
-#pragma unroll 1
-              for (int ch = 0; ch < CH; ++ch) {
-                const uint4 v = *reinterpret_cast<const uint4*>(in + ((ch ^ sw) << 4));
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
                 for (int j = 0; j < 4; ++j) {
-                  const float2 lo = e4m3x2_to_float2(w[j] & 0xffffu), hi = e4m3x2_to_float2(w[j] >> 16);
-                  const int at = 2 * ch + (j >> 1);
-                  *reinterpret_cast<uint2*>(out + (at >> 3) * 16384 + (((at & 7) ^ (r & 7)) << 4) + (j & 1) * 8) =
-                      kDirect ? make_uint2(pack2(lo.x * s, lo.y * s), pack2(hi.x * s, hi.y * s)) : make_uint2(pack2(lo.x * s, hi.x * s), pack2(lo.y * s, hi.y * s));
+                  spread_codes(w[j], o[2 * j], o[2 * j + 1]);
+                  nan |= (w[j] & 0x7f7f7f7fu) + 0x01010101u;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = mul_bf16x2(o[j], scale);
+                if (kDirect) {                                      // there in their order
+#pragma unroll
+                  for (int j = 0; j < 8; j += 2) {
+                    const uint32_t even = o[j], odd = o[j + 1];
+                    o[j] = __byte_perm(even, odd, 0x5410);
+                    o[j + 1] = __byte_perm(even, odd, 0x7632);
+                  }
+                }
+                uint8_t* q = out + (ch >> 2) * 16384;
+                const int j0 = (2 * ch) & 7;
+                *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4*>(q + (((j0 + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+               }
+              }
+              if (((nan & 0x80808080u) != 0 || e > 134u) && valid) {
+                // a NaN code in the row, or a scale beyond one factor: the plain way
+                const float s = exponent_up(e);
+#pragma unroll 1
+                for (int ch = 0; ch < CH; ++ch) {
+                  const uint4 v = *reinterpret_cast<const uint4*>(in + ((ch ^ sw) << 4));
+                  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                  for (int j = 0; j < 4; ++j) {
+                    const float2 lo = e4m3x2_to_float2(w[j] & 0xffffu), hi = e4m3x2_to_float2(w[j] >> 16);
+                    const int at = 2 * ch + (j >> 1);
+                    *reinterpret_cast<uint2*>(out + (at >> 3) * 16384 + (((at & 7) ^ (r & 7)) << 4) + (j & 1) * 8) =
+                        kDirect ? make_uint2(pack2(lo.x * s, lo.y * s), pack2(hi.x * s, hi.y * s)) : make_uint2(pack2(lo.x * s, hi.x * s), pack2(lo.y * s, hi.y * s));
+                  }
                 }
               }
-            }
             }
             fence_proxy_async();
             mbar_arrive(full + 8 * slot);
