@@ -1493,8 +1493,9 @@ struct Plan {
   bool chunk;
 };
 // Trees (split): 17 to 128 rows go to this kernel alone, whose block then works on one row tile.  Measured, us, the few-rows
-// kernel and this one, 4 query heads of 128 a KV head: 24 requests of 4K, 32 rows, bf16 115 and 89, 8 bits 208 and 129; of 600
-// keys 67 and 38, 94 and 54; 16 rows of 4K 88 and 85, 103 and 128.  (Chains without a tree stay where they were.)
+// kernel and this one, 24 requests, 4 query heads of 128 a KV head: 4K keys, 32 rows, bf16 105 and 77, 8 bits 189 and 105; 600
+// keys 63 and 34, 89 and 50; 16 rows of 4K 83 and 76, 96 and 106, of 600 33 and 31, 46 and 48 (one border for both kinds of
+// cache, so that up to there a chain has the bits of the call without a tree).  Chains without a tree stay where they were.
 static bool split_rows(int64_t rows) { return rows > kSplitAbove && rows <= kSplitRows; }
 static Plan attend_plan(int n, int max_q, int max_kv, int G, int H, bool split) {
   const int64_t rows = (int64_t)max_q * G;
