@@ -45,16 +45,14 @@
 // piece through tensor memory: 97 us, 1900 cycles a tile in the middle of the run, where memory bounds it; start, the
 // epilogues of two or three pieces a block and the join are the rest.  Over 8-bit caches the keys stay codes:
 //     q 2^-b = t1 + t2  (e4m3, into one sum) ,   S = (t1 + t2) K 2^b 2^e ,
-// their scales are the softmax's, and the converting warps have the values alone.  32 values' rows (a converting warp's)
-// become f16 where their scales allow it, and the probabilities that meet them as well: one instruction makes two codes a
-// pair, where bf16 takes five.  They allow it between 2^-15 and 2^-1: every code is then exact, and what f16 cuts off a
-// probability, 2^-25 of the largest, weighs with a value of 224 no more than bf16's rounding of an output that the smallest
-// rows make (2^-9 of 2^-7).  Everything else goes as bf16, 32 keys at a time, into the same sums.
-// Measured, four agents of 5-9 drafts over 27K, 64 / 8 heads: 104 us, 115 where no row's scale allows f16 (by the way of the
-// other calls 170).  The softmax's chain bounds it, 32 logits at a time, and with it the instruction cache that it shares with the
-// conversion: the loop twice as long takes 140 us, with the masks of a tile inside it 110, with the next logits asked for
-// ahead (copies between registers) 122, the conversion in four rounds instead of unrolled 115.  Eight converting warps
-// instead of four: 134 us.
+// their scales are the softmax's, and the converting warps have the values alone, as bf16 like the probabilities that meet
+// them.  (Float16 turns two codes into a pair in one instruction, bf16 takes four; but it ends at 2^-24 of a row's largest
+// probability, and where that one's value is small, thousands of keys below it are the answer.  With float16 where the
+// values' scales allowed it: 104 us.)
+// Measured, four agents of 5-9 drafts over 27K, 64 / 8 heads: 106 us (by the way of the other calls 170).  The softmax's
+// chain bounds it, 32 logits at a time, and with it the instruction cache that it shares with the conversion: the loop twice
+// as long takes a third more, with the masks of a tile inside it 6 us more, with the next logits asked for ahead (copies
+// between registers) 18, and eight converting warps instead of four 30.
 //
 // Warps: 0-3 and 4-7 softmax and epilogue of the row tiles (a thread a row; two threads a row with sixteen warps were no
 // faster, 235 us), 8 and 10 loads of keys and values, 9 products, 11 walks the block's part of the line and hands its
@@ -108,7 +106,7 @@ struct Shape {
   static constexpr int kScales = kDirect ? 4 : 1;                 // tiles whose keys' scales are held
 
   static constexpr int kThreads = Q8 ? 512 : 384;
-  static constexpr int kRegs = kDirect ? 168 : Q8 ? 184 : 208;    // of the softmax warps (kDirect, four agents of 27K: 152: 107 us, 168 and 184: 104)
+  static constexpr int kRegs = kDirect ? 168 : Q8 ? 184 : 208;    // of the softmax warps (kDirect, four agents of 27K: 152 3 us more than 168 and 184)
   static constexpr int kRegsOthers = kDirect ? 88 : Q8 ? 72 : 88;
   static constexpr int kSmem = 1024 + kQTiles * kTile + kSlots * kTile + (Q8 ? kRawSlots * kRaw : 0) + (kDirect ? kKeySlots * kRaw + kScales * 512 + 512 + 8192 : 0);
 };
@@ -288,7 +286,6 @@ struct Bars {
   uint64_t q_full[2], s_full[2], p_ready[2][2], o_done[2], o_most[2];   // o_most: the first 96 keys' product (kDirect)
   uint64_t full[NS], empty[NS], raw_full[NR], raw_empty[NR], key_full[NK], key_empty[NK], scale_full[NE], scale_empty[NE], piece_full[kPieces], piece_empty[kPieces];
   Piece piece[kPieces];
-  uint32_t part_f16[NE], value_f16[NS];    // kDirect: a byte for every 32 keys, whether P and V are f16 there (else bf16)
   uint32_t tmem;
   int abort_flag;
 };
@@ -333,22 +330,6 @@ __device__ __forceinline__ void spread_codes(uint32_t w, uint32_t& even, uint32_
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-__device__ __forceinline__ uint32_t to_f16x2(float lo, float hi) {
-  uint32_t d;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-  return d;
-}
-// two e4m3 codes as an f16 pair: exact, a NaN stays one
-__device__ __forceinline__ uint32_t codes_to_f16x2(uint32_t two) {
-  uint32_t d;
-  asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(d) : "r"(two));
   return d;
 }
 
@@ -587,11 +568,9 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           // 32 logits at a time: all of a tile in registers beside the rest found no room (300 bytes of spills: 159 us on four
           // requests of 27K), and the instruction cache holds a short loop.  The maximum is taken before the probabilities;
           // where a later part's is far above, the probabilities before it, which lie over their logits by then, are scaled:
-          // by a power of two, so that bf16 loses nothing, and f16 half a step of its subnormals.  mc is the maximum in steps
-          // of 2.
+          // by a power of two, so that bf16 loses nothing.  mc is the maximum in steps of 2.
           const int es = (g + kt) % SH::kScales;
           const float4* ks = reinterpret_cast<const float4*>(sscale + es * 128);
-          const uint32_t types = *reinterpret_cast<const volatile uint32_t*>(&bars.part_f16[es]);
           const bool hidden = lowest < t0 + 127 || (kTree && t0 + 127 >= fresh);
           if (!(kTree && t0 + 127 >= fresh)) sees[0] = sees[1] = sees[2] = sees[3] = 0xffffffffu;
           const f32x2 c2 = f2_pack(c, c);
@@ -653,17 +632,9 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
                 uint32_t w[8];
                 tmem_ld8(s_at + k, reinterpret_cast<float*>(w));
                 tmem_ld_wait();
-                if ((types >> (k >> 4 << 3)) & 1u) {
-                  // in two steps: f16 ends at 2^-24, and probabilities may stand 2^kLazy above the old maximum
-                  const float first = fmaxf(keep, 0x1p-12f), then = keep < 0x1p-12f ? keep * 0x1p12f : 1.f;
-                  const uint32_t one = to_f16x2(first, first), two = to_f16x2(then, then);
+                const uint32_t two = pack2(keep, keep);
 #pragma unroll
-                  for (int j = 0; j < 8; ++j) w[j] = mul_f16x2(mul_f16x2(w[j], one), two);
-                } else {
-                  const uint32_t two = pack2(keep, keep);
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) w[j] = mul_bf16x2(w[j], two);
-                }
+                for (int j = 0; j < 8; ++j) w[j] = mul_bf16x2(w[j], two);
                 tmem_st8(s_at + k, w);
               }
               if (it > 0 || late) {                               // the sums so far, once the product that wrote them last is done
@@ -684,21 +655,15 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             const float at = mc == minus_inf ? 0.f : mc;
             const f32x2 mc2 = f2_pack(-at, -at);
             uint32_t w[W / 2];
-            auto probabilities = [&](auto to_pair) {
 #pragma unroll
-              for (int k = 0; k < W / 2; ++k) {
-                float a, b;
-                f2_unpack(f2_fma(f2_pack(s[2 * k], s[2 * k + 1]), c2, mc2), a, b);
-                a = exp2_fast(a);
-                b = exp2_fast(b);
-                sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(a, b));
-                w[k] = to_pair(a, b);
-              }
-            };
-            if ((types >> (q >> 5 << 3)) & 1u)
-              probabilities([](float a, float b) { return to_f16x2(a, b); });
-            else
-              probabilities([](float a, float b) { return pack2(a, b); });
+            for (int k = 0; k < W / 2; ++k) {
+              float a, b;
+              f2_unpack(f2_fma(f2_pack(s[2 * k], s[2 * k + 1]), c2, mc2), a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+              sum2[k & 1] = f2_add(sum2[k & 1], f2_pack(a, b));
+              w[k] = pack2(a, b);
+            }
             tmem_st16(s_at + q / 2, w);                     // over logits that have been read
             if (!twin && (q + W == 96 || q + W == 128)) {         // behind 96 and behind all 128 keys
               tmem_st_wait();
@@ -908,7 +873,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         if (!live || !ok || second) continue;
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[j] = dead ? 0.f : o[j] * inv;
-        if (Q8 && !kDirect) {                                     // channels back in their places
+        if (Q8) {                                                 // channels back in their places
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
             const float v = o[j + 1];
@@ -1055,20 +1020,18 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             const uint32_t par = (uint32_t)count[t]++ & 1u;
             if (!loaded(vu)) break;
             const uint64_t vd = v_desc + (uint32_t)(vs * (SH::kTile >> 4));
-            const uint32_t types = kDirect ? *reinterpret_cast<const volatile uint32_t*>(&bars.value_f16[vs]) : 0u;
-            auto idesc = [&](int k) { return kDirect && ((types >> (k >> 1 << 3)) & 1u) ? idesc_f16(idesc_o) : idesc_o; };
             if (!wait(p_ready + 16 * t, par)) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc(k), i > 1 || k > 0);
+              for (int k = 0; k < 6; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, i > 1 || k > 0);
               if (kDirect) umma_commit(o_most + 8 * t);
             }
             if (!wait(p_ready + 16 * t + 8, par)) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-              for (int k = 6; k < 8; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc(k), 1);
+              for (int k = 6; k < 8; ++k) umma_bf16_ts(tmem + 256 + t * D, tmem + t * 128 + 8 * k, vd + k * v_step, idesc_o, 1);
               umma_commit(o_done + 8 * t);
             }
             release(vs);
@@ -1171,15 +1134,12 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           exponents(next, page, nk, nv);
           if (kDirect) page = page_of(it + 2 < n ? tt + 256 : x.kv);
           const bool valid = tt < x.kv;
-          bool f16 = false;                                       // of the warp's rows: f16 takes their values (2^-15 <= scale <= 2^-1)
           if constexpr (kDirect) {
             // the keys' scales go to the softmax; the values alone are converted
             const int es = scales % SH::kScales;
             ok = wait_all(scale_empty + 8 * es, ((scales / SH::kScales) & 1) ^ 1, abort_flag);
             if (!ok) break;
             sscale[es * 128 + r] = exponent_up(ek);
-            f16 = __all_sync(0xffffffffu, valid && ev - 112u <= 14u);
-            if (lane == 0) reinterpret_cast<volatile uint8_t*>(&bars.part_f16[es])[warp - 12] = f16;
             mbar_arrive(scale_full + 8 * es);
             ++scales;
           }
@@ -1191,87 +1151,51 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
             uint8_t* out = skv + slot * SH::kTile + (r >> 3) * 1024 + (r & 7) * 128;
             // 2^120 2^(e - 127), in one factor where bf16 holds it; exponent 255 reads as NaN
             const uint32_t e = kv ? ev : ek;
-            if (kDirect && lane == 0) reinterpret_cast<volatile uint8_t*>(&bars.value_f16[slot])[warp - 12] = f16;
-            if (kDirect && f16) {
-              // unrolled whole, short as it is: four requests of 12 drafts over 27K 102 us, in rounds of four chunks 108
-              const uint32_t two = to_f16x2(exponent_up(e), exponent_up(e));
-              uint4 raw[2];
+            const uint32_t f1 = e == 255u ? 0x7fc0u : e > 134u ? 254u << 7 : (e + 120u) << 7;
+            const uint32_t scale = f1 | (f1 << 16);
+            uint32_t nan = 0;
+            // two chunks a round, the next round's on their way: unrolled whole, this code and the softmax's displace each
+            // other in the instruction cache
+            uint4 raw[2];
 #pragma unroll
-              for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + ((j ^ sw) << 4));
-#pragma unroll
-              for (int c0 = 0; c0 < CH; c0 += 2) {
-                const uint4 now[2] = {raw[0], raw[1]};
-                if (c0 + 2 < CH) {
-#pragma unroll
-                  for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + (((c0 + 2 + j) ^ sw) << 4));
-                }
-#pragma unroll
-                for (int jj = 0; jj < 2; ++jj) {
-                  const uint32_t w[4] = {now[jj].x, now[jj].y, now[jj].z, now[jj].w};
-                  uint32_t o[8];
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) o[j] = mul_f16x2(codes_to_f16x2(j & 1 ? w[j >> 1] >> 16 : w[j >> 1]), two);
-                  const int ch = c0 + jj, j0 = (2 * ch) & 7;
-                  uint8_t* q = out + (ch >> 2) * 16384;
-                  *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-                  *reinterpret_cast<uint4*>(q + (((j0 + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
-                }
-              }
-            } else {
-              const uint32_t f1 = e == 255u ? 0x7fc0u : e > 134u ? 254u << 7 : (e + 120u) << 7;
-              const uint32_t scale = f1 | (f1 << 16);
-              uint32_t nan = 0;
-              // two chunks a round, the next round's on their way: unrolled whole, this code and the softmax's displace each
-              // other in the instruction cache
-              uint4 raw[2];
-#pragma unroll
-              for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + ((j ^ sw) << 4));
+            for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + ((j ^ sw) << 4));
 #pragma unroll 1
-              for (int c0 = 0; c0 < CH; c0 += 2) {
-               const uint4 now[2] = {raw[0], raw[1]};
-               if (c0 + 2 < CH) {
+            for (int c0 = 0; c0 < CH; c0 += 2) {
+             const uint4 now[2] = {raw[0], raw[1]};
+             if (c0 + 2 < CH) {
 #pragma unroll
-                 for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + (((c0 + 2 + j) ^ sw) << 4));
-               }
+               for (int j = 0; j < 2; ++j) raw[j] = *reinterpret_cast<const uint4*>(in + (((c0 + 2 + j) ^ sw) << 4));
+             }
 #pragma unroll
-               for (int jj = 0; jj < 2; ++jj) {
-                const int ch = c0 + jj;
-                const uint32_t w[4] = {valid ? now[jj].x : 0u, valid ? now[jj].y : 0u, valid ? now[jj].z : 0u, valid ? now[jj].w : 0u};
-                uint32_t o[8];
+             for (int jj = 0; jj < 2; ++jj) {
+              const int ch = c0 + jj;
+              const uint32_t w[4] = {valid ? now[jj].x : 0u, valid ? now[jj].y : 0u, valid ? now[jj].z : 0u, valid ? now[jj].w : 0u};
+              uint32_t o[8];
 #pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                spread_codes(w[j], o[2 * j], o[2 * j + 1]);
+                nan |= (w[j] & 0x7f7f7f7fu) + 0x01010101u;
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) o[j] = mul_bf16x2(o[j], scale);
+              uint8_t* q = out + (ch >> 2) * 16384;
+              const int j0 = (2 * ch) & 7;
+              *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+              *reinterpret_cast<uint4*>(q + (((j0 + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+             }
+            }
+            if (((nan & 0x80808080u) != 0 || e > 134u) && valid) {
+              // a NaN code in the row, or a scale beyond one factor: the plain way
+              const float s = exponent_up(e);
+#pragma unroll 1
+              for (int ch = 0; ch < CH; ++ch) {
+                const uint4 v = *reinterpret_cast<const uint4*>(in + ((ch ^ sw) << 4));
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
                 for (int j = 0; j < 4; ++j) {
-                  spread_codes(w[j], o[2 * j], o[2 * j + 1]);
-                  nan |= (w[j] & 0x7f7f7f7fu) + 0x01010101u;
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = mul_bf16x2(o[j], scale);
-                if (kDirect) {                                      // there in their order
-#pragma unroll
-                  for (int j = 0; j < 8; j += 2) {
-                    const uint32_t even = o[j], odd = o[j + 1];
-                    o[j] = __byte_perm(even, odd, 0x5410);
-                    o[j + 1] = __byte_perm(even, odd, 0x7632);
-                  }
-                }
-                uint8_t* q = out + (ch >> 2) * 16384;
-                const int j0 = (2 * ch) & 7;
-                *reinterpret_cast<uint4*>(q + ((j0 ^ (r & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-                *reinterpret_cast<uint4*>(q + (((j0 + 1) ^ (r & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
-               }
-              }
-              if (((nan & 0x80808080u) != 0 || e > 134u) && valid) {
-                // a NaN code in the row, or a scale beyond one factor: the plain way
-                const float s = exponent_up(e);
-#pragma unroll 1
-                for (int ch = 0; ch < CH; ++ch) {
-                  const uint4 v = *reinterpret_cast<const uint4*>(in + ((ch ^ sw) << 4));
-                  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                  for (int j = 0; j < 4; ++j) {
-                    const float2 lo = e4m3x2_to_float2(w[j] & 0xffffu), hi = e4m3x2_to_float2(w[j] >> 16);
-                    const int at = 2 * ch + (j >> 1);
-                    *reinterpret_cast<uint2*>(out + (at >> 3) * 16384 + (((at & 7) ^ (r & 7)) << 4) + (j & 1) * 8) =
-                        kDirect ? make_uint2(pack2(lo.x * s, lo.y * s), pack2(hi.x * s, hi.y * s)) : make_uint2(pack2(lo.x * s, hi.x * s), pack2(lo.y * s, hi.y * s));
-                  }
+                  const float2 lo = e4m3x2_to_float2(w[j] & 0xffffu), hi = e4m3x2_to_float2(w[j] >> 16);
+                  const int at = 2 * ch + (j >> 1);
+                  *reinterpret_cast<uint2*>(out + (at >> 3) * 16384 + (((at & 7) ^ (r & 7)) << 4) + (j & 1) * 8) =
+                      make_uint2(pack2(lo.x * s, hi.x * s), pack2(lo.y * s, hi.y * s));
                 }
               }
             }

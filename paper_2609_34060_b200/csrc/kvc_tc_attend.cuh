@@ -155,8 +155,6 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lbo, ui
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int a_mn, int b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
-// the same with both operands f16
-__host__ __device__ constexpr uint32_t idesc_f16(uint32_t bf16) { return bf16 & ~((1u << 7) | (1u << 10)); }
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
