@@ -640,8 +640,9 @@ int kvc_attend(const kvc_requests *req, const kvc_heads *q, const kvc_cache *cac
                kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 int kvc_attend_q8(const kvc_requests *req, const kvc_heads *q, const kvc_qcache *cache, int32_t layer, double scale,
                   int32_t causal, kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
-/* Scratch of either call for requests within max_q, max_kv (0 on bad arguments); a function of n, max_q, max_kv, the head
- * counts, d and the current device's SM count alone. */
+/* Scratch of any of these calls, with a tree (kvc_attend_tree) or without one, for requests within max_q, max_kv (0 on bad
+ * arguments); a function of n, max_q, max_kv, the head counts, d and the current device's SM count alone.  A call takes a
+ * smaller one where its own kernels find room in it (KVC_E_WORKSPACE otherwise). */
 size_t kvc_attend_workspace_bytes(const kvc_requests *req, int32_t n_heads, int32_t H, int32_t d);
 
 /*

@@ -96,7 +96,7 @@ int attend_common(const kvc_requests* req, const kvc_heads* q, const kvc_cache* 
   };
   if (reads_meet(eo) || reads_meet(el) || overlap(el, eo)) return KVC_E_ALIAS;
   if (req->n == 0 || a.req.max_q == 0 || a.req.n_rows == 0) return KVC_OK;
-  const size_t need = kvc_attend_workspace_bytes(req, q->n_heads, geo->H, geo->d);
+  const size_t need = tc_attend_workspace_bytes(req->n, req->max_q, req->max_kv, q->n_heads / geo->H, geo->H, geo->d, tree != nullptr);   // of this call
   if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return KVC_E_WORKSPACE;
   const Extent ew = extent_of(workspace, (int64_t)need, 1);
   if (reads_meet(ew) || overlap(ew, eo) || overlap(ew, el)) return KVC_E_ALIAS;
@@ -148,7 +148,9 @@ int kvc_append_q8(const kvc_requests* req, const kvc_heads* k_new, const kvc_hea
 
 size_t kvc_attend_workspace_bytes(const kvc_requests* req, int32_t n_heads, int32_t H, int32_t d) {
   if (!req || req->n <= 0 || req->max_q <= 0 || req->max_kv < 0 || req->max_kv > kMaxTokens || H <= 0 || n_heads <= 0 || n_heads % H || (d != 64 && d != 128)) return 0;
-  return tc_attend_workspace_bytes(req->n, req->max_q, req->max_kv, n_heads / H, H, d);
+  const size_t plain = tc_attend_workspace_bytes(req->n, req->max_q, req->max_kv, n_heads / H, H, d, false);
+  const size_t tree = req->max_q > KVC_TREE_MAX_Q ? 0 : tc_attend_workspace_bytes(req->n, req->max_q, req->max_kv, n_heads / H, H, d, true);
+  return plain > tree ? plain : tree;
 }
 
 int kvc_attend(const kvc_requests* req, const kvc_heads* q, const kvc_cache* cache, int32_t layer, double scale, int32_t causal,

@@ -28,7 +28,7 @@ int tc_apply_multi(const DevCache& src, const DevCache& dst, int L, int H, int d
 int tc_project(const UpdateLaunch& U, int d, cudaStream_t s);
 int tc_gram(const FitLaunch& F, int d, cudaStream_t s, const SegTable* seg = nullptr);
 struct AttendLaunch;
-size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d);
+size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d, bool tree);   // of a call with a tree, or without one
 int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s);
 int tc_backproject(const GroupFitLaunch& G, cudaStream_t s, const SegTable* seg = nullptr);
 

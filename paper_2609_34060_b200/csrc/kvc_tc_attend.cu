@@ -75,7 +75,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.f, kJump = 16.f; // log2 of the growth of a row's maximum that is let pass, and that a tile bears
 constexpr int kUnitRows = 256;
 // rows a cut unit's partial result has room for
-constexpr int slot_rows(bool split) { return split ? 128 : kUnitRows; }
+constexpr int slot_rows(bool split, int64_t rows) { return !split ? kUnitRows : rows <= 32 ? 32 : 128; }
 // trees whose requests have more rows than this and at most 128 share a row tile between the halves of a block (kSplit below)
 constexpr int kSplitAbove = 16, kSplitRows = 128;
 
@@ -88,10 +88,11 @@ struct ChunkLaunch {
   TileGeo g;                               // of the raw tile
   int32_t blocks;
   int32_t min_rows;                        // requests with fewer rows belong to the other kernel
+  int32_t slots;                           // slot_rows
   bool fine;                               // few units in many pieces: the join's small blocks
   UnitStart* starts;                       // [blocks]
-  float* ml;                               // [blocks][2][256][2] maximum and sum of the rows of a block's two cut units
-  float* part;                             // [blocks][2][256][d] their sums
+  float* ml;                               // [blocks][2][slots][2] maximum and sum of the rows of a block's two cut units
+  float* part;                             // [blocks][2][d][slots] their sums
 };
 
 template <int D, bool Q8, bool kSplit>
@@ -416,6 +417,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
   };
   // the tile's strides as the tensor cores see it
   const uint32_t gs = Q8 ? 1024u : (uint32_t)p.g.gs, ps = Q8 ? 16384u : (uint32_t)p.g.ps;
+  const int slots = kSplit ? p.slots : kUnitRows;
 
   if (warp < 8) {
     regs_inc<SH::kRegs>();
@@ -835,7 +837,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       // no key seen: decided by the sum, which a NaN logit makes NaN (maxima pass over NaN: m may still be minus infinity)
       const bool dead = l == 0.f;
       const bool whole = y.whole;
-      const int64_t slot = ((int64_t)blockIdx.x * 2 + (y.t0 > 0 ? 0 : 1)) * slot_rows(kSplit) + tile_row + row;
+      const int64_t slot = ((int64_t)blockIdx.x * 2 + (y.t0 > 0 ? 0 : 1)) * slots + tile_row + row;
       const float inv = whole ? (dead ? 0.f : 1.f / l) : 1.f;
       __nv_bfloat16* dst = p.a.out.p + (int64_t)(y.q0 + tok) * p.a.out.s_row + (int64_t)head * p.a.out.s_head;
       // partial sums lie channel by channel: a warp's rows are neighbours
@@ -884,8 +886,16 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
         if (whole) {
           store32(dst + k, pack8(o), pack8(o + 8));
         } else if (n + n_other > 0) {
+          auto store = [&](auto stride) {                         // the stride known where it is compiled: 5 us on four agents of 27K
 #pragma unroll
-          for (int j = 0; j < 16; ++j) pdst[(k + j) * slot_rows(kSplit)] = o[j];
+            for (int j = 0; j < 16; ++j) pdst[(k + j) * stride()] = o[j];
+          };
+          if (!kSplit)
+            store([] { return kUnitRows; });
+          else if (slots == 32)
+            store([] { return 32; });
+          else
+            store([] { return 128; });
         }
       }
       if (live && ok && !second && (!kSplit || t == 0)) {
@@ -1378,6 +1388,14 @@ int64_t chunk_blocks(int n, int max_q, int max_kv, int G, int H) {
 }
 size_t chunk_starts_bytes(int64_t blocks) { return ((size_t)blocks * sizeof(UnitStart) + 255) / 256 * 256; }
 
+template <int D, int kSlotRows>
+cudaError_t launch_join(const ChunkLaunch& p, cudaStream_t s) {
+  constexpr int kRowBlocks = kSlotRows / 32;
+  if (p.fine)
+    return launch_after(attend_chunk_join_kernel<D, 4, kSlotRows>, dim3((unsigned)chunk_units(p.a.req.n, p.a.req.max_q, p.a.G, p.a.H), kRowBlocks * (D / 32)), 256, 0, s, p);
+  return launch_after(attend_chunk_join_kernel<D, D / 8, kSlotRows>, dim3((unsigned)p.blocks - 1, kRowBlocks), 256, 0, s, p);
+}
+
 template <int D, bool Q8, bool kTree, bool kSplit>
 cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
   using SH = Shape<D, Q8, kSplit>;
@@ -1390,10 +1408,8 @@ cudaError_t launch_chunk(const ChunkLaunch& p, const CUtensorMap& mk, const CUte
   }
   const cudaError_t e = launch_after(attend_chunk_kernel<D, Q8, kTree, kSplit>, dim3((unsigned)p.blocks), SH::kThreads, SH::kSmem, s, p, mk, mv);
   if (e != cudaSuccess || p.blocks < 2) return e;
-  constexpr int kSlotRows = slot_rows(kSplit), kRowBlocks = kSlotRows / 32;
-  if (p.fine)
-    return launch_after(attend_chunk_join_kernel<D, 4, kSlotRows>, dim3((unsigned)chunk_units(p.a.req.n, p.a.req.max_q, p.a.G, p.a.H), kRowBlocks * (D / 32)), 256, 0, s, p);
-  return launch_after(attend_chunk_join_kernel<D, D / 8, kSlotRows>, dim3((unsigned)p.blocks - 1, kRowBlocks), 256, 0, s, p);
+  if (!kSplit) return launch_join<D, kUnitRows>(p, s);
+  return p.slots == 32 ? launch_join<D, 32>(p, s) : launch_join<D, 128>(p, s);
 }
 
 }  // namespace
@@ -1428,15 +1444,14 @@ static Plan attend_plan(int n, int max_q, int max_kv, int G, int H, bool split) 
   return {both ? few_capacity(G) : 0, true};
 }
 
-size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d) {
-  // with a tree or without one
-  const Plan p = attend_plan(n, max_q, max_kv, G, H, false);
+size_t tc_attend_workspace_bytes(int n, int max_q, int max_kv, int G, int H, int d, bool tree) {
   const int64_t rows = (int64_t)max_q * G;
+  const bool split = tree && split_rows(rows);
+  const Plan p = attend_plan(n, max_q, max_kv, G, H, split);
   size_t bytes = p.rc ? (few_workspace_bytes(n, max_kv, H, d, p.rc) + 255) / 256 * 256 : 0;
-  if (p.chunk || split_rows(rows)) {
+  if (p.chunk) {
     const int64_t blocks = chunk_blocks(n, max_q, max_kv, G, H);
-    const size_t chunk = chunk_starts_bytes(blocks) + (size_t)(blocks * 2 * slot_rows(!p.chunk) * (d + 2) * 4);
-    bytes = p.chunk ? bytes + chunk : chunk > bytes ? chunk : bytes;
+    bytes += chunk_starts_bytes(blocks) + (size_t)(blocks * 2 * slot_rows(split, rows) * (d + 2) * 4);
   }
   return bytes;
 }
@@ -1451,6 +1466,7 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   p.min_rows = plan.rc + 1;
   p.blocks = (int)chunk_blocks(a.req.n, a.req.max_q, a.req.max_kv, a.G, a.H);
   if (p.blocks <= 0) return KVC_E_CUDA;
+  p.slots = slot_rows(split, (int64_t)a.req.max_q * a.G);
   p.fine = 4 * chunk_units(a.req.n, a.req.max_q, a.G, a.H) <= p.blocks;
   CUtensorMap mk, mv;
   bool ok;
@@ -1468,7 +1484,7 @@ int tc_attend(const AttendLaunch& a, int L, int d, cudaStream_t s) {
   if (!plan.chunk) return KVC_OK;
   p.starts = reinterpret_cast<UnitStart*>(ws);
   p.ml = reinterpret_cast<float*>(ws + chunk_starts_bytes(p.blocks));
-  p.part = p.ml + (int64_t)p.blocks * 2 * slot_rows(split) * 2;
+  p.part = p.ml + (int64_t)p.blocks * 2 * p.slots * 2;
   cudaError_t e;
 #define KVC_CHUNK(D, Q, T, S) \
   if (d == D && q8 == Q && (a.mask != nullptr) == T && split == S) e = launch_chunk<D, Q, T, S>(p, mk, mv, s);
