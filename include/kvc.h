@@ -774,10 +774,11 @@ int kvc_verify(const kvc_requests *req, const int32_t *parent, const int32_t *to
  *   kept         DEVICE int32 [n, kept_stride], ascending places below n_q, as kvc_verify leaves them
  *   n_kept       DEVICE int32 [n]
  *   kv_out       DEVICE int32 [n] or NULL: kv_len - n_q + n_kept, the length behind the step; not kv_len itself
- * A list that is not ascending or leaves the request's rows, or a negative position, raises KVC_FLAG_BAD_TREE: nothing of
- * that request is moved and kv_out gets kv_len.  A request whose numbers break the rules of kvc_requests is left, kv_out
- * too.  A page id outside the pool raises KVC_FLAG_BAD_PAGE, its row is not moved.  Requests must not share the pages they
- * move rows in; without a page table n == 1 (KVC_E_INVALID_ARG otherwise).  max_q up to KVC_TREE_MAX_Q.
+ * A list that is not ascending or leaves the request's rows, or more new tokens than the cache holds (n_q > kv_len, with an
+ * empty list too), raises KVC_FLAG_BAD_TREE: nothing of that request is moved and kv_out gets kv_len.  A request whose
+ * numbers break the rules of kvc_requests is left, kv_out too.  A page id outside the pool raises KVC_FLAG_BAD_PAGE, its row
+ * is not moved.  Requests must not share the pages they move rows in; without a page table n == 1 (KVC_E_INVALID_ARG
+ * otherwise).  max_q up to KVC_TREE_MAX_Q.
  */
 int kvc_keep(const kvc_requests *req, const int32_t *kept, int32_t kept_stride, const int32_t *n_kept, kvc_cache *cache, int32_t *kv_out,
              void *stream);

@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const __grid_constan
     int q0, nq, kv;
     const bool valid = request_span(p.req, b, first_block ? p.status : nullptr, q0, nq, kv);
     const int first = kv - nq;
-    bool bad = nk < 0 || nk > nq || (nk > 0 && first < 0);
+    bool bad = nk < 0 || nk > nq || first < 0;                   // kv_out would be negative, whatever is kept
     if (!bad) {
       for (int j = tid; j < nk; j += kKeepThreads) {
         const int a = j == tid ? place : kept[j];
