@@ -758,8 +758,8 @@ typedef struct kvc_probs {
  *   n_kept       DEVICE int32 [n]: their number (0 only for a request without rows)
  *   next         DEVICE int32 [n]: the next token; -1 for a request without rows
  * Where a rejection leaves no residual (P <= q everywhere, as rounding may have it), the remaining siblings are rejected
- * and the token is drawn from the node's own distribution.  A distribution without a positive finite sum gives -1 and
- * KVC_FLAG_BAD_PROB.  A drafted token outside [0, n) is rejected and leaves P as it is; it, and a parent out of range,
+ * and the token is drawn from the node's own distribution.  A distribution without a positive finite sum, or with an
+ * entry of 2^104 and more, gives -1 and KVC_FLAG_BAD_PROB.  A drafted token outside [0, n) is rejected and leaves P as it is; it, and a parent out of range,
  * raises KVC_FLAG_BAD_TREE.  A request whose numbers break the rules of kvc_requests is answered like one without rows.
  * Sums and comparisons are float64: results do not depend on the order of execution.  max_kv and the page table are not
  * used, kv_len is (bounds).  max_q up to KVC_TREE_MAX_Q.

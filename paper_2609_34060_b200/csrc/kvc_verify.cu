@@ -35,11 +35,13 @@ constexpr int kRowBytes = 24;              // of shared memory for a row of the 
 constexpr int kStep = 128;                 // entries a warp takes at a time
 constexpr int kList = 512;                 // entries of a warp's part that are kept from one pass over a node to the next
 
-// A non-negative float as a double, by moving its bits (the conversion unit takes 16 a cycle and SM, four times fewer than
-// the integer pipe; subnormal floats come out as other numbers below 2^-126).
+// A float below kTooLarge, not negative, as a double, by moving its bits: the conversion unit takes 16 a cycle and SM, four
+// times fewer than the integer pipe (64 trees over 128000 entries 47 us with it for subnormal numbers alone).  2^24 first, so
+// that subnormal numbers are normal ones.  (0 comes out as 2^-151: the callers look at that before.)
+constexpr float kTooLarge = 0x1p104f;
 __device__ __forceinline__ double widen(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return __hiloint2double((int)((u >> 3) + 0x38000000u), (int)(u << 29));
+  const uint32_t u = __float_as_uint(x * 0x1p24f);
+  return __hiloint2double((int)((u >> 3) + 0x36800000u), (int)(u << 29));
 }
 // P(x) from the node's two distributions; NaN and negative entries count as 0
 __device__ __forceinline__ double residual(float p, float q, double A, double B) {
@@ -201,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         }
       }
     }
-    if (top > 3.4028235e38f) sum = __longlong_as_double(0x7ff0000000000000ll);   // no sum with an infinity in it
+    if (top >= kTooLarge) sum = __longlong_as_double(0x7ff0000000000000ll);   // no sum with an infinity in it
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     __syncthreads();                       // s_warp of the pass before has been read
@@ -243,7 +245,8 @@ __global__ void __launch_bounds__(kThreads, 4) verify_kernel(const __grid_consta
         bool fresh = true;
         const double px = (double)s_p[child];
         if (kDraft) {
-          yes = (double)s_u[child] * (double)fmaxf(s_q[child], 0.f) < residual(s_p[child], s_q[child], n.A, n.B);
+          const double qx = (double)fmaxf(s_q[child], 0.f);       // u q is not below a P of 0, nor below one that is negative
+          yes = (double)s_u[child] * qx < px * n.A - qx * n.B;
         } else {
           for (int g = 0; g < n.gone; ++g) fresh = fresh && s_gone[g] != s_token[child];
           yes = fresh && (double)s_u[child] * n.left < px;
