@@ -1020,7 +1020,7 @@ def _pack(*args) -> bytes:
     try:
         from . import _marshal
     except ImportError as e:
-        raise RuntimeError("_marshal.so not found: build it with `python -m paper_2609_34060_b200.build`") from e
+        raise RuntimeError("_marshal not found for this interpreter: build it with `python -m paper_2609_34060_b200.build`") from e
     _marshal.setup(KvcError, torch.bfloat16, torch.float32, torch.int32)
     _pack = _marshal.pack
     return _pack(*args)
