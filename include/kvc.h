@@ -709,7 +709,7 @@ typedef struct kvc_rotary {
  *   q, q_out     [n_rows, any number of heads, d], or both NULL; q_out may be q itself (in place), also where q, k_new and
  *                v_new are slices of one projection's output
  * Everything else as in kvc_append.  Queries are rotated whether or not their keys found a place.  KVC_E_ALIAS: what is
- * written meets what is read.
+ * written meets what is read.  max_q beyond 2^31 - 257: KVC_E_UNSUPPORTED.
  */
 int kvc_append_rotated(const kvc_requests *req, const kvc_rotary *rot, const kvc_heads *q, kvc_heads *q_out, const kvc_heads *k_new,
                        const kvc_heads *v_new, int32_t layer, kvc_cache *dst, void *stream);

@@ -52,6 +52,7 @@ int rotated_common(const kvc_requests* req, const kvc_rotary* rot, const kvc_hea
   if (geo->H > 32767 || (q && q->n_heads > 65535)) return KVC_E_UNSUPPORTED;
   if ((rc = resolve_requests(req, geo, kn->n_rows, &a.req)) != KVC_OK) return rc;
   if (!req->page_table && req->n > 1) return KVC_E_INVALID_ARG;
+  if (req->max_q > kMaxTokens) return KVC_E_UNSUPPORTED;         // a tile behind the last token is still a 32-bit number
   if (!frequencies(rot->rope, a.rot, a.turns)) return KVC_E_INVALID_ARG;
   // what is written lies apart from what is read, and from one another
   const int64_t reach = cache_reach(geo, a.dst);

@@ -164,7 +164,7 @@ cudaError_t launch_append_rotated(const RotateLaunch& r, int d, cudaStream_t s) 
   const int tokens = r.req.max_q >= 64 ? 8 : 1;
   const int64_t each = ((int64_t)tokens * (r.Hq + 2 * r.H) * (d / 16) + kUnroll - 1) / kUnroll;
   const int threads = each < kMaxHalfD ? kMaxHalfD : each > 256 ? 256 : (int)((each + 31) / 32 * 32);
-  const dim3 g((unsigned)((r.req.max_q + tokens - 1) / tokens), (unsigned)(r.req.n < 65535 ? r.req.n : 65535));
+  const dim3 g((unsigned)(((int64_t)r.req.max_q + tokens - 1) / tokens), (unsigned)(r.req.n < 65535 ? r.req.n : 65535));
   const bool q8 = r.e.k != nullptr;
 #define KVC_ROTATE(D, Q, T) \
   if (d == D && q8 == Q && tokens == T) return tc::launch_after(append_rotated_kernel<D, Q, T>, g, threads, 0, s, r);
