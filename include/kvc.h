@@ -722,8 +722,8 @@ int kvc_append_rotated_q8(const kvc_requests *req, const kvc_rotary *rot, const 
  * own).  A row that sees nothing gets zeros and minus infinity.  parent and depth of the tree are not used.  Workspace,
  * rounding, limits and errors as in kvc_attend; max_q up to KVC_TREE_MAX_Q.  One thing differs: over an 8-bit cache, where
  * max_q times query heads per KV head is 17 to 128, a query meets the codes as two e4m3 parts whose sum is off by at most
- * 2^-17 of the query's largest channel in each of the others (exact in those above 2^-10 of it), and probabilities meet the
- * values rounded to bf16 (2^-8 of themselves).
+ * 2^-17 of the query's largest channel in each of the others (exact in those above 2^-10 of it), probabilities meet the
+ * values rounded to bf16 (2^-8 of themselves), and products q . K (before `scale`) of 2^64 and more may overflow.
  */
 int kvc_attend_tree(const kvc_requests *req, const kvc_tree *tree, const kvc_heads *q, const kvc_cache *cache, int32_t layer, double scale,
                     kvc_heads *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);

@@ -523,7 +523,10 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
       }
       const int lowest = __reduce_min_sync(0xffffffffu, lim);     // of the warp's rows
       const bool idle = kSplit && lowest == 0x7fffffff;           // a warp without rows hands on whatever its lanes hold
-      const float c = kDirect ? c_all * q_scale : c_all;          // kDirect: logits are those of the codes
+      // kDirect: logits are those of the codes, times the keys' scales.  A query's scale counts behind that; of one so small that
+      // large keys' would not fit (both are those of bf16), what is below 2^-64 goes in before.
+      const float c = kDirect ? c_all * fmaxf(q_scale, 0x1p-64f) : c_all;
+      const bool tiny = kDirect && __any_sync(0xffffffffu, q_scale < 0x1p-64f && lim != 0x7fffffff);
       const bool twin = kDirect && y.rows <= 64, second = twin && row >= 64;
       const int key0 = second ? 64 : 0, key1 = twin && !second ? 64 : 128;   // the lane's keys of a tile
       float m = minus_inf, l = 0.f;
@@ -573,13 +576,14 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
           // by a power of two, so that bf16 loses nothing.  mc is the maximum in steps of 2.
           const int es = (g + kt) % SH::kScales;
           const float4* ks = reinterpret_cast<const float4*>(sscale + es * 128);
-          const bool hidden = lowest < t0 + 127 || (kTree && t0 + 127 >= fresh);
+          const bool hidden = tiny || lowest < t0 + 127 || (kTree && t0 + 127 >= fresh);
           if (!(kTree && t0 + 127 >= fresh)) sees[0] = sees[1] = sees[2] = sees[3] = 0xffffffffu;
           const f32x2 c2 = f2_pack(c, c);
           f32x2 sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
           if (hidden) {
-            // masked tiles: their logits are scaled and masked in place, beside scales of one (masking the parts in the loop
-            // below would put cold code between its instructions)
+            // masked tiles (and those of tiny queries): their logits are scaled and masked in place, beside scales of one
+            // (masking the parts in the loop below would put cold code between its instructions)
+            const float before = fminf(q_scale * 0x1p64f, 1.f);
 #pragma unroll 1
             for (int q = key0; q < key1; q += 8) {
               float s[8];
@@ -589,7 +593,7 @@ attend_chunk_kernel(const __grid_constant__ ChunkLaunch p, const __grid_constant
               uint32_t bits = last >= 31 ? 0xffffffffu : last < 0 ? 0u : (2u << last) - 1u;
               bits &= (q < 32 ? sees[0] : q < 64 ? sees[1] : q < 96 ? sees[2] : sees[3]) >> (q & 31);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) s[k] = (bits >> k) & 1u ? s[k] * sscale[es * 128 + q + k] : minus_inf;
+              for (int k = 0; k < 8; ++k) s[k] = (bits >> k) & 1u ? s[k] * before * sscale[es * 128 + q + k] : minus_inf;
               tmem_st8(s_at + q, reinterpret_cast<const uint32_t*>(s));
             }
             tmem_st_wait();
