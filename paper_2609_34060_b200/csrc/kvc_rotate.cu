@@ -6,7 +6,7 @@
 // An angle is p f_k / 2 pi turns, less the whole ones, in float64 (position 2^20: off by 2e-10 of a turn), cos and sin of
 // the rest in float32.
 //
-// Measured: five prompts of 1500-2500 tokens, 28 / 4 heads of 128 into bf16 pages (167 MB): 32 us, 5.2 TB/s of 6.5 copied
+// Measured: five prompts of 1500-2500 tokens, 28 / 4 heads of 128 into bf16 pages (167 MB): 33 us, 5.1 TB/s of 6.5 copied
 // (a block a token 36, four 37, 32 tokens 57; streaming loads and stores no better); 32 trees of 9-63 drafts 6.8 us, 64
 // single tokens into 8-bit pages 3.2 us, where launch and the chain lists -> pages -> rows bound it.
 //
@@ -50,6 +50,7 @@ __device__ __forceinline__ void encode16(float* x, uint32_t& b, uint2& lo, uint2
 }
 
 constexpr int kUnroll = 2;
+constexpr int64_t kManyTokens = 7000;
 
 // grid: x = tiles of TOKENS tokens of a request, y = requests (strided)
 template <int D, bool Q8, int TOKENS>
@@ -159,9 +160,15 @@ __global__ void __launch_bounds__(256) append_rotated_kernel(const __grid_consta
 }  // namespace
 
 cudaError_t launch_append_rotated(const RotateLaunch& r, int d, cudaStream_t s) {
-  // prompts: tiles of eight tokens, whose rows stream through a block (five prompts of 1500-2500 tokens 32 us, a block a token
-  // 36); few tokens: a block each, as many threads as it has work (32 trees of 9-63 drafts 8.1 us a call, in tiles of four 9.5)
-  const int tokens = r.req.max_q >= 64 ? 8 : 1;
+  // Where the bounds allow 7000 tokens and more, eight a block, whose rows stream behind one set of angles; otherwise one, as
+  // many threads as it has work (eight would leave SMs without a block).  Measured, us, one token a block and eight, heads of
+  // 128, tokens in all:
+  //                  64        2100       4000       6000       8000       32000
+  //     32 / 8 bf16  3.0  7.8  13.0 14.7  22.2 20.8  30.8 34.4  40.0 37.9  145 129
+  //     32 / 8 8-bit 3.1  9.6  15.2 17.7  25.7 29.9  36.1 34.5  47.0 46.1  174 149
+  //     8 / 1 bf16   2.9  4.3  4.8  5.3   7.5  7.8   10.8 12.8  14.7 15.3  47  46
+  // and 64 single tokens under bounds of 2000 each 141 and 32: most blocks find nothing.
+  const int tokens = (int64_t)r.req.n * r.req.max_q >= kManyTokens ? 8 : 1;
   const int64_t each = ((int64_t)tokens * (r.Hq + 2 * r.H) * (d / 16) + kUnroll - 1) / kUnroll;
   const int threads = each < kMaxHalfD ? kMaxHalfD : each > 256 ? 256 : (int)((each + 31) / 32 * 32);
   const dim3 g((unsigned)(((int64_t)r.req.max_q + tokens - 1) / tokens), (unsigned)(r.req.n < 65535 ? r.req.n : 65535));
