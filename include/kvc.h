@@ -749,9 +749,10 @@ typedef struct kvc_probs {
  *   parent       as in kvc_tree
  *   token        DEVICE int32 [n_rows]: drafted tokens (of a request's row 0 not looked at)
  *   target       distributions of the target; NaN and negative entries count as 0 (in draft too), sums need not be exactly 1
- *   draft        distributions the children of every row were drawn from; same n and n_rows.  NULL: the drafts were chosen,
- *                not drawn: child c is accepted where u[c] (1 - the probabilities of the siblings rejected before it) <
- *                P(x), and a rejected token's probability becomes 0
+ *   draft        distributions the children of every row were drawn from, independently of one another (siblings drawn without
+ *                replacement need another rule); same n and n_rows.  NULL: the drafts were chosen, not drawn: child c is
+ *                accepted where u[c] (1 - the probabilities of the siblings rejected before it) < P(x), and a rejected
+ *                token's probability becomes 0 (a few siblings are meant: every entry is compared with all rejected ones)
  *   u            DEVICE float32 [n_rows], u_next DEVICE float32 [n]: uniform in [0, 1)
  *   kept         DEVICE int32 [n, kept_stride], kept_stride >= max_q: places of the accepted rows within the request, row 0
  *                first, ascending; -1 behind them, up to max_q

@@ -1088,8 +1088,8 @@ def kvc_attend_tree(req: Requests, tree: Tree, q: torch.Tensor, cache, layer: in
 def kvc_verify(req: Requests, parent: torch.Tensor, token: torch.Tensor, target: torch.Tensor, u: torch.Tensor, u_next: torch.Tensor,
                kept: torch.Tensor, n_kept: torch.Tensor, next_token: torch.Tensor, draft: Optional[torch.Tensor] = None, stream=None) -> None:
     """Which drafted tokens stay (`kept` int32 [n, max_q], `n_kept` int32 [n]) and the token behind them (`next_token` int32
-    [n]), from the target's distributions float32 [rows, vocabulary], those the drafts were drawn from (None: they were
-    chosen) and uniform random numbers `u` [rows], `u_next` [n]."""
+    [n]), from the target's distributions float32 [rows, vocabulary], those the drafts were drawn from, siblings independently
+    of one another (None: they were chosen), and uniform random numbers `u` [rows], `u_next` [n]."""
     what = "kvc_verify"
     at, dev = _address(req, what), req._dev
     block = _pack("PpprrfuKnnPP", _VERIFY_NAMES, dev, 0, req.n, req.max_q, at, target, draft, parent, token, u, u_next, kept, n_kept, next_token,

@@ -40,10 +40,12 @@
 //
 // Trees of drafted tokens (kvc_attend_tree): a row sees the context and those new tokens whose bits its mask has; masks are
 // looked at in the tiles that hold new tokens.  Where no request has more than 128 rows there is one row tile, and its chain
-// alone would leave the tensor cores and the memory waiting (24 requests of 4K, 32 drafts: 133 us).  The two halves of the
+// alone would leave the tensor cores and the memory waiting (24 requests of 4K, 32 drafts: 133 us; 102 this way).  The two halves of the
 // block then take its key tiles in turn, each with a maximum, sums and accumulators of its own, and meet at the end of a
-// piece through tensor memory: 97 us, 1900 cycles a tile in the middle of the run, where memory bounds it; start, the
-// epilogues of two or three pieces a block and the join are the rest.  Over 8-bit caches the keys stay codes:
+// piece through tensor memory: 1900 cycles a tile in the middle of the run, where memory bounds it; start, the epilogues of
+// two or three pieces a block and the join are the rest (25 us).  More than 128 rows take two row tiles as chunks do: 24 requests
+// of 4K, 50 drafts of 4 heads, 133 us as without a tree, in 8 bits 189 (168 without
+// one; that instance spills 140 bytes).  Over 8-bit caches the keys stay codes:
 //     q 2^-b = t1 + t2  (e4m3, into one sum) ,   S = (t1 + t2) K 2^b 2^e ,
 // their scales are the softmax's, and the converting warps have the values alone, as bf16 like the probabilities that meet
 // them.  (Float16 turns two codes into a pair in one instruction, bf16 takes four; but it ends at 2^-24 of a row's largest

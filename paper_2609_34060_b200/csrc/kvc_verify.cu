@@ -15,9 +15,15 @@
 // over the warp's part.
 // Sums are float64, in a fixed order.
 //
-// Measured: 64 trees of 8-16 drafts over 128000 entries, up to five passes a request: 33 us (77 MB from HBM, of which the
-// first pass takes 10; then the longest chain of passes bounds it); all drafts accepted 17 us; one chain of five drafts over
-// 32000 entries 6 us: launch, lists, gathers, two cluster barriers, draw.
+// Measured on the device, inputs that change from call to call: 64 trees of 8-16 drafts over 128000 entries, up to five passes
+// a request, 40 us (66 MB from HBM, a fifth of its rate: the longest chain of passes bounds it, and a pass the latency of the
+// few loads that 64 registers let fly); nothing rejected, or one draft, 17-18 us; one chain of five drafts over 32000 entries 6 us:
+// launch, lists, gathers, two cluster barriers, draw.  Those trees' distributions have their small entries cut off, and the
+// lists of what is left (kList) hold it: 43 us without lists.  Distributions that keep their tails overflow them, which costs
+// more than it gives: 49 us, 45 without lists (of flatter ones 51 and 46; 4 and 16 trees 13 / 18 us cut, 16 / 23 whole, by
+// no lists 15 / 20 and 15 / 22).
+// Chosen drafts: every entry is compared with every sibling rejected at the node, so a wide node costs vocabulary times
+// siblings: 64 requests with 10 rejected 63 us, 16 with 64 209 us, one with 300 1.3 ms, one with 1000 9.7 ms.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -392,8 +398,7 @@ template <bool kDraft, bool kWide>
 cudaError_t launch(const VerifyLaunch& v, cudaStream_t s) {
   // A small vocabulary is one block's.  Else eight blocks a request (four fit on an SM: 74 requests at once), or, while all
   // requests are resident with them, sixteen: 4 / 16 trees over 128000 entries 20 / 27 us with eight, 15 / 20 with sixteen;
-  // 64 trees 42 and 45.  (All before the lists: with them 13 / 17 and, with eight blocks, 33 us; lists of 1024 entries leave
-  // room for three blocks on an SM, 34 us.)
+  // 64 trees 42 and 45 (all without lists).  Lists of 1024 entries would leave room for three blocks on an SM.
   const int blocks = v.vocab <= 4096 ? 1 : v.req.n <= 32 ? kMaxCluster : kMaxCluster / 2;
   static DeviceOnce once;
   int dev;
